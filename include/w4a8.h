@@ -230,6 +230,207 @@ int gdn_chunked_scan(const float *q, const float *k, const float *v, const float
                      void *stream);
 
 /*
+ * Rotary positions of the softmax-attention layers (Sec. 2.2: 10 of the 40
+ * blocks are softmax attention; the paper does not spell its positions out,
+ * so this is the standard rotary embedding).  Pair i of a head's first n_rot
+ * elements turns by the angle pos * inv_freq[i]:
+ *   y_a = mscale * (x_a cos - x_b sin),  y_b = mscale * (x_b cos + x_a sin)
+ * with (a, b) = (i, i + n_rot / 2) in W4A8_ROPE_HALF and (2i, 2i + 1) in
+ * W4A8_ROPE_INTERLEAVED; elements from n_rot on pass through unchanged.  The
+ * angle, its cosine and sine and the rotation are taken in fp64 and rounded
+ * once to fp32, so far positions lose nothing.
+ *   inv_freq  [n_rot / 2] fp64, radians per position (rope_frequencies, or
+ *             the caller's own);  pos [T] int32, any sign;  mscale finite.
+ * As the `rope` of another entry point NULL means no rotation.  Errors (there
+ * and in rope_rotate): n_rot odd, < 2 or > D, layout unknown or mscale not
+ * finite -> W4A8_ESHAPE; inv_freq or pos NULL -> W4A8_ENULL; inv_freq not 8-,
+ * pos not 4-byte aligned -> W4A8_EALIGN.
+ */
+#define W4A8_ROPE_HALF        0
+#define W4A8_ROPE_INTERLEAVED 1
+typedef struct w4a8_rope {
+  const double *inv_freq;
+  const int32_t *pos;
+  int64_t n_rot;
+  int32_t layout;
+  float mscale;
+} w4a8_rope;
+
+/*
+ * Frequencies for w4a8_rope: inv_freq[i] = base^(-2i / n_rot), fp64, then
+ *   W4A8_ROPE_PLAIN   as they are (factor and the rest are not used; a base
+ *                     raised for long contexts is passed as base);
+ *   W4A8_ROPE_LINEAR  divided by factor (positions interpolated);
+ *   W4A8_ROPE_PARTS   by parts: pairs that turn more than beta_fast times
+ *                     within orig_len positions stay, pairs that turn less
+ *                     than beta_slow times are divided by factor, and between
+ *                     the two (lo the pair index of beta_fast rounded down, at
+ *                     least 0, hi that of beta_slow rounded up, at most
+ *                     n_rot - 1) a linear ramp in i mixes both.
+ * inv_freq NULL -> W4A8_ENULL; n_rot odd or < 2, base <= 1, factor <= 0, an
+ * unknown kind, or (by parts) orig_len <= 0, beta_slow <= 0 or beta_fast <
+ * beta_slow, or a value that is not finite -> W4A8_ESHAPE; n_rot > 1024 ->
+ * W4A8_ERANGE; inv_freq not 8-byte aligned -> W4A8_EALIGN.
+ */
+#define W4A8_ROPE_PLAIN  0
+#define W4A8_ROPE_LINEAR 1
+#define W4A8_ROPE_PARTS  2
+int rope_frequencies(double *inv_freq, int64_t n_rot, double base, int kind, double factor,
+                     double orig_len, double beta_fast, double beta_slow, void *stream);
+
+/*
+ * Rotation of T rows of NH heads (w4a8_rope).  x and out are fp32, head h of
+ * row t at element t * stride + h * D (strides in elements, so a slice of a
+ * fused projection's rows works); out may be x itself with the same stride.
+ * Errors: D < 4, D % 4 != 0, NH < 1, T < 0, a stride below NH * D or not a
+ * multiple of 4 -> W4A8_ESHAPE; D > 1024, T >= 2^31, NH >= 2^16 or a stride
+ * >= 2^31 -> W4A8_ERANGE; out equal to x with another stride -> W4A8_EALIAS;
+ * x or out not 16-byte aligned -> W4A8_EALIGN.  T == 0 is a no-op.
+ */
+int rope_rotate(const w4a8_rope *rope, const float *x, int64_t x_stride, float *out,
+                int64_t out_stride, int64_t T, int64_t NH, int64_t D, void *stream);
+
+/*
+ * The paged 4-bit key/value cache of the softmax-attention layers.  A page
+ * holds W4A8_KV_PAGE tokens; a pool is [n_pages][NKV] tiles, a tile one KV
+ * head's rows of one page in 4-bit blocks of 32 elements along D (NB = D/32
+ * blocks a row): W4A8_KV_Q4_0 (the Q4_0 quantizer, fp16 scales) or
+ * W4A8_KV_Q4_SYM (the Q4_SYM quantizer, fp32 scales).  kv_q4_tile_bytes(D,
+ * format) bytes each: NB * 1024 of codes, then the scales.  With t the token
+ * of the page, b the block, payload byte j as in the block formats (element j
+ * in the low nibble, element j + 16 in the high one):
+ *   K codes   dword b*256 + c*64 + (t%16)*4 + t/16: payload bytes 4c .. 4c+3,
+ *             each nibble code - 8 in two's complement;
+ *   V codes   byte b*1024 + ((t%16)/4)*256 + j*16 + (t/16)*4 + p(t%4),
+ *             p = 0, 2, 1, 3: payload byte j, each nibble the code;
+ *   scales    (K and V) number b*64 + ((t%16)/4)*16 + (t/16)*4 + t%4.
+ * The pools start with any contents.  A plan names the sequences of a call:
+ *   page_table [B][max_pages] int32: page i of a sequence's tokens is pool
+ *              page page_table[s][i]; an id outside [0, n_pages) is an absent
+ *              page (nothing is stored there, its keys are not attended);
+ *   kv_len     [B] int32: tokens of each sequence, this call's included;
+ *   cu_rows    [B + 1] int32, not decreasing: sequence s has the rows
+ *              cu_rows[s] .. cu_rows[s+1] - 1 of this call, its last tokens:
+ *              row r is token kv_len[s] - (cu_rows[s+1] - r).
+ * The arrays are read on the device and may change between replays of a
+ * captured graph.  Tokens before 0 or past max_pages * W4A8_KV_PAGE do not
+ * exist; rows outside every sequence are left as they were.  Two sequences
+ * may share pages that neither writes in the call.
+ * Errors of every entry point that takes a plan: NULL plan, or a NULL pointer
+ * to something its sizes say is there (pools with n_pages > 0, arrays with
+ * B > 0, page_table with max_pages > 0 too) -> W4A8_ENULL; D not 64, 128 or 256, NKV < 1, B < 0, n_pages < 0, max_pages
+ * < 0 or an unknown format -> W4A8_ESHAPE; NKV >= 2^16, B >= 2^20, n_pages
+ * >= 2^31 or max_pages >= 2^24 -> W4A8_ERANGE; pools not 16-byte, arrays not
+ * 4-byte aligned -> W4A8_EALIGN.
+ */
+#define W4A8_KV_PAGE   64
+#define W4A8_KV_Q4_0   0
+#define W4A8_KV_Q4_SYM 1
+typedef struct w4a8_kv {
+  void *k_pages;
+  void *v_pages;
+  const int32_t *page_table;
+  const int32_t *kv_len;
+  const int32_t *cu_rows;
+  int64_t n_pages;
+  int64_t max_pages;
+  int64_t B;
+  int64_t NKV;
+  int64_t D;
+  int32_t format;
+} w4a8_kv;
+size_t kv_q4_tile_bytes(int64_t D, int32_t format);   /* 0: invalid */
+
+/*
+ * Stores this call's keys and values: row r of k (rotated by `rope` unless it
+ * is NULL, then rounded to fp32) and of v, each head in 4-bit blocks, at the
+ * row's token.  With q (may be NULL, then q_out and NH are not used) the same
+ * launch rotates the rows' NH query heads into q_out [T][NH][D]; rows of no
+ * sequence are rotated too.
+ *   k, v [T][NKV][D], q [T][NH][D] fp32, row r at r * stride elements, heads
+ *   contiguous; q_out contiguous, may be q itself if q is.
+ * Each stored block is bit-identical to the format definition for the fp32
+ * row.  Errors beside the plan's and rope's: T < 0, a stride below heads * D
+ * or not a multiple of 4, q without rope, NH < 1 -> W4A8_ESHAPE; T >= 2^31,
+ * NH >= 2^16 or a stride >= 2^31 -> W4A8_ERANGE; k, v or q_out NULL ->
+ * W4A8_ENULL; k, v, q or q_out not 16-byte aligned -> W4A8_EALIGN; q_out
+ * equal to k, v, or to q with a q_stride other than NH * D -> W4A8_EALIAS.
+ * T == 0 or B == 0 is a no-op (with q and B == 0 only q is rotated).
+ */
+int kv_q4_append(const w4a8_kv *kv, const w4a8_rope *rope, const float *k, int64_t k_stride,
+                 const float *v, int64_t v_stride, const float *q, int64_t q_stride, float *q_out,
+                 int64_t NH, int64_t T, void *stream);
+
+/*
+ * Reads the rows of a plan back as fp32 values (code - 8) * scale (a whole
+ * sequence when its rows are all its tokens): k_out, v_out [T][NKV][D],
+ * either NULL to skip it.  Rows whose token or page is absent get zeros.
+ * T < 0 -> W4A8_ESHAPE; T >= 2^31 -> W4A8_ERANGE; an output not 16-byte
+ * aligned -> W4A8_EALIGN, both the same -> W4A8_EALIAS.
+ */
+int kv_q4_read(const w4a8_kv *kv, float *k_out, float *v_out, int64_t T, void *stream);
+
+/*
+ * Softmax attention of a plan's rows over the 4-bit cache (Sec. 2.2: grouped
+ * query heads, NH a multiple of NKV; head h reads KV head h / (NH / NKV)).
+ * For row r at token i of its sequence, over the keys j of present pages with
+ * 0 <= j <= i and, if window > 0, j > i - window:
+ *   s_j = scale * sum_b d_q[b] * d_k[j][b] * <q codes, k codes>
+ *   out = sum_j p_j v_j,  p = softmax(s),  lse = log sum_j exp(s_j)
+ * q is quantized to 8 bits per 32 elements as the library's products take
+ * their activations (Q8_0, or Q8_F32 for W4A8_KV_Q4_SYM), so the block dots
+ * are exact integers; the softmax and every sum are fp32, and each
+ * probability times value scale enters the matrix cores as two fp16 halves
+ * (about 22 bits).  A row that sees no key gives out 0 and lse -infinity.
+ * Keys that a row does not see cannot change its result, whatever their
+ * codes and scales hold.
+ *   q [T][NH][D] fp32 with row stride q_stride, out [T][NH][D], lse [T][NH]
+ *   (NULL: not written).  workspace >= attn_q4_workspace_size bytes, no
+ *   initialisation; one or two launches.  The result does not depend on
+ *   timing, and a sequence's does not on the values of the others'.
+ * Errors beside the plan's: NH < 1, NH % NKV != 0, T < 0, window < 0,
+ * q_stride < NH * D or not a multiple of 4, scale not finite -> W4A8_ESHAPE;
+ * T * NH >= 2^31 or q_stride >= 2^31 -> W4A8_ERANGE; q, out or workspace NULL
+ * -> W4A8_ENULL; q, out or workspace not 16-, lse not 4-byte aligned ->
+ * W4A8_EALIGN; out equal to q -> W4A8_EALIAS; workspace too small ->
+ * W4A8_EWORKSPACE.  T == 0 or B == 0 is a no-op.  attn_q4_workspace_size
+ * returns 0 for invalid sizes; it reads only the plan's sizes and format.
+ */
+size_t attn_q4_workspace_size(const w4a8_kv *kv, int64_t T, int64_t NH);
+int attn_q4_forward(const w4a8_kv *kv, const float *q, int64_t q_stride, float *out, float *lse,
+                    int64_t T, int64_t NH, float scale, int64_t window, void *workspace,
+                    size_t ws_bytes, void *stream);
+
+/*
+ * Log probabilities read off the output head's logits (the decode head of
+ * Sec. 5.2).  Per row t of logits [T] rows of V fp32, row t at t * stride:
+ *   m = max_j l_j,  Z = sum_j exp(l_j - m),  log p_j = l_j - m - log Z
+ *   logprob[t] = log p of targets[t] (0 when the target lies outside [0, V))
+ *   entropy[t] = -sum_j p_j log p_j
+ *   top_ids[t][0..n_top), top_logprobs: the n_top largest logits in
+ *                descending order, equal ones by increasing index.
+ * -infinity (a banned token) has probability 0.  Z is summed without its
+ * largest term, so a confident row's small values keep their precision.  A
+ * row of -infinity only gives log probabilities -infinity and entropy 0 (its
+ * ids are 0 .. n_top - 1); a row with NaN or +infinity gives NaN for its log
+ * probabilities and entropy (ids in range: NaN first, then by value).
+ * -0 and 0 are equal.
+ *   targets [T] int32 and logprob [T] (both NULL: skipped), entropy [T] (NULL:
+ *   skipped), top_ids [T][n_top] int32 and top_logprobs [T][n_top] fp32 (both
+ *   NULL when n_top is 0).  workspace >= token_logprobs_workspace_size bytes,
+ *   no initialisation; one or two launches.
+ * Errors: T < 0, V < 1, stride < V -> W4A8_ESHAPE; V >= 2^24, T >= 2^31,
+ * n_top < 0, n_top > 32, n_top > V, T * stride >= 2^40 -> W4A8_ERANGE; logits,
+ * only one of a pair, or the workspace NULL -> W4A8_ENULL; logits or the
+ * workspace not 16-byte, other arrays not 4-byte aligned -> W4A8_EALIGN;
+ * workspace too small -> W4A8_EWORKSPACE.  T == 0 is a no-op.
+ */
+size_t token_logprobs_workspace_size(int64_t T, int64_t V, int64_t n_top);
+int token_logprobs(const float *logits, int64_t stride, const int32_t *targets, float *logprob,
+                   float *entropy, int32_t *top_ids, float *top_logprobs, int64_t T, int64_t V,
+                   int64_t n_top, void *workspace, size_t ws_bytes, void *stream);
+
+/*
  * Bytes of device workspace moe_w4a8_forward needs for these sizes, or 0 if
  * the sizes are invalid.  The workspace must be zero-filled once before its
  * first use (moe_w4a8_workspace_init does that); the library leaves its

@@ -23,6 +23,10 @@ Q4_SYM_BLOCK_BYTES = 20
 Q8_F32_BLOCK_BYTES = 36
 WS_XQ, WS_H, WS_HQ, WS_PERM, WS_COUNT, WS_SYNC, WS_SYNC_END, WS_XN = 0, 1, 2, 3, 4, 5, 6, 7
 WS_NFIELDS = 8
+KV_PAGE = 64
+KV_FORMATS = {"q4_0": 0, "q4_sym": 1}
+ROPE_LAYOUTS = {"half": 0, "interleaved": 1}
+ROPE_KINDS = {"none": 0, "linear": 1, "parts": 2}
 
 EXPORTS = ("w4a8_strerror", "q8_0_quantize", "q4_0_quantize", "q4q8_gemv",
            "moe_w4a8_workspace_size", "moe_w4a8_workspace_init",
@@ -31,9 +35,24 @@ EXPORTS = ("w4a8_strerror", "q8_0_quantize", "q4_0_quantize", "q4q8_gemv",
            "q4_sym_quantize", "q8_f32_quantize", "q4sym_q8f32_gemv",
            "w4a8_decode_wait_bound", "moe_w4a8_forward_noalloc", "q4q8_gemm_workspace_size",
            "q4q8_gemm", "moe_sym_workspace_size", "moe_sym_workspace_layout", "moe_sym_forward",
-           "gdn_workspace_size", "gdn_chunked_scan")
+           "gdn_workspace_size", "gdn_chunked_scan", "rope_frequencies", "rope_rotate",
+           "kv_q4_tile_bytes", "kv_q4_append", "kv_q4_read", "attn_q4_workspace_size",
+           "attn_q4_forward", "token_logprobs_workspace_size", "token_logprobs")
 
 _lib = None
+
+
+class _RopeArgs(ctypes.Structure):     # w4a8_rope
+    _fields_ = [("inv_freq", ctypes.c_void_p), ("pos", ctypes.c_void_p),
+                ("n_rot", ctypes.c_int64), ("layout", ctypes.c_int32), ("mscale", ctypes.c_float)]
+
+
+class _KvArgs(ctypes.Structure):       # w4a8_kv
+    _fields_ = [("k_pages", ctypes.c_void_p), ("v_pages", ctypes.c_void_p),
+                ("page_table", ctypes.c_void_p), ("kv_len", ctypes.c_void_p),
+                ("cu_rows", ctypes.c_void_p), ("n_pages", ctypes.c_int64),
+                ("max_pages", ctypes.c_int64), ("B", ctypes.c_int64), ("NKV", ctypes.c_int64),
+                ("D", ctypes.c_int64), ("format", ctypes.c_int32)]
 
 
 class W4A8Error(RuntimeError):
@@ -97,6 +116,23 @@ def lib() -> ctypes.CDLL:
     L.gdn_workspace_size.restype = SZ
     L.gdn_chunked_scan.argtypes = [P, P, P, P, P, P, P, P, I64, I64, I64, I64, P, SZ, P]
     L.gdn_chunked_scan.restype = ctypes.c_int
+    F64, INT, KV, RO = ctypes.c_double, ctypes.c_int, ctypes.POINTER(_KvArgs), \
+        ctypes.POINTER(_RopeArgs)
+    L.rope_frequencies.argtypes = [P, I64, F64, INT, F64, F64, F64, F64, P]
+    L.rope_rotate.argtypes = [RO, P, I64, P, I64, I64, I64, I64, P]
+    L.kv_q4_tile_bytes.argtypes = [I64, ctypes.c_int32]
+    L.kv_q4_tile_bytes.restype = SZ
+    L.kv_q4_append.argtypes = [KV, RO, P, I64, P, I64, P, I64, P, I64, I64, P]
+    L.kv_q4_read.argtypes = [KV, P, P, I64, P]
+    L.attn_q4_workspace_size.argtypes = [KV, I64, I64]
+    L.attn_q4_workspace_size.restype = SZ
+    L.attn_q4_forward.argtypes = [KV, P, I64, P, P, I64, I64, ctypes.c_float, I64, P, SZ, P]
+    L.token_logprobs_workspace_size.argtypes = [I64, I64, I64]
+    L.token_logprobs_workspace_size.restype = SZ
+    L.token_logprobs.argtypes = [P, I64, P, P, P, P, P, I64, I64, I64, P, SZ, P]
+    for name in ("rope_frequencies", "rope_rotate", "kv_q4_append", "kv_q4_read",
+                 "attn_q4_forward", "token_logprobs"):
+        getattr(L, name).restype = INT
     _lib = L
     return L
 
@@ -416,3 +452,271 @@ def moe_forward_noalloc(hidden, topk_ids, topk_w, w_gate_up, w_down, ws_gate_up,
                                         T, H, I, E, k, _stream(stream))
     _check(rc, "moe_w4a8_forward_noalloc")
     return out
+
+
+# ------------------------------------------------------------------ attention and logits
+class _on:
+    """Makes the tensors' device the current one for a call (the library
+    launches on the current device; streams belong to one)."""
+
+    def __init__(self, *tensors):
+        import torch
+        dev = None
+        for t in tensors:
+            if t is None:
+                continue
+            if dev is None:
+                dev = t.device
+            elif t.device != dev:
+                raise ValueError(f"tensors on {dev} and {t.device} in one call")
+        if dev is None or dev.type != "cuda":
+            raise ValueError(f"tensors on {dev}: a GPU's are needed")
+        self.guard = None if dev.index == torch.cuda.current_device() else torch.cuda.device(dev)
+
+    def __enter__(self):
+        if self.guard is not None:
+            self.guard.__enter__()
+
+    def __exit__(self, *exc):
+        if self.guard is not None:
+            self.guard.__exit__(*exc)
+
+
+def _need(ok, what):
+    if not ok:
+        raise ValueError(what)
+
+
+def _is(t, dtype, shape, what):
+    """A contiguous tensor of this type and shape (None: any size)."""
+    _need(t.dtype == dtype and t.is_contiguous() and t.dim() == len(shape) and
+          all(n is None or n == m for n, m in zip(shape, t.shape)),
+          f"{what}: a contiguous {dtype} tensor of shape {shape} is needed, "
+          f"got {t.dtype} {tuple(t.shape)} with strides {t.stride()}")
+
+
+def _heads(x, what):
+    """[rows, heads, D] fp32 with contiguous heads; returns the row stride."""
+    import torch
+    _need(x.dtype == torch.float32 and x.dim() == 3 and
+          (x.numel() == 0 or (x.stride(2) == 1 and (x.shape[1] == 1 or x.stride(1) == x.shape[2]))),
+          f"{what}: fp32 [rows, heads, D] with contiguous heads is needed, "
+          f"got {x.dtype} {tuple(x.shape)} with strides {x.stride()}")
+    return x.stride(0) if x.shape[0] > 1 else max(x.stride(0), x.shape[1] * x.shape[2])
+
+
+def _rope(pos, inv_freq, layout, mscale, T):
+    import torch
+    _is(pos, torch.int32, (T,), "pos")
+    _is(inv_freq, torch.float64, (None,), "inv_freq")
+    _need(layout in ROPE_LAYOUTS, f"layout {layout!r}")
+    return _RopeArgs(inv_freq.data_ptr(), pos.data_ptr(), 2 * inv_freq.numel(),
+                     ROPE_LAYOUTS[layout], float(mscale))
+
+
+def rope_frequencies(n_rot, base=10000.0, kind="none", factor=1.0, orig_len=0, beta_fast=32.0,
+                     beta_slow=1.0, device="cuda", out=None, stream=None):
+    """Frequencies of the n_rot / 2 rotated pairs, fp64 radians per position:
+    base^(-2i / n_rot), as they are ("none"), over factor ("linear"), or mixed
+    by how often a pair turns within orig_len positions ("parts")."""
+    import torch
+    _need(kind in ROPE_KINDS, f"kind {kind!r}")
+    if out is None:
+        out = torch.empty(max(0, n_rot // 2), dtype=torch.float64, device=device)
+    _is(out, torch.float64, (n_rot // 2,), "out")
+    with _on(out):
+        _check(lib().rope_frequencies(_p(out), n_rot, base, ROPE_KINDS[kind], factor, orig_len,
+                                      beta_fast, beta_slow, _stream(stream)), "rope_frequencies")
+    return out
+
+
+def rope_rotate(x, pos, inv_freq, layout="half", mscale=1.0, out=None, stream=None):
+    """The heads of x [T, NH, D] turned by their rows' positions pos [T] (the
+    first 2 * len(inv_freq) elements; out may be x)."""
+    import torch
+    T, NH, D = x.shape
+    xs = _heads(x, "x")
+    r = _rope(pos, inv_freq, layout, mscale, T)
+    if out is None:
+        out = torch.empty((T, NH, D), dtype=torch.float32, device=x.device)
+    _need(out.shape == x.shape, f"out: shape {tuple(x.shape)} is needed, got {tuple(out.shape)}")
+    os_ = _heads(out, "out")
+    if T == 0:
+        return out
+    with _on(x, pos, inv_freq, out):
+        _check(lib().rope_rotate(ctypes.byref(r), _p(x), xs, _p(out), os_, T, NH, D,
+                                 _stream(stream)), "rope_rotate")
+    return out
+
+
+def kv_tile_bytes(D, fmt="q4_0") -> int:
+    return int(lib().kv_q4_tile_bytes(D, KV_FORMATS[fmt]))
+
+
+def kv_pools(n_pages, NKV, D, fmt="q4_0", device="cuda"):
+    """Key and value pools of n_pages pages (any contents) for NKV heads."""
+    import torch
+    n = kv_tile_bytes(D, fmt)
+    if n == 0:
+        raise W4A8Error(ESHAPE, "kv_q4_tile_bytes")
+    new = lambda: torch.empty((n_pages, NKV, n), dtype=torch.uint8, device=device)
+    return new(), new()
+
+
+class KVCache:
+    """A plan of the paged 4-bit cache (w4a8_kv): the pools [n_pages, NKV,
+    tile bytes] (kv_pools), page_table [B, max_pages], kv_len [B] (this call's
+    rows included) and cu_rows [B + 1].  It keeps the tensors, which are read
+    on the device at each call: update them in place between steps."""
+
+    def __init__(self, k_pages, v_pages, page_table, kv_len, cu_rows, D, fmt="q4_0"):
+        import torch
+        _need(fmt in KV_FORMATS, f"format {fmt!r}")
+        n = kv_tile_bytes(D, fmt)
+        if n == 0:
+            raise W4A8Error(ESHAPE, "KVCache")
+        _is(k_pages, torch.uint8, (None, None, n), "k_pages")
+        _is(v_pages, torch.uint8, tuple(k_pages.shape), "v_pages")
+        _is(page_table, torch.int32, (None, None), "page_table")
+        B, max_pages = page_table.shape
+        _is(kv_len, torch.int32, (B,), "kv_len")
+        _is(cu_rows, torch.int32, (B + 1,), "cu_rows")
+        self.tensors = (k_pages, v_pages, page_table, kv_len, cu_rows)
+        self.NKV, self.D, self.device = k_pages.shape[1], D, k_pages.device
+        self.args = _KvArgs(*(t.data_ptr() for t in self.tensors), k_pages.shape[0], max_pages, B,
+                            self.NKV, D, KV_FORMATS[fmt])
+
+
+def kv_append(kv, k, v, pos=None, inv_freq=None, layout="half", mscale=1.0, q=None, q_out=None,
+              stream=None):
+    """Stores the rows k, v [T, NKV, D] as the last tokens of kv's sequences,
+    the keys rotated when pos [T] and inv_freq are given; with q [T, NH, D] the
+    same launch rotates the queries, which are returned."""
+    import torch
+    T = k.shape[0]
+    shape = (T, kv.NKV, kv.D)
+    ks, vs = _heads(k, "k"), _heads(v, "v")
+    _need(tuple(k.shape) == shape and tuple(v.shape) == shape,
+          f"k, v: shape {shape} is needed, got {tuple(k.shape)}, {tuple(v.shape)}")
+    _need((pos is None) == (inv_freq is None), "pos and inv_freq go together")
+    r = None if pos is None else _rope(pos, inv_freq, layout, mscale, T)
+    NH = qs = 0
+    if q is not None:
+        qs, NH = _heads(q, "q"), q.shape[1]
+        _need(q.shape[0] == T and q.shape[2] == kv.D, f"q: shape ({T}, heads, {kv.D}) is needed")
+        if q_out is None:
+            q_out = torch.empty((T, NH, kv.D), dtype=torch.float32, device=q.device)
+        _is(q_out, torch.float32, (T, NH, kv.D), "q_out")
+    else:
+        q_out = None
+    if T == 0:
+        return q_out
+    with _on(*kv.tensors, k, v, pos, inv_freq, q, q_out):
+        _check(lib().kv_q4_append(ctypes.byref(kv.args), None if r is None else ctypes.byref(r),
+                                  _p(k), ks, _p(v), vs, _p(q), qs, _p(q_out), NH, T,
+                                  _stream(stream)), "kv_q4_append")
+    return q_out
+
+
+def kv_read(kv, T, k_out=None, v_out=None, stream=None):
+    """The T rows of kv's sequences as fp32 (k, v) [T, NKV, D]."""
+    import torch
+    shape = (T, kv.NKV, kv.D)
+    new = lambda: torch.empty(shape, dtype=torch.float32, device=kv.device)
+    k_out = new() if k_out is None else k_out
+    v_out = new() if v_out is None else v_out
+    _is(k_out, torch.float32, shape, "k_out")
+    _is(v_out, torch.float32, shape, "v_out")
+    if T == 0:
+        return k_out, v_out
+    with _on(*kv.tensors, k_out, v_out):
+        _check(lib().kv_q4_read(ctypes.byref(kv.args), _p(k_out), _p(v_out), T, _stream(stream)),
+               "kv_q4_read")
+    return k_out, v_out
+
+
+def attn_workspace(kv, T, NH):
+    """A workspace for attn_forward with T rows of NH heads on kv's plan."""
+    import torch
+    n = int(lib().attn_q4_workspace_size(ctypes.byref(kv.args), T, NH))
+    if n == 0:
+        raise W4A8Error(ESHAPE, "attn_q4_workspace_size")
+    return torch.empty(n, dtype=torch.uint8, device=kv.device)
+
+
+def attn_forward(kv, q, scale, window=0, out=None, lse=None, want_lse=True, workspace=None,
+                 stream=None):
+    """Softmax attention of q [T, NH, D] (kv's rows) over the 4-bit cache;
+    returns (out [T, NH, D], lse [T, NH] or None)."""
+    import torch
+    qs = _heads(q, "q")
+    T, NH, D = q.shape
+    _need(D == kv.D, f"q: heads of {kv.D} are needed, got {D}")
+    if out is None:
+        out = torch.empty((T, NH, D), dtype=torch.float32, device=q.device)
+    _is(out, torch.float32, (T, NH, D), "out")
+    if lse is None and want_lse:
+        lse = torch.empty((T, NH), dtype=torch.float32, device=q.device)
+    if lse is not None:
+        _is(lse, torch.float32, (T, NH), "lse")
+    if T == 0:
+        return out, lse
+    with _on(*kv.tensors, q, out, lse, workspace):
+        if workspace is None:
+            workspace = attn_workspace(kv, T, NH)
+        _check(lib().attn_q4_forward(ctypes.byref(kv.args), _p(q), qs, _p(out), _p(lse), T, NH,
+                                     scale, window, _p(workspace),
+                                     workspace.numel() * workspace.element_size(),
+                                     _stream(stream)), "attn_q4_forward")
+    return out, lse
+
+
+def logprobs_workspace(T, V, n_top=0, device="cuda"):
+    """A workspace for token_logprobs."""
+    import torch
+    n = int(lib().token_logprobs_workspace_size(T, V, n_top))
+    if n == 0:
+        raise W4A8Error(ERANGE, "token_logprobs_workspace_size")
+    return torch.empty(n, dtype=torch.uint8, device=device)
+
+
+def token_logprobs(logits, targets=None, n_top=0, want_entropy=True, logprob=None, entropy=None,
+                   top_ids=None, top_logprobs=None, workspace=None, stream=None):
+    """From fp32 logits [T, V] (rows may be strided): (log probability of
+    targets [T] int32, entropy [T], the n_top largest logits' ids int32 and log
+    probabilities [T, n_top]); None where not asked for."""
+    import torch
+    _need(logits.dtype == torch.float32 and logits.dim() == 2 and
+          (logits.shape[1] == 1 or logits.stride(1) == 1),
+          f"logits: fp32 [T, V] with contiguous rows is needed, got {logits.dtype} "
+          f"{tuple(logits.shape)} with strides {logits.stride()}")
+    T, V = logits.shape
+    stride = logits.stride(0) if T > 1 else max(V, logits.stride(0))
+    new = lambda *s, dt=torch.float32: torch.empty(s, dtype=dt, device=logits.device)
+    if targets is not None:
+        _is(targets, torch.int32, (T,), "targets")
+        logprob = new(T) if logprob is None else logprob
+        _is(logprob, torch.float32, (T,), "logprob")
+    else:
+        logprob = None
+    if want_entropy and entropy is None:
+        entropy = new(T)
+    if entropy is not None:
+        _is(entropy, torch.float32, (T,), "entropy")
+    if n_top > 0:
+        top_ids = new(T, n_top, dt=torch.int32) if top_ids is None else top_ids
+        top_logprobs = new(T, n_top) if top_logprobs is None else top_logprobs
+        _is(top_ids, torch.int32, (T, n_top), "top_ids")
+        _is(top_logprobs, torch.float32, (T, n_top), "top_logprobs")
+    else:
+        top_ids = top_logprobs = None
+    if T == 0:
+        return logprob, entropy, top_ids, top_logprobs
+    with _on(logits, targets, logprob, entropy, top_ids, top_logprobs, workspace):
+        if workspace is None:
+            workspace = logprobs_workspace(T, V, n_top, logits.device)
+        _check(lib().token_logprobs(_p(logits), stride, _p(targets), _p(logprob), _p(entropy),
+                                    _p(top_ids), _p(top_logprobs), T, V, n_top, _p(workspace),
+                                    workspace.numel() * workspace.element_size(),
+                                    _stream(stream)), "token_logprobs")
+    return logprob, entropy, top_ids, top_logprobs

@@ -29,34 +29,8 @@ __global__ __launch_bounds__(256) void q4_0_kernel(const float *__restrict__ w,
     const float4 t = reinterpret_cast<const float4 *>(w + blk * QK)[j];
     v[0] = t.x; v[1] = t.y; v[2] = t.z; v[3] = t.w;
   }
-  // signed element of largest magnitude, first index on ties
-  float amax = 0.0f, m = 0.0f;
-  int idx = 4 * j;
-#pragma unroll
-  for (int i = 0; i < 4; i++) {
-    const float a = fabsf(v[i]);
-    if (a > amax) { amax = a; m = v[i]; idx = 4 * j + i; }
-  }
-#pragma unroll
-  for (int o = 4; o > 0; o >>= 1) {
-    const float a2 = __shfl_xor(amax, o, 8);
-    const float m2 = __shfl_xor(m, o, 8);
-    const int i2 = __shfl_xor(idx, o, 8);
-    if (a2 > amax || (a2 == amax && i2 < idx)) { amax = a2; m = m2; idx = i2; }
-  }
-  const float d32 = m / -8.0f;
-  const uint32_t d16 = f32_to_f16_bits(d32);
-  const float df = f16_bits_to_f32(d16);
-  const float id = (df != 0.0f) ? 1.0f / df : 0.0f;
-  uint32_t codes = 0;  // four 4-bit codes, element i in byte i
-#pragma unroll
-  for (int i = 0; i < 4; i++) {
-    const float p = v[i] * id;      // one fp32 multiply (no contraction)
-    const float s = p + 8.5f;       // one fp32 add
-    int q = (int)floorf(s);
-    q = q > 15 ? 15 : (q < 0 ? 0 : q);
-    codes |= (uint32_t)q << (8 * i);
-  }
+  uint32_t d16;
+  const uint32_t codes = q4_0_block8(v, j, d16);   // element i in byte i
   const uint32_t hi = __shfl_xor(codes, 4, 8);  // lanes 4..7 hold elements 16..31
   if (live && j < 4) {
     const uint32_t bytes = codes | (hi << 4);

@@ -44,14 +44,8 @@ __global__ __launch_bounds__(256) void q4_sym_kernel(const float *__restrict__ w
   const bool live = blk < nblocks;
   float v[4];
   load4(w, blk, j, live, v);
-  const float d = amax8(v) / 7.0f;
-  const float id = sym_inverse(d);
-  uint32_t nib = 0;   // four stored nibbles q + 8, element i in byte i
-#pragma unroll
-  for (int i = 0; i < 4; i++) {
-    const int q = id == 0.0f ? 0 : round_clamp(v[i] * id, 7);
-    nib |= (uint32_t)(q + 8) << (8 * i);
-  }
+  float d;
+  const uint32_t nib = q4_sym_block8(v, d);     // stored nibbles q + 8, element i in byte i
   const uint32_t hi = __shfl_xor(nib, 4, 8);    // lanes 4..7 hold elements 16..31
   if (live && j < 4) {
     uint8_t *b = wq + blk * Q4SB;

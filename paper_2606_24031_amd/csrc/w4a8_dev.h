@@ -339,6 +339,55 @@ __device__ __forceinline__ uint32_t q8_f32_block8(const float v[4], float &d) {
   return packed;
 }
 
+// Q4_0 of one 32-value block held by 8 consecutive lanes (lane j: elements
+// 4j..4j+3; all 8 active): the lane's four codes, one a byte, and the block's
+// fp16 scale bits.  The signed element of largest magnitude (the first on
+// ties) over -8, then one multiply, one add, floor and clamp an element.
+__device__ __forceinline__ uint32_t q4_0_block8(const float v[4], int j, uint32_t &d16) {
+  float amax = 0.0f, m = 0.0f;
+  int idx = 4 * j;
+#pragma unroll
+  for (int i = 0; i < 4; i++) {
+    const float a = fabsf(v[i]);
+    if (a > amax) { amax = a; m = v[i]; idx = 4 * j + i; }
+  }
+#pragma unroll
+  for (int o = 4; o > 0; o >>= 1) {
+    const float a2 = __shfl_xor(amax, o, 8);
+    const float m2 = __shfl_xor(m, o, 8);
+    const int i2 = __shfl_xor(idx, o, 8);
+    if (a2 > amax || (a2 == amax && i2 < idx)) { amax = a2; m = m2; idx = i2; }
+  }
+  const float d32 = m / -8.0f;
+  d16 = f32_to_f16_bits(d32);
+  const float df = f16_bits_to_f32(d16);
+  const float id = (df != 0.0f) ? 1.0f / df : 0.0f;
+  uint32_t codes = 0;
+#pragma unroll
+  for (int i = 0; i < 4; i++) {
+    const float p = v[i] * id;      // one fp32 multiply (no contraction)
+    const float s = p + 8.5f;       // one fp32 add
+    int q = (int)floorf(s);
+    q = q > 15 ? 15 : (q < 0 ? 0 : q);
+    codes |= (uint32_t)q << (8 * i);
+  }
+  return codes;
+}
+
+// Q4_SYM of one block by 8 lanes: the lane's four stored nibbles (code + 8),
+// one a byte, and the fp32 scale.
+__device__ __forceinline__ uint32_t q4_sym_block8(const float v[4], float &d) {
+  d = max8(fmaxf(fmaxf(fabsf(v[0]), fabsf(v[1])), fmaxf(fabsf(v[2]), fabsf(v[3])))) / 7.0f;
+  const float id = sym_inverse(d);
+  uint32_t nib = 0;
+#pragma unroll
+  for (int i = 0; i < 4; i++) {
+    const int q = id == 0.0f ? 0 : round_clamp(v[i] * id, 7);
+    nib |= (uint32_t)(q + 8) << (8 * i);
+  }
+  return nib;
+}
+
 // Activation block blk of a row-major array by 8 lanes, lane j the elements
 // 4j..4j+3: quantized (Q8_0, or with SYM Q8_F32), stored as its 34- or 36-byte
 // block (live lanes), and returned with its fp32 scale.
