@@ -295,7 +295,8 @@ int rope_rotate(const w4a8_rope *rope, const float *x, int64_t x_stride, float *
  * holds W4A8_KV_PAGE tokens; a pool is [n_pages][NKV] tiles, a tile one KV
  * head's rows of one page in 4-bit blocks of 32 elements along D (NB = D/32
  * blocks a row): W4A8_KV_Q4_0 (the Q4_0 quantizer, fp16 scales) or
- * W4A8_KV_Q4_SYM (the Q4_SYM quantizer, fp32 scales).  kv_q4_tile_bytes(D,
+ * W4A8_KV_Q4_SYM (the Q4_SYM quantizer with d = amax * fl(1/7), the binary32
+ * product with the rounded reciprocal, in place of the quotient; fp32 scales).  kv_q4_tile_bytes(D,
  * format) bytes each: NB * 1024 of codes, then the scales.  With t the token
  * of the page, b the block, payload byte j as in the block formats (element j
  * in the low nibble, element j + 16 in the high one):
@@ -349,8 +350,7 @@ size_t kv_q4_tile_bytes(int64_t D, int32_t format);   /* 0: invalid */
  * sequence are rotated too.
  *   k, v [T][NKV][D], q [T][NH][D] fp32, row r at r * stride elements, heads
  *   contiguous; q_out contiguous, may be q itself if q is.
- * Each stored block is bit-identical to the format definition for the fp32
- * row.  Errors beside the plan's and rope's: T < 0, a stride below heads * D
+ * Each stored block is bit-identical to its definition for the fp32 row.  Errors beside the plan's and rope's: T < 0, a stride below heads * D
  * or not a multiple of 4, q without rope, NH < 1 -> W4A8_ESHAPE; T >= 2^31,
  * NH >= 2^16 or a stride >= 2^31 -> W4A8_ERANGE; k, v or q_out NULL ->
  * W4A8_ENULL; k, v, q or q_out not 16-byte aligned -> W4A8_EALIGN; q_out
@@ -378,8 +378,9 @@ int kv_q4_read(const w4a8_kv *kv, float *k_out, float *v_out, int64_t T, void *s
  *   s_j = scale * sum_b d_q[b] * d_k[j][b] * <q codes, k codes>
  *   out = sum_j p_j v_j,  p = softmax(s),  lse = log sum_j exp(s_j)
  * q is quantized to 8 bits per 32 elements as the library's products take
- * their activations (Q8_0, or Q8_F32 for W4A8_KV_Q4_SYM), so the block dots
- * are exact integers; the softmax and every sum are fp32, and each
+ * their activations (Q8_0, or Q8_F32 for W4A8_KV_Q4_SYM, with the scale's
+ * amax / 127 taken as the binary32 product amax * fl(1/127)), so the block
+ * dots are exact integers; the softmax and every sum are fp32, and each
  * probability times value scale enters the matrix cores as two fp16 halves
  * (about 22 bits).  A row that sees no key gives out 0 and lse -infinity.
  * Keys that a row does not see cannot change its result, whatever their

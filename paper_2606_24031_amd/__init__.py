@@ -455,63 +455,86 @@ def moe_forward_noalloc(hidden, topk_ids, topk_w, w_gate_up, w_down, ws_gate_up,
 
 
 # ------------------------------------------------------------------ attention and logits
-class _on:
-    """Makes the tensors' device the current one for a call (the library
-    launches on the current device; streams belong to one)."""
+class _On:
+    """Makes a GPU the current one for a call (the library launches on the
+    current device; streams belong to one)."""
 
-    def __init__(self, *tensors):
-        import torch
-        dev = None
-        for t in tensors:
-            if t is None:
-                continue
-            if dev is None:
-                dev = t.device
-            elif t.device != dev:
-                raise ValueError(f"tensors on {dev} and {t.device} in one call")
-        if dev is None or dev.type != "cuda":
-            raise ValueError(f"tensors on {dev}: a GPU's are needed")
-        self.guard = None if dev.index == torch.cuda.current_device() else torch.cuda.device(dev)
+    def __init__(self, index):
+        self.index = index
 
     def __enter__(self):
-        if self.guard is not None:
-            self.guard.__enter__()
+        import torch
+        self.back = torch.cuda.current_device()
+        torch.cuda.set_device(self.index)
 
     def __exit__(self, *exc):
-        if self.guard is not None:
-            self.guard.__exit__(*exc)
+        import torch
+        torch.cuda.set_device(self.back)
 
 
-def _need(ok, what):
-    if not ok:
-        raise ValueError(what)
+class _Here:
+    def __enter__(self):
+        pass
+
+    def __exit__(self, *exc):
+        pass
+
+
+_HERE = _Here()
+
+
+def _on(*tensors):
+    """A context in which the tensors' device (one GPU for all) is current."""
+    import torch
+    dev = tensors[0].device
+    for t in tensors:
+        if t is not None and t.device != dev:
+            raise ValueError(f"tensors on {dev} and {t.device} in one call")
+    if dev.type != "cuda":
+        raise ValueError(f"tensors on {dev}: a GPU's are needed")
+    return _HERE if dev.index == torch.cuda.current_device() else _On(dev.index)
+
+
+def _raw(stream):
+    """The raw handle of `stream`, or of the current one."""
+    import torch
+    if stream is not None:
+        return stream.cuda_stream
+    return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
+
+
+def _ptr(t):
+    return None if t is None else t.data_ptr()
 
 
 def _is(t, dtype, shape, what):
     """A contiguous tensor of this type and shape (None: any size)."""
-    _need(t.dtype == dtype and t.is_contiguous() and t.dim() == len(shape) and
-          all(n is None or n == m for n, m in zip(shape, t.shape)),
-          f"{what}: a contiguous {dtype} tensor of shape {shape} is needed, "
-          f"got {t.dtype} {tuple(t.shape)} with strides {t.stride()}")
+    if t.dtype is not dtype or not t.is_contiguous() or t.dim() != len(shape) or \
+            any(n is not None and n != m for n, m in zip(shape, t.shape)):
+        raise ValueError(f"{what}: a contiguous {dtype} tensor of shape {shape} is needed, "
+                         f"got {t.dtype} {tuple(t.shape)} with strides {t.stride()}")
 
 
 def _heads(x, what):
     """[rows, heads, D] fp32 with contiguous heads; returns the row stride."""
     import torch
-    _need(x.dtype == torch.float32 and x.dim() == 3 and
-          (x.numel() == 0 or (x.stride(2) == 1 and (x.shape[1] == 1 or x.stride(1) == x.shape[2]))),
-          f"{what}: fp32 [rows, heads, D] with contiguous heads is needed, "
-          f"got {x.dtype} {tuple(x.shape)} with strides {x.stride()}")
-    return x.stride(0) if x.shape[0] > 1 else max(x.stride(0), x.shape[1] * x.shape[2])
+    if x.dtype is torch.float32 and x.dim() == 3:
+        T, NH, D = x.shape
+        s0, s1, s2 = x.stride()
+        if T * NH * D == 0 or (s2 == 1 and (NH == 1 or s1 == D)):
+            return s0 if T > 1 else max(s0, NH * D)
+    raise ValueError(f"{what}: fp32 [rows, heads, D] with contiguous heads is needed, "
+                     f"got {x.dtype} {tuple(x.shape)} with strides {x.stride()}")
 
 
 def _rope(pos, inv_freq, layout, mscale, T):
     import torch
     _is(pos, torch.int32, (T,), "pos")
     _is(inv_freq, torch.float64, (None,), "inv_freq")
-    _need(layout in ROPE_LAYOUTS, f"layout {layout!r}")
+    if layout not in ROPE_LAYOUTS:
+        raise ValueError(f"layout {layout!r}: one of {sorted(ROPE_LAYOUTS)}")
     return _RopeArgs(inv_freq.data_ptr(), pos.data_ptr(), 2 * inv_freq.numel(),
-                     ROPE_LAYOUTS[layout], float(mscale))
+                     ROPE_LAYOUTS[layout], mscale)
 
 
 def rope_frequencies(n_rot, base=10000.0, kind="none", factor=1.0, orig_len=0, beta_fast=32.0,
@@ -520,13 +543,14 @@ def rope_frequencies(n_rot, base=10000.0, kind="none", factor=1.0, orig_len=0, b
     base^(-2i / n_rot), as they are ("none"), over factor ("linear"), or mixed
     by how often a pair turns within orig_len positions ("parts")."""
     import torch
-    _need(kind in ROPE_KINDS, f"kind {kind!r}")
+    if kind not in ROPE_KINDS:
+        raise ValueError(f"kind {kind!r}: one of {sorted(ROPE_KINDS)}")
     if out is None:
         out = torch.empty(max(0, n_rot // 2), dtype=torch.float64, device=device)
     _is(out, torch.float64, (n_rot // 2,), "out")
     with _on(out):
-        _check(lib().rope_frequencies(_p(out), n_rot, base, ROPE_KINDS[kind], factor, orig_len,
-                                      beta_fast, beta_slow, _stream(stream)), "rope_frequencies")
+        _check(lib().rope_frequencies(_ptr(out), n_rot, base, ROPE_KINDS[kind], factor, orig_len,
+                                      beta_fast, beta_slow, _raw(stream)), "rope_frequencies")
     return out
 
 
@@ -539,13 +563,14 @@ def rope_rotate(x, pos, inv_freq, layout="half", mscale=1.0, out=None, stream=No
     r = _rope(pos, inv_freq, layout, mscale, T)
     if out is None:
         out = torch.empty((T, NH, D), dtype=torch.float32, device=x.device)
-    _need(out.shape == x.shape, f"out: shape {tuple(x.shape)} is needed, got {tuple(out.shape)}")
+    if out.shape != x.shape:
+        raise ValueError(f"out: shape {tuple(x.shape)} is needed, got {tuple(out.shape)}")
     os_ = _heads(out, "out")
     if T == 0:
         return out
     with _on(x, pos, inv_freq, out):
-        _check(lib().rope_rotate(ctypes.byref(r), _p(x), xs, _p(out), os_, T, NH, D,
-                                 _stream(stream)), "rope_rotate")
+        _check(lib().rope_rotate(ctypes.byref(r), _ptr(x), xs, _ptr(out), os_, T, NH, D,
+                                 _raw(stream)), "rope_rotate")
     return out
 
 
@@ -571,7 +596,8 @@ class KVCache:
 
     def __init__(self, k_pages, v_pages, page_table, kv_len, cu_rows, D, fmt="q4_0"):
         import torch
-        _need(fmt in KV_FORMATS, f"format {fmt!r}")
+        if fmt not in KV_FORMATS:
+            raise ValueError(f"format {fmt!r}: one of {sorted(KV_FORMATS)}")
         n = kv_tile_bytes(D, fmt)
         if n == 0:
             raise W4A8Error(ESHAPE, "KVCache")
@@ -582,6 +608,9 @@ class KVCache:
         _is(kv_len, torch.int32, (B,), "kv_len")
         _is(cu_rows, torch.int32, (B + 1,), "cu_rows")
         self.tensors = (k_pages, v_pages, page_table, kv_len, cu_rows)
+        for t in self.tensors:
+            if t.device != k_pages.device:
+                raise ValueError(f"tensors on {k_pages.device} and {t.device} in one plan")
         self.NKV, self.D, self.device = k_pages.shape[1], D, k_pages.device
         self.args = _KvArgs(*(t.data_ptr() for t in self.tensors), k_pages.shape[0], max_pages, B,
                             self.NKV, D, KV_FORMATS[fmt])
@@ -596,14 +625,16 @@ def kv_append(kv, k, v, pos=None, inv_freq=None, layout="half", mscale=1.0, q=No
     T = k.shape[0]
     shape = (T, kv.NKV, kv.D)
     ks, vs = _heads(k, "k"), _heads(v, "v")
-    _need(tuple(k.shape) == shape and tuple(v.shape) == shape,
-          f"k, v: shape {shape} is needed, got {tuple(k.shape)}, {tuple(v.shape)}")
-    _need((pos is None) == (inv_freq is None), "pos and inv_freq go together")
+    if k.shape != shape or v.shape != shape:
+        raise ValueError(f"k, v: shape {shape} is needed, got {tuple(k.shape)}, {tuple(v.shape)}")
+    if (pos is None) != (inv_freq is None):
+        raise ValueError("pos and inv_freq go together")
     r = None if pos is None else _rope(pos, inv_freq, layout, mscale, T)
     NH = qs = 0
     if q is not None:
         qs, NH = _heads(q, "q"), q.shape[1]
-        _need(q.shape[0] == T and q.shape[2] == kv.D, f"q: shape ({T}, heads, {kv.D}) is needed")
+        if q.shape[0] != T or q.shape[2] != kv.D:
+            raise ValueError(f"q: shape ({T}, heads, {kv.D}) is needed, got {tuple(q.shape)}")
         if q_out is None:
             q_out = torch.empty((T, NH, kv.D), dtype=torch.float32, device=q.device)
         _is(q_out, torch.float32, (T, NH, kv.D), "q_out")
@@ -611,10 +642,10 @@ def kv_append(kv, k, v, pos=None, inv_freq=None, layout="half", mscale=1.0, q=No
         q_out = None
     if T == 0:
         return q_out
-    with _on(*kv.tensors, k, v, pos, inv_freq, q, q_out):
+    with _on(kv.tensors[0], k, v, pos, inv_freq, q, q_out):
         _check(lib().kv_q4_append(ctypes.byref(kv.args), None if r is None else ctypes.byref(r),
-                                  _p(k), ks, _p(v), vs, _p(q), qs, _p(q_out), NH, T,
-                                  _stream(stream)), "kv_q4_append")
+                                  _ptr(k), ks, _ptr(v), vs, _ptr(q), qs, _ptr(q_out), NH, T,
+                                  _raw(stream)), "kv_q4_append")
     return q_out
 
 
@@ -629,8 +660,8 @@ def kv_read(kv, T, k_out=None, v_out=None, stream=None):
     _is(v_out, torch.float32, shape, "v_out")
     if T == 0:
         return k_out, v_out
-    with _on(*kv.tensors, k_out, v_out):
-        _check(lib().kv_q4_read(ctypes.byref(kv.args), _p(k_out), _p(v_out), T, _stream(stream)),
+    with _on(kv.tensors[0], k_out, v_out):
+        _check(lib().kv_q4_read(ctypes.byref(kv.args), _ptr(k_out), _ptr(v_out), T, _raw(stream)),
                "kv_q4_read")
     return k_out, v_out
 
@@ -651,7 +682,8 @@ def attn_forward(kv, q, scale, window=0, out=None, lse=None, want_lse=True, work
     import torch
     qs = _heads(q, "q")
     T, NH, D = q.shape
-    _need(D == kv.D, f"q: heads of {kv.D} are needed, got {D}")
+    if D != kv.D:
+        raise ValueError(f"q: heads of {kv.D} are needed, got {D}")
     if out is None:
         out = torch.empty((T, NH, D), dtype=torch.float32, device=q.device)
     _is(out, torch.float32, (T, NH, D), "out")
@@ -661,13 +693,13 @@ def attn_forward(kv, q, scale, window=0, out=None, lse=None, want_lse=True, work
         _is(lse, torch.float32, (T, NH), "lse")
     if T == 0:
         return out, lse
-    with _on(*kv.tensors, q, out, lse, workspace):
+    with _on(kv.tensors[0], q, out, lse, workspace):
         if workspace is None:
             workspace = attn_workspace(kv, T, NH)
-        _check(lib().attn_q4_forward(ctypes.byref(kv.args), _p(q), qs, _p(out), _p(lse), T, NH,
-                                     scale, window, _p(workspace),
+        _check(lib().attn_q4_forward(ctypes.byref(kv.args), _ptr(q), qs, _ptr(out), _ptr(lse), T, NH,
+                                     scale, window, _ptr(workspace),
                                      workspace.numel() * workspace.element_size(),
-                                     _stream(stream)), "attn_q4_forward")
+                                     _raw(stream)), "attn_q4_forward")
     return out, lse
 
 
@@ -686,10 +718,10 @@ def token_logprobs(logits, targets=None, n_top=0, want_entropy=True, logprob=Non
     targets [T] int32, entropy [T], the n_top largest logits' ids int32 and log
     probabilities [T, n_top]); None where not asked for."""
     import torch
-    _need(logits.dtype == torch.float32 and logits.dim() == 2 and
-          (logits.shape[1] == 1 or logits.stride(1) == 1),
-          f"logits: fp32 [T, V] with contiguous rows is needed, got {logits.dtype} "
-          f"{tuple(logits.shape)} with strides {logits.stride()}")
+    if logits.dtype is not torch.float32 or logits.dim() != 2 or \
+            (logits.shape[1] != 1 and logits.stride(1) != 1):
+        raise ValueError(f"logits: fp32 [T, V] with contiguous rows is needed, got {logits.dtype} "
+                         f"{tuple(logits.shape)} with strides {logits.stride()}")
     T, V = logits.shape
     stride = logits.stride(0) if T > 1 else max(V, logits.stride(0))
     new = lambda *s, dt=torch.float32: torch.empty(s, dtype=dt, device=logits.device)
@@ -715,8 +747,8 @@ def token_logprobs(logits, targets=None, n_top=0, want_entropy=True, logprob=Non
     with _on(logits, targets, logprob, entropy, top_ids, top_logprobs, workspace):
         if workspace is None:
             workspace = logprobs_workspace(T, V, n_top, logits.device)
-        _check(lib().token_logprobs(_p(logits), stride, _p(targets), _p(logprob), _p(entropy),
-                                    _p(top_ids), _p(top_logprobs), T, V, n_top, _p(workspace),
+        _check(lib().token_logprobs(_ptr(logits), stride, _ptr(targets), _ptr(logprob), _ptr(entropy),
+                                    _ptr(top_ids), _ptr(top_logprobs), T, V, n_top, _ptr(workspace),
                                     workspace.numel() * workspace.element_size(),
-                                    _stream(stream)), "token_logprobs")
+                                    _raw(stream)), "token_logprobs")
     return logprob, entropy, top_ids, top_logprobs

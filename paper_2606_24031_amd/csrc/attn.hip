@@ -268,14 +268,7 @@ __global__ __launch_bounds__(AT, (NB * NT > 4 ? 1 : 2)) void attn_kernel(AttnArg
           a.q + (sq.r0 + fr / a.G) * a.qs + (int64_t)(h * a.G + fr % a.G) * D + b * 32 + 4 * j);
       const float v[4] = {x.x, x.y, x.z, x.w};
       float d;
-      uint32_t codes;
-      if (SYM) {
-        codes = q8_f32_block8(v, d);
-      } else {
-        uint32_t d16;
-        codes = q8_0_block8(v, d16);
-        d = f16_bits_to_f32(d16);
-      }
+      const uint32_t codes = kv_q8_block8<SYM>(v, d);
       const int nt = row >> 4, r = row & 15;
       lds.in.q[((nt * NB + b) * 64 + 16 * (j & 3) + r) * 2 + (j >> 2)] = codes;
       if (j == 0) lds.in.qd[(nt * NB + b) * 16 + r] = d * a.sign;

@@ -13,7 +13,7 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
-#include "../../include/w4a8.h"
+#include "w4a8_dev.h"
 
 namespace w4a8 {
 
@@ -31,6 +31,34 @@ __host__ __device__ constexpr int kv_v_byte(int b, int j, int t) {
 }
 __host__ __device__ constexpr int kv_scale_at(int b, int t) {
   return b * KV_PAGE + (t % 16) / 4 * 16 + t / 16 * 4 + t % 4;
+}
+
+// The cache's and attention's quantizers take a block's scale as the product
+// amax * fl(1/7) or amax * fl(1/127), at most an ulp from the quotient of the
+// block formats' own quantizers: one multiply where a correctly rounded
+// division is a dozen instructions, in a prologue that every run of pages
+// repeats.  (Q4_0's m / -8 is exact either way.)
+__device__ __forceinline__ float kv_amax8(const float v[4]) {
+  return max8(fmaxf(fmaxf(fabsf(v[0]), fabsf(v[1])), fmaxf(fabsf(v[2]), fabsf(v[3]))));
+}
+__device__ __forceinline__ uint32_t kv_q4_sym_block8(const float v[4], float &d) {
+  d = kv_amax8(v) * (1.0f / 7.0f);
+  return q4_sym_codes(v, d);
+}
+// 8-bit codes of a query's block; d: its scale (a fp16 number, or with SYM
+// any), whose reciprocal the codes are taken with.
+template <bool SYM>
+__device__ __forceinline__ uint32_t kv_q8_block8(const float v[4], float &d) {
+  d = kv_amax8(v) * (1.0f / 127.0f);
+  if (!SYM) d = f16_bits_to_f32(f32_to_f16_bits(d));
+  const float id = SYM ? sym_inverse(d) : d != 0.0f ? 1.0f / d : 0.0f;
+  uint32_t packed = 0;
+#pragma unroll
+  for (int i = 0; i < 4; i++) {
+    const int c = id == 0.0f ? 0 : round_clamp(v[i] * id, 127);
+    packed |= ((uint32_t)c & 0xFFu) << (8 * i);
+  }
+  return packed;
 }
 
 // Device view of a plan.

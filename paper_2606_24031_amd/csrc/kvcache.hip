@@ -72,7 +72,7 @@ __global__ __launch_bounds__(KT) void append_kernel(KvPlan p, RopeArgs r,
       const int b = e4 / 8, j = e4 % 8, t = slot[row];
       uint32_t d16 = 0;
       float d32 = 0.0f;
-      const uint32_t codes = SYM ? q4_sym_block8(x, d32) : q4_0_block8(x, j, d16);
+      const uint32_t codes = SYM ? kv_q4_sym_block8(x, d32) : q4_0_block8(x, j, d16);
       const uint32_t pay = codes | (uint32_t)__shfl_xor((int)codes, 4, 8) << 4;
       if (j >= 4) continue;
       uint8_t *tile = (isv ? p.v : p.k) + (tile0[row] + h) * kv_tile_bytes(D, SYM);

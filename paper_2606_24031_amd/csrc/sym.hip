@@ -44,8 +44,8 @@ __global__ __launch_bounds__(256) void q4_sym_kernel(const float *__restrict__ w
   const bool live = blk < nblocks;
   float v[4];
   load4(w, blk, j, live, v);
-  float d;
-  const uint32_t nib = q4_sym_block8(v, d);     // stored nibbles q + 8, element i in byte i
+  const float d = amax8(v) / 7.0f;
+  const uint32_t nib = q4_sym_codes(v, d);      // stored nibbles q + 8, element i in byte i
   const uint32_t hi = __shfl_xor(nib, 4, 8);    // lanes 4..7 hold elements 16..31
   if (live && j < 4) {
     uint8_t *b = wq + blk * Q4SB;

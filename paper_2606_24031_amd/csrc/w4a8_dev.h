@@ -374,10 +374,9 @@ __device__ __forceinline__ uint32_t q4_0_block8(const float v[4], int j, uint32_
   return codes;
 }
 
-// Q4_SYM of one block by 8 lanes: the lane's four stored nibbles (code + 8),
-// one a byte, and the fp32 scale.
-__device__ __forceinline__ uint32_t q4_sym_block8(const float v[4], float &d) {
-  d = max8(fmaxf(fmaxf(fabsf(v[0]), fabsf(v[1])), fmaxf(fabsf(v[2]), fabsf(v[3])))) / 7.0f;
+// The four stored Q4_SYM nibbles (code + 8) of a lane, one a byte, for the
+// block's scale d.
+__device__ __forceinline__ uint32_t q4_sym_codes(const float v[4], float d) {
   const float id = sym_inverse(d);
   uint32_t nib = 0;
 #pragma unroll

@@ -40,26 +40,43 @@ def rotate(x, pos, f, layout="half", mscale=1.0):
 
 
 # ------------------------------------------------------------------ blocks
+# Q4_0 comes from the oracle.  The others take a scale as the binary32 product
+# with the rounded reciprocal of 7 or 127; apart from the scale their steps are
+# the oracle's Q4_SYM, Q8_0 and Q8_F32, which test_attn_abi.py checks.
+def _away(v):
+    t = np.trunc(v)
+    return np.where(np.abs(v - t) >= 0.5, t + np.sign(v), t)
+
+
+def _scaled(x, n):
+    b = np.ascontiguousarray(x, np.float32).reshape(-1, x.shape[-1] // 32, 32)
+    return b, np.abs(b).max(-1) * (np.float32(1.0) / np.float32(n))
+
+
+def _codes(b, d, n):
+    with np.errstate(divide="ignore", invalid="ignore", over="ignore"):
+        inv = np.float32(1.0) / d
+    inv = np.where((d == 0) | np.isinf(inv), np.float32(0), inv)
+    return np.clip(_away(b * inv[..., None]), -n, n)
+
+
 def codes4(x, fmt):
     """4-bit rows: (codes 0..15 with the value (code - 8) * d, scales)."""
+    if fmt == "q4_sym":
+        b, d = _scaled(x, 7)
+        return (_codes(b, d, 7) + 8).astype(np.uint8), d
     rows = np.ascontiguousarray(x, np.float32).reshape(-1, x.shape[-1])
-    raw = (oracle.q4_0_quantize if fmt == "q4_0" else oracle.q4_sym_quantize)(rows)
-    n = 18 if fmt == "q4_0" else 20
-    b = np.asarray(raw).reshape(rows.shape[0], -1, n)
-    d = np.ascontiguousarray(b[..., :n - 16]).view(np.float16 if n == 18 else np.float32)[..., 0]
-    pay = b[..., n - 16:]
-    return np.concatenate([pay & 15, pay >> 4], -1), d
+    b = np.asarray(oracle.q4_0_quantize(rows)).reshape(rows.shape[0], -1, 18)
+    d = np.ascontiguousarray(b[..., :2]).view(np.float16)[..., 0]
+    return np.concatenate([b[..., 2:] & 15, b[..., 2:] >> 4], -1), d
 
 
 def values8(x, fmt):
     """8-bit rows: the values they stand for, fp64."""
-    rows = np.ascontiguousarray(x, np.float32).reshape(-1, x.shape[-1])
-    raw = (oracle.q8_0_quantize if fmt == "q4_0" else oracle.q8_f32_quantize)(rows)
-    n = 34 if fmt == "q4_0" else 36
-    b = np.asarray(raw).reshape(rows.shape[0], -1, n)
-    d = np.ascontiguousarray(b[..., :n - 32]).view(np.float16 if n == 34 else np.float32)
-    q = np.ascontiguousarray(b[..., n - 32:]).view(np.int8)
-    return (q.astype(np.float64) * d.astype(np.float64)).reshape(x.shape)
+    b, d = _scaled(x, 127)
+    if fmt == "q4_0":
+        d = d.astype(np.float16).astype(np.float32)
+    return (_codes(b, d, 127).astype(np.float64) * d.astype(np.float64)[..., None]).reshape(x.shape)
 
 
 # ------------------------------------------------------------------ page tiles

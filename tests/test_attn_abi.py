@@ -243,3 +243,24 @@ def test_plain_logprobs_on_a_known_row():
     lp, ent, ids, top, *_ = ref.logprobs(x, [2], 3)
     assert abs(lp[0] - math.log(0.125)) < 1e-15 and abs(ent[0] - 1.75 * math.log(2)) < 1e-15
     assert list(ids[0]) == [0, 1, 2] and abs(top[0, 1] - math.log(0.25)) < 1e-15
+
+
+def test_plain_quantizers_are_the_oracles_but_for_an_ulp_of_the_scale():
+    import oracle
+    oracle.build()
+    g = np.random.default_rng(3)
+    x = (g.standard_normal((400, 64)) * np.exp2(g.integers(-8, 8, (400, 1)))).astype(np.float32)
+    raw = np.asarray(oracle.q4_sym_quantize(x)).reshape(400, 2, 20)
+    d0 = np.ascontiguousarray(raw[..., :4]).view(np.float32)[..., 0]
+    codes, d = ref.codes4(x, "q4_sym")
+    assert np.all(np.abs(d - d0) <= np.spacing(d0)) and (d != d0).any() and (d == d0).any()
+    pay = np.concatenate([raw[..., 4:] & 15, raw[..., 4:] >> 4], -1)
+    assert np.array_equal(codes[d == d0], pay[d == d0])
+    for fmt, n, q in (("q4_0", 34, oracle.q8_0_quantize), ("q4_sym", 36, oracle.q8_f32_quantize)):
+        raw = np.asarray(q(x)).reshape(400, 2, n)
+        d0 = np.ascontiguousarray(raw[..., :n - 32]).view(np.float16 if n == 34 else np.float32)
+        v0 = np.ascontiguousarray(raw[..., n - 32:]).view(np.int8).astype(np.float64) * d0
+        v = ref.values8(x, fmt).reshape(v0.shape)
+        same = (v == v0).all(-1)
+        assert same.mean() > (0.99 if n == 34 else 0.2)
+        assert np.all(np.abs(v - v0) <= 1.01 * np.abs(d0))
