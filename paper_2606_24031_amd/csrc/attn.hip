@@ -45,10 +45,6 @@ namespace w4a8 {
 
 namespace {
 
-constexpr int AT = 256;               // threads: four waves
-constexpr int AW = AT / 64;
-constexpr int CMIN = AW;              // fewest pages of a run: one a wave
-constexpr int TARGET = 512;           // runs wanted: two workgroups a compute unit
 constexpr int JT = 512;               // threads of the joining kernel
 
 typedef int v4i __attribute__((ext_vector_type(4)));
@@ -68,11 +64,12 @@ struct AttnArgs {
   float *out, *lse;
   int64_t T;
   int NH, G;
-  float k;          // |scale| * log2(e) / 16
-  float sign;       // of scale
+  float k;          // |scale| * log2(e) / 16, 1 for 0
+  float sign;       // of scale: -1, 0 or 1
   int64_t window;
   float *part;      // partial results, `slots` of them
   int slots;
+  int cmin, target; // fewest pages of a run; runs wanted
 };
 
 // What a sequence asks for.
@@ -100,10 +97,6 @@ __device__ __forceinline__ Seq seq_of(const AttnArgs &a, int s) {
   return r;
 }
 
-__device__ __forceinline__ int runs_of(const Seq &s, int C) {
-  return s.pages > C ? (s.pages + C - 1) / C : 1;
-}
-
 // Item or run `id` of the call, found by every wave on its own: 64 sequences
 // a round.  Runs (split = false): the sequence, the number within it and the
 // first partial slot of its runs; joins (split = true): counted over items
@@ -114,26 +107,29 @@ struct Found {
 template <int RT_>
 __device__ __forceinline__ bool plan_find(const AttnArgs &a, int id, bool split, Found &f) {
   const int lane = threadIdx.x & 63, B = a.p.B;
-  int64_t total = 0;
-  for (int s0 = 0; s0 < B; s0 += 64) {
-    if (s0 + lane < B) {
-      const Seq q = seq_of<RT_>(a, s0 + lane);
-      total += (int64_t)q.tiles * a.p.NKV * q.pages;
+  int items = 0, pages = 0;          // of sequence lane
+  const auto look = [&](int s) {
+    items = pages = 0;
+    if (s < B) {
+      const Seq q = seq_of<RT_>(a, s);
+      items = q.tiles * a.p.NKV;
+      pages = q.pages;
     }
+  };
+  int64_t total = 0;
+  for (int s0 = (B - 1) / 64 * 64; s0 >= 0; s0 -= 64) {     // ends with the first 64
+    look(s0 + lane);
+    total += (int64_t)items * pages;
   }
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) total += __shfl_xor(total, o);
-  const int C = (int)max((int64_t)CMIN, (total + TARGET - 1) / TARGET);
+  const int C = (int)max((int64_t)a.cmin, (total + a.target - 1) / a.target);
   int base = 0, slots = 0;
   for (int s0 = 0; s0 < B; s0 += 64) {
-    int n = 0, ns = 0, runs = 1;
-    if (s0 + lane < B) {
-      const Seq q = seq_of<RT_>(a, s0 + lane);
-      runs = runs_of(q, C);
-      const int items = q.tiles * a.p.NKV;
-      ns = runs > 1 ? items * runs : 0;
-      n = split ? (runs > 1 ? items : 0) : items * runs;
-    }
+    if (s0) look(s0 + lane);
+    const int runs = pages > C ? (pages + C - 1) / C : 1;
+    const int ns = runs > 1 ? items * runs : 0;
+    const int n = split ? (runs > 1 ? items : 0) : items * runs;
     int in = n, is = ns;              // inclusive scans
 #pragma unroll
     for (int o = 1; o < 64; o <<= 1) {
@@ -143,12 +139,10 @@ __device__ __forceinline__ bool plan_find(const AttnArgs &a, int id, bool split,
     const uint64_t hit = __ballot(id >= base + in - n && id < base + in);
     if (hit) {
       const int l = __ffsll((long long)hit) - 1;
-      f.s = s0 + l;
-      f.local = id - base - __builtin_amdgcn_readlane(in - n, l);
+      f.s = __builtin_amdgcn_readfirstlane(s0 + l);
+      f.local = __builtin_amdgcn_readfirstlane(id - base - __builtin_amdgcn_readlane(in - n, l));
       f.runs = __builtin_amdgcn_readlane(runs, l);
       f.slot0 = slots + __builtin_amdgcn_readlane(is - ns, l);
-      f.s = __builtin_amdgcn_readfirstlane(f.s);
-      f.local = __builtin_amdgcn_readfirstlane(f.local);
       return true;
     }
     base += __builtin_amdgcn_readlane(in, 63);
@@ -180,6 +174,13 @@ __device__ __forceinline__ float sum4(float x) {
   return b[0] + b[1];
 }
 
+// x * y, and 0 where either is 0, whatever the other.
+__device__ __forceinline__ float mul_zero(float x, float y) {
+  float r;
+  asm("v_mul_legacy_f32 %0, %1, %2" : "=v"(r) : "v"(x), "v"(y));
+  return r;
+}
+
 __device__ __forceinline__ float exp2_f(float x) { return __builtin_amdgcn_exp2f(x); }
 
 template <bool SYM> struct ScaleT { typedef _Float16 type; };
@@ -187,21 +188,22 @@ template <> struct ScaleT<true> { typedef float type; };
 
 // Floats between the rows of the waves' partial results in LDS: four more
 // than the columns, so rows start in different banks.
-template <int NB, int NT> struct Shape {
+template <int NB, int NT, int AW> struct Shape {
   static constexpr int D = 32 * NB;
   static constexpr int ROWS = 16 * NT;
-  static constexpr int CB = NB < 4 / NT ? NB : 4 / NT;     // blocks joined at a time (32 KB)
+  static constexpr int CB = NB < 16 / (NT * AW) ? NB : 16 / (NT * AW);   // blocks joined at a time (35 KB)
   static constexpr int LD = 32 * CB + 4;
 };
 
-template <int NB, bool SYM, int NT>
+template <int NB, bool SYM, int NT, int AW>
 struct __align__(16) Lds {
-  typedef Shape<NB, NT> Sh;
+  typedef Shape<NB, NT, AW> Sh;
   union {
     struct {
       uint32_t q[NT * NB * 64 * 2];            // Q codes in operand order
       float qd[NT * NB * 16];
-      typename ScaleT<SYM>::type ks[AW][NB * 64], vs[AW][NB * 64];
+      float vs[AW][NB * 64];
+      typename ScaleT<SYM>::type ks[AW][NB * 64];
     } in;
     float o[AW][Sh::ROWS * Sh::LD];
   };
@@ -233,13 +235,21 @@ __device__ __forceinline__ void load_words(const uint8_t *p, uint32_t (&w)[N]) {
   }
 }
 
-template <int NB, bool SYM, int NT>
-__global__ __launch_bounds__(AT, (NB * NT > 4 ? 1 : 2)) void attn_kernel(AttnArgs a) {
-  typedef Shape<NB, NT> Sh;
+// Tokens of the scales that lane `lane` stages, number i of its NB: tbase +
+// toff(i) (the inverse of kv_scale_at within a block).
+template <int NB> __device__ __forceinline__ int scale_token(int lane) {
+  const int n = lane * NB & 63;
+  return n >> 4 << 2 | (n >> 2 & 3) << 4 | (n & 3);
+}
+constexpr int scale_token_off(int i) { return (i >> 2) * 16 + (i & 3); }
+
+template <int NB, bool SYM, int NT, int AW>
+__global__ __launch_bounds__(64 * AW, 2) void attn_kernel(AttnArgs a) {
+  typedef Shape<NB, NT, AW> Sh;
   typedef typename ScaleT<SYM>::type sc_t;
-  constexpr int D = Sh::D, ROWS = Sh::ROWS, SW = Page<NB, SYM>::SW;
+  constexpr int D = Sh::D, ROWS = Sh::ROWS, SW = Page<NB, SYM>::SW, AT = 64 * AW;
   constexpr int64_t TILE = kv_tile_bytes(D, SYM);
-  __shared__ Lds<NB, SYM, NT> lds;
+  __shared__ Lds<NB, SYM, NT, AW> lds;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
   const int g = lane >> 4;
 
@@ -260,29 +270,66 @@ __global__ __launch_bounds__(AT, (NB * NT > 4 ? 1 : 2)) void attn_kernel(AttnArg
     int phi = min(sq.lo + min(sq.pages, (run + 1) * per), pos1 < 0 ? 0 : pos1 / KV_PAGE + 1);
     if (a.p.n_pages == 0) phi = plo;
 
-    // Q codes and scales of the tile's rows (rows past the last repeat it)
-    for (int i = threadIdx.x; i < ROWS * NB * 8; i += AT) {
-      const int j = i & 7, blk = i >> 3, row = blk / NB, b = blk % NB;
-      const int fr = f0 + min(row, fn - 1);
-      const float4 x = *reinterpret_cast<const float4 *>(
+    const int32_t *table = a.p.pages + (int64_t)f.s * a.p.max_pages;
+    const int64_t head = (int64_t)h * TILE;
+    const auto present = [&](int page) { return page >= 0 && page < a.p.n_pages; };
+    const auto tile_at = [&](int page) {
+      return (int64_t)(present(page) ? page : 0) * a.p.NKV * TILE + head;
+    };
+    Page<NB, SYM> pg;
+    const auto load_k = [&](int page) {
+      const uint8_t *t = a.p.k + tile_at(page);
+#pragma unroll
+      for (int b = 0; b < NB; b++) pg.k[b] = reinterpret_cast<const v4u *>(t + b * 1024)[lane];
+      load_words(t + NB * 1024 + lane * (SW * 4), pg.ks);
+    };
+    const auto load_v = [&](int page) {
+      const uint8_t *t = a.p.v + tile_at(page);
+      load_words(t + NB * 1024 + lane * (SW * 4), pg.vs);
+#pragma unroll
+      for (int b = 0; b < NB; b++) pg.v[b] = reinterpret_cast<const v4u *>(t + b * 1024)[lane];
+    };
+    int at = plo + wave;
+    int page = at < phi ? table[at] : -1;
+
+    // Q codes and scales of the tile's rows (rows past the last repeat it);
+    // the first page's loads go out behind Q's
+    constexpr int QI = ROWS * NB * 8 / AT > 0 ? ROWS * NB * 8 / AT : 1;
+    v4f x[QI];
+#pragma unroll
+    for (int k = 0; k < QI; k++) {
+      const int i = threadIdx.x + k * AT, j = i & 7, blk = i >> 3;
+      const int row = min(blk / NB, ROWS - 1), b = blk % NB, fr = f0 + min(row, fn - 1);
+      x[k] = *reinterpret_cast<const v4f *>(
           a.q + (sq.r0 + fr / a.G) * a.qs + (int64_t)(h * a.G + fr % a.G) * D + b * 32 + 4 * j);
-      const float v[4] = {x.x, x.y, x.z, x.w};
+    }
+    if (at < phi) {
+      load_k(page);
+      load_v(page);
+    }
+#pragma unroll
+    for (int k = 0; k < QI; k++) {
+      const int i = threadIdx.x + k * AT, j = i & 7, blk = i >> 3, row = blk / NB, b = blk % NB;
+      const float v[4] = {x[k][0], x[k][1], x[k][2], x[k][3]};
       float d;
       const uint32_t codes = kv_q8_block8<SYM>(v, d);
       const int nt = row >> 4, r = row & 15;
-      lds.in.q[((nt * NB + b) * 64 + 16 * (j & 3) + r) * 2 + (j >> 2)] = codes;
-      if (j == 0) lds.in.qd[(nt * NB + b) * 16 + r] = d * a.sign;
+      if (row < ROWS) {
+        lds.in.q[((nt * NB + b) * 64 + 16 * (j & 3) + r) * 2 + (j >> 2)] = codes;
+        if (j == 0) lds.in.qd[(nt * NB + b) * 16 + r] = d * a.sign;
+      }
     }
     __syncthreads();
 
-    // this lane's rows
-    int hi_key[NT], lo_key[NT];       // sees lo_key < key <= hi_key
+    // this lane's rows see lo_key < key <= hi_key; both less 4 g, the lane's first key of a page
+    int hi_key[NT], lo_key[NT];
 #pragma unroll
     for (int nt = 0; nt < NT; nt++) {
       const int pos = base_pos + (f0 + min(16 * nt + (lane & 15), fn - 1)) / a.G;
-      hi_key[nt] = pos;
-      lo_key[nt] = a.window > 0 && a.window <= pos ? (int)(pos - a.window) : -1;
+      hi_key[nt] = pos - 4 * g;
+      lo_key[nt] = (a.window > 0 && a.window <= pos ? (int)(pos - a.window) : -1) - 4 * g;
     }
+    const int tbase = scale_token<NB>(lane);
 
     float m[NT], mk[NT], l[NT];
     v4f acc[NT][NB][2];
@@ -296,75 +343,55 @@ __global__ __launch_bounds__(AT, (NB * NT > 4 ? 1 : 2)) void attn_kernel(AttnArg
     }
     // value scales are below 2^vexp and enter the product times 2^(15 - vexp)
     int vexp = -126;
-    const int32_t *table = a.p.pages + (int64_t)f.s * a.p.max_pages;
-    const int64_t head = (int64_t)h * TILE;
-    const auto tile_at = [&](int page) {
-      return ((int64_t)page * a.p.NKV) * TILE + head;
-    };
-    const auto present = [&](int page) { return page >= 0 && page < a.p.n_pages; };
-
-    Page<NB, SYM> pg;
-    const auto load_k = [&](int page) {
-      const uint8_t *t = a.p.k + tile_at(present(page) ? page : 0);
-#pragma unroll
-      for (int b = 0; b < NB; b++) pg.k[b] = reinterpret_cast<const v4u *>(t + b * 1024)[lane];
-      load_words(t + NB * 1024 + lane * (SW * 4), pg.ks);
-    };
-    const auto load_v = [&](int page) {
-      const uint8_t *t = a.p.v + tile_at(present(page) ? page : 0);
-      load_words(t + NB * 1024 + lane * (SW * 4), pg.vs);
-#pragma unroll
-      for (int b = 0; b < NB; b++) pg.v[b] = reinterpret_cast<const v4u *>(t + b * 1024)[lane];
-    };
-
-    int at = plo + wave;
-    int page = at < phi ? table[at] : -1;
-    if (at < phi) {
-      load_k(page);
-      load_v(page);
-    }
-    sc_t *ks = lds.in.ks[wave], *vs = lds.in.vs[wave];
+    sc_t *ks = lds.in.ks[wave];
+    float *vs = lds.in.vs[wave];
+    float minus = -1.0f;               // opaque, so that the halves' difference is one mixed FMA
+    asm("" : "+v"(minus));
     for (; at < phi; at += AW) {
       const int next_page = at + AW < phi ? table[at + AW] : -1;
-      const bool here = present(page);
       const int key = at * KV_PAGE;
-      const bool masked = key + KV_PAGE - 1 > pos0 || (a.window > 0 && key <= pos1 - a.window);
+      // pages that some row does not see whole; an absent page is seen by none
+      const bool here = present(page);
+      const bool masked = !here || key + KV_PAGE - 1 > pos0 ||
+                          (a.window > 0 && key <= pos1 - a.window);
       // stage the scales; keys that no row sees count for nothing
-      float vmax = 0.0f;
-      bool odd = false;
 #pragma unroll
       for (int w = 0; w < SW; w++) reinterpret_cast<word *>(ks)[lane * SW + w] = pg.ks[w];
-      float dv[NB];
+      {
+        float dv[NB], vmax = 0.0f;
 #pragma unroll
-      for (int i = 0; i < NB; i++) {
-        dv[i] = SYM ? __builtin_bit_cast(float, pg.vs[i % SW])
-                    : f16_bits_to_f32(pg.vs[(i / 2) % SW] >> (16 * (i & 1)));
+        for (int i = 0; i < NB; i++)
+          dv[i] = SYM ? __builtin_bit_cast(float, pg.vs[i % SW])
+                      : f16_bits_to_f32(pg.vs[(i / 2) % SW] >> (16 * (i & 1)));
         if (masked) {
-          const int n = (lane * NB + i) & 63, t = n >> 4 << 2 | (n >> 2 & 3) << 4 | (n & 3);
-          if (key + t > pos1 || key + t < key0) dv[i] = 0.0f;
+          const int last = here ? pos1 - key - tbase : -1;
+          const int before = (int)max((int64_t)0, key0 - key) - tbase;
+#pragma unroll
+          for (int i = 0; i < NB; i++)
+            if (scale_token_off(i) > last || scale_token_off(i) < before) dv[i] = 0.0f;
         }
-        const float x = fabsf(dv[i]);
-        const bool fin = x < INFINITY;
-        odd |= !fin;
-        vmax = fmaxf(vmax, fin ? x : 0.0f);
+#pragma unroll
+        for (int i = 0; i < NB; i++) {
+          const float y = fabsf(dv[i]);
+          vmax = fmaxf(vmax, y < INFINITY ? y : 0.0f);
+        }
+        if (__ballot(vmax >= ldexpf(1.0f, vexp))) {
+#pragma unroll
+          for (int o = 32; o > 0; o >>= 1) vmax = fmaxf(vmax, __shfl_xor(vmax, o));
+          const int e = __builtin_amdgcn_readfirstlane(ilogbf(vmax) + 1);
+#pragma unroll
+          for (int nt = 0; nt < NT; nt++)
+#pragma unroll
+            for (int b = 0; b < NB; b++)
+#pragma unroll
+              for (int s = 0; s < 2; s++)
+#pragma unroll
+                for (int y = 0; y < 4; y++) acc[nt][b][s][y] = ldexpf(acc[nt][b][s][y], vexp - e);
+          vexp = e;
+        }
+#pragma unroll
+        for (int i = 0; i < NB; i++) vs[lane * NB + i] = ldexpf(dv[i], 15 - vexp);
       }
-      const bool guard = masked && __ballot(odd);
-      if (here && __ballot(vmax >= ldexpf(1.0f, vexp))) {
-#pragma unroll
-        for (int o = 32; o > 0; o >>= 1) vmax = fmaxf(vmax, __shfl_xor(vmax, o));
-        const int e = __builtin_amdgcn_readfirstlane(ilogbf(vmax) + 1);
-#pragma unroll
-        for (int nt = 0; nt < NT; nt++)
-#pragma unroll
-          for (int b = 0; b < NB; b++)
-#pragma unroll
-            for (int s = 0; s < 2; s++)
-#pragma unroll
-              for (int x = 0; x < 4; x++) acc[nt][b][s][x] = ldexpf(acc[nt][b][s][x], vexp - e);
-        vexp = e;
-      }
-#pragma unroll
-      for (int i = 0; i < NB; i++) vs[lane * NB + i] = (sc_t)ldexpf(dv[i], 15 - vexp);
 
       // scores
       float S[NT][16];
@@ -387,8 +414,8 @@ __global__ __launch_bounds__(AT, (NB * NT > 4 ? 1 : 2)) void attn_kernel(AttnArg
         for (int i = 0; i < 16; i++) dk[i] = ks[b * 64 + g * 16 + i];
 #pragma unroll
         for (int i = 0; i < 4; i++) {
-          const uint32_t x = pg.k[b][i];
-          const long kb = (long)((uint64_t)(x & 0xF0F0F0F0u) << 32 | (x << 4 & 0xF0F0F0F0u));
+          const uint32_t y = pg.k[b][i];
+          const long kb = (long)((uint64_t)(y & 0xF0F0F0F0u) << 32 | (y << 4 & 0xF0F0F0F0u));
 #pragma unroll
           for (int nt = 0; nt < NT; nt++) {
             const v4i c = {0x4B400000, 0x4B400000, 0x4B400000, 0x4B400000};
@@ -402,115 +429,112 @@ __global__ __launch_bounds__(AT, (NB * NT > 4 ? 1 : 2)) void attn_kernel(AttnArg
             }
           }
         }
+        // one block at a time: moved together, the blocks' products and scales
+        // would all be live at once
+#pragma unroll
+        for (int nt = 0; nt < NT; nt++)
+#pragma unroll
+          for (int i = 0; i < 16; i++) asm volatile("" : "+v"(S[nt][i]));
       }
       if (at + AW < phi) load_k(next_page);
 
-      if (here) {
-        // running maximum
-        float mx[NT];
-        bool grow = false;
+      // running maximum
+      float mx[NT];
+      bool grow = false;
+#pragma unroll
+      for (int nt = 0; nt < NT; nt++) {
+        if (masked) {
+          const int last = here ? hi_key[nt] - key : -1, before = lo_key[nt] - key;
+#pragma unroll
+          for (int i = 0; i < 16; i++)
+            if (scale_token_off(i) > last || scale_token_off(i) <= before) S[nt][i] = -INFINITY;
+        }
+        mx[nt] = -FLT_MAX;
+#pragma unroll
+        for (int i = 0; i < 16; i++) mx[nt] = fmaxf(mx[nt], S[nt][i]);
+        mx[nt] = max4(mx[nt]);
+        grow |= mx[nt] > m[nt];
+      }
+      if (__ballot(grow)) {
 #pragma unroll
         for (int nt = 0; nt < NT; nt++) {
-          mx[nt] = -FLT_MAX;
-          if (masked) {
+          const float mn = fmaxf(m[nt], mx[nt]), mkn = mn * a.k;
+          const float al = m[nt] == -FLT_MAX ? 0.0f : exp2_f(mk[nt] - mkn);
+          m[nt] = mn;
+          mk[nt] = mkn;
+          l[nt] *= al;
 #pragma unroll
-            for (int i = 0; i < 16; i++) {
-              const int kk = key + (i >> 2) * 16 + g * 4 + (i & 3);
-              if (!(kk <= hi_key[nt] && kk > lo_key[nt])) S[nt][i] = -INFINITY;
-            }
-          }
-#pragma unroll
-          for (int i = 0; i < 16; i++) mx[nt] = fmaxf(mx[nt], S[nt][i]);
-          mx[nt] = max4(mx[nt]);
-          grow |= mx[nt] > m[nt];
-        }
-        if (__ballot(grow)) {
-#pragma unroll
-          for (int nt = 0; nt < NT; nt++) {
-            const float mn = fmaxf(m[nt], mx[nt]), mkn = mn * a.k;
-            const float al = m[nt] == -FLT_MAX ? 0.0f : exp2_f(mk[nt] - mkn);
-            m[nt] = mn;
-            mk[nt] = mkn;
-            l[nt] *= al;
-#pragma unroll
-            for (int b = 0; b < NB; b++) {
-              acc[nt][b][0] *= al;
-              acc[nt][b][1] *= al;
-            }
+          for (int b = 0; b < NB; b++) {
+            acc[nt][b][0] *= al;
+            acc[nt][b][1] *= al;
           }
         }
-        // probabilities
+      }
+      // probabilities (a masked score's is exp2(-infinity) = 0)
 #pragma unroll
-        for (int nt = 0; nt < NT; nt++) {
+      for (int nt = 0; nt < NT; nt++) {
 #pragma unroll
-          for (int i = 0; i < 16; i++) {
-            const float x = S[nt][i];
-            const float p = exp2_f(fmaf(x, a.k, -mk[nt]));
-            S[nt][i] = masked && x == -INFINITY ? 0.0f : p;
-          }
-          float s[8];
+        for (int i = 0; i < 16; i++) S[nt][i] = exp2_f(fmaf(S[nt][i], a.k, -mk[nt]));
+        float s[8];
 #pragma unroll
-          for (int i = 0; i < 8; i++) s[i] = S[nt][i] + S[nt][i + 8];
+        for (int i = 0; i < 8; i++) s[i] = S[nt][i] + S[nt][i + 8];
 #pragma unroll
-          for (int o = 4; o > 0; o >>= 1)
+        for (int o = 4; o > 0; o >>= 1)
 #pragma unroll
-            for (int i = 0; i < o; i++) s[i] += s[i + o];
-          l[nt] += s[0];
-        }
-        // values
+          for (int i = 0; i < o; i++) s[i] += s[i + o];
+        l[nt] += s[0];
+      }
+      __builtin_amdgcn_sched_barrier(0);
+      // values, 32 keys at a time
 #pragma unroll
-        for (int b = 0; b < NB; b++) {
-          sc_t d[16];
+      for (int b = 0; b < NB; b++) {
 #pragma unroll
-          for (int i = 0; i < 16; i++) d[i] = vs[b * 64 + g * 16 + i];
-          h8 hi[NT][2], lo[NT][2];
+        for (int hh = 0; hh < 2; hh++) {
+          float d[8];
 #pragma unroll
-          for (int nt = 0; nt < NT; nt++) {
-            float w[16];
+          for (int i = 0; i < 8; i++) d[i] = vs[b * 64 + g * 16 + 8 * hh + i];
+          h8 c[2];                       // elements l % 16 and + 16
 #pragma unroll
-            for (int i = 0; i < 16; i++) w[i] = fmaf(S[nt][i], (float)d[i], 0.0f);
-            if (guard) {
-#pragma unroll
-              for (int i = 0; i < 16; i++) w[i] = S[nt][i] == 0.0f ? 0.0f : w[i];
-            }
-#pragma unroll
-            for (int i = 0; i < 16; i++) {
-              const _Float16 x = (_Float16)w[i];
-              hi[nt][i >> 3][i & 7] = x;
-              lo[nt][i >> 3][i & 7] = (_Float16)fmaf((float)x, -1.0f, w[i]);
-            }
-          }
-          h8 c[2][2];                      // [element half][key half]
-#pragma unroll
-          for (int i = 0; i < 4; i++) {
-            const uint32_t x = pg.v[b][i], y = x >> 8;
+          for (int i = 0; i < 2; i++) {
+            const uint32_t y = pg.v[b][2 * hh + i], z = y >> 8;
             const h2 off = {(_Float16)-1032.0f, (_Float16)-1032.0f};
             const h2 six = {(_Float16)0.0625f, (_Float16)0.0625f};
             const h2 off2 = {(_Float16)-72.0f, (_Float16)-72.0f};
-            const h2 a0 = __builtin_bit_cast(h2, (x & 0x000F000Fu) | 0x64006400u) + off;
-            const h2 a1 = __builtin_bit_cast(h2, (y & 0x000F000Fu) | 0x64006400u) + off;
+            const h2 a0 = __builtin_bit_cast(h2, (y & 0x000F000Fu) | 0x64006400u) + off;
+            const h2 a1 = __builtin_bit_cast(h2, (z & 0x000F000Fu) | 0x64006400u) + off;
             const h2 b0 = __builtin_elementwise_fma(
-                __builtin_bit_cast(h2, (x & 0x00F000F0u) | 0x64006400u), six, off2);
-            const h2 b1 = __builtin_elementwise_fma(
                 __builtin_bit_cast(h2, (y & 0x00F000F0u) | 0x64006400u), six, off2);
-            const int at4 = 4 * (i & 1);
-            c[0][i >> 1][at4] = a0[0]; c[0][i >> 1][at4 + 1] = a0[1];
-            c[0][i >> 1][at4 + 2] = a1[0]; c[0][i >> 1][at4 + 3] = a1[1];
-            c[1][i >> 1][at4] = b0[0]; c[1][i >> 1][at4 + 1] = b0[1];
-            c[1][i >> 1][at4 + 2] = b1[0]; c[1][i >> 1][at4 + 3] = b1[1];
+            const h2 b1 = __builtin_elementwise_fma(
+                __builtin_bit_cast(h2, (z & 0x00F000F0u) | 0x64006400u), six, off2);
+            c[0][4 * i] = a0[0]; c[0][4 * i + 1] = a0[1]; c[0][4 * i + 2] = a1[0]; c[0][4 * i + 3] = a1[1];
+            c[1][4 * i] = b0[0]; c[1][4 * i + 1] = b0[1]; c[1][4 * i + 2] = b1[0]; c[1][4 * i + 3] = b1[1];
           }
 #pragma unroll
-          for (int nt = 0; nt < NT; nt++)
+          for (int nt = 0; nt < NT; nt++) {
+            h8 hi, lo;
 #pragma unroll
-            for (int s = 0; s < 2; s++)
+            for (int i = 0; i < 8; i += 2) {
+              v2f w;
+              // 0 times anything is 0: a key that the row does not see may have any scale
+              w[0] = mul_zero(S[nt][8 * hh + i], d[i]);
+              w[1] = mul_zero(S[nt][8 * hh + i + 1], d[i + 1]);
+              const h2 y = __builtin_convertvector(w, h2);
+              v2f z;
+              z[0] = fmaf((float)y[0], minus, w[0]);
+              z[1] = fmaf((float)y[1], minus, w[1]);
+              const h2 y2 = __builtin_convertvector(z, h2);
+              hi[i] = y[0]; hi[i + 1] = y[1];
+              lo[i] = y2[0]; lo[i + 1] = y2[1];
+            }
 #pragma unroll
-              for (int hh = 0; hh < 2; hh++) {
-                acc[nt][b][s] = __builtin_amdgcn_mfma_f32_16x16x32_f16(c[s][hh], hi[nt][hh],
-                                                                       acc[nt][b][s], 0, 0, 0);
-                acc[nt][b][s] = __builtin_amdgcn_mfma_f32_16x16x32_f16(c[s][hh], lo[nt][hh],
-                                                                       acc[nt][b][s], 0, 0, 0);
-              }
+            for (int s = 0; s < 2; s++) {
+              acc[nt][b][s] = __builtin_amdgcn_mfma_f32_16x16x32_f16(c[s], hi, acc[nt][b][s], 0, 0, 0);
+              acc[nt][b][s] = __builtin_amdgcn_mfma_f32_16x16x32_f16(c[s], lo, acc[nt][b][s], 0, 0, 0);
+            }
+          }
         }
+        #pragma unroll
+          for (int nt = 0; nt < NT; nt++) asm volatile("" : "+v"(acc[nt][b][0]), "+v"(acc[nt][b][1]));
       }
       if (at + AW < phi) load_v(next_page);
       page = next_page;
@@ -663,10 +687,14 @@ __global__ __launch_bounds__(JT) void join_kernel(AttnArgs a) {
 // Rows of a tile: 32 once sequences have more than 16 on average (a tile's
 // rows share the page's loads and decoded codes), 16 for the few rows of a
 // decode step, and for D = 256, whose 32-row sums would not fit in registers.
+// Waves of a workgroup: 8 on 16-row tiles, so that a short context needs no
+// second launch, 4 on 32-row ones.
 int tile_rows(const w4a8_kv *kv, int64_t T, int64_t NH) {
   const int64_t rows = T * (NH / kv->NKV);
   return kv->D <= 128 && kv->B > 0 && rows > 16 * kv->B ? 32 : 16;
 }
+constexpr int CMIN = 16;              // fewest pages of a run
+constexpr int TARGET = 512;           // runs wanted
 
 // Bounds on the call's items, and on the partial results it can need: a
 // sequence is split only into runs of more than half of C = total / TARGET
@@ -690,14 +718,21 @@ int attn_sizes(const w4a8_kv *kv, int64_t T, int64_t NH) {
   return W4A8_OK;
 }
 
-template <int NB, bool SYM, int NT>
+template <int NB, bool SYM, int NT, int AW>
 int launch(const AttnArgs &a, int64_t items, hipStream_t s) {
   const int64_t grid = std::min<int64_t>(items + a.slots, 1 << 20);
-  attn_kernel<NB, SYM, NT><<<dim3((unsigned)grid), dim3(AT), 0, s>>>(a);
+  attn_kernel<NB, SYM, NT, AW><<<dim3((unsigned)grid), dim3(64 * AW), 0, s>>>(a);
   if (int rc = check_launch(); rc != W4A8_OK || a.slots == 0) return rc;
   const int64_t joins = std::min<int64_t>(items, TARGET);
   join_kernel<NB, NT><<<dim3((unsigned)joins, 16 * NT), dim3(JT), 0, s>>>(a);
   return check_launch();
+}
+
+template <int NB, bool SYM>
+int launch_rows(const AttnArgs &a, bool wide, int64_t items, hipStream_t s) {
+  if constexpr (NB <= 4)
+    if (wide) return launch<NB, SYM, 2, 4>(a, items, s);
+  return launch<NB, SYM, 1, 8>(a, items, s);
 }
 
 }  // namespace
@@ -728,18 +763,14 @@ extern "C" int attn_q4_forward(const w4a8_kv *kv, const float *q, int64_t q_stri
   if (T == 0 || kv->B == 0) return W4A8_OK;
   if (int rc = check_device(); rc != W4A8_OK) return rc;
   AttnArgs a = {kv_plan(kv), q, q_stride, out, lse, T, (int)NH, (int)(NH / kv->NKV),
-                std::fabs(scale) * 1.44269504f / 16.0f, scale < 0.0f ? -1.0f : 1.0f, window,
-                reinterpret_cast<float *>(workspace), (int)slots_bound(kv, T, NH)};
+                // a factor of 0 goes to Q, so that a masked score's -infinity stays one
+                scale != 0.0f ? std::fabs(scale) * 1.44269504f / 16.0f : 1.0f,
+                scale < 0.0f ? -1.0f : scale == 0.0f ? 0.0f : 1.0f, window,
+                reinterpret_cast<float *>(workspace), (int)slots_bound(kv, T, NH), CMIN, TARGET};
   const int64_t items = items_bound(kv, T, NH);
   const bool sym = kv->format == W4A8_KV_Q4_SYM, wide = tile_rows(kv, T, NH) == 32;
   const hipStream_t s = as_stream(stream);
-  if (kv->D == 64) {
-    if (wide) return sym ? launch<2, true, 2>(a, items, s) : launch<2, false, 2>(a, items, s);
-    return sym ? launch<2, true, 1>(a, items, s) : launch<2, false, 1>(a, items, s);
-  }
-  if (kv->D == 128) {
-    if (wide) return sym ? launch<4, true, 2>(a, items, s) : launch<4, false, 2>(a, items, s);
-    return sym ? launch<4, true, 1>(a, items, s) : launch<4, false, 1>(a, items, s);
-  }
-  return sym ? launch<8, true, 1>(a, items, s) : launch<8, false, 1>(a, items, s);
+  if (kv->D == 64) return sym ? launch_rows<2, true>(a, wide, items, s) : launch_rows<2, false>(a, wide, items, s);
+  if (kv->D == 128) return sym ? launch_rows<4, true>(a, wide, items, s) : launch_rows<4, false>(a, wide, items, s);
+  return sym ? launch_rows<8, true>(a, wide, items, s) : launch_rows<8, false>(a, wide, items, s);
 }
