@@ -2,33 +2,37 @@
 // are softmax attention with grouped query heads; Sec. 3.2 runs it in one
 // pass with a running maximum and sum).
 //
-// A work item is a tile of 16 or 32 query rows of one KV head of a sequence
-// (row f of a sequence: token f / G, head f % G of the group), times a run of
-// pages when the rows alone would leave compute units idle; a second launch
-// then joins the runs' partial results in a fixed order.  The four waves of a
-// workgroup take the item's pages in turn, each on its own: no barrier until
-// they join.  A wave takes a page of 64 keys at a time, everything in
-// registers but the block scales:
-//   scores   S^T = K Q^T: one v_mfma_i32_16x16x32_i8 per 16 keys, 16 rows and
-//            block of 32, K codes straight from the page (a 16-byte load a
-//            lane and block), Q codes from LDS.  The accumulator starts at
-//            0x4B400000, so the int32 result read as a float is 1.5 2^23 +
-//            16 s; with the row's fp16 scale d_q one FMA gives 16 s d_q
-//            rounded once, the second adds it times d_k.
-//   softmax  base 2 with a running maximum m per row: rescaled only on pages
-//            where some row's maximum grows.  fp32.
-//   values   O^T += V^T W^T with W = p d_v per block of 32 columns: V codes
-//            are small integers, exact in fp16, and W goes in as hi + lo, two
-//            fp16 halves (22 bits; one fp16 or bf16 would be off by 2^-12 or
-//            2^-9, more than everything else here together).  d_v is scaled
-//            by a power of two, kept per wave, to put the largest value scale
-//            met so far just below 2^15: halves neither overflow nor lose
-//            bits unless a block's scale lies 2^17 and more below it.
-// The lane layout of the score product's result (row l % 16, keys 4 (l / 16)
-// + e) is the one the value product wants for W, so probabilities never leave
-// the lane, and both products keep a query row in one lane column, so the
-// running maximum and sum need only exchanges between lanes l, l+16, l+32,
-// l+48.
+// A work item is a tile of 16 NT query rows of one KV head of a sequence (row
+// f of a sequence: token f / G, head f % G of the group), times a run of pages
+// when the rows alone would leave compute units idle; a second launch then
+// joins the runs' partial results in a fixed order.  A workgroup of AW waves
+// takes AW pages of 64 keys a step:
+//   scores   each wave its own page.  S^T = K Q^T: one
+//            v_mfma_i32_16x16x32_i8 per 16 keys, 16 rows and block of 32, K
+//            codes straight from the page (a 16-byte load a lane and block), Q
+//            codes from LDS.  The accumulator starts at 0x4B400000, so the
+//            int32 result read as a float is 1.5 2^23 + 16 s; with the row's
+//            fp16 scale d_q one FMA gives 16 s d_q rounded once, the second
+//            adds it times d_k.
+//   softmax  base 2 with a running maximum per row, exchanged between the
+//            waves through LDS; sums rescaled only on steps where some row's
+//            maximum grows.  fp32.  The probabilities go to LDS, as each
+//            lane holds them.
+//   values   each wave its own block of 32 columns (of PS sets of the step's
+//            pages where there are more waves than blocks): O^T += V^T W^T
+//            with W = p d_v.  V codes are small integers, exact in fp16; W
+//            goes in as hi + lo, two fp16 halves (22 bits; one fp16 or bf16
+//            would be off by 2^-12 or 2^-9, more than everything else here
+//            together).  d_v is scaled by a power of two, kept per wave, to
+//            put the largest value scale met so far just below 2^15: halves
+//            neither overflow nor lose bits unless a key's scale lies 2^17
+//            and more below it.
+// Scores by keys and values by columns: a wave's sums are 32 columns, not D,
+// so registers leave room for two and more waves a SIMD, the code stays small
+// (a short decode is bound by fetching it once) and no sums are exchanged at
+// the end.  The lane layout of the score product's result (row l % 16, keys
+// 4 (l / 16) + e + 16 i) is the one the value product wants for W, so a lane
+// reads back from LDS what the same lane of another wave wrote.
 // Bound: long decodes by HBM (36 bytes a key and 32 columns of K and V, read
 // once for all G heads of a group) and by VALU issue, which is close behind;
 // prompts by VALU issue: the two scaling operations a score and block and the
@@ -45,7 +49,8 @@ namespace w4a8 {
 
 namespace {
 
-constexpr int JT = 512;               // threads of the joining kernel
+constexpr int TARGET = 512;           // runs wanted: two workgroups a compute unit
+constexpr int JOIN_MAX = 2 * TARGET;  // most runs of an item
 
 typedef int v4i __attribute__((ext_vector_type(4)));
 typedef float v4f __attribute__((ext_vector_type(4)));
@@ -69,7 +74,8 @@ struct AttnArgs {
   int64_t window;
   float *part;      // partial results, `slots` of them
   int slots;
-  int cmin, target; // fewest pages of a run; runs wanted
+  int cmin;         // fewest pages of a run
+  float inv_G;      // 1 / G
 };
 
 // What a sequence asks for.
@@ -97,50 +103,66 @@ __device__ __forceinline__ Seq seq_of(const AttnArgs &a, int s) {
   return r;
 }
 
-// Item or run `id` of the call, found by every wave on its own: 64 sequences
-// a round.  Runs (split = false): the sequence, the number within it and the
-// first partial slot of its runs; joins (split = true): counted over items
-// with several runs only.  Returns false past the end.
+// Inclusive scan of a wave's values by DPP moves.
+template <int CTRL, int ROWS_, typename T_> __device__ __forceinline__ T_ dpp_or_0(T_ x) {
+  const int v = __builtin_bit_cast(int, x);
+  return __builtin_bit_cast(T_, __builtin_amdgcn_update_dpp(0, v, CTRL, ROWS_, 0xF, true));
+}
+template <typename T_> __device__ __forceinline__ T_ wave_scan(T_ x) {
+  x += dpp_or_0<0x111, 0xF>(x);      // row_shr 1, 2, 4, 8
+  x += dpp_or_0<0x112, 0xF>(x);
+  x += dpp_or_0<0x114, 0xF>(x);
+  x += dpp_or_0<0x118, 0xF>(x);
+  x += dpp_or_0<0x142, 0xA>(x);      // row 0's and 2's last into rows 1 and 3
+  x += dpp_or_0<0x143, 0xC>(x);      // row 1's last into rows 2 and 3
+  return x;
+}
+
+// Item or run `id` of the call, found by every wave on its own, 64 sequences
+// a round.  A sequence's items fall into runs of at most C pages, C such that
+// the call has about TARGET runs (of several tiles, whose first see half the
+// pages of the last on average, only from 2 C on).  Runs (split = false): the sequence, the
+// number within it and the first partial slot of its runs; joins (split =
+// true): counted over items with several runs only.  False past the end.
 struct Found {
   int s, local, runs, slot0;
 };
 template <int RT_>
 __device__ __forceinline__ bool plan_find(const AttnArgs &a, int id, bool split, Found &f) {
   const int lane = threadIdx.x & 63, B = a.p.B;
-  int items = 0, pages = 0;          // of sequence lane
+  int tiles = 0, items = 0, pages = 0;          // of sequence lane
   const auto look = [&](int s) {
-    items = pages = 0;
+    tiles = items = pages = 0;
     if (s < B) {
       const Seq q = seq_of<RT_>(a, s);
-      items = q.tiles * a.p.NKV;
+      tiles = q.tiles;
+      items = tiles * a.p.NKV;
       pages = q.pages;
     }
   };
-  int64_t total = 0;
+  float total = 0.0f;
   for (int s0 = (B - 1) / 64 * 64; s0 >= 0; s0 -= 64) {     // ends with the first 64
     look(s0 + lane);
-    total += (int64_t)items * pages;
+    total += (float)items * (float)pages;
   }
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) total += __shfl_xor(total, o);
-  const int C = (int)max((int64_t)a.cmin, (total + a.target - 1) / a.target);
+  total = __builtin_bit_cast(
+      float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, wave_scan(total)), 63));
+  // (rounded up past the sum's own rounding: the partial slots are counted on C)
+  const float c = fminf(total * (1.001f / TARGET), 1e9f);
+  int C = max(a.cmin, (int)c + 1);
+  C = (C + a.cmin - 1) / a.cmin * a.cmin;            // whole steps
   int base = 0, slots = 0;
   for (int s0 = 0; s0 < B; s0 += 64) {
     if (s0) look(s0 + lane);
-    const int runs = pages > C ? (pages + C - 1) / C : 1;
+    const int runs = pages > (tiles > 1 ? 2 * C : C) ? (pages + C - 1) / C : 1;
     const int ns = runs > 1 ? items * runs : 0;
     const int n = split ? (runs > 1 ? items : 0) : items * runs;
-    int in = n, is = ns;              // inclusive scans
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-      const int x = __shfl_up(in, o), y = __shfl_up(is, o);
-      if (lane >= o) { in += x; is += y; }
-    }
+    const int in = wave_scan(n), is = wave_scan(ns);
     const uint64_t hit = __ballot(id >= base + in - n && id < base + in);
     if (hit) {
       const int l = __ffsll((long long)hit) - 1;
-      f.s = __builtin_amdgcn_readfirstlane(s0 + l);
-      f.local = __builtin_amdgcn_readfirstlane(id - base - __builtin_amdgcn_readlane(in - n, l));
+      f.s = s0 + l;
+      f.local = id - base - __builtin_amdgcn_readlane(in - n, l);
       f.runs = __builtin_amdgcn_readlane(runs, l);
       f.slot0 = slots + __builtin_amdgcn_readlane(is - ns, l);
       return true;
@@ -150,6 +172,23 @@ __device__ __forceinline__ bool plan_find(const AttnArgs &a, int id, bool split,
   }
   return false;
 }
+
+// Rows of a tile: row r is head head(r) of the group of the sequence's token
+// token(r).  G < 2^16 and r < 64, so the quotient is exact in fp32.
+struct RowMap {
+  int t0, rem, G;
+  float inv;
+  __device__ RowMap(const AttnArgs &a, int f0) {
+    G = a.G;
+    inv = a.inv_G;
+    t0 = f0 / G;
+    rem = f0 - t0 * G;
+  }
+  __device__ __forceinline__ int token(int r) const {
+    return t0 + (int)(((float)(rem + r) + 0.5f) * inv);
+  }
+  __device__ __forceinline__ int head(int r, int t) const { return rem + r - (t - t0) * G; }
+};
 
 // Maximum and sum over lanes l, l ^ 16, l ^ 32, l ^ 48.  (The results are cast
 // as whole vectors: a bit cast of one element folds to element 0.)
@@ -186,38 +225,29 @@ __device__ __forceinline__ float exp2_f(float x) { return __builtin_amdgcn_exp2f
 template <bool SYM> struct ScaleT { typedef _Float16 type; };
 template <> struct ScaleT<true> { typedef float type; };
 
-// Floats between the rows of the waves' partial results in LDS: four more
-// than the columns, so rows start in different banks.
-template <int NB, int NT, int AW> struct Shape {
+template <int NB, bool SYM, int NT> struct Shape {
   static constexpr int D = 32 * NB;
   static constexpr int ROWS = 16 * NT;
-  static constexpr int CB = NB < 16 / (NT * AW) ? NB : 16 / (NT * AW);   // blocks joined at a time (35 KB)
-  static constexpr int LD = 32 * CB + 4;
+  static constexpr int AW = NB > 4 ? NB : 4;   // waves; pages of a step
+  static constexpr int PS = AW / NB;           // waves that share a block of columns
+  static constexpr int NP = AW / PS;           // pages of a step whose values a wave takes: NB
+  static constexpr int AT = 64 * AW;
 };
 
-template <int NB, bool SYM, int NT, int AW>
-struct __align__(16) Lds {
-  typedef Shape<NB, NT, AW> Sh;
-  union {
-    struct {
-      uint32_t q[NT * NB * 64 * 2];            // Q codes in operand order
-      float qd[NT * NB * 16];
-      float vs[AW][NB * 64];
-      typename ScaleT<SYM>::type ks[AW][NB * 64];
-    } in;
-    float o[AW][Sh::ROWS * Sh::LD];
-  };
-  float R[AW][Sh::ROWS], l[AW][Sh::ROWS];      // the waves' references and sums
-  float whole[Sh::ROWS];                       // the joined sum
+template <int NB, bool SYM, int NT> struct __align__(16) Lds {
+  typedef Shape<NB, SYM, NT> Sh;
+  uint32_t q[NT * NB * 64 * 2];                // Q codes in operand order
+  v4f p[Sh::AW][NT * 4][64];                   // a step's probabilities, as the lanes hold them
+  float vs[Sh::AW][Sh::NP * 64];               // the waves' value scales, times a power of two
+  typename ScaleT<SYM>::type ks[Sh::AW][NB * 64];
+  float qd[NT * NB * 16];
+  float mx[Sh::ROWS][Sh::AW];                  // the waves' maxima
 };
 
-// A lane's share of a page.
-template <int NB, bool SYM> struct Page {
-  v4u k[NB], v[NB];
-  // NB scales each of K and V: numbers lane * NB .. + NB - 1 of the tile
-  static constexpr int SW = NB * (SYM ? 4 : 2) / 4;
-  uint32_t ks[SW], vs[SW];
-};
+// N scales of raw words.
+template <bool SYM> __device__ __forceinline__ float scale_of(const uint32_t *w, int i) {
+  return SYM ? __builtin_bit_cast(float, w[i]) : f16_bits_to_f32(w[i / 2] >> (16 * (i & 1)));
+}
 
 template <int N>
 __device__ __forceinline__ void load_words(const uint8_t *p, uint32_t (&w)[N]) {
@@ -235,88 +265,102 @@ __device__ __forceinline__ void load_words(const uint8_t *p, uint32_t (&w)[N]) {
   }
 }
 
-// Tokens of the scales that lane `lane` stages, number i of its NB: tbase +
-// toff(i) (the inverse of kv_scale_at within a block).
-template <int NB> __device__ __forceinline__ int scale_token(int lane) {
-  const int n = lane * NB & 63;
-  return n >> 4 << 2 | (n >> 2 & 3) << 4 | (n & 3);
-}
-constexpr int scale_token_off(int i) { return (i >> 2) * 16 + (i & 3); }
+// Number i of the 16 keys that a lane holds of a page, less its 4 (l / 16).
+constexpr int key_off(int i) { return (i >> 2) * 16 + (i & 3); }
 
-template <int NB, bool SYM, int NT, int AW>
-__global__ __launch_bounds__(64 * AW, 2) void attn_kernel(AttnArgs a) {
-  typedef Shape<NB, NT, AW> Sh;
+template <int NB, bool SYM, int NT>
+__global__ __launch_bounds__((Shape<NB, SYM, NT>::AT), 2) void attn_kernel(AttnArgs a) {
+  typedef Shape<NB, SYM, NT> Sh;
   typedef typename ScaleT<SYM>::type sc_t;
-  constexpr int D = Sh::D, ROWS = Sh::ROWS, SW = Page<NB, SYM>::SW, AT = 64 * AW;
+  constexpr int D = Sh::D, ROWS = Sh::ROWS, AW = Sh::AW, AT = Sh::AT, PS = Sh::PS, NP = Sh::NP;
   constexpr int64_t TILE = kv_tile_bytes(D, SYM);
-  __shared__ Lds<NB, SYM, NT, AW> lds;
+  constexpr int SB = kv_scale_bytes(SYM);
+  constexpr int KSW = NB * SB / 4, VSW = NP * SB / 4;     // words of scales a lane stages
+  __shared__ Lds<NB, SYM, NT> lds;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
   const int g = lane >> 4;
+  const int blk = wave % NB, sub = wave / NB;      // its columns; its set of a step's pages
 
   for (int id = blockIdx.x;; id += gridDim.x) {
     Found f;
     if (!plan_find<ROWS>(a, id, false, f)) return;
     const Seq sq = seq_of<ROWS>(a, f.s);
-    const int run = f.local % f.runs, it = f.local / f.runs;
-    const int h = it % a.p.NKV, tile = sq.tiles - 1 - it / a.p.NKV;   // longest first
+    const int it = f.runs == 1 ? f.local : f.local / f.runs, run = f.local - it * f.runs;
+    const int tl = it / a.p.NKV, h = it - tl * a.p.NKV, tile = sq.tiles - 1 - tl;  // longest first
     const int f0 = tile * ROWS, fn = min(ROWS, sq.qlen * a.G - f0);  // rows of the tile
+    const RowMap rm(a, f0);
     const int base_pos = sq.len - sq.qlen;
-    const int pos0 = base_pos + f0 / a.G, pos1 = base_pos + (f0 + fn - 1) / a.G;
+    const int pos0 = base_pos + rm.token(0), pos1 = base_pos + rm.token(fn - 1);
     // the tile's pages within this run
     int64_t key0 = 0;
     if (a.window > 0) key0 = max((int64_t)0, (int64_t)pos0 - a.window + 1);
-    const int per = (sq.pages + f.runs - 1) / f.runs;
+    const int per = f.runs == 1 ? sq.pages : (sq.pages + f.runs - 1) / f.runs;
     const int plo = max((int)(key0 / KV_PAGE), sq.lo + run * per);
     int phi = min(sq.lo + min(sq.pages, (run + 1) * per), pos1 < 0 ? 0 : pos1 / KV_PAGE + 1);
     if (a.p.n_pages == 0) phi = plo;
 
+    // page ids of a step: lane j < AW has page at0 + j's (-1: none)
     const int32_t *table = a.p.pages + (int64_t)f.s * a.p.max_pages;
-    const int64_t head = (int64_t)h * TILE;
-    const auto present = [&](int page) { return page >= 0 && page < a.p.n_pages; };
-    const auto tile_at = [&](int page) {
-      return (int64_t)(present(page) ? page : 0) * a.p.NKV * TILE + head;
+    const auto ids_at = [&](int at0) {
+      int v = -1;
+      if (lane < AW && at0 + lane < phi) v = table[at0 + lane];
+      return v < 0 || v >= a.p.n_pages ? -1 : v;
     };
-    Page<NB, SYM> pg;
-    const auto load_k = [&](int page) {
-      const uint8_t *t = a.p.k + tile_at(page);
-#pragma unroll
-      for (int b = 0; b < NB; b++) pg.k[b] = reinterpret_cast<const v4u *>(t + b * 1024)[lane];
-      load_words(t + NB * 1024 + lane * (SW * 4), pg.ks);
+    // lane l's word of the value scales: page l / (64 / NP) of the wave's set
+    const int spg = lane / (64 / NP), sof = lane % (64 / NP) * NP;
+    const int64_t head = (int64_t)h * TILE, stride = (int64_t)a.p.NKV * TILE;
+    // One buffer for both: K block b of the wave's page, and once that is used,
+    // the wave's columns of V page b (AW / PS = NB of them), and so on: half a
+    // step lies between a load and its use, in half the registers.
+    v4u buf[NB];
+    uint32_t ksr[KSW], vsr[VSW];
+    const auto k_tile = [&](int ids) {
+      return a.p.k + (int64_t)max(__builtin_amdgcn_readlane(ids, wave), 0) * stride + head;
     };
-    const auto load_v = [&](int page) {
-      const uint8_t *t = a.p.v + tile_at(page);
-      load_words(t + NB * 1024 + lane * (SW * 4), pg.vs);
-#pragma unroll
-      for (int b = 0; b < NB; b++) pg.v[b] = reinterpret_cast<const v4u *>(t + b * 1024)[lane];
+    const auto load_k = [&](const uint8_t *t, int b) {
+      buf[b] = reinterpret_cast<const v4u *>(t + b * 1024)[lane];
     };
-    int at = plo + wave;
-    int page = at < phi ? table[at] : -1;
+    const auto load_ks = [&](const uint8_t *t) {
+      load_words(t + NB * 1024 + lane * (KSW * 4), ksr);
+    };
+    const auto load_vs = [&](int ids) {
+      const int64_t page = max(__shfl(ids, sub * NP + spg), 0);
+      load_words(a.p.v + page * stride + head + NB * 1024 + (blk * 64 + sof) * SB, vsr);
+    };
+    const auto load_v = [&](int ids, int j) {
+      const int64_t page = max(__builtin_amdgcn_readlane(ids, sub * NP + j), 0);
+      buf[j] = reinterpret_cast<const v4u *>(a.p.v + page * stride + head + blk * 1024)[lane];
+    };
+    int ids = ids_at(plo);
 
     // Q codes and scales of the tile's rows (rows past the last repeat it);
-    // the first page's loads go out behind Q's
-    constexpr int QI = ROWS * NB * 8 / AT > 0 ? ROWS * NB * 8 / AT : 1;
+    // the first step's loads go out behind Q's
+    constexpr int QI = (ROWS * NB * 8 + AT - 1) / AT;
     v4f x[QI];
 #pragma unroll
     for (int k = 0; k < QI; k++) {
-      const int i = threadIdx.x + k * AT, j = i & 7, blk = i >> 3;
-      const int row = min(blk / NB, ROWS - 1), b = blk % NB, fr = f0 + min(row, fn - 1);
-      x[k] = *reinterpret_cast<const v4f *>(
-          a.q + (sq.r0 + fr / a.G) * a.qs + (int64_t)(h * a.G + fr % a.G) * D + b * 32 + 4 * j);
+      const int i = threadIdx.x + k * AT, row = min((i >> 3) / NB, fn - 1), b = (i >> 3) % NB;
+      const int t = rm.token(row);
+      x[k] = *reinterpret_cast<const v4f *>(a.q + (sq.r0 + t) * a.qs +
+                                            (int64_t)(h * a.G + rm.head(row, t)) * D + b * 32 + 4 * (i & 7));
     }
-    if (at < phi) {
-      load_k(page);
-      load_v(page);
+    {
+      const uint8_t *t = k_tile(ids);
+      load_ks(t);
+#pragma unroll
+      for (int b = 0; b < NB; b++) load_k(t, b);
     }
+    load_vs(ids);
 #pragma unroll
     for (int k = 0; k < QI; k++) {
-      const int i = threadIdx.x + k * AT, j = i & 7, blk = i >> 3, row = blk / NB, b = blk % NB;
+      const int i = threadIdx.x + k * AT, j = i & 7, row = (i >> 3) / NB, b = (i >> 3) % NB;
       const float v[4] = {x[k][0], x[k][1], x[k][2], x[k][3]};
       float d;
       const uint32_t codes = kv_q8_block8<SYM>(v, d);
       const int nt = row >> 4, r = row & 15;
       if (row < ROWS) {
-        lds.in.q[((nt * NB + b) * 64 + 16 * (j & 3) + r) * 2 + (j >> 2)] = codes;
-        if (j == 0) lds.in.qd[(nt * NB + b) * 16 + r] = d * a.sign;
+        lds.q[((nt * NB + b) * 64 + 16 * (j & 3) + r) * 2 + (j >> 2)] = codes;
+        if (j == 0) lds.qd[(nt * NB + b) * 16 + r] = d * a.sign;
       }
     }
     __syncthreads();
@@ -325,75 +369,36 @@ __global__ __launch_bounds__(64 * AW, 2) void attn_kernel(AttnArgs a) {
     int hi_key[NT], lo_key[NT];
 #pragma unroll
     for (int nt = 0; nt < NT; nt++) {
-      const int pos = base_pos + (f0 + min(16 * nt + (lane & 15), fn - 1)) / a.G;
+      const int pos = base_pos + rm.token(min(16 * nt + (lane & 15), fn - 1));
       hi_key[nt] = pos - 4 * g;
       lo_key[nt] = (a.window > 0 && a.window <= pos ? (int)(pos - a.window) : -1) - 4 * g;
     }
-    const int tbase = scale_token<NB>(lane);
+    // first token of the lane's NP value scales within its page, as kv_scale_at has them
+    const int vtok = sof / 16 * 4 + sof / 4 % 4 * 16 + sof % 4;
 
     float m[NT], mk[NT], l[NT];
-    v4f acc[NT][NB][2];
+    v4f acc[NT][2];
 #pragma unroll
     for (int nt = 0; nt < NT; nt++) {
       m[nt] = -FLT_MAX;
       mk[nt] = -FLT_MAX;
       l[nt] = 0.0f;
-#pragma unroll
-      for (int b = 0; b < NB; b++) acc[nt][b][0] = acc[nt][b][1] = v4f{0.f, 0.f, 0.f, 0.f};
+      acc[nt][0] = acc[nt][1] = v4f{0.f, 0.f, 0.f, 0.f};
     }
     // value scales are below 2^vexp and enter the product times 2^(15 - vexp)
     int vexp = -126;
-    sc_t *ks = lds.in.ks[wave];
-    float *vs = lds.in.vs[wave];
+    sc_t *ks = lds.ks[wave];
+    float *vs = lds.vs[wave];
     float minus = -1.0f;               // opaque, so that the halves' difference is one mixed FMA
     asm("" : "+v"(minus));
-    for (; at < phi; at += AW) {
-      const int next_page = at + AW < phi ? table[at + AW] : -1;
-      const int key = at * KV_PAGE;
-      // pages that some row does not see whole; an absent page is seen by none
-      const bool here = present(page);
-      const bool masked = !here || key + KV_PAGE - 1 > pos0 ||
-                          (a.window > 0 && key <= pos1 - a.window);
-      // stage the scales; keys that no row sees count for nothing
+    for (int at0 = plo; at0 < phi; at0 += AW) {
+      const int next = at0 + AW < phi ? ids_at(at0 + AW) : -1;
+      const bool more = at0 + AW < phi;
+      const int key = (at0 + wave) * KV_PAGE;
+      // ---- scores of page at0 + wave
+      const bool here = __builtin_amdgcn_readlane(ids, wave) >= 0;
 #pragma unroll
-      for (int w = 0; w < SW; w++) reinterpret_cast<word *>(ks)[lane * SW + w] = pg.ks[w];
-      {
-        float dv[NB], vmax = 0.0f;
-#pragma unroll
-        for (int i = 0; i < NB; i++)
-          dv[i] = SYM ? __builtin_bit_cast(float, pg.vs[i % SW])
-                      : f16_bits_to_f32(pg.vs[(i / 2) % SW] >> (16 * (i & 1)));
-        if (masked) {
-          const int last = here ? pos1 - key - tbase : -1;
-          const int before = (int)max((int64_t)0, key0 - key) - tbase;
-#pragma unroll
-          for (int i = 0; i < NB; i++)
-            if (scale_token_off(i) > last || scale_token_off(i) < before) dv[i] = 0.0f;
-        }
-#pragma unroll
-        for (int i = 0; i < NB; i++) {
-          const float y = fabsf(dv[i]);
-          vmax = fmaxf(vmax, y < INFINITY ? y : 0.0f);
-        }
-        if (__ballot(vmax >= ldexpf(1.0f, vexp))) {
-#pragma unroll
-          for (int o = 32; o > 0; o >>= 1) vmax = fmaxf(vmax, __shfl_xor(vmax, o));
-          const int e = __builtin_amdgcn_readfirstlane(ilogbf(vmax) + 1);
-#pragma unroll
-          for (int nt = 0; nt < NT; nt++)
-#pragma unroll
-            for (int b = 0; b < NB; b++)
-#pragma unroll
-              for (int s = 0; s < 2; s++)
-#pragma unroll
-                for (int y = 0; y < 4; y++) acc[nt][b][s][y] = ldexpf(acc[nt][b][s][y], vexp - e);
-          vexp = e;
-        }
-#pragma unroll
-        for (int i = 0; i < NB; i++) vs[lane * NB + i] = ldexpf(dv[i], 15 - vexp);
-      }
-
-      // scores
+      for (int w = 0; w < KSW; w++) reinterpret_cast<word *>(ks)[lane * KSW + w] = ksr[w];
       float S[NT][16];
 #pragma unroll
       for (int nt = 0; nt < NT; nt++)
@@ -405,8 +410,8 @@ __global__ __launch_bounds__(64 * AW, 2) void attn_kernel(AttnArgs a) {
         float dq[NT], cq[NT];
 #pragma unroll
         for (int nt = 0; nt < NT; nt++) {
-          qb[nt] = reinterpret_cast<const long *>(lds.in.q)[(nt * NB + b) * 64 + lane];
-          dq[nt] = lds.in.qd[(nt * NB + b) * 16 + (lane & 15)];
+          qb[nt] = reinterpret_cast<const long *>(lds.q)[(nt * NB + b) * 64 + lane];
+          dq[nt] = lds.qd[(nt * NB + b) * 16 + (lane & 15)];
           cq[nt] = -12582912.0f * dq[nt];
         }
         sc_t dk[16];
@@ -414,7 +419,7 @@ __global__ __launch_bounds__(64 * AW, 2) void attn_kernel(AttnArgs a) {
         for (int i = 0; i < 16; i++) dk[i] = ks[b * 64 + g * 16 + i];
 #pragma unroll
         for (int i = 0; i < 4; i++) {
-          const uint32_t y = pg.k[b][i];
+          const uint32_t y = buf[b][i];
           const long kb = (long)((uint64_t)(y & 0xF0F0F0F0u) << 32 | (y << 4 & 0xF0F0F0F0u));
 #pragma unroll
           for (int nt = 0; nt < NT; nt++) {
@@ -435,190 +440,210 @@ __global__ __launch_bounds__(64 * AW, 2) void attn_kernel(AttnArgs a) {
         for (int nt = 0; nt < NT; nt++)
 #pragma unroll
           for (int i = 0; i < 16; i++) asm volatile("" : "+v"(S[nt][i]));
+        load_v(ids, b);
       }
-      if (at + AW < phi) load_k(next_page);
-
-      // running maximum
-      float mx[NT];
-      bool grow = false;
+      // keys that not every row sees; an absent page's are seen by none
+      if (!here || key + KV_PAGE - 1 > pos0 || (a.window > 0 && key <= pos1 - a.window)) {
 #pragma unroll
-      for (int nt = 0; nt < NT; nt++) {
-        if (masked) {
-          const int last = here ? hi_key[nt] - key : -1, before = lo_key[nt] - key;
+        for (int nt = 0; nt < NT; nt++) {
+          const int last = here ? hi_key[nt] - key : -100, before = lo_key[nt] - key;
 #pragma unroll
           for (int i = 0; i < 16; i++)
-            if (scale_token_off(i) > last || scale_token_off(i) <= before) S[nt][i] = -INFINITY;
+            if (key_off(i) > last || key_off(i) <= before) S[nt][i] = -INFINITY;
         }
-        mx[nt] = -FLT_MAX;
+      }
 #pragma unroll
-        for (int i = 0; i < 16; i++) mx[nt] = fmaxf(mx[nt], S[nt][i]);
-        mx[nt] = max4(mx[nt]);
-        grow |= mx[nt] > m[nt];
+      for (int nt = 0; nt < NT; nt++) {
+        float mx = -FLT_MAX;
+#pragma unroll
+        for (int i = 0; i < 16; i++) mx = fmaxf(mx, S[nt][i]);
+        mx = max4(mx);
+        if (lane < 16) lds.mx[16 * nt + lane][wave] = mx;
+      }
+
+      // ---- the wave's value scales of the step; keys that no row sees count for nothing
+      {
+        const int vkey = (at0 + sub * NP + spg) * KV_PAGE + vtok;
+        const bool vhere = __shfl(ids, sub * NP + spg) >= 0;
+        float dv[NP], vmax = 0.0f;
+#pragma unroll
+        for (int i = 0; i < NP; i++) {
+          dv[i] = scale_of<SYM>(vsr, i);
+          const int kk = vkey + key_off(i);
+          if (!vhere || kk > pos1 || kk < key0) dv[i] = 0.0f;
+          const float y = fabsf(dv[i]);
+          vmax = fmaxf(vmax, y < INFINITY ? y : 0.0f);
+        }
+        if (__ballot(vmax >= ldexpf(1.0f, vexp))) {
+#pragma unroll
+          for (int o = 32; o > 0; o >>= 1) vmax = fmaxf(vmax, __shfl_xor(vmax, o));
+          const int e = __builtin_amdgcn_readfirstlane(ilogbf(vmax) + 1);
+#pragma unroll
+          for (int nt = 0; nt < NT; nt++)
+#pragma unroll
+            for (int s = 0; s < 2; s++)
+#pragma unroll
+              for (int y = 0; y < 4; y++) acc[nt][s][y] = ldexpf(acc[nt][s][y], vexp - e);
+          vexp = e;
+        }
+#pragma unroll
+        for (int i = 0; i < NP; i++) vs[lane * NP + i] = ldexpf(dv[i], 15 - vexp);
+      }
+      const uint8_t *const kt = k_tile(next);
+      if (more) {
+        load_vs(next);
+        load_ks(kt);
+      }
+      __syncthreads();
+
+      // ---- running maximum, the same in every wave
+      bool grow = false;
+      float mn[NT];
+#pragma unroll
+      for (int nt = 0; nt < NT; nt++) {
+        mn[nt] = m[nt];
+#pragma unroll
+        for (int w = 0; w < AW; w++) mn[nt] = fmaxf(mn[nt], lds.mx[16 * nt + (lane & 15)][w]);
+        grow |= mn[nt] > m[nt];
       }
       if (__ballot(grow)) {
 #pragma unroll
         for (int nt = 0; nt < NT; nt++) {
-          const float mn = fmaxf(m[nt], mx[nt]), mkn = mn * a.k;
+          const float mkn = mn[nt] * a.k;
           const float al = m[nt] == -FLT_MAX ? 0.0f : exp2_f(mk[nt] - mkn);
-          m[nt] = mn;
+          m[nt] = mn[nt];
           mk[nt] = mkn;
           l[nt] *= al;
-#pragma unroll
-          for (int b = 0; b < NB; b++) {
-            acc[nt][b][0] *= al;
-            acc[nt][b][1] *= al;
-          }
+          acc[nt][0] *= al;
+          acc[nt][1] *= al;
         }
       }
-      // probabilities (a masked score's is exp2(-infinity) = 0)
+      // ---- probabilities (a masked score's is exp2(-infinity) = 0)
 #pragma unroll
       for (int nt = 0; nt < NT; nt++) {
+        v4f p[4];
 #pragma unroll
-        for (int i = 0; i < 16; i++) S[nt][i] = exp2_f(fmaf(S[nt][i], a.k, -mk[nt]));
-        float s[8];
+        for (int i = 0; i < 4; i++) {
 #pragma unroll
-        for (int i = 0; i < 8; i++) s[i] = S[nt][i] + S[nt][i + 8];
-#pragma unroll
-        for (int o = 4; o > 0; o >>= 1)
-#pragma unroll
-          for (int i = 0; i < o; i++) s[i] += s[i + o];
-        l[nt] += s[0];
+          for (int e = 0; e < 4; e++) p[i][e] = exp2_f(fmaf(S[nt][4 * i + e], a.k, -mk[nt]));
+          lds.p[wave][4 * nt + i][lane] = p[i];
+        }
+        const v4f s = (p[0] + p[1]) + (p[2] + p[3]);
+        l[nt] += (s[0] + s[1]) + (s[2] + s[3]);
       }
-      __builtin_amdgcn_sched_barrier(0);
-      // values, 32 keys at a time
+      __syncthreads();
+
+      // ---- values of the wave's columns
 #pragma unroll
-      for (int b = 0; b < NB; b++) {
+      for (int j = 0; j < NP; j++) {
+        const int pgj = sub * NP + j;
+        if (at0 + pgj < phi) {
 #pragma unroll
-        for (int hh = 0; hh < 2; hh++) {
-          float d[8];
+          for (int hh = 0; hh < 2; hh++) {         // 32 keys at a time
+            float d[8];
 #pragma unroll
-          for (int i = 0; i < 8; i++) d[i] = vs[b * 64 + g * 16 + 8 * hh + i];
-          h8 c[2];                       // elements l % 16 and + 16
+            for (int i = 0; i < 8; i++) d[i] = vs[j * 64 + g * 16 + 8 * hh + i];
+            h8 c[2];                               // elements l % 16 and + 16
 #pragma unroll
-          for (int i = 0; i < 2; i++) {
-            const uint32_t y = pg.v[b][2 * hh + i], z = y >> 8;
-            const h2 off = {(_Float16)-1032.0f, (_Float16)-1032.0f};
-            const h2 six = {(_Float16)0.0625f, (_Float16)0.0625f};
-            const h2 off2 = {(_Float16)-72.0f, (_Float16)-72.0f};
-            const h2 a0 = __builtin_bit_cast(h2, (y & 0x000F000Fu) | 0x64006400u) + off;
-            const h2 a1 = __builtin_bit_cast(h2, (z & 0x000F000Fu) | 0x64006400u) + off;
-            const h2 b0 = __builtin_elementwise_fma(
-                __builtin_bit_cast(h2, (y & 0x00F000F0u) | 0x64006400u), six, off2);
-            const h2 b1 = __builtin_elementwise_fma(
-                __builtin_bit_cast(h2, (z & 0x00F000F0u) | 0x64006400u), six, off2);
-            c[0][4 * i] = a0[0]; c[0][4 * i + 1] = a0[1]; c[0][4 * i + 2] = a1[0]; c[0][4 * i + 3] = a1[1];
-            c[1][4 * i] = b0[0]; c[1][4 * i + 1] = b0[1]; c[1][4 * i + 2] = b1[0]; c[1][4 * i + 3] = b1[1];
-          }
-#pragma unroll
-          for (int nt = 0; nt < NT; nt++) {
-            h8 hi, lo;
-#pragma unroll
-            for (int i = 0; i < 8; i += 2) {
-              v2f w;
-              // 0 times anything is 0: a key that the row does not see may have any scale
-              w[0] = mul_zero(S[nt][8 * hh + i], d[i]);
-              w[1] = mul_zero(S[nt][8 * hh + i + 1], d[i + 1]);
-              const h2 y = __builtin_convertvector(w, h2);
-              v2f z;
-              z[0] = fmaf((float)y[0], minus, w[0]);
-              z[1] = fmaf((float)y[1], minus, w[1]);
-              const h2 y2 = __builtin_convertvector(z, h2);
-              hi[i] = y[0]; hi[i + 1] = y[1];
-              lo[i] = y2[0]; lo[i + 1] = y2[1];
+            for (int i = 0; i < 2; i++) {
+              const uint32_t y = buf[j][2 * hh + i], z = y >> 8;
+              const h2 off = {(_Float16)-1032.0f, (_Float16)-1032.0f};
+              const h2 six = {(_Float16)0.0625f, (_Float16)0.0625f};
+              const h2 off2 = {(_Float16)-72.0f, (_Float16)-72.0f};
+              const h2 a0 = __builtin_bit_cast(h2, (y & 0x000F000Fu) | 0x64006400u) + off;
+              const h2 a1 = __builtin_bit_cast(h2, (z & 0x000F000Fu) | 0x64006400u) + off;
+              const h2 b0 = __builtin_elementwise_fma(
+                  __builtin_bit_cast(h2, (y & 0x00F000F0u) | 0x64006400u), six, off2);
+              const h2 b1 = __builtin_elementwise_fma(
+                  __builtin_bit_cast(h2, (z & 0x00F000F0u) | 0x64006400u), six, off2);
+              c[0][4 * i] = a0[0]; c[0][4 * i + 1] = a0[1]; c[0][4 * i + 2] = a1[0]; c[0][4 * i + 3] = a1[1];
+              c[1][4 * i] = b0[0]; c[1][4 * i + 1] = b0[1]; c[1][4 * i + 2] = b1[0]; c[1][4 * i + 3] = b1[1];
             }
 #pragma unroll
-            for (int s = 0; s < 2; s++) {
-              acc[nt][b][s] = __builtin_amdgcn_mfma_f32_16x16x32_f16(c[s], hi, acc[nt][b][s], 0, 0, 0);
-              acc[nt][b][s] = __builtin_amdgcn_mfma_f32_16x16x32_f16(c[s], lo, acc[nt][b][s], 0, 0, 0);
+            for (int nt = 0; nt < NT; nt++) {
+              h8 hi, lo;
+#pragma unroll
+              for (int i = 0; i < 2; i++) {
+                const v4f p = lds.p[pgj][4 * nt + 2 * hh + i][lane];
+#pragma unroll
+                for (int e = 0; e < 4; e += 2) {
+                  v2f w, z;
+                  // 0 times anything is 0: a key that the row does not see may have any scale
+                  w[0] = mul_zero(p[e], d[4 * i + e]);
+                  w[1] = mul_zero(p[e + 1], d[4 * i + e + 1]);
+                  const h2 y = __builtin_convertvector(w, h2);
+                  z[0] = fmaf((float)y[0], minus, w[0]);
+                  z[1] = fmaf((float)y[1], minus, w[1]);
+                  const h2 y2 = __builtin_convertvector(z, h2);
+                  hi[4 * i + e] = y[0]; hi[4 * i + e + 1] = y[1];
+                  lo[4 * i + e] = y2[0]; lo[4 * i + e + 1] = y2[1];
+                }
+              }
+#pragma unroll
+              for (int s = 0; s < 2; s++) {
+                acc[nt][s] = __builtin_amdgcn_mfma_f32_16x16x32_f16(c[s], hi, acc[nt][s], 0, 0, 0);
+                acc[nt][s] = __builtin_amdgcn_mfma_f32_16x16x32_f16(c[s], lo, acc[nt][s], 0, 0, 0);
+              }
             }
+#pragma unroll
+            for (int nt = 0; nt < NT; nt++) asm volatile("" : "+v"(acc[nt][0]), "+v"(acc[nt][1]));
           }
         }
-        #pragma unroll
-          for (int nt = 0; nt < NT; nt++) asm volatile("" : "+v"(acc[nt][b][0]), "+v"(acc[nt][b][1]));
+        if (more) load_k(kt, j);
       }
-      if (at + AW < phi) load_v(next_page);
-      page = next_page;
+      ids = next;
     }
 
-    // join the waves: reference R (base-2 exponent taken out of l and acc)
+    // the waves' sums; where PS waves share columns, their products too
+    __syncthreads();
+    float *const red = reinterpret_cast<float *>(lds.p);      // [AW][ROWS], then [AW][2 NT][64] v4f
 #pragma unroll
     for (int nt = 0; nt < NT; nt++) {
       l[nt] = sum4(l[nt]);
-      if (lane < 16) {
-        lds.R[wave][16 * nt + lane] = mk[nt];
-        lds.l[wave][16 * nt + lane] = l[nt];
-      }
+      if (lane < 16) red[wave * ROWS + 16 * nt + lane] = l[nt];
+#pragma unroll
+      for (int s = 0; s < 2; s++)
+#pragma unroll
+        for (int y = 0; y < 4; y++) acc[nt][s][y] = ldexpf(acc[nt][s][y], vexp - 15);
     }
-    __syncthreads();               // also: nobody reads lds.in any more
-    float Rj[NT], lj[NT];
-#pragma unroll
-    for (int nt = 0; nt < NT; nt++) {
-      const int row = 16 * nt + (lane & 15);
-      float R = -FLT_MAX, s = 0.0f;
-#pragma unroll
-      for (int w = 0; w < AW; w++)
-        if (lds.l[w][row] != 0.0f) R = fmaxf(R, lds.R[w][row]);
-#pragma unroll
-      for (int w = 0; w < AW; w++)
-        if (lds.l[w][row] != 0.0f) s = fmaf(lds.l[w][row], exp2_f(lds.R[w][row] - R), s);
-      Rj[nt] = R;
-      lj[nt] = s;
-      const float fac = l[nt] != 0.0f ? exp2_f(mk[nt] - R) : 0.0f;
-#pragma unroll
-      for (int b = 0; b < NB; b++)
-#pragma unroll
-        for (int s2 = 0; s2 < 2; s2++)
-#pragma unroll
-          for (int x = 0; x < 4; x++)
-            acc[nt][b][s2][x] = l[nt] != 0.0f ? ldexpf(acc[nt][b][s2][x], vexp - 15) * fac : 0.0f;
-    }
-    const bool whole = f.runs == 1;
-    const int slot = whole ? 0 : f.slot0 + f.local;
-    float *part = a.part + (int64_t)slot * (ROWS * (D + 2));
-    const bool fits = whole || slot < a.slots;
-    if (wave == 0 && lane < 16) {
-#pragma unroll
-      for (int nt = 0; nt < NT; nt++) {
-        const int row = 16 * nt + lane;
-        lds.whole[row] = lj[nt];
-        if (!whole && fits) {
-          part[ROWS * D + 2 * row] = Rj[nt];
-          part[ROWS * D + 2 * row + 1] = lj[nt];
-        } else if (whole && a.lse && row < fn) {
-          const int fr = f0 + row;
-          a.lse[(sq.r0 + fr / a.G) * a.NH + h * a.G + fr % a.G] =
-              lj[nt] != 0.0f ? (Rj[nt] + log2f(lj[nt])) * 0.693147180559945f : -INFINITY;
-        }
-      }
-    }
-#pragma unroll
-    for (int b0 = 0; b0 < NB; b0 += Sh::CB) {
-      __syncthreads();
+    v4f *const pr = reinterpret_cast<v4f *>(red + AW * ROWS);
+    if (PS > 1 && sub > 0) {
 #pragma unroll
       for (int nt = 0; nt < NT; nt++)
 #pragma unroll
-        for (int b = 0; b < Sh::CB; b++)
+        for (int s = 0; s < 2; s++) pr[(wave * 2 * NT + 2 * nt + s) * 64 + lane] = acc[nt][s];
+    }
+    __syncthreads();
+    const bool whole = f.runs == 1;
+    const int slot = whole ? 0 : f.slot0 + f.local;
+    float *part = a.part + (int64_t)slot * (ROWS * (D + 2));
+    if (sub == 0 && (whole || slot < a.slots)) {
 #pragma unroll
-          for (int s = 0; s < 2; s++)
-            *reinterpret_cast<v4f *>(&lds.o[wave][(16 * nt + (lane & 15)) * Sh::LD + b * 32 +
-                                                  s * 16 + 4 * g]) = acc[nt][b0 + b][s];
-      __syncthreads();
-      constexpr int C4 = Sh::CB * 8;           // 16-byte pieces of a row
-      for (int i = threadIdx.x; i < ROWS * C4; i += AT) {
-        const int row = i / C4, c4 = i % C4;
-        v4f s = v4f{0.f, 0.f, 0.f, 0.f};
+      for (int nt = 0; nt < NT; nt++) {
+        const int row = 16 * nt + (lane & 15);
+        float lt = 0.0f;
 #pragma unroll
-        for (int w = 0; w < AW; w++) s += *reinterpret_cast<const v4f *>(&lds.o[w][row * Sh::LD + 4 * c4]);
-        if (whole) {
-          if (row < fn) {
-            const int fr = f0 + row;
-            const float lr = lds.whole[row];
-            const float inv = lr != 0.0f ? 1.0f / lr : 0.0f;
-            *reinterpret_cast<v4f *>(a.out + ((sq.r0 + fr / a.G) * a.NH + h * a.G + fr % a.G) * D +
-                                     b0 * 32 + 4 * c4) = s * inv;
+        for (int w = 0; w < AW; w++) lt += red[w * ROWS + row];
+#pragma unroll
+        for (int q = 1; q < PS; q++)
+#pragma unroll
+          for (int s = 0; s < 2; s++) acc[nt][s] += pr[((wave + q * NB) * 2 * NT + 2 * nt + s) * 64 + lane];
+        const int col = blk * 32 + 4 * g;
+        if (!whole) {
+          *reinterpret_cast<v4f *>(part + row * D + col) = acc[nt][0];
+          *reinterpret_cast<v4f *>(part + row * D + col + 16) = acc[nt][1];
+          if (wave == 0 && g == 0) {
+            part[ROWS * D + 2 * row] = mk[nt];
+            part[ROWS * D + 2 * row + 1] = lt;
           }
-        } else if (fits) {
-          *reinterpret_cast<v4f *>(part + row * D + b0 * 32 + 4 * c4) = s;
+        } else if (row < fn) {
+          const int t = rm.token(row);
+          const int64_t o = (sq.r0 + t) * a.NH + h * a.G + rm.head(row, t);
+          const float inv = lt != 0.0f ? 1.0f / lt : 0.0f;
+          *reinterpret_cast<v4f *>(a.out + o * D + col) = acc[nt][0] * inv;
+          *reinterpret_cast<v4f *>(a.out + o * D + col + 16) = acc[nt][1] * inv;
+          if (a.lse && wave == 0 && g == 0)
+            a.lse[o] = lt != 0.0f ? (mk[nt] + log2f(lt)) * 0.693147180559945f : -INFINITY;
         }
       }
     }
@@ -627,77 +652,79 @@ __global__ __launch_bounds__(64 * AW, 2) void attn_kernel(AttnArgs a) {
 }
 
 // Joins the runs of item blockIdx.x (counted over the items with several
-// runs), row blockIdx.y of its tile: D / 4 lanes by groups that take the runs
-// in turn, summed in a fixed order.
-template <int NB, int NT>
+// runs), rows blockIdx.y * JR .. of its tile: a row by JT / JR threads, D / 4
+// lanes by groups that take the runs in turn, summed in a fixed order.
+template <int NB, int NT, int JT, int JR>
 __global__ __launch_bounds__(JT) void join_kernel(AttnArgs a) {
-  constexpr int D = 32 * NB, ROWS = 16 * NT, L = D / 4, NG = JT / L;
-  __shared__ v4f so[NG][L];
-  __shared__ float sr[NG], sl[NG];
+  constexpr int D = 32 * NB, ROWS = 16 * NT, L = D / 4, TR = JT / JR, NG = TR / L;
+  __shared__ v4f so[JR][NG][L];
+  __shared__ float sw[JR][JOIN_MAX], sl[JR];
   Found f;
   if (!plan_find<ROWS>(a, blockIdx.x, true, f)) return;
   const Seq sq = seq_of<ROWS>(a, f.s);
-  const int h = f.local % a.p.NKV, tile = sq.tiles - 1 - f.local / a.p.NKV;
-  const int row = blockIdx.y, fr = tile * ROWS + row;
-  if (fr >= sq.qlen * a.G) return;
-  const int grp = threadIdx.x / L, c4 = threadIdx.x % L;
+  const int tl = f.local / a.p.NKV, h = f.local - tl * a.p.NKV, f0 = (sq.tiles - 1 - tl) * ROWS;
+  const int fn = min(ROWS, sq.qlen * a.G - f0);
+  if ((int)blockIdx.y * JR >= fn) return;
+  const int jr = threadIdx.x / TR, th = threadIdx.x % TR;
+  const int row = min((int)blockIdx.y * JR + jr, fn - 1);
   const int slot = f.slot0 + f.local * f.runs;
-  const int n = min(f.runs, a.slots - slot);
-  const float *part = a.part + (int64_t)slot * (ROWS * (D + 2));
-  // the reference first: every thread's runs, then all groups'
+  const int n = min(f.runs, a.slots - slot);     // at most JOIN_MAX
+  constexpr int64_t PB = ROWS * (D + 2);
+  const float *part = a.part + slot * PB;
+  // the runs' weights: one wave a row
   float R = -FLT_MAX;
-  for (int i = threadIdx.x; i < n; i += JT) {
-    const float *p = part + (int64_t)i * (ROWS * (D + 2)) + ROWS * D + 2 * row;
-    if (p[1] != 0.0f) R = fmaxf(R, p[0]);
+  if (th < 64) {
+    for (int i = th; i < n; i += 64) {
+      const v2f q = *reinterpret_cast<const v2f *>(part + i * PB + ROWS * D + 2 * row);
+      if (q[1] != 0.0f) R = fmaxf(R, q[0]);
+    }
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) R = fmaxf(R, __shfl_xor(R, o));
+    float l = 0.0f;
+    for (int i = th; i < n; i += 64) {
+      const v2f q = *reinterpret_cast<const v2f *>(part + i * PB + ROWS * D + 2 * row);
+      const float w = q[1] != 0.0f ? exp2_f(q[0] - R) : 0.0f;
+      sw[jr][i] = w;
+      l = fmaf(q[1], w, l);
+    }
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) l += __shfl_xor(l, o);
+    if (th == 0) sl[jr] = l;
   }
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) R = fmaxf(R, __shfl_xor(R, o));
-  if ((threadIdx.x & 63) == 0) sr[threadIdx.x >> 6] = R;
   __syncthreads();
-#pragma unroll
-  for (int w = 0; w < JT / 64; w++) R = fmaxf(R, sr[w]);
+  const int grp = th / L, c4 = th % L;
   v4f s = v4f{0.f, 0.f, 0.f, 0.f};
-  float l = 0.0f;
+  const float *src = part + row * D + 4 * c4;
+#pragma unroll 8
+  for (int i = grp; i < n; i += NG) s += *reinterpret_cast<const v4f *>(src + i * PB) * sw[jr][i];
+  if (NG > 1) {
+    so[jr][grp][c4] = s;
+    __syncthreads();
+    if (grp != 0) return;
+    s = v4f{0.f, 0.f, 0.f, 0.f};
 #pragma unroll 4
-  for (int i = grp; i < n; i += NG) {
-    const float *p = part + (int64_t)i * (ROWS * (D + 2));
-    const float lr = p[ROWS * D + 2 * row + 1];
-    const float w = lr != 0.0f ? exp2_f(p[ROWS * D + 2 * row] - R) : 0.0f;
-    const v4f x = *reinterpret_cast<const v4f *>(p + row * D + 4 * c4);
-    s += x * w;
-    l = fmaf(lr, w, l);
+    for (int i = 0; i < NG; i++) s += so[jr][i][c4];
   }
-  so[grp][c4] = s;
-  if (c4 == 0) sl[grp] = l;
-  __syncthreads();
-  if (grp != 0) return;
-  l = 0.0f;
-  s = v4f{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-  for (int i = 0; i < NG; i++) {
-    s += so[i][c4];
-    l += sl[i];
-  }
-  const int64_t at = (sq.r0 + fr / a.G) * a.NH + h * a.G + fr % a.G;
-  *reinterpret_cast<v4f *>(a.out + at * D + 4 * c4) = l != 0.0f ? s * (1.0f / l) : s * 0.0f;
-  if (c4 == 0 && a.lse)
-    a.lse[at] = l != 0.0f ? (R + log2f(l)) * 0.693147180559945f : -INFINITY;
+  if ((int)blockIdx.y * JR + jr >= fn) return;
+  const RowMap rm(a, f0);
+  const int t = rm.token(row);
+  const int64_t o = (sq.r0 + t) * a.NH + h * a.G + rm.head(row, t);
+  const float l = sl[jr];
+  *reinterpret_cast<v4f *>(a.out + o * D + 4 * c4) = l != 0.0f ? s * (1.0f / l) : s * 0.0f;
+  if (c4 == 0 && a.lse) a.lse[o] = l != 0.0f ? (R + log2f(l)) * 0.693147180559945f : -INFINITY;
 }
 
 // Rows of a tile: 32 once sequences have more than 16 on average (a tile's
-// rows share the page's loads and decoded codes), 16 for the few rows of a
-// decode step, and for D = 256, whose 32-row sums would not fit in registers.
-// Waves of a workgroup: 8 on 16-row tiles, so that a short context needs no
-// second launch, 4 on 32-row ones.
+// rows share the page's loads and decoded codes), else the 16 of one product.
 int tile_rows(const w4a8_kv *kv, int64_t T, int64_t NH) {
   const int64_t rows = T * (NH / kv->NKV);
-  return kv->D <= 128 && kv->B > 0 && rows > 16 * kv->B ? 32 : 16;
+  return kv->B > 0 && rows > 16 * kv->B ? 32 : 16;
 }
-constexpr int CMIN = 16;              // fewest pages of a run
-constexpr int TARGET = 512;           // runs wanted
+// Fewest pages of a run: one step.
+int run_min(const w4a8_kv *kv) { return kv->D == 256 ? 8 : 4; }
 
 // Bounds on the call's items, and on the partial results it can need: a
-// sequence is split only into runs of more than half of C = total / TARGET
+// sequence is split only into runs of more than half of C >= total / TARGET
 // pages, so the runs of split items number at most 2 TARGET.
 int64_t items_bound(const w4a8_kv *kv, int64_t T, int64_t NH) {
   const int rt = tile_rows(kv, T, NH);
@@ -705,8 +732,9 @@ int64_t items_bound(const w4a8_kv *kv, int64_t T, int64_t NH) {
   return ((T * G) / rt + std::min(kv->B, T)) * kv->NKV;
 }
 int64_t slots_bound(const w4a8_kv *kv, int64_t T, int64_t NH) {
-  if (kv->max_pages <= CMIN) return 0;
-  const int64_t runs = (kv->max_pages + CMIN - 1) / CMIN;
+  const int c = run_min(kv);
+  if (kv->max_pages <= c) return 0;
+  const int64_t runs = (kv->max_pages + c - 1) / c;
   return std::min<int64_t>(2 * TARGET, items_bound(kv, T, NH) * runs);
 }
 
@@ -718,21 +746,25 @@ int attn_sizes(const w4a8_kv *kv, int64_t T, int64_t NH) {
   return W4A8_OK;
 }
 
-template <int NB, bool SYM, int NT, int AW>
+template <int NB, bool SYM, int NT>
 int launch(const AttnArgs &a, int64_t items, hipStream_t s) {
   const int64_t grid = std::min<int64_t>(items + a.slots, 1 << 20);
-  attn_kernel<NB, SYM, NT, AW><<<dim3((unsigned)grid), dim3(64 * AW), 0, s>>>(a);
+  attn_kernel<NB, SYM, NT><<<dim3((unsigned)grid), dim3(Shape<NB, SYM, NT>::AT), 0, s>>>(a);
   if (int rc = check_launch(); rc != W4A8_OK || a.slots == 0) return rc;
+  // Joins: with few items, which then have many runs, 1024 threads a row;
+  // else a wave a row.
   const int64_t joins = std::min<int64_t>(items, TARGET);
-  join_kernel<NB, NT><<<dim3((unsigned)joins, 16 * NT), dim3(JT), 0, s>>>(a);
+  const int rows = (int)std::min<int64_t>(16 * NT, a.T * a.G);
+  if (items <= 16)
+    join_kernel<NB, NT, 1024, 1><<<dim3((unsigned)joins, rows), dim3(1024), 0, s>>>(a);
+  else
+    join_kernel<NB, NT, 256, 4><<<dim3((unsigned)joins, (rows + 3) / 4), dim3(256), 0, s>>>(a);
   return check_launch();
 }
 
 template <int NB, bool SYM>
 int launch_rows(const AttnArgs &a, bool wide, int64_t items, hipStream_t s) {
-  if constexpr (NB <= 4)
-    if (wide) return launch<NB, SYM, 2, 4>(a, items, s);
-  return launch<NB, SYM, 1, 8>(a, items, s);
+  return wide ? launch<NB, SYM, 2>(a, items, s) : launch<NB, SYM, 1>(a, items, s);
 }
 
 }  // namespace
@@ -766,7 +798,8 @@ extern "C" int attn_q4_forward(const w4a8_kv *kv, const float *q, int64_t q_stri
                 // a factor of 0 goes to Q, so that a masked score's -infinity stays one
                 scale != 0.0f ? std::fabs(scale) * 1.44269504f / 16.0f : 1.0f,
                 scale < 0.0f ? -1.0f : scale == 0.0f ? 0.0f : 1.0f, window,
-                reinterpret_cast<float *>(workspace), (int)slots_bound(kv, T, NH), CMIN, TARGET};
+                reinterpret_cast<float *>(workspace), (int)slots_bound(kv, T, NH), run_min(kv),
+                1.0f / (float)(NH / kv->NKV)};
   const int64_t items = items_bound(kv, T, NH);
   const bool sym = kv->format == W4A8_KV_Q4_SYM, wide = tile_rows(kv, T, NH) == 32;
   const hipStream_t s = as_stream(stream);
