@@ -50,6 +50,7 @@ namespace w4a8 {
 namespace {
 
 constexpr int TARGET = 512;           // runs wanted: two workgroups a compute unit
+constexpr int AW = 4, AT = 64 * AW;   // waves of a workgroup; pages of a step
 constexpr int JOIN_MAX = 2 * TARGET;  // most runs of an item
 
 typedef int v4i __attribute__((ext_vector_type(4)));
@@ -74,7 +75,6 @@ struct AttnArgs {
   int64_t window;
   float *part;      // partial results, `slots` of them
   int slots;
-  int cmin;         // fewest pages of a run
   float inv_G;      // 1 / G
 };
 
@@ -149,8 +149,7 @@ __device__ __forceinline__ bool plan_find(const AttnArgs &a, int id, bool split,
       float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, wave_scan(total)), 63));
   // (rounded up past the sum's own rounding: the partial slots are counted on C)
   const float c = fminf(total * (1.001f / TARGET), 1e9f);
-  int C = max(a.cmin, (int)c + 1);
-  C = (C + a.cmin - 1) / a.cmin * a.cmin;            // whole steps
+  const int C = ((int)c + AW) / AW * AW;             // whole steps
   int base = 0, slots = 0;
   for (int s0 = 0; s0 < B; s0 += 64) {
     if (s0) look(s0 + lane);
@@ -222,26 +221,64 @@ __device__ __forceinline__ float mul_zero(float x, float y) {
 
 __device__ __forceinline__ float exp2_f(float x) { return __builtin_amdgcn_exp2f(x); }
 
+// W = p d of four keys as the sum of two fp16 halves.  (0 times anything is 0:
+// a key that the row does not see may have any scale.)
+__device__ __forceinline__ void make_w(v4f p, const float *d, float minus, h4 &hi, h4 &lo) {
+  const v4f dv = *reinterpret_cast<const v4f *>(d);
+#pragma unroll
+  for (int e = 0; e < 4; e += 2) {
+    v2f w, z;
+    w[0] = mul_zero(p[e], dv[e]);
+    w[1] = mul_zero(p[e + 1], dv[e + 1]);
+    const h2 y = __builtin_convertvector(w, h2);
+    z[0] = fmaf((float)y[0], minus, w[0]);
+    z[1] = fmaf((float)y[1], minus, w[1]);
+    const h2 y2 = __builtin_convertvector(z, h2);
+    hi[e] = y[0]; hi[e + 1] = y[1];
+    lo[e] = y2[0]; lo[e + 1] = y2[1];
+  }
+}
+__device__ __forceinline__ void put(h8 &v, int i, h4 x) {
+#pragma unroll
+  for (int e = 0; e < 4; e++) v[4 * i + e] = x[e];
+}
+__device__ __forceinline__ h4 only(h4 x, bool take) {
+  const v2u u = __builtin_bit_cast(v2u, x);
+  v2u r;
+  r[0] = take ? u[0] : 0u;
+  r[1] = take ? u[1] : 0u;
+  return __builtin_bit_cast(h4, r);
+}
+
 template <bool SYM> struct ScaleT { typedef _Float16 type; };
 template <> struct ScaleT<true> { typedef float type; };
 
-template <int NB, bool SYM, int NT> struct Shape {
+// NT tiles of 16 product columns, or with PK > 1 one of 16 / PK rows: the
+// columns c, c + 16 / PK, .. then hold one row's scores for PK groups of 16
+// keys (see the kernel).
+template <int NB, bool SYM, int NT, int PK> struct Shape {
+  static_assert(NT == 1 || PK == 1, "packed rows are one tile");
   static constexpr int D = 32 * NB;
-  static constexpr int ROWS = 16 * NT;
-  static constexpr int AW = NB > 4 ? NB : 4;   // waves; pages of a step
-  static constexpr int PS = AW / NB;           // waves that share a block of columns
-  static constexpr int NP = AW / PS;           // pages of a step whose values a wave takes: NB
-  static constexpr int AT = 64 * AW;
+  static constexpr int ROWS = 16 * NT / PK;
+  static constexpr int BW = NB > AW ? NB / AW : 1;   // blocks of columns of a wave
+  static constexpr int PS = NB < AW ? AW / NB : 1;   // waves that share a block
+  static constexpr int NP = AW / PS;                 // pages of a step whose values a wave takes
+  static constexpr int CH = 4 / PK;                  // score products kept apart: 16 PK keys each
+  static_assert(NP * BW == NB, "one buffer for keys and values");
 };
 
-template <int NB, bool SYM, int NT> struct __align__(16) Lds {
-  typedef Shape<NB, SYM, NT> Sh;
-  uint32_t q[NT * NB * 64 * 2];                // Q codes in operand order
-  v4f p[Sh::AW][NT * 4][64];                   // a step's probabilities, as the lanes hold them
-  float vs[Sh::AW][Sh::NP * 64];               // the waves' value scales, times a power of two
-  typename ScaleT<SYM>::type ks[Sh::AW][NB * 64];
+template <int NB, bool SYM, int NT, int PK> struct __align__(16) Lds {
+  typedef Shape<NB, SYM, NT, PK> Sh;
+  uint32_t q[NT * NB * PK * 64 * 2];           // Q codes in operand order
+  union {
+    v4f p[AW][NT * Sh::CH][64];                // a step's probabilities, as the lanes hold them
+    v4f sums[Sh::PS > 1 ? AW : 1][2 * NT][64]; // at the end
+  };
+  float vs[AW][NB * 64];                       // the waves' value scales, times a power of two
+  typename ScaleT<SYM>::type ks[AW][NB * 64];
   float qd[NT * NB * 16];
-  float mx[Sh::ROWS][Sh::AW];                  // the waves' maxima
+  float mx[16 * NT][AW];                       // the waves' maxima
+  float l[AW][16 * NT];
 };
 
 // N scales of raw words.
@@ -265,21 +302,43 @@ __device__ __forceinline__ void load_words(const uint8_t *p, uint32_t (&w)[N]) {
   }
 }
 
-// Number i of the 16 keys that a lane holds of a page, less its 4 (l / 16).
-constexpr int key_off(int i) { return (i >> 2) * 16 + (i & 3); }
+// Over the lanes that hold one row's scores: l ^ 16, ^ 32, ^ 48 and with
+// packed rows the columns 16 / PK apart.
+template <int PK> __device__ __forceinline__ float max_row(float x) {
+  if (PK > 1) x = fmaxf(x, dpp_f<DPP_ROR8>(x));
+  if (PK > 2) x = fmaxf(x, dpp_f<DPP_ROR4>(x));
+  return max4(x);
+}
+template <int PK> __device__ __forceinline__ float sum_cols(float x) {
+  if (PK > 1) x += dpp_f<DPP_ROR8>(x);
+  if (PK > 2) x += dpp_f<DPP_ROR4>(x);
+  return x;
+}
 
-template <int NB, bool SYM, int NT>
-__global__ __launch_bounds__((Shape<NB, SYM, NT>::AT), 2) void attn_kernel(AttnArgs a) {
-  typedef Shape<NB, SYM, NT> Sh;
+// Number i of the 16 / PK keys that a lane holds of a page, less the lane's
+// first.
+template <int PK> __device__ __forceinline__ constexpr int key_off(int i) {
+  return (i >> 2) * 16 * PK + (i & 3);
+}
+
+// Packed rows (PK = 2 or 4): a tile of 8 or 4 rows would leave half or three
+// quarters of a product's columns, and of every lane's work on scores, empty.
+// Instead PK products of 16 keys each accumulate into one result, with Q's
+// codes in columns 16 / PK s .. of product s and zeros in the others, so
+// column c holds row c % ROWS against key group c / ROWS.  The value products
+// get W with the same columns zeroed where the keys are another group's, and
+// the PK columns of a row are summed once at the end.
+template <int NB, bool SYM, int NT, int PK>
+__global__ __launch_bounds__(AT, (NB * NT > 8 ? 2 : NT > 1 || NB > 4 ? 3 : 4)) void attn_kernel(AttnArgs a) {
+  typedef Shape<NB, SYM, NT, PK> Sh;
   typedef typename ScaleT<SYM>::type sc_t;
-  constexpr int D = Sh::D, ROWS = Sh::ROWS, AW = Sh::AW, AT = Sh::AT, PS = Sh::PS, NP = Sh::NP;
+  constexpr int D = Sh::D, ROWS = Sh::ROWS, PS = Sh::PS, NP = Sh::NP, BW = Sh::BW, CH = Sh::CH;
   constexpr int64_t TILE = kv_tile_bytes(D, SYM);
-  constexpr int SB = kv_scale_bytes(SYM);
-  constexpr int KSW = NB * SB / 4, VSW = NP * SB / 4;     // words of scales a lane stages
-  __shared__ Lds<NB, SYM, NT> lds;
+  constexpr int SB = kv_scale_bytes(SYM), SW = NB * SB / 4;   // words of scales a lane stages
+  __shared__ Lds<NB, SYM, NT, PK> lds;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
-  const int g = lane >> 4;
-  const int blk = wave % NB, sub = wave / NB;      // its columns; its set of a step's pages
+  const int g = lane >> 4, col = lane & 15, grp = PK > 1 ? col / ROWS : 0;
+  const int blk = NB < AW ? wave % NB : wave * BW, sub = NB < AW ? wave / NB : 0;
 
   for (int id = blockIdx.x;; id += gridDim.x) {
     Found f;
@@ -301,40 +360,11 @@ __global__ __launch_bounds__((Shape<NB, SYM, NT>::AT), 2) void attn_kernel(AttnA
 
     // page ids of a step: lane j < AW has page at0 + j's (-1: none)
     const int32_t *table = a.p.pages + (int64_t)f.s * a.p.max_pages;
-    const auto ids_at = [&](int at0) {
-      int v = -1;
-      if (lane < AW && at0 + lane < phi) v = table[at0 + lane];
-      return v < 0 || v >= a.p.n_pages ? -1 : v;
-    };
-    // lane l's word of the value scales: page l / (64 / NP) of the wave's set
-    const int spg = lane / (64 / NP), sof = lane % (64 / NP) * NP;
-    const int64_t head = (int64_t)h * TILE, stride = (int64_t)a.p.NKV * TILE;
-    // One buffer for both: K block b of the wave's page, and once that is used,
-    // the wave's columns of V page b (AW / PS = NB of them), and so on: half a
-    // step lies between a load and its use, in half the registers.
-    v4u buf[NB];
-    uint32_t ksr[KSW], vsr[VSW];
-    const auto k_tile = [&](int ids) {
-      return a.p.k + (int64_t)max(__builtin_amdgcn_readlane(ids, wave), 0) * stride + head;
-    };
-    const auto load_k = [&](const uint8_t *t, int b) {
-      buf[b] = reinterpret_cast<const v4u *>(t + b * 1024)[lane];
-    };
-    const auto load_ks = [&](const uint8_t *t) {
-      load_words(t + NB * 1024 + lane * (KSW * 4), ksr);
-    };
-    const auto load_vs = [&](int ids) {
-      const int64_t page = max(__shfl(ids, sub * NP + spg), 0);
-      load_words(a.p.v + page * stride + head + NB * 1024 + (blk * 64 + sof) * SB, vsr);
-    };
-    const auto load_v = [&](int ids, int j) {
-      const int64_t page = max(__builtin_amdgcn_readlane(ids, sub * NP + j), 0);
-      buf[j] = reinterpret_cast<const v4u *>(a.p.v + page * stride + head + blk * 1024)[lane];
-    };
-    int ids = ids_at(plo);
+    const auto raw_ids = [&](int at0) { return lane < AW && at0 + lane < phi ? table[at0 + lane] : -1; };
+    const auto checked = [&](int v) { return v < 0 || v >= a.p.n_pages ? -1 : v; };
+    int ids = raw_ids(plo);
 
-    // Q codes and scales of the tile's rows (rows past the last repeat it);
-    // the first step's loads go out behind Q's
+    // Q rows (rows past the last repeat it); the first step's loads go out behind them
     constexpr int QI = (ROWS * NB * 8 + AT - 1) / AT;
     v4f x[QI];
 #pragma unroll
@@ -344,6 +374,34 @@ __global__ __launch_bounds__((Shape<NB, SYM, NT>::AT), 2) void attn_kernel(AttnA
       x[k] = *reinterpret_cast<const v4f *>(a.q + (sq.r0 + t) * a.qs +
                                             (int64_t)(h * a.G + rm.head(row, t)) * D + b * 32 + 4 * (i & 7));
     }
+    ids = checked(ids);
+
+    // One buffer for both: K block b of the wave's page, and once that is used,
+    // the wave's columns of a V page (NP BW = NB pieces), and so on: half a
+    // step lies between a load and its use, in half the registers.
+    v4u buf[NB];
+    uint32_t ksr[SW], vsr[SW];
+    // where lane l's NB scales of the wave's value blocks are: piece l / (64 / NB)
+    const int spc = lane / (64 / NB), sof = lane % (64 / NB) * NB;
+    const int spg = sub * NP + spc / BW, sbk = blk + spc % BW;
+    const int64_t head = (int64_t)h * TILE, stride = (int64_t)a.p.NKV * TILE;
+    const auto k_tile = [&](int ids) {
+      return a.p.k + (int64_t)max(__builtin_amdgcn_readlane(ids, wave), 0) * stride + head;
+    };
+    const auto load_k = [&](const uint8_t *t, int b) {
+      buf[b] = reinterpret_cast<const v4u *>(t + b * 1024)[lane];
+    };
+    const auto load_ks = [&](const uint8_t *t) {
+      load_words(t + NB * 1024 + lane * (SW * 4), ksr);
+    };
+    const auto load_vs = [&](int ids) {
+      const int64_t page = max(__shfl(ids, spg), 0);
+      load_words(a.p.v + page * stride + head + NB * 1024 + (sbk * 64 + sof) * SB, vsr);
+    };
+    const auto load_v = [&](int ids, int c) {
+      const int64_t page = max(__builtin_amdgcn_readlane(ids, sub * NP + c / BW), 0);
+      buf[c] = reinterpret_cast<const v4u *>(a.p.v + page * stride + head + (blk + c % BW) * 1024)[lane];
+    };
     {
       const uint8_t *t = k_tile(ids);
       load_ks(t);
@@ -359,31 +417,38 @@ __global__ __launch_bounds__((Shape<NB, SYM, NT>::AT), 2) void attn_kernel(AttnA
       const uint32_t codes = kv_q8_block8<SYM>(v, d);
       const int nt = row >> 4, r = row & 15;
       if (row < ROWS) {
-        lds.q[((nt * NB + b) * 64 + 16 * (j & 3) + r) * 2 + (j >> 2)] = codes;
-        if (j == 0) lds.qd[(nt * NB + b) * 16 + r] = d * a.sign;
+#pragma unroll
+        for (int s = 0; s < PK; s++)
+#pragma unroll
+          for (int z = 0; z < PK; z++)
+            lds.q[(((nt * NB + b) * PK + s) * 64 + 16 * (j & 3) + r + ROWS * z) * 2 + (j >> 2)] =
+                s == z ? codes : 0u;
+        if (j < PK) lds.qd[(nt * NB + b) * 16 + r + (PK > 1 ? ROWS * j : 0)] = d * a.sign;
       }
     }
     __syncthreads();
 
-    // this lane's rows see lo_key < key <= hi_key; both less 4 g, the lane's first key of a page
+    // this lane's rows see lo_key < key <= hi_key; both less the lane's first key of a page
+    const int kbase = 4 * g + 16 * grp;
     int hi_key[NT], lo_key[NT];
 #pragma unroll
     for (int nt = 0; nt < NT; nt++) {
-      const int pos = base_pos + rm.token(min(16 * nt + (lane & 15), fn - 1));
-      hi_key[nt] = pos - 4 * g;
-      lo_key[nt] = (a.window > 0 && a.window <= pos ? (int)(pos - a.window) : -1) - 4 * g;
+      const int pos = base_pos + rm.token(min(16 * nt + (PK > 1 ? col % ROWS : col), fn - 1));
+      hi_key[nt] = pos - kbase;
+      lo_key[nt] = (a.window > 0 && a.window <= pos ? (int)(pos - a.window) : -1) - kbase;
     }
-    // first token of the lane's NP value scales within its page, as kv_scale_at has them
+    // first token of the lane's NB value scales within its page, as kv_scale_at has them
     const int vtok = sof / 16 * 4 + sof / 4 % 4 * 16 + sof % 4;
 
     float m[NT], mk[NT], l[NT];
-    v4f acc[NT][2];
+    v4f acc[NT][BW][2];
 #pragma unroll
     for (int nt = 0; nt < NT; nt++) {
       m[nt] = -FLT_MAX;
       mk[nt] = -FLT_MAX;
       l[nt] = 0.0f;
-      acc[nt][0] = acc[nt][1] = v4f{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int b = 0; b < BW; b++) acc[nt][b][0] = acc[nt][b][1] = v4f{0.f, 0.f, 0.f, 0.f};
     }
     // value scales are below 2^vexp and enter the product times 2^(15 - vexp)
     int vexp = -126;
@@ -392,54 +457,65 @@ __global__ __launch_bounds__((Shape<NB, SYM, NT>::AT), 2) void attn_kernel(AttnA
     float minus = -1.0f;               // opaque, so that the halves' difference is one mixed FMA
     asm("" : "+v"(minus));
     for (int at0 = plo; at0 < phi; at0 += AW) {
-      const int next = at0 + AW < phi ? ids_at(at0 + AW) : -1;
       const bool more = at0 + AW < phi;
+      const int raw_next = raw_ids(at0 + AW);
       const int key = (at0 + wave) * KV_PAGE;
       // ---- scores of page at0 + wave
       const bool here = __builtin_amdgcn_readlane(ids, wave) >= 0;
 #pragma unroll
-      for (int w = 0; w < KSW; w++) reinterpret_cast<word *>(ks)[lane * KSW + w] = ksr[w];
-      float S[NT][16];
+      for (int w = 0; w < SW; w++) reinterpret_cast<word *>(ks)[lane * SW + w] = ksr[w];
+      float S[NT][4 * CH];
 #pragma unroll
       for (int nt = 0; nt < NT; nt++)
 #pragma unroll
-        for (int i = 0; i < 16; i++) S[nt][i] = 0.0f;
+        for (int i = 0; i < 4 * CH; i++) S[nt][i] = 0.0f;
 #pragma unroll
       for (int b = 0; b < NB; b++) {
-        long qb[NT];
+        long qb[NT][PK];
         float dq[NT], cq[NT];
 #pragma unroll
         for (int nt = 0; nt < NT; nt++) {
-          qb[nt] = reinterpret_cast<const long *>(lds.q)[(nt * NB + b) * 64 + lane];
-          dq[nt] = lds.qd[(nt * NB + b) * 16 + (lane & 15)];
+#pragma unroll
+          for (int s = 0; s < PK; s++)
+            qb[nt][s] = reinterpret_cast<const long *>(lds.q)[((nt * NB + b) * PK + s) * 64 + lane];
+          dq[nt] = lds.qd[(nt * NB + b) * 16 + col];
           cq[nt] = -12582912.0f * dq[nt];
         }
-        sc_t dk[16];
+        sc_t dk[4 * CH];
 #pragma unroll
-        for (int i = 0; i < 16; i++) dk[i] = ks[b * 64 + g * 16 + i];
+        for (int i = 0; i < 4 * CH; i++) dk[i] = ks[b * 64 + g * 16 + 4 * grp + 4 * PK * (i >> 2) + (i & 3)];
 #pragma unroll
-        for (int i = 0; i < 4; i++) {
-          const uint32_t y = buf[b][i];
-          const long kb = (long)((uint64_t)(y & 0xF0F0F0F0u) << 32 | (y << 4 & 0xF0F0F0F0u));
+        for (int c = 0; c < CH; c++) {
+          v4i r[NT];
+#pragma unroll
+          for (int nt = 0; nt < NT; nt++) r[nt] = v4i{0x4B400000, 0x4B400000, 0x4B400000, 0x4B400000};
+#pragma unroll
+          for (int s = 0; s < PK; s++) {
+            const uint32_t y = buf[b][c * PK + s];
+            const long kb = (long)((uint64_t)(y & 0xF0F0F0F0u) << 32 | (y << 4 & 0xF0F0F0F0u));
+#pragma unroll
+            for (int nt = 0; nt < NT; nt++)
+              r[nt] = __builtin_amdgcn_mfma_i32_16x16x32_i8(kb, qb[nt][s], r[nt], 0, 0, 0);
+          }
 #pragma unroll
           for (int nt = 0; nt < NT; nt++) {
-            const v4i c = {0x4B400000, 0x4B400000, 0x4B400000, 0x4B400000};
-            const v4f r = __builtin_bit_cast(
-                v4f, __builtin_amdgcn_mfma_i32_16x16x32_i8(kb, qb[nt], c, 0, 0, 0));
+            const v4f rf = __builtin_bit_cast(v4f, r[nt]);
 #pragma unroll
             for (int e = 0; e < 4; e++) {
               // SYM: an fp32 scale times 1.5 2^23 would round, so s comes first
-              const float t = SYM ? (r[e] - 12582912.0f) * dq[nt] : fmaf(r[e], dq[nt], cq[nt]);
-              S[nt][4 * i + e] = fmaf(t, (float)dk[4 * i + e], S[nt][4 * i + e]);
+              const float t = SYM ? (rf[e] - 12582912.0f) * dq[nt] : fmaf(rf[e], dq[nt], cq[nt]);
+              S[nt][4 * c + e] = fmaf(t, (float)dk[4 * c + e], S[nt][4 * c + e]);
             }
           }
+          // pinned in order: moved together, the products and scales of all
+          // blocks would be live at once
+          if (c == CH - 1 || c == 1) {
+#pragma unroll
+            for (int nt = 0; nt < NT; nt++)
+#pragma unroll
+              for (int i = 0; i < 4 * CH; i++) asm volatile("" : "+v"(S[nt][i]));
+          }
         }
-        // one block at a time: moved together, the blocks' products and scales
-        // would all be live at once
-#pragma unroll
-        for (int nt = 0; nt < NT; nt++)
-#pragma unroll
-          for (int i = 0; i < 16; i++) asm volatile("" : "+v"(S[nt][i]));
         load_v(ids, b);
       }
       // keys that not every row sees; an absent page's are seen by none
@@ -448,28 +524,28 @@ __global__ __launch_bounds__((Shape<NB, SYM, NT>::AT), 2) void attn_kernel(AttnA
         for (int nt = 0; nt < NT; nt++) {
           const int last = here ? hi_key[nt] - key : -100, before = lo_key[nt] - key;
 #pragma unroll
-          for (int i = 0; i < 16; i++)
-            if (key_off(i) > last || key_off(i) <= before) S[nt][i] = -INFINITY;
+          for (int i = 0; i < 4 * CH; i++)
+            if (key_off<PK>(i) > last || key_off<PK>(i) <= before) S[nt][i] = -INFINITY;
         }
       }
 #pragma unroll
       for (int nt = 0; nt < NT; nt++) {
         float mx = -FLT_MAX;
 #pragma unroll
-        for (int i = 0; i < 16; i++) mx = fmaxf(mx, S[nt][i]);
-        mx = max4(mx);
+        for (int i = 0; i < 4 * CH; i++) mx = fmaxf(mx, S[nt][i]);
+        mx = max_row<PK>(mx);
         if (lane < 16) lds.mx[16 * nt + lane][wave] = mx;
       }
 
       // ---- the wave's value scales of the step; keys that no row sees count for nothing
       {
-        const int vkey = (at0 + sub * NP + spg) * KV_PAGE + vtok;
-        const bool vhere = __shfl(ids, sub * NP + spg) >= 0;
-        float dv[NP], vmax = 0.0f;
+        const int vkey = (at0 + spg) * KV_PAGE + vtok;
+        const bool vhere = __shfl(ids, spg) >= 0;
+        float dv[NB], vmax = 0.0f;
 #pragma unroll
-        for (int i = 0; i < NP; i++) {
+        for (int i = 0; i < NB; i++) {
           dv[i] = scale_of<SYM>(vsr, i);
-          const int kk = vkey + key_off(i);
+          const int kk = vkey + (i >> 2) * 16 + (i & 3);
           if (!vhere || kk > pos1 || kk < key0) dv[i] = 0.0f;
           const float y = fabsf(dv[i]);
           vmax = fmaxf(vmax, y < INFINITY ? y : 0.0f);
@@ -481,14 +557,17 @@ __global__ __launch_bounds__((Shape<NB, SYM, NT>::AT), 2) void attn_kernel(AttnA
 #pragma unroll
           for (int nt = 0; nt < NT; nt++)
 #pragma unroll
-            for (int s = 0; s < 2; s++)
+            for (int b = 0; b < BW; b++)
 #pragma unroll
-              for (int y = 0; y < 4; y++) acc[nt][s][y] = ldexpf(acc[nt][s][y], vexp - e);
+              for (int s = 0; s < 2; s++)
+#pragma unroll
+                for (int y = 0; y < 4; y++) acc[nt][b][s][y] = ldexpf(acc[nt][b][s][y], vexp - e);
           vexp = e;
         }
 #pragma unroll
-        for (int i = 0; i < NP; i++) vs[lane * NP + i] = ldexpf(dv[i], 15 - vexp);
+        for (int i = 0; i < NB; i++) vs[lane * NB + i] = ldexpf(dv[i], 15 - vexp);
       }
+      const int next = checked(raw_next);
       const uint8_t *const kt = k_tile(next);
       if (more) {
         load_vs(next);
@@ -501,9 +580,8 @@ __global__ __launch_bounds__((Shape<NB, SYM, NT>::AT), 2) void attn_kernel(AttnA
       float mn[NT];
 #pragma unroll
       for (int nt = 0; nt < NT; nt++) {
-        mn[nt] = m[nt];
-#pragma unroll
-        for (int w = 0; w < AW; w++) mn[nt] = fmaxf(mn[nt], lds.mx[16 * nt + (lane & 15)][w]);
+        const v4f w = *reinterpret_cast<const v4f *>(lds.mx[16 * nt + col]);
+        mn[nt] = fmaxf(m[nt], fmaxf(fmaxf(w[0], w[1]), fmaxf(w[2], w[3])));
         grow |= mn[nt] > m[nt];
       }
       if (__ballot(grow)) {
@@ -514,21 +592,25 @@ __global__ __launch_bounds__((Shape<NB, SYM, NT>::AT), 2) void attn_kernel(AttnA
           m[nt] = mn[nt];
           mk[nt] = mkn;
           l[nt] *= al;
-          acc[nt][0] *= al;
-          acc[nt][1] *= al;
+#pragma unroll
+          for (int b = 0; b < BW; b++) {
+            acc[nt][b][0] *= al;
+            acc[nt][b][1] *= al;
+          }
         }
       }
       // ---- probabilities (a masked score's is exp2(-infinity) = 0)
 #pragma unroll
       for (int nt = 0; nt < NT; nt++) {
-        v4f p[4];
+        v4f s = v4f{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int i = 0; i < 4; i++) {
+        for (int c = 0; c < CH; c++) {
+          v4f p;
 #pragma unroll
-          for (int e = 0; e < 4; e++) p[i][e] = exp2_f(fmaf(S[nt][4 * i + e], a.k, -mk[nt]));
-          lds.p[wave][4 * nt + i][lane] = p[i];
+          for (int e = 0; e < 4; e++) p[e] = exp2_f(fmaf(S[nt][4 * c + e], a.k, -mk[nt]));
+          lds.p[wave][CH * nt + c][lane] = p;
+          s += p;
         }
-        const v4f s = (p[0] + p[1]) + (p[2] + p[3]);
         l[nt] += (s[0] + s[1]) + (s[2] + s[3]);
       }
       __syncthreads();
@@ -539,111 +621,126 @@ __global__ __launch_bounds__((Shape<NB, SYM, NT>::AT), 2) void attn_kernel(AttnA
         const int pgj = sub * NP + j;
         if (at0 + pgj < phi) {
 #pragma unroll
-          for (int hh = 0; hh < 2; hh++) {         // 32 keys at a time
-            float d[8];
+          for (int bb = 0; bb < BW; bb++) {
+            const int pc = j * BW + bb;
+            // W of the lane's keys, as two halves
+            h4 whi[NT][CH], wlo[NT][CH];
+            if (PK > 1) make_w(lds.p[pgj][0][lane], vs + pc * 64 + g * 16 + 4 * grp, minus, whi[0][0], wlo[0][0]);
+            if (PK == 2) make_w(lds.p[pgj][CH - 1][lane], vs + pc * 64 + g * 16 + 4 * grp + 8, minus, whi[0][CH - 1], wlo[0][CH - 1]);
 #pragma unroll
-            for (int i = 0; i < 8; i++) d[i] = vs[j * 64 + g * 16 + 8 * hh + i];
-            h8 c[2];                               // elements l % 16 and + 16
-#pragma unroll
-            for (int i = 0; i < 2; i++) {
-              const uint32_t y = buf[j][2 * hh + i], z = y >> 8;
-              const h2 off = {(_Float16)-1032.0f, (_Float16)-1032.0f};
-              const h2 six = {(_Float16)0.0625f, (_Float16)0.0625f};
-              const h2 off2 = {(_Float16)-72.0f, (_Float16)-72.0f};
-              const h2 a0 = __builtin_bit_cast(h2, (y & 0x000F000Fu) | 0x64006400u) + off;
-              const h2 a1 = __builtin_bit_cast(h2, (z & 0x000F000Fu) | 0x64006400u) + off;
-              const h2 b0 = __builtin_elementwise_fma(
-                  __builtin_bit_cast(h2, (y & 0x00F000F0u) | 0x64006400u), six, off2);
-              const h2 b1 = __builtin_elementwise_fma(
-                  __builtin_bit_cast(h2, (z & 0x00F000F0u) | 0x64006400u), six, off2);
-              c[0][4 * i] = a0[0]; c[0][4 * i + 1] = a0[1]; c[0][4 * i + 2] = a1[0]; c[0][4 * i + 3] = a1[1];
-              c[1][4 * i] = b0[0]; c[1][4 * i + 1] = b0[1]; c[1][4 * i + 2] = b1[0]; c[1][4 * i + 3] = b1[1];
-            }
-#pragma unroll
-            for (int nt = 0; nt < NT; nt++) {
-              h8 hi, lo;
+            for (int hh = 0; hh < 2; hh++) {         // 32 keys at a time
+              h8 c[2];                               // elements l % 16 and + 16
 #pragma unroll
               for (int i = 0; i < 2; i++) {
-                const v4f p = lds.p[pgj][4 * nt + 2 * hh + i][lane];
+                const uint32_t y = buf[pc][2 * hh + i], z = y >> 8;
+                const h2 off = {(_Float16)-1032.0f, (_Float16)-1032.0f};
+                const h2 six = {(_Float16)0.0625f, (_Float16)0.0625f};
+                const h2 off2 = {(_Float16)-72.0f, (_Float16)-72.0f};
+                const h2 a0 = __builtin_bit_cast(h2, (y & 0x000F000Fu) | 0x64006400u) + off;
+                const h2 a1 = __builtin_bit_cast(h2, (z & 0x000F000Fu) | 0x64006400u) + off;
+                const h2 b0 = __builtin_elementwise_fma(
+                    __builtin_bit_cast(h2, (y & 0x00F000F0u) | 0x64006400u), six, off2);
+                const h2 b1 = __builtin_elementwise_fma(
+                    __builtin_bit_cast(h2, (z & 0x00F000F0u) | 0x64006400u), six, off2);
+                c[0][4 * i] = a0[0]; c[0][4 * i + 1] = a0[1]; c[0][4 * i + 2] = a1[0]; c[0][4 * i + 3] = a1[1];
+                c[1][4 * i] = b0[0]; c[1][4 * i + 1] = b0[1]; c[1][4 * i + 2] = b1[0]; c[1][4 * i + 3] = b1[1];
+              }
 #pragma unroll
-                for (int e = 0; e < 4; e += 2) {
-                  v2f w, z;
-                  // 0 times anything is 0: a key that the row does not see may have any scale
-                  w[0] = mul_zero(p[e], d[4 * i + e]);
-                  w[1] = mul_zero(p[e + 1], d[4 * i + e + 1]);
-                  const h2 y = __builtin_convertvector(w, h2);
-                  z[0] = fmaf((float)y[0], minus, w[0]);
-                  z[1] = fmaf((float)y[1], minus, w[1]);
-                  const h2 y2 = __builtin_convertvector(z, h2);
-                  hi[4 * i + e] = y[0]; hi[4 * i + e + 1] = y[1];
-                  lo[4 * i + e] = y2[0]; lo[4 * i + e + 1] = y2[1];
+              for (int nt = 0; nt < NT; nt++) {
+                h8 hi, lo;
+                if constexpr (PK == 1) {
+#pragma unroll
+                  for (int i = 0; i < 2; i++) {
+                    h4 x, y;
+                    make_w(lds.p[pgj][4 * nt + 2 * hh + i][lane], vs + pc * 64 + g * 16 + 8 * hh + 4 * i, minus, x, y);
+                    put(hi, i, x);
+                    put(lo, i, y);
+                  }
+                } else {
+#pragma unroll
+                  for (int i = 0; i < 2; i++) {        // key group 2 hh + i
+                    const int ch = (2 * hh + i) / PK, mine = (2 * hh + i) % PK;
+                    put(hi, i, only(whi[0][ch], grp == mine));
+                    put(lo, i, only(wlo[0][ch], grp == mine));
+                  }
+                }
+#pragma unroll
+                for (int s = 0; s < 2; s++) {
+                  acc[nt][bb][s] = __builtin_amdgcn_mfma_f32_16x16x32_f16(c[s], hi, acc[nt][bb][s], 0, 0, 0);
+                  acc[nt][bb][s] = __builtin_amdgcn_mfma_f32_16x16x32_f16(c[s], lo, acc[nt][bb][s], 0, 0, 0);
                 }
               }
 #pragma unroll
-              for (int s = 0; s < 2; s++) {
-                acc[nt][s] = __builtin_amdgcn_mfma_f32_16x16x32_f16(c[s], hi, acc[nt][s], 0, 0, 0);
-                acc[nt][s] = __builtin_amdgcn_mfma_f32_16x16x32_f16(c[s], lo, acc[nt][s], 0, 0, 0);
-              }
+              for (int nt = 0; nt < NT; nt++) asm volatile("" : "+v"(acc[nt][bb][0]), "+v"(acc[nt][bb][1]));
             }
-#pragma unroll
-            for (int nt = 0; nt < NT; nt++) asm volatile("" : "+v"(acc[nt][0]), "+v"(acc[nt][1]));
           }
         }
-        if (more) load_k(kt, j);
+        if (more) {
+#pragma unroll
+          for (int bb = 0; bb < BW; bb++) load_k(kt, j * BW + bb);
+        }
       }
       ids = next;
     }
 
     // the waves' sums; where PS waves share columns, their products too
-    __syncthreads();
-    float *const red = reinterpret_cast<float *>(lds.p);      // [AW][ROWS], then [AW][2 NT][64] v4f
 #pragma unroll
     for (int nt = 0; nt < NT; nt++) {
-      l[nt] = sum4(l[nt]);
-      if (lane < 16) red[wave * ROWS + 16 * nt + lane] = l[nt];
+      l[nt] = sum_cols<PK>(sum4(l[nt]));
+      if (lane < 16) lds.l[wave][16 * nt + lane] = l[nt];
 #pragma unroll
-      for (int s = 0; s < 2; s++)
+      for (int b = 0; b < BW; b++)
 #pragma unroll
-        for (int y = 0; y < 4; y++) acc[nt][s][y] = ldexpf(acc[nt][s][y], vexp - 15);
+        for (int s = 0; s < 2; s++)
+#pragma unroll
+          for (int y = 0; y < 4; y++)
+            acc[nt][b][s][y] = ldexpf(sum_cols<PK>(acc[nt][b][s][y]), vexp - 15);
     }
-    v4f *const pr = reinterpret_cast<v4f *>(red + AW * ROWS);
-    if (PS > 1 && sub > 0) {
+    if constexpr (PS > 1) {
+      __syncthreads();                 // the last step's probabilities have been read
+      if (sub > 0) {
 #pragma unroll
-      for (int nt = 0; nt < NT; nt++)
+        for (int nt = 0; nt < NT; nt++)
 #pragma unroll
-        for (int s = 0; s < 2; s++) pr[(wave * 2 * NT + 2 * nt + s) * 64 + lane] = acc[nt][s];
+          for (int s = 0; s < 2; s++) lds.sums[wave][2 * nt + s][lane] = acc[nt][0][s];
+      }
     }
     __syncthreads();
     const bool whole = f.runs == 1;
     const int slot = whole ? 0 : f.slot0 + f.local;
     float *part = a.part + (int64_t)slot * (ROWS * (D + 2));
-    if (sub == 0 && (whole || slot < a.slots)) {
+    if (sub == 0 && col < ROWS && (whole || slot < a.slots)) {
 #pragma unroll
       for (int nt = 0; nt < NT; nt++) {
-        const int row = 16 * nt + (lane & 15);
-        float lt = 0.0f;
+        const int row = 16 * nt + col;
+        const float lt = (lds.l[0][row] + lds.l[1][row]) + (lds.l[2][row] + lds.l[3][row]);
+        if constexpr (PS > 1) {
 #pragma unroll
-        for (int w = 0; w < AW; w++) lt += red[w * ROWS + row];
+          for (int q = 1; q < PS; q++)
 #pragma unroll
-        for (int q = 1; q < PS; q++)
+            for (int s = 0; s < 2; s++) acc[nt][0][s] += lds.sums[wave + q * NB][2 * nt + s][lane];
+        }
+        const int t = rm.token(min(row, fn - 1));
+        const int64_t o = (sq.r0 + t) * a.NH + h * a.G + rm.head(min(row, fn - 1), t);
+        const float inv = lt != 0.0f ? 1.0f / lt : 0.0f;
 #pragma unroll
-          for (int s = 0; s < 2; s++) acc[nt][s] += pr[((wave + q * NB) * 2 * NT + 2 * nt + s) * 64 + lane];
-        const int col = blk * 32 + 4 * g;
-        if (!whole) {
-          *reinterpret_cast<v4f *>(part + row * D + col) = acc[nt][0];
-          *reinterpret_cast<v4f *>(part + row * D + col + 16) = acc[nt][1];
-          if (wave == 0 && g == 0) {
+        for (int b = 0; b < BW; b++) {
+          const int at = (blk + b) * 32 + 4 * g;
+          if (!whole) {
+            *reinterpret_cast<v4f *>(part + row * D + at) = acc[nt][b][0];
+            *reinterpret_cast<v4f *>(part + row * D + at + 16) = acc[nt][b][1];
+          } else if (row < fn) {
+            *reinterpret_cast<v4f *>(a.out + o * D + at) = acc[nt][b][0] * inv;
+            *reinterpret_cast<v4f *>(a.out + o * D + at + 16) = acc[nt][b][1] * inv;
+          }
+        }
+        if (wave == 0 && g == 0) {
+          if (!whole) {
             part[ROWS * D + 2 * row] = mk[nt];
             part[ROWS * D + 2 * row + 1] = lt;
-          }
-        } else if (row < fn) {
-          const int t = rm.token(row);
-          const int64_t o = (sq.r0 + t) * a.NH + h * a.G + rm.head(row, t);
-          const float inv = lt != 0.0f ? 1.0f / lt : 0.0f;
-          *reinterpret_cast<v4f *>(a.out + o * D + col) = acc[nt][0] * inv;
-          *reinterpret_cast<v4f *>(a.out + o * D + col + 16) = acc[nt][1] * inv;
-          if (a.lse && wave == 0 && g == 0)
+          } else if (a.lse && row < fn) {
             a.lse[o] = lt != 0.0f ? (mk[nt] + log2f(lt)) * 0.693147180559945f : -INFINITY;
+          }
         }
       }
     }
@@ -654,9 +751,9 @@ __global__ __launch_bounds__((Shape<NB, SYM, NT>::AT), 2) void attn_kernel(AttnA
 // Joins the runs of item blockIdx.x (counted over the items with several
 // runs), rows blockIdx.y * JR .. of its tile: a row by JT / JR threads, D / 4
 // lanes by groups that take the runs in turn, summed in a fixed order.
-template <int NB, int NT, int JT, int JR>
+template <int NB, int ROWS, int JT, int JR>
 __global__ __launch_bounds__(JT) void join_kernel(AttnArgs a) {
-  constexpr int D = 32 * NB, ROWS = 16 * NT, L = D / 4, TR = JT / JR, NG = TR / L;
+  constexpr int D = 32 * NB, L = D / 4, TR = JT / JR, NG = TR / L;
   __shared__ v4f so[JR][NG][L];
   __shared__ float sw[JR][JOIN_MAX], sl[JR];
   Found f;
@@ -714,14 +811,13 @@ __global__ __launch_bounds__(JT) void join_kernel(AttnArgs a) {
   if (c4 == 0 && a.lse) a.lse[o] = l != 0.0f ? (R + log2f(l)) * 0.693147180559945f : -INFINITY;
 }
 
-// Rows of a tile: 32 once sequences have more than 16 on average (a tile's
-// rows share the page's loads and decoded codes), else the 16 of one product.
+// Rows of a tile by the rows a sequence has of a KV head on average: 4 or 8
+// packed (a decode step of few heads a group), the 16 of one product, or 32,
+// which share the page's loads and decoded codes.
 int tile_rows(const w4a8_kv *kv, int64_t T, int64_t NH) {
-  const int64_t rows = T * (NH / kv->NKV);
-  return kv->B > 0 && rows > 16 * kv->B ? 32 : 16;
+  const int64_t rows = T * (NH / kv->NKV), B = std::max<int64_t>(1, kv->B);
+  return rows <= 4 * B ? 4 : rows <= 8 * B ? 8 : rows <= 16 * B ? 16 : 32;
 }
-// Fewest pages of a run: one step.
-int run_min(const w4a8_kv *kv) { return kv->D == 256 ? 8 : 4; }
 
 // Bounds on the call's items, and on the partial results it can need: a
 // sequence is split only into runs of more than half of C >= total / TARGET
@@ -732,9 +828,8 @@ int64_t items_bound(const w4a8_kv *kv, int64_t T, int64_t NH) {
   return ((T * G) / rt + std::min(kv->B, T)) * kv->NKV;
 }
 int64_t slots_bound(const w4a8_kv *kv, int64_t T, int64_t NH) {
-  const int c = run_min(kv);
-  if (kv->max_pages <= c) return 0;
-  const int64_t runs = (kv->max_pages + c - 1) / c;
+  if (kv->max_pages <= AW) return 0;
+  const int64_t runs = (kv->max_pages + AW - 1) / AW;
   return std::min<int64_t>(2 * TARGET, items_bound(kv, T, NH) * runs);
 }
 
@@ -746,25 +841,31 @@ int attn_sizes(const w4a8_kv *kv, int64_t T, int64_t NH) {
   return W4A8_OK;
 }
 
-template <int NB, bool SYM, int NT>
+template <int NB, bool SYM, int NT, int PK>
 int launch(const AttnArgs &a, int64_t items, hipStream_t s) {
+  constexpr int ROWS = 16 * NT / PK;
   const int64_t grid = std::min<int64_t>(items + a.slots, 1 << 20);
-  attn_kernel<NB, SYM, NT><<<dim3((unsigned)grid), dim3(Shape<NB, SYM, NT>::AT), 0, s>>>(a);
+  attn_kernel<NB, SYM, NT, PK><<<dim3((unsigned)grid), dim3(AT), 0, s>>>(a);
   if (int rc = check_launch(); rc != W4A8_OK || a.slots == 0) return rc;
   // Joins: with few items, which then have many runs, 1024 threads a row;
   // else a wave a row.
   const int64_t joins = std::min<int64_t>(items, TARGET);
-  const int rows = (int)std::min<int64_t>(16 * NT, a.T * a.G);
+  const int rows = (int)std::min<int64_t>(ROWS, a.T * a.G);
   if (items <= 16)
-    join_kernel<NB, NT, 1024, 1><<<dim3((unsigned)joins, rows), dim3(1024), 0, s>>>(a);
+    join_kernel<NB, ROWS, 1024, 1><<<dim3((unsigned)joins, rows), dim3(1024), 0, s>>>(a);
   else
-    join_kernel<NB, NT, 256, 4><<<dim3((unsigned)joins, (rows + 3) / 4), dim3(256), 0, s>>>(a);
+    join_kernel<NB, ROWS, 256, 4><<<dim3((unsigned)joins, (rows + 3) / 4), dim3(256), 0, s>>>(a);
   return check_launch();
 }
 
 template <int NB, bool SYM>
-int launch_rows(const AttnArgs &a, bool wide, int64_t items, hipStream_t s) {
-  return wide ? launch<NB, SYM, 2>(a, items, s) : launch<NB, SYM, 1>(a, items, s);
+int launch_rows(const AttnArgs &a, int rows, int64_t items, hipStream_t s) {
+  switch (rows) {
+    case 4: return launch<NB, SYM, 1, 4>(a, items, s);
+    case 8: return launch<NB, SYM, 1, 2>(a, items, s);
+    case 16: return launch<NB, SYM, 1, 1>(a, items, s);
+    default: return launch<NB, SYM, 2, 1>(a, items, s);
+  }
 }
 
 }  // namespace
@@ -798,12 +899,13 @@ extern "C" int attn_q4_forward(const w4a8_kv *kv, const float *q, int64_t q_stri
                 // a factor of 0 goes to Q, so that a masked score's -infinity stays one
                 scale != 0.0f ? std::fabs(scale) * 1.44269504f / 16.0f : 1.0f,
                 scale < 0.0f ? -1.0f : scale == 0.0f ? 0.0f : 1.0f, window,
-                reinterpret_cast<float *>(workspace), (int)slots_bound(kv, T, NH), run_min(kv),
+                reinterpret_cast<float *>(workspace), (int)slots_bound(kv, T, NH),
                 1.0f / (float)(NH / kv->NKV)};
   const int64_t items = items_bound(kv, T, NH);
-  const bool sym = kv->format == W4A8_KV_Q4_SYM, wide = tile_rows(kv, T, NH) == 32;
+  const bool sym = kv->format == W4A8_KV_Q4_SYM;
+  const int rows = tile_rows(kv, T, NH);
   const hipStream_t s = as_stream(stream);
-  if (kv->D == 64) return sym ? launch_rows<2, true>(a, wide, items, s) : launch_rows<2, false>(a, wide, items, s);
-  if (kv->D == 128) return sym ? launch_rows<4, true>(a, wide, items, s) : launch_rows<4, false>(a, wide, items, s);
-  return sym ? launch_rows<8, true>(a, wide, items, s) : launch_rows<8, false>(a, wide, items, s);
+  if (kv->D == 64) return sym ? launch_rows<2, true>(a, rows, items, s) : launch_rows<2, false>(a, rows, items, s);
+  if (kv->D == 128) return sym ? launch_rows<4, true>(a, rows, items, s) : launch_rows<4, false>(a, rows, items, s);
+  return sym ? launch_rows<8, true>(a, rows, items, s) : launch_rows<8, false>(a, rows, items, s);
 }
