@@ -49,7 +49,7 @@ namespace w4a8 {
 
 namespace {
 
-constexpr int TARGET = 512;           // runs wanted: two workgroups a compute unit
+constexpr int TARGET = 768;           // runs wanted: three workgroups a compute unit
 constexpr int AW = 4, AT = 64 * AW;   // waves of a workgroup; pages of a step
 constexpr int JOIN_MAX = 2 * TARGET;  // most runs of an item
 
@@ -242,11 +242,25 @@ __device__ __forceinline__ void put(h8 &v, int i, h4 x) {
 #pragma unroll
   for (int e = 0; e < 4; e++) v[4 * i + e] = x[e];
 }
-__device__ __forceinline__ h4 only(h4 x, bool take) {
+// A rotation within 16 lanes (every lane valid, so no old value is kept).
+template <int CTRL> __device__ __forceinline__ int ror(int x) {
+  return __builtin_amdgcn_mov_dpp(x, CTRL, 0xF, 0xF, true);
+}
+template <int CTRL> __device__ __forceinline__ float ror_f(float x) {
+  return __builtin_bit_cast(float, ror<CTRL>(__builtin_bit_cast(int, x)));
+}
+
+// Of lane l + (16 / PK) z of the 16.
+template <int PK> __device__ __forceinline__ h4 from_col(h4 x, int z) {
   const v2u u = __builtin_bit_cast(v2u, x);
+  const int by = 16 / PK * z;
   v2u r;
-  r[0] = take ? u[0] : 0u;
-  r[1] = take ? u[1] : 0u;
+#pragma unroll
+  for (int i = 0; i < 2; i++)
+    r[i] = (uint32_t)(by == 0   ? (int)u[i]
+                      : by == 4 ? ror<DPP_ROR12>((int)u[i])
+                      : by == 8 ? ror<DPP_ROR8>((int)u[i])
+                                : ror<DPP_ROR4>((int)u[i]));
   return __builtin_bit_cast(h4, r);
 }
 
@@ -305,13 +319,13 @@ __device__ __forceinline__ void load_words(const uint8_t *p, uint32_t (&w)[N]) {
 // Over the lanes that hold one row's scores: l ^ 16, ^ 32, ^ 48 and with
 // packed rows the columns 16 / PK apart.
 template <int PK> __device__ __forceinline__ float max_row(float x) {
-  if (PK > 1) x = fmaxf(x, dpp_f<DPP_ROR8>(x));
-  if (PK > 2) x = fmaxf(x, dpp_f<DPP_ROR4>(x));
+  if (PK > 1) x = fmaxf(x, ror_f<DPP_ROR8>(x));
+  if (PK > 2) x = fmaxf(x, ror_f<DPP_ROR4>(x));
   return max4(x);
 }
 template <int PK> __device__ __forceinline__ float sum_cols(float x) {
-  if (PK > 1) x += dpp_f<DPP_ROR8>(x);
-  if (PK > 2) x += dpp_f<DPP_ROR4>(x);
+  if (PK > 1) x += ror_f<DPP_ROR8>(x);
+  if (PK > 2) x += ror_f<DPP_ROR4>(x);
   return x;
 }
 
@@ -325,9 +339,9 @@ template <int PK> __device__ __forceinline__ constexpr int key_off(int i) {
 // quarters of a product's columns, and of every lane's work on scores, empty.
 // Instead PK products of 16 keys each accumulate into one result, with Q's
 // codes in columns 16 / PK s .. of product s and zeros in the others, so
-// column c holds row c % ROWS against key group c / ROWS.  The value products
-// get W with the same columns zeroed where the keys are another group's, and
-// the PK columns of a row are summed once at the end.
+// column c holds row c % ROWS against key group c / ROWS.  W is formed so
+// packed too; for the value products the groups' halves move to the row's
+// first column, and what they give in the other columns is not used.
 template <int NB, bool SYM, int NT, int PK>
 __global__ __launch_bounds__(AT, (NB * NT > 8 ? 2 : NT > 1 || NB > 4 ? 3 : 4)) void attn_kernel(AttnArgs a) {
   typedef Shape<NB, SYM, NT, PK> Sh;
@@ -456,6 +470,10 @@ __global__ __launch_bounds__(AT, (NB * NT > 8 ? 2 : NT > 1 || NB > 4 ? 3 : 4)) v
     float *vs = lds.vs[wave];
     float minus = -1.0f;               // opaque, so that the halves' difference is one mixed FMA
     asm("" : "+v"(minus));
+    // opaque too: as literals they would keep the mask and the bias apart
+    uint32_t low4 = 0x000F000Fu, high4 = 0x00F000F0u, bias = 0x64006400u;
+    asm("" : "+v"(low4), "+v"(high4), "+v"(bias));
+    const v4i c0 = {0x4B400000, 0x4B400000, 0x4B400000, 0x4B400000};
     for (int at0 = plo; at0 < phi; at0 += AW) {
       const bool more = at0 + AW < phi;
       const int raw_next = raw_ids(at0 + AW);
@@ -488,14 +506,12 @@ __global__ __launch_bounds__(AT, (NB * NT > 8 ? 2 : NT > 1 || NB > 4 ? 3 : 4)) v
         for (int c = 0; c < CH; c++) {
           v4i r[NT];
 #pragma unroll
-          for (int nt = 0; nt < NT; nt++) r[nt] = v4i{0x4B400000, 0x4B400000, 0x4B400000, 0x4B400000};
-#pragma unroll
           for (int s = 0; s < PK; s++) {
             const uint32_t y = buf[b][c * PK + s];
             const long kb = (long)((uint64_t)(y & 0xF0F0F0F0u) << 32 | (y << 4 & 0xF0F0F0F0u));
 #pragma unroll
             for (int nt = 0; nt < NT; nt++)
-              r[nt] = __builtin_amdgcn_mfma_i32_16x16x32_i8(kb, qb[nt][s], r[nt], 0, 0, 0);
+              r[nt] = __builtin_amdgcn_mfma_i32_16x16x32_i8(kb, qb[nt][s], s ? r[nt] : c0, 0, 0, 0);
           }
 #pragma unroll
           for (int nt = 0; nt < NT; nt++) {
@@ -632,16 +648,15 @@ __global__ __launch_bounds__(AT, (NB * NT > 8 ? 2 : NT > 1 || NB > 4 ? 3 : 4)) v
               h8 c[2];                               // elements l % 16 and + 16
 #pragma unroll
               for (int i = 0; i < 2; i++) {
+                // a nibble n in an fp16 number's low bits: 1024 + n or 1024 + 16 n
                 const uint32_t y = buf[pc][2 * hh + i], z = y >> 8;
                 const h2 off = {(_Float16)-1032.0f, (_Float16)-1032.0f};
                 const h2 six = {(_Float16)0.0625f, (_Float16)0.0625f};
                 const h2 off2 = {(_Float16)-72.0f, (_Float16)-72.0f};
-                const h2 a0 = __builtin_bit_cast(h2, (y & 0x000F000Fu) | 0x64006400u) + off;
-                const h2 a1 = __builtin_bit_cast(h2, (z & 0x000F000Fu) | 0x64006400u) + off;
-                const h2 b0 = __builtin_elementwise_fma(
-                    __builtin_bit_cast(h2, (y & 0x00F000F0u) | 0x64006400u), six, off2);
-                const h2 b1 = __builtin_elementwise_fma(
-                    __builtin_bit_cast(h2, (z & 0x00F000F0u) | 0x64006400u), six, off2);
+                const h2 a0 = __builtin_bit_cast(h2, (y & low4) | bias) + off;
+                const h2 a1 = __builtin_bit_cast(h2, (z & low4) | bias) + off;
+                const h2 b0 = __builtin_elementwise_fma(__builtin_bit_cast(h2, (y & high4) | bias), six, off2);
+                const h2 b1 = __builtin_elementwise_fma(__builtin_bit_cast(h2, (z & high4) | bias), six, off2);
                 c[0][4 * i] = a0[0]; c[0][4 * i + 1] = a0[1]; c[0][4 * i + 2] = a1[0]; c[0][4 * i + 3] = a1[1];
                 c[1][4 * i] = b0[0]; c[1][4 * i + 1] = b0[1]; c[1][4 * i + 2] = b1[0]; c[1][4 * i + 3] = b1[1];
               }
@@ -659,9 +674,9 @@ __global__ __launch_bounds__(AT, (NB * NT > 8 ? 2 : NT > 1 || NB > 4 ? 3 : 4)) v
                 } else {
 #pragma unroll
                   for (int i = 0; i < 2; i++) {        // key group 2 hh + i
-                    const int ch = (2 * hh + i) / PK, mine = (2 * hh + i) % PK;
-                    put(hi, i, only(whi[0][ch], grp == mine));
-                    put(lo, i, only(wlo[0][ch], grp == mine));
+                    const int ch = (2 * hh + i) / PK, z = (2 * hh + i) % PK;
+                    put(hi, i, from_col<PK>(whi[0][ch], z));
+                    put(lo, i, from_col<PK>(wlo[0][ch], z));
                   }
                 }
 #pragma unroll
@@ -694,7 +709,7 @@ __global__ __launch_bounds__(AT, (NB * NT > 8 ? 2 : NT > 1 || NB > 4 ? 3 : 4)) v
         for (int s = 0; s < 2; s++)
 #pragma unroll
           for (int y = 0; y < 4; y++)
-            acc[nt][b][s][y] = ldexpf(sum_cols<PK>(acc[nt][b][s][y]), vexp - 15);
+            acc[nt][b][s][y] = ldexpf(acc[nt][b][s][y], vexp - 15);
     }
     if constexpr (PS > 1) {
       __syncthreads();                 // the last step's probabilities have been read
