@@ -386,9 +386,11 @@ int kv_q4_read(const w4a8_kv *kv, float *k_out, float *v_out, int64_t T, void *s
  * Keys that a row does not see cannot change its result, whatever their
  * codes and scales hold.
  *   q [T][NH][D] fp32 with row stride q_stride, out [T][NH][D], lse [T][NH]
- *   (NULL: not written).  workspace >= attn_q4_workspace_size bytes, no
- *   initialisation; one or two launches.  The result does not depend on
- *   timing, and a sequence's does not on the values of the others'.
+ *   (NULL: not written).  One launch.  workspace >= attn_q4_workspace_size
+ *   bytes, zero-filled before its first use (moe_w4a8_workspace_init does
+ *   that); each call leaves it ready for later ones of any sizes it suffices
+ *   for.  The result does not depend on timing, and a sequence's does not on
+ *   the values of the others'.
  * Errors beside the plan's: NH < 1, NH % NKV != 0, T < 0, window < 0,
  * q_stride < NH * D or not a multiple of 4, scale not finite -> W4A8_ESHAPE;
  * T * NH >= 2^31 or q_stride >= 2^31 -> W4A8_ERANGE; q, out or workspace NULL

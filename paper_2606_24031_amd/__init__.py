@@ -667,12 +667,13 @@ def kv_read(kv, T, k_out=None, v_out=None, stream=None):
 
 
 def attn_workspace(kv, T, NH):
-    """A workspace for attn_forward with T rows of NH heads on kv's plan."""
+    """A workspace for attn_forward with T rows of NH heads on kv's plan
+    (zero-filled; each call leaves it ready for the next)."""
     import torch
     n = int(lib().attn_q4_workspace_size(ctypes.byref(kv.args), T, NH))
     if n == 0:
         raise W4A8Error(ESHAPE, "attn_q4_workspace_size")
-    return torch.empty(n, dtype=torch.uint8, device=kv.device)
+    return torch.zeros(n, dtype=torch.uint8, device=kv.device)
 
 
 def attn_forward(kv, q, scale, window=0, out=None, lse=None, want_lse=True, workspace=None,

@@ -4,8 +4,8 @@
 //
 // A work item is a tile of 16 NT query rows of one KV head of a sequence (row
 // f of a sequence: token f / G, head f % G of the group), times a run of pages
-// when the rows alone would leave compute units idle; a second launch then
-// joins the runs' partial results in a fixed order.  A workgroup of AW waves
+// when the rows alone would leave compute units idle; the last workgroup to
+// finish then joins the runs' partial results, in their order whoever is last.  A workgroup of AW waves
 // takes AW pages of 64 keys a step:
 //   scores   each wave its own page.  S^T = K Q^T: one
 //            v_mfma_i32_16x16x32_i8 per 16 keys, 16 rows and block of 32, K
@@ -51,7 +51,11 @@ namespace {
 
 constexpr int TARGET = 768;           // runs wanted: three workgroups a compute unit
 constexpr int AW = 4, AT = 64 * AW;   // waves of a workgroup; pages of a step
-constexpr int JOIN_MAX = 2 * TARGET;  // most runs of an item
+constexpr int GROUP = 16;             // runs joined at a time
+constexpr int JT = 1024;              // threads of the joining kernel
+constexpr int SLOTS_MAX = 2 * TARGET; // most runs of split items
+constexpr int64_t COUNTERS = (2 * SLOTS_MAX * 4 + 255) / 256 * 256;   // bytes before the partial results
+static_assert(SLOTS_MAX / GROUP / GROUP <= GROUP, "two levels of joins");
 
 typedef int v4i __attribute__((ext_vector_type(4)));
 typedef float v4f __attribute__((ext_vector_type(4)));
@@ -73,8 +77,10 @@ struct AttnArgs {
   float k;          // |scale| * log2(e) / 16, 1 for 0
   float sign;       // of scale: -1, 0 or 1
   int64_t window;
+  int *count;       // arrivals: [SLOTS_MAX] of a group of runs, [SLOTS_MAX] of an item's groups
   float *part;      // partial results, `slots` of them
   int slots;
+  int fused;        // the last workgroups join, not a second launch
   float inv_G;      // 1 / G
 };
 
@@ -118,17 +124,17 @@ template <typename T_> __device__ __forceinline__ T_ wave_scan(T_ x) {
   return x;
 }
 
-// Item or run `id` of the call, found by every wave on its own, 64 sequences
-// a round.  A sequence's items fall into runs of at most C pages, C such that
-// the call has about TARGET runs (of several tiles, whose first see half the
-// pages of the last on average, only from 2 C on).  Runs (split = false): the sequence, the
-// number within it and the first partial slot of its runs; joins (split =
-// true): counted over items with several runs only.  False past the end.
+// Run `id` of the call, found by every wave on its own, 64 sequences a round:
+// its sequence, its number within it, the runs of an item and the first
+// partial slot of the sequence's runs.  A sequence's items fall into runs of
+// at most C pages, C such that the call has about TARGET runs (of several
+// tiles, whose first see half the pages of the last on average, only from 2 C
+// on).  SPLIT: item `id` of those with several runs.  False past the end.
 struct Found {
   int s, local, runs, slot0;
 };
-template <int RT_>
-__device__ __forceinline__ bool plan_find(const AttnArgs &a, int id, bool split, Found &f) {
+template <int RT_, bool SPLIT = false>
+__device__ __forceinline__ bool plan_find(const AttnArgs &a, int id, Found &f) {
   const int lane = threadIdx.x & 63, B = a.p.B;
   int tiles = 0, items = 0, pages = 0;          // of sequence lane
   const auto look = [&](int s) {
@@ -155,7 +161,7 @@ __device__ __forceinline__ bool plan_find(const AttnArgs &a, int id, bool split,
     if (s0) look(s0 + lane);
     const int runs = pages > (tiles > 1 ? 2 * C : C) ? (pages + C - 1) / C : 1;
     const int ns = runs > 1 ? items * runs : 0;
-    const int n = split ? (runs > 1 ? items : 0) : items * runs;
+    const int n = !SPLIT ? items * runs : runs > 1 ? items : 0;
     const int in = wave_scan(n), is = wave_scan(ns);
     const uint64_t hit = __ballot(id >= base + in - n && id < base + in);
     if (hit) {
@@ -293,6 +299,8 @@ template <int NB, bool SYM, int NT, int PK> struct __align__(16) Lds {
   float qd[NT * NB * 16];
   float mx[16 * NT][AW];                       // the waves' maxima
   float l[AW][16 * NT];
+  float2 rl[Sh::ROWS];                         // joins: references and sums
+  int flag;
 };
 
 // N scales of raw words.
@@ -335,6 +343,100 @@ template <int PK> __device__ __forceinline__ constexpr int key_off(int i) {
   return (i >> 2) * 16 * PK + (i & 3);
 }
 
+// Partial results pass between workgroups that may run on different XCDs,
+// whose L2 caches do not see each other's ordinary stores.  They are written
+// and read with the agent-scope bit, past those caches; fences that write back
+// and drop whole caches cost 2 to 4 times the attention itself (48 rows over
+// 6000 keys: 260 us a call against 59).
+constexpr int AGENT = 1 << 4;                    // sc1
+typedef __amdgpu_buffer_rsrc_t Rsrc;
+__device__ __forceinline__ Rsrc shared_at(float *p) {
+  return __builtin_amdgcn_make_buffer_rsrc(p, 0, 0x7FFFFFFF, 0x00027000);
+}
+__device__ __forceinline__ void share(Rsrc r, int at, v4f x) {
+  __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(v4u, x), r, at * 4, 0, AGENT);
+}
+__device__ __forceinline__ void share(Rsrc r, int at, v2f x) {
+  __builtin_amdgcn_raw_buffer_store_b64(__builtin_bit_cast(v2u, x), r, at * 4, 0, AGENT);
+}
+__device__ __forceinline__ v4f shared4(Rsrc r, int at) {
+  return __builtin_bit_cast(v4f, __builtin_amdgcn_raw_buffer_load_b128(r, at * 4, 0, AGENT));
+}
+__device__ __forceinline__ v2f shared2(Rsrc r, int at) {
+  return __builtin_bit_cast(v2f, __builtin_amdgcn_raw_buffer_load_b64(r, at * 4, 0, AGENT));
+}
+
+// Joins n partial results, `step` slots apart, of the slots at `part`: a row's
+// weights by 16 lanes (w: LDS, n x ROWS), then every thread its columns of all
+// of them, in order; the first JB of those are on their way meanwhile.
+// fin(row, column, sum, R, l) takes 4 columns at a time; w is free afterwards.
+template <int D, int ROWS, typename F>
+__device__ __forceinline__ void join(int tid, float *part, int step, int n, float *w, float2 *rl,
+                                     F &&fin) {
+  constexpr int PB = ROWS * (D + 2), PER = D / 4, IT = (ROWS * PER + AT - 1) / AT;
+  constexpr int JB = IT >= 8 ? 1 : 8 / IT;
+  const Rsrc rs = shared_at(part);
+  const int last = n - 1;
+  v4f x[IT][JB];
+#pragma unroll
+  for (int it = 0; it < IT; it++) {
+    const int i = tid + it * AT, row = min(i / PER, ROWS - 1), c = i % PER * 4;
+#pragma unroll
+    for (int k = 0; k < JB; k++) x[it][k] = shared4(rs, min(k, last) * step * PB + row * D + c);
+  }
+  for (int r = tid / 16; r < ROWS; r += AT / 16) {
+    const int k0 = tid % 16;
+    const v2f q0 = shared2(rs, min(k0, last) * step * PB + ROWS * D + 2 * r);
+    float R = k0 < n && q0[1] != 0.0f ? q0[0] : -FLT_MAX, l = 0.0f;
+    for (int k = k0 + 16; k < n; k += 16) {
+      const v2f q = shared2(rs, k * step * PB + ROWS * D + 2 * r);
+      if (q[1] != 0.0f) R = fmaxf(R, q[0]);
+    }
+    R = fmaxf(R, ror_f<DPP_ROR8>(R));
+    R = fmaxf(R, ror_f<DPP_ROR4>(R));
+    R = fmaxf(R, ror_f<0x122>(R));
+    R = fmaxf(R, ror_f<0x121>(R));
+    for (int k = k0; k < n; k += 16) {
+      const v2f q = k < 16 ? q0 : shared2(rs, k * step * PB + ROWS * D + 2 * r);
+      const float f = q[1] != 0.0f ? exp2_f(q[0] - R) : 0.0f;
+      w[k * ROWS + r] = f;
+      l = fmaf(q[1], f, l);
+    }
+    l += ror_f<DPP_ROR8>(l);
+    l += ror_f<DPP_ROR4>(l);
+    l += ror_f<0x122>(l);
+    l += ror_f<0x121>(l);
+    if (k0 == 0) rl[r] = make_float2(R, l);
+  }
+  __syncthreads();
+#pragma unroll
+  for (int it = 0; it < IT; it++) {
+    const int i = tid + it * AT, row = min(i / PER, ROWS - 1), c = i % PER * 4;
+    v4f s = v4f{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int k = 0; k < JB; k++)
+      if (k < n) s += x[it][k] * w[k * ROWS + row];
+#pragma unroll 8
+    for (int k = JB; k < n; k++) s += shared4(rs, k * step * PB + row * D + c) * w[k * ROWS + row];
+    if (i < ROWS * PER) fin(row, c, s, rl[row].x, rl[row].y);
+  }
+}
+
+// Counts an arrival at *c; true in the last of n, which sets it back to 0.
+// Every wave first waits for its stores, so whoever finds the count complete
+// loads after all of them.
+__device__ __forceinline__ bool last_of(int *c, int n, int *flag) {
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    const int old = __hip_atomic_fetch_add(c, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    *flag = old == n - 1;
+    if (old == n - 1) __hip_atomic_store(c, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  }
+  __syncthreads();
+  return *flag;
+}
+
 // Packed rows (PK = 2 or 4): a tile of 8 or 4 rows would leave half or three
 // quarters of a product's columns, and of every lane's work on scores, empty.
 // Instead PK products of 16 keys each accumulate into one result, with Q's
@@ -350,13 +452,16 @@ __global__ __launch_bounds__(AT, (NB * NT > 8 ? 2 : NT > 1 || NB > 4 ? 3 : 4)) v
   constexpr int64_t TILE = kv_tile_bytes(D, SYM);
   constexpr int SB = kv_scale_bytes(SYM), SW = NB * SB / 4;   // words of scales a lane stages
   __shared__ Lds<NB, SYM, NT, PK> lds;
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
-  const int g = lane >> 4, col = lane & 15, grp = PK > 1 ? col / ROWS : 0;
-  const int blk = NB < AW ? wave % NB : wave * BW, sub = NB < AW ? wave / NB : 0;
-
   for (int id = blockIdx.x;; id += gridDim.x) {
+    // (taken anew each time round: what depends on it alone would otherwise
+    // move out of this loop, that few go round twice, and hold registers)
+    int tid = threadIdx.x;
+    asm volatile("" : "+v"(tid));
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
+    const int g = lane >> 4, col = lane & 15, grp = PK > 1 ? col / ROWS : 0;
+    const int blk = NB < AW ? wave % NB : wave * BW, sub = NB < AW ? wave / NB : 0;
     Found f;
-    if (!plan_find<ROWS>(a, id, false, f)) return;
+    if (!plan_find<ROWS>(a, id, f)) return;
     const Seq sq = seq_of<ROWS>(a, f.s);
     const int it = f.runs == 1 ? f.local : f.local / f.runs, run = f.local - it * f.runs;
     const int tl = it / a.p.NKV, h = it - tl * a.p.NKV, tile = sq.tiles - 1 - tl;  // longest first
@@ -383,7 +488,7 @@ __global__ __launch_bounds__(AT, (NB * NT > 8 ? 2 : NT > 1 || NB > 4 ? 3 : 4)) v
     v4f x[QI];
 #pragma unroll
     for (int k = 0; k < QI; k++) {
-      const int i = threadIdx.x + k * AT, row = min((i >> 3) / NB, fn - 1), b = (i >> 3) % NB;
+      const int i = tid + k * AT, row = min((i >> 3) / NB, fn - 1), b = (i >> 3) % NB;
       const int t = rm.token(row);
       x[k] = *reinterpret_cast<const v4f *>(a.q + (sq.r0 + t) * a.qs +
                                             (int64_t)(h * a.G + rm.head(row, t)) * D + b * 32 + 4 * (i & 7));
@@ -425,7 +530,7 @@ __global__ __launch_bounds__(AT, (NB * NT > 8 ? 2 : NT > 1 || NB > 4 ? 3 : 4)) v
     load_vs(ids);
 #pragma unroll
     for (int k = 0; k < QI; k++) {
-      const int i = threadIdx.x + k * AT, j = i & 7, row = (i >> 3) / NB, b = (i >> 3) % NB;
+      const int i = tid + k * AT, j = i & 7, row = (i >> 3) / NB, b = (i >> 3) % NB;
       const float v[4] = {x[k][0], x[k][1], x[k][2], x[k][3]};
       float d;
       const uint32_t codes = kv_q8_block8<SYM>(v, d);
@@ -722,9 +827,11 @@ __global__ __launch_bounds__(AT, (NB * NT > 8 ? 2 : NT > 1 || NB > 4 ? 3 : 4)) v
     }
     __syncthreads();
     const bool whole = f.runs == 1;
-    const int slot = whole ? 0 : f.slot0 + f.local;
-    float *part = a.part + (int64_t)slot * (ROWS * (D + 2));
-    if (sub == 0 && col < ROWS && (whole || slot < a.slots)) {
+    const int first = f.slot0 + it * f.runs;              // slot of the item's run 0
+    const Rsrc pr = shared_at(a.part + (int64_t)(whole ? 0 : first + run) * (ROWS * (D + 2)));
+    // (an item whose slots do not fit, as rows that overlap could make one, is left out)
+    const bool fits = whole || first + f.runs <= a.slots;
+    if (sub == 0 && col < ROWS && fits) {
 #pragma unroll
       for (int nt = 0; nt < NT; nt++) {
         const int row = 16 * nt + col;
@@ -742,8 +849,8 @@ __global__ __launch_bounds__(AT, (NB * NT > 8 ? 2 : NT > 1 || NB > 4 ? 3 : 4)) v
         for (int b = 0; b < BW; b++) {
           const int at = (blk + b) * 32 + 4 * g;
           if (!whole) {
-            *reinterpret_cast<v4f *>(part + row * D + at) = acc[nt][b][0];
-            *reinterpret_cast<v4f *>(part + row * D + at + 16) = acc[nt][b][1];
+            share(pr, row * D + at, acc[nt][b][0]);
+            share(pr, row * D + at + 16, acc[nt][b][1]);
           } else if (row < fn) {
             *reinterpret_cast<v4f *>(a.out + o * D + at) = acc[nt][b][0] * inv;
             *reinterpret_cast<v4f *>(a.out + o * D + at + 16) = acc[nt][b][1] * inv;
@@ -751,10 +858,39 @@ __global__ __launch_bounds__(AT, (NB * NT > 8 ? 2 : NT > 1 || NB > 4 ? 3 : 4)) v
         }
         if (wave == 0 && g == 0) {
           if (!whole) {
-            part[ROWS * D + 2 * row] = mk[nt];
-            part[ROWS * D + 2 * row + 1] = lt;
+            share(pr, ROWS * D + 2 * row, v2f{mk[nt], lt});
           } else if (a.lse && row < fn) {
             a.lse[o] = lt != 0.0f ? (mk[nt] + log2f(lt)) * 0.693147180559945f : -INFINITY;
+          }
+        }
+      }
+    }
+    // The last of a group of runs to get here joins the group, the last group
+    // the item: in the order of the runs, whoever was last.
+    if (!whole && fits && a.fused) {
+      const auto store = [&](int row, int c, v4f s, float R, float l) {
+        if (row >= fn) return;
+        const int t = rm.token(row);
+        const int64_t o = (sq.r0 + t) * a.NH + h * a.G + rm.head(row, t);
+        *reinterpret_cast<v4f *>(a.out + o * D + c) = l != 0.0f ? s * (1.0f / l) : s * 0.0f;
+        if (c == 0 && a.lse) a.lse[o] = l != 0.0f ? (R + log2f(l)) * 0.693147180559945f : -INFINITY;
+      };
+      constexpr int64_t PB = ROWS * (D + 2);
+      float *const w = reinterpret_cast<float *>(lds.p);
+      const int groups = (f.runs + GROUP - 1) / GROUP, gr = run / GROUP;
+      const int n = min(GROUP, f.runs - gr * GROUP);
+      float *const gp = a.part + (first + gr * GROUP) * PB;
+      if (last_of(a.count + first + gr * GROUP, n, &lds.flag)) {
+        if (groups == 1) {
+          join<D, ROWS>(tid, gp, 1, n, w, lds.rl, store);
+        } else {
+          // a thread writes only the columns that it alone has read
+          join<D, ROWS>(tid, gp, 1, n, w, lds.rl, [&](int row, int c, v4f s, float R, float l) {
+            share(shared_at(gp), row * D + c, s);
+            if (c == 0) share(shared_at(gp), ROWS * D + 2 * row, v2f{R, l});
+          });
+          if (last_of(a.count + SLOTS_MAX + first, groups, &lds.flag)) {
+            join<D, ROWS>(tid, a.part + first * PB, GROUP, groups, w, lds.rl, store);
           }
         }
       }
@@ -763,65 +899,58 @@ __global__ __launch_bounds__(AT, (NB * NT > 8 ? 2 : NT > 1 || NB > 4 ? 3 : 4)) v
   }
 }
 
-// Joins the runs of item blockIdx.x (counted over the items with several
-// runs), rows blockIdx.y * JR .. of its tile: a row by JT / JR threads, D / 4
-// lanes by groups that take the runs in turn, summed in a fixed order.
-template <int NB, int ROWS, int JT, int JR>
-__global__ __launch_bounds__(JT) void join_kernel(AttnArgs a) {
-  constexpr int D = 32 * NB, L = D / 4, TR = JT / JR, NG = TR / L;
-  __shared__ v4f so[JR][NG][L];
-  __shared__ float sw[JR][JOIN_MAX], sl[JR];
+// The same as a launch of its own, for few items of many runs: a workgroup a
+// row of item blockIdx.x (counted over the items with several runs), D / 4
+// lanes by groups that take the runs in turn.
+template <int NB, int ROWS> __global__ __launch_bounds__(JT) void join_kernel(AttnArgs a) {
+  constexpr int D = 32 * NB, L = D / 4, NG = JT / L;
+  constexpr int64_t PB = ROWS * (D + 2);
+  __shared__ v4f so[NG][L];
+  __shared__ float sw[SLOTS_MAX], sl;
   Found f;
-  if (!plan_find<ROWS>(a, blockIdx.x, true, f)) return;
+  if (!plan_find<ROWS, true>(a, blockIdx.x, f)) return;
   const Seq sq = seq_of<ROWS>(a, f.s);
   const int tl = f.local / a.p.NKV, h = f.local - tl * a.p.NKV, f0 = (sq.tiles - 1 - tl) * ROWS;
-  const int fn = min(ROWS, sq.qlen * a.G - f0);
-  if ((int)blockIdx.y * JR >= fn) return;
-  const int jr = threadIdx.x / TR, th = threadIdx.x % TR;
-  const int row = min((int)blockIdx.y * JR + jr, fn - 1);
-  const int slot = f.slot0 + f.local * f.runs;
-  const int n = min(f.runs, a.slots - slot);     // at most JOIN_MAX
-  constexpr int64_t PB = ROWS * (D + 2);
+  const int row = blockIdx.y;
+  if (row >= min(ROWS, sq.qlen * a.G - f0)) return;
+  const int slot = f.slot0 + f.local * f.runs, n = f.runs;
+  if (slot + n > a.slots) return;
   const float *part = a.part + slot * PB;
-  // the runs' weights: one wave a row
   float R = -FLT_MAX;
-  if (th < 64) {
-    for (int i = th; i < n; i += 64) {
+  if (threadIdx.x < 64) {
+    for (int i = threadIdx.x; i < n; i += 64) {
       const v2f q = *reinterpret_cast<const v2f *>(part + i * PB + ROWS * D + 2 * row);
       if (q[1] != 0.0f) R = fmaxf(R, q[0]);
     }
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) R = fmaxf(R, __shfl_xor(R, o));
     float l = 0.0f;
-    for (int i = th; i < n; i += 64) {
+    for (int i = threadIdx.x; i < n; i += 64) {
       const v2f q = *reinterpret_cast<const v2f *>(part + i * PB + ROWS * D + 2 * row);
       const float w = q[1] != 0.0f ? exp2_f(q[0] - R) : 0.0f;
-      sw[jr][i] = w;
+      sw[i] = w;
       l = fmaf(q[1], w, l);
     }
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) l += __shfl_xor(l, o);
-    if (th == 0) sl[jr] = l;
+    if (threadIdx.x == 0) sl = l;
   }
   __syncthreads();
-  const int grp = th / L, c4 = th % L;
+  const int grp = threadIdx.x / L, c4 = threadIdx.x % L;
   v4f s = v4f{0.f, 0.f, 0.f, 0.f};
   const float *src = part + row * D + 4 * c4;
 #pragma unroll 8
-  for (int i = grp; i < n; i += NG) s += *reinterpret_cast<const v4f *>(src + i * PB) * sw[jr][i];
-  if (NG > 1) {
-    so[jr][grp][c4] = s;
-    __syncthreads();
-    if (grp != 0) return;
-    s = v4f{0.f, 0.f, 0.f, 0.f};
+  for (int i = grp; i < n; i += NG) s += *reinterpret_cast<const v4f *>(src + i * PB) * sw[i];
+  so[grp][c4] = s;
+  __syncthreads();
+  if (grp != 0) return;
+  s = v4f{0.f, 0.f, 0.f, 0.f};
 #pragma unroll 4
-    for (int i = 0; i < NG; i++) s += so[jr][i][c4];
-  }
-  if ((int)blockIdx.y * JR + jr >= fn) return;
+  for (int i = 0; i < NG; i++) s += so[i][c4];
   const RowMap rm(a, f0);
   const int t = rm.token(row);
   const int64_t o = (sq.r0 + t) * a.NH + h * a.G + rm.head(row, t);
-  const float l = sl[jr];
+  const float l = sl;
   *reinterpret_cast<v4f *>(a.out + o * D + 4 * c4) = l != 0.0f ? s * (1.0f / l) : s * 0.0f;
   if (c4 == 0 && a.lse) a.lse[o] = l != 0.0f ? (R + log2f(l)) * 0.693147180559945f : -INFINITY;
 }
@@ -843,9 +972,20 @@ int64_t items_bound(const w4a8_kv *kv, int64_t T, int64_t NH) {
   return ((T * G) / rt + std::min(kv->B, T)) * kv->NKV;
 }
 int64_t slots_bound(const w4a8_kv *kv, int64_t T, int64_t NH) {
-  if (kv->max_pages <= AW) return 0;
+  if (kv->max_pages <= AW || kv->B == 0) return 0;
   const int64_t runs = (kv->max_pages + AW - 1) / AW;
-  return std::min<int64_t>(2 * TARGET, items_bound(kv, T, NH) * runs);
+  return std::min<int64_t>(SLOTS_MAX, items_bound(kv, T, NH) * runs);
+}
+
+// Whether the last workgroups join the runs.  They read past the L2 caches,
+// some 30 KB a round trip: right for a few runs an item, which they join while
+// others still work, in place of a launch (4 sequences' 4 .. 5 runs an item:
+// 12.5 us a call against 15.0), but one row over 131072 keys, 256 runs an
+// item, takes 37 us so and 30 with a launch that puts 1024 threads on a row.
+bool joins_fused(const w4a8_kv *kv, int64_t T, int64_t NH) {
+  const int64_t runs = std::min<int64_t>((kv->max_pages + AW - 1) / AW,
+                                         TARGET / std::max<int64_t>(1, items_bound(kv, T, NH)));
+  return runs <= 2 * GROUP;
 }
 
 int attn_sizes(const w4a8_kv *kv, int64_t T, int64_t NH) {
@@ -858,18 +998,13 @@ int attn_sizes(const w4a8_kv *kv, int64_t T, int64_t NH) {
 
 template <int NB, bool SYM, int NT, int PK>
 int launch(const AttnArgs &a, int64_t items, hipStream_t s) {
-  constexpr int ROWS = 16 * NT / PK;
   const int64_t grid = std::min<int64_t>(items + a.slots, 1 << 20);
   attn_kernel<NB, SYM, NT, PK><<<dim3((unsigned)grid), dim3(AT), 0, s>>>(a);
-  if (int rc = check_launch(); rc != W4A8_OK || a.slots == 0) return rc;
-  // Joins: with few items, which then have many runs, 1024 threads a row;
-  // else a wave a row.
+  if (int rc = check_launch(); rc != W4A8_OK || a.slots == 0 || a.fused) return rc;
+  constexpr int ROWS = 16 * NT / PK;
   const int64_t joins = std::min<int64_t>(items, TARGET);
-  const int rows = (int)std::min<int64_t>(ROWS, a.T * a.G);
-  if (items <= 16)
-    join_kernel<NB, ROWS, 1024, 1><<<dim3((unsigned)joins, rows), dim3(1024), 0, s>>>(a);
-  else
-    join_kernel<NB, ROWS, 256, 4><<<dim3((unsigned)joins, (rows + 3) / 4), dim3(256), 0, s>>>(a);
+  join_kernel<NB, ROWS><<<dim3((unsigned)joins, (unsigned)std::min<int64_t>(ROWS, a.T * a.G)),
+                          dim3(JT), 0, s>>>(a);
   return check_launch();
 }
 
@@ -890,8 +1025,8 @@ using namespace w4a8;
 
 extern "C" size_t attn_q4_workspace_size(const w4a8_kv *kv, int64_t T, int64_t NH) {
   if (attn_sizes(kv, T, NH) != W4A8_OK) return 0;
-  const int64_t n = slots_bound(kv, T, NH) * tile_rows(kv, T, NH) * (kv->D + 2) * 4;
-  return (size_t)std::max<int64_t>(16, n);
+  const int64_t n = slots_bound(kv, T, NH);
+  return n == 0 ? 16 : (size_t)(COUNTERS + n * tile_rows(kv, T, NH) * (kv->D + 2) * 4);
 }
 
 extern "C" int attn_q4_forward(const w4a8_kv *kv, const float *q, int64_t q_stride, float *out,
@@ -914,7 +1049,9 @@ extern "C" int attn_q4_forward(const w4a8_kv *kv, const float *q, int64_t q_stri
                 // a factor of 0 goes to Q, so that a masked score's -infinity stays one
                 scale != 0.0f ? std::fabs(scale) * 1.44269504f / 16.0f : 1.0f,
                 scale < 0.0f ? -1.0f : scale == 0.0f ? 0.0f : 1.0f, window,
-                reinterpret_cast<float *>(workspace), (int)slots_bound(kv, T, NH),
+                reinterpret_cast<int *>(workspace),
+                reinterpret_cast<float *>(reinterpret_cast<uint8_t *>(workspace) + COUNTERS), (int)slots_bound(kv, T, NH),
+                joins_fused(kv, T, NH),
                 1.0f / (float)(NH / kv->NKV)};
   const int64_t items = items_bound(kv, T, NH);
   const bool sym = kv->format == W4A8_KV_Q4_SYM;

@@ -192,6 +192,20 @@ def test_equal_bits_each_time_and_whatever_the_others_hold():
     assert not torch.equal(a[0][1:10], b[0][1:10])
 
 
+def test_one_workspace_for_calls_of_several_shapes():
+    """A workspace large enough for all serves calls of any shape in turn, on
+    either way of joining runs; its arrival counters are zero after each."""
+    calls = [case(50, [9000], [1], 8, 1, 256, "q4_0"), case(51, [5000] + [100] * 39, [1] * 40, 4, 1, 64, "q4_0"),
+             case(52, [900, 3000], [4, 2], 8, 2, 128, "q4_sym"), case(53, [70], [70], 2, 1, 64, "q4_0")]
+    kvs = [attn_cases.on_gpu(c) for c, _ in calls]
+    size = max(w4.attn_workspace(kv, c.T, q.shape[1]).numel() for kv, (c, q) in zip(kvs, calls))
+    ws = torch.zeros(size, dtype=torch.uint8, device="cuda")
+    for i in (0, 1, 2, 3, 1, 0, 2):
+        c, q = calls[i]
+        check(c, q, 0.1, got=w4.attn_forward(kvs[i], dev(q), 0.1, workspace=ws), what=f"shared workspace, call {i}")
+        assert not bool(ws[:12288].any())
+
+
 def test_empty_calls():
     c, q = case(18, [10], [1], 2, 1, 64, "q4_0")
     kv = attn_cases.on_gpu(c)
