@@ -420,8 +420,10 @@ int attn_q4_forward(const w4a8_kv *kv, const float *q, int64_t q_stride, float *
  * -0 and 0 are equal.
  *   targets [T] int32 and logprob [T] (both NULL: skipped), entropy [T] (NULL:
  *   skipped), top_ids [T][n_top] int32 and top_logprobs [T][n_top] fp32 (both
- *   NULL when n_top is 0).  workspace >= token_logprobs_workspace_size bytes,
- *   no initialisation; one or two launches.
+ *   NULL when n_top is 0).  One launch.  workspace >=
+ *   token_logprobs_workspace_size bytes, zero-filled before its first use
+ *   (moe_w4a8_workspace_init does that); each call leaves it ready for later
+ *   ones of any sizes it suffices for.
  * Errors: T < 0, V < 1, stride < V -> W4A8_ESHAPE; V >= 2^24, T >= 2^31,
  * n_top < 0, n_top > 32, n_top > V, T * stride >= 2^40 -> W4A8_ERANGE; logits,
  * only one of a pair, or the workspace NULL -> W4A8_ENULL; logits or the

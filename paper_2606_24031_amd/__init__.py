@@ -705,12 +705,13 @@ def attn_forward(kv, q, scale, window=0, out=None, lse=None, want_lse=True, work
 
 
 def logprobs_workspace(T, V, n_top=0, device="cuda"):
-    """A workspace for token_logprobs."""
+    """A workspace for token_logprobs (zero-filled; each call leaves it ready
+    for the next)."""
     import torch
     n = int(lib().token_logprobs_workspace_size(T, V, n_top))
     if n == 0:
         raise W4A8Error(ERANGE, "token_logprobs_workspace_size")
-    return torch.empty(n, dtype=torch.uint8, device=device)
+    return torch.zeros(n, dtype=torch.uint8, device=device)
 
 
 def token_logprobs(logits, targets=None, n_top=0, want_entropy=True, logprob=None, entropy=None,

@@ -42,6 +42,7 @@
 #include <cmath>
 
 #include "kv_dev.h"
+#include "share_dev.h"
 #include "w4a8_dev.h"
 #include "w4a8_host.h"
 
@@ -58,10 +59,6 @@ constexpr int64_t COUNTERS = (2 * SLOTS_MAX * 4 + 255) / 256 * 256;   // bytes b
 static_assert(SLOTS_MAX / GROUP / GROUP <= GROUP, "two levels of joins");
 
 typedef int v4i __attribute__((ext_vector_type(4)));
-typedef float v4f __attribute__((ext_vector_type(4)));
-typedef float v2f __attribute__((ext_vector_type(2)));
-typedef uint32_t v4u __attribute__((ext_vector_type(4)));
-typedef uint32_t v2u __attribute__((ext_vector_type(2)));
 typedef uint32_t __attribute__((may_alias)) word;    // raw access to LDS of other types
 typedef _Float16 h2 __attribute__((ext_vector_type(2)));
 typedef _Float16 h4 __attribute__((ext_vector_type(4)));
@@ -343,29 +340,6 @@ template <int PK> __device__ __forceinline__ constexpr int key_off(int i) {
   return (i >> 2) * 16 * PK + (i & 3);
 }
 
-// Partial results pass between workgroups that may run on different XCDs,
-// whose L2 caches do not see each other's ordinary stores.  They are written
-// and read with the agent-scope bit, past those caches; fences that write back
-// and drop whole caches cost 2 to 4 times the attention itself (48 rows over
-// 6000 keys: 260 us a call against 59).
-constexpr int AGENT = 1 << 4;                    // sc1
-typedef __amdgpu_buffer_rsrc_t Rsrc;
-__device__ __forceinline__ Rsrc shared_at(float *p) {
-  return __builtin_amdgcn_make_buffer_rsrc(p, 0, 0x7FFFFFFF, 0x00027000);
-}
-__device__ __forceinline__ void share(Rsrc r, int at, v4f x) {
-  __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(v4u, x), r, at * 4, 0, AGENT);
-}
-__device__ __forceinline__ void share(Rsrc r, int at, v2f x) {
-  __builtin_amdgcn_raw_buffer_store_b64(__builtin_bit_cast(v2u, x), r, at * 4, 0, AGENT);
-}
-__device__ __forceinline__ v4f shared4(Rsrc r, int at) {
-  return __builtin_bit_cast(v4f, __builtin_amdgcn_raw_buffer_load_b128(r, at * 4, 0, AGENT));
-}
-__device__ __forceinline__ v2f shared2(Rsrc r, int at) {
-  return __builtin_bit_cast(v2f, __builtin_amdgcn_raw_buffer_load_b64(r, at * 4, 0, AGENT));
-}
-
 // Joins n partial results, `step` slots apart, of the slots at `part`: a row's
 // weights by 16 lanes (w: LDS, n x ROWS), then every thread its columns of all
 // of them, in order; the first JB of those are on their way meanwhile.
@@ -420,21 +394,6 @@ __device__ __forceinline__ void join(int tid, float *part, int step, int n, floa
     for (int k = JB; k < n; k++) s += shared4(rs, k * step * PB + row * D + c) * w[k * ROWS + row];
     if (i < ROWS * PER) fin(row, c, s, rl[row].x, rl[row].y);
   }
-}
-
-// Counts an arrival at *c; true in the last of n, which sets it back to 0.
-// Every wave first waits for its stores, so whoever finds the count complete
-// loads after all of them.
-__device__ __forceinline__ bool last_of(int *c, int n, int *flag) {
-  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-  __syncthreads();
-  if (threadIdx.x == 0) {
-    const int old = __hip_atomic_fetch_add(c, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    *flag = old == n - 1;
-    if (old == n - 1) __hip_atomic_store(c, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-  }
-  __syncthreads();
-  return *flag;
 }
 
 // Packed rows (PK = 2 or 4): a tile of 8 or 4 rows would leave half or three

@@ -2,7 +2,8 @@
 // the output head's logits (the decode head of Sec. 5.2) in one pass.
 //
 // A row is cut into S spans, one workgroup each (S = 1 once the rows fill the
-// compute units); every wave streams its share of a span in chunks of 16
+// compute units), and the last of them to finish joins their results, in their
+// order; every wave streams its share of a span in chunks of 16
 // values a lane, the next chunk's loads under way, and keeps
 //   - per lane the softmax statistics (m, z, w): the maximum so far, the sum
 //     of exp(l - m) WITHOUT the maximum's own 1, and sum exp(l - m) (l - m).
@@ -10,14 +11,16 @@
 //     confident row too, whose log Z may be 1e-6;
 //   - per wave the n largest logits: a list in LDS of candidates that beat a
 //     threshold, cut back to the n best (by counting, for each candidate, the
-//     larger ones) when it fills.  The first threshold is the n-th largest of
-//     the 64 lane maxima of the first chunk: n lanes hold a value at least as
-//     large, so it is below nothing that belongs to the n best.  After that a
-//     random row sends a candidate every few hundred values.
+//     larger ones) when it fills.  The first threshold is a value that n of
+//     the 64 lanes reach in the first chunk, so nothing below it belongs to
+//     the n best.  After that a random row sends a candidate every few hundred
+//     values.
 // Bound by HBM: 4 bytes a logit, read once, about 14 VALU ops a value.
 #include <algorithm>
 #include <cfloat>
+#include <type_traits>
 
+#include "share_dev.h"
 #include "w4a8_dev.h"
 #include "w4a8_host.h"
 
@@ -30,6 +33,7 @@ constexpr int LW = LT / 64;
 constexpr int UG = 4;                    // 4-value groups of a lane's chunk
 constexpr int CHUNK = 64 * UG;           // groups of a wave's chunk
 constexpr int CAP = 192;                 // candidates of a wave's list
+constexpr int PAD = 8;
 constexpr int NTOP_MAX = 32;
 constexpr float FAR = -1e30f;            // logits further below the maximum have probability 0
 
@@ -98,31 +102,54 @@ struct Top {
   __device__ __forceinline__ void set(u64 t) {
     if (t > thr) {
       thr = t;
-      thrf = comp_value(t);
+      // (just below -infinity's key lie NaN's bits)
+      thrf = (uint32_t)(t >> 32) < 0x007FFFFFu ? -INFINITY : comp_value(t);
     }
   }
-  // Keeps the n largest, in order.  Entries are distinct, so ranks are too.
-  __device__ void cut() {
+  // Entries of buf larger than each of e (eight at a time: the list is padded
+  // with zeros, which are larger than nothing).
+  template <int N> __device__ __forceinline__ void ranks(const u64 (&e)[N], int (&rank)[N]) {
     const int lane = threadIdx.x & 63;
-    u64 e[CAP / 64];
-    int rank[CAP / 64];
 #pragma unroll
-    for (int k = 0; k < CAP / 64; k++) {
-      e[k] = lane + 64 * k < count ? buf[lane + 64 * k] : 0;
-      rank[k] = 0;
-    }
-    for (int j = 0; j < count; j++) {
-      const u64 x = buf[j];
+    for (int k = 0; k < N; k++) rank[k] = 0;
+    if (lane < 8) buf[count + lane] = 0;
+    __builtin_amdgcn_wave_barrier();
+#pragma unroll 1
+    for (int j = 0; j < count; j += 8) {
+      u64 x[8];
 #pragma unroll
-      for (int k = 0; k < CAP / 64; k++) rank[k] += x > e[k] ? 1 : 0;
+      for (int i = 0; i < 8; i++) x[i] = buf[j + i];
+#pragma unroll
+      for (int i = 0; i < 8; i++)
+#pragma unroll
+        for (int k = 0; k < N; k++) rank[k] += x[i] > e[k] ? 1 : 0;
     }
     __builtin_amdgcn_wave_barrier();
+  }
+  // Keeps the n largest, in order.  Entries are distinct, so ranks are too.
+  template <int N> __device__ __forceinline__ void cut_of() {
+    const int lane = threadIdx.x & 63;
+    u64 e[N];
+    int rank[N];
 #pragma unroll
-    for (int k = 0; k < CAP / 64; k++)
+    for (int k = 0; k < N; k++) e[k] = lane + 64 * k < count ? buf[lane + 64 * k] : 0;
+    ranks<N>(e, rank);
+#pragma unroll
+    for (int k = 0; k < N; k++)
       if (e[k] && rank[k] < n) buf[rank[k]] = e[k];
     __builtin_amdgcn_wave_barrier();
     count = min(count, n);
     if (count == n) set(buf[n - 1]);
+  }
+  __device__ __forceinline__ void cut() {
+    if (count <= 64) cut_of<1>();
+    else cut_of<CAP / 64>();
+  }
+  __device__ __forceinline__ void append(u64 c, bool take, u64 mask) {
+    if (take)
+      buf[count + __builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32),
+                                            __builtin_amdgcn_mbcnt_lo((uint32_t)mask, 0))] = c;
+    count += __popcll(mask);
   }
   // One candidate of each lane with `c` above the threshold (0: none).
   __device__ __forceinline__ void push(u64 c) {
@@ -132,25 +159,36 @@ struct Top {
       cut();
       mask = __ballot(c > thr);
     }
-    if (c > thr)
-      buf[count + __builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32),
-                                            __builtin_amdgcn_mbcnt_lo((uint32_t)mask, 0))] = c;
-    count += __popcll(mask);
+    append(c, c > thr, mask);
   }
-  // A first threshold: just below the n-th largest of the lanes' own maxima.
-  __device__ void seed(u64 own) {
-    const uint32_t lo = (uint32_t)own, hi = (uint32_t)(own >> 32);
-    int rank = 0;
-    for (int j = 0; j < 64; j++) {
-      const u64 o = (u64)(uint32_t)__builtin_amdgcn_readlane((int)hi, j) << 32 |
-                    (uint32_t)__builtin_amdgcn_readlane((int)lo, j);
-      rank += o > own ? 1 : 0;
+  // N of each lane, those that take(i) names with candidates comp(i), where
+  // they fit; else false, and nothing has changed.
+  template <int N, typename F, typename G>
+  __device__ __forceinline__ bool push_all(F &&take, G &&comp) {
+    u64 mask[N];
+    int total = count;
+#pragma unroll
+    for (int i = 0; i < N; i++) {
+      mask[i] = __ballot(take(i));
+      total += __popcll(mask[i]);
     }
-    const u64 at = __ballot(rank == n - 1 && own != 0);
-    if (!at) return;                         // fewer than n lanes hold a value
-    const int l = __ffsll((long long)at) - 1;
-    set(((u64)(uint32_t)__builtin_amdgcn_readlane((int)hi, l) << 32 |
-         (uint32_t)__builtin_amdgcn_readlane((int)lo, l)) - 1);
+    if (total > CAP) return false;
+#pragma unroll
+    for (int i = 0; i < N; i++)
+      if (mask[i]) append(comp(i), mask[i] >> (threadIdx.x & 63) & 1, mask[i]);
+    return true;
+  }
+  // A first threshold from the lanes' own maxima: the largest 16-bit prefix of
+  // a value that n lanes reach, found bit by bit.
+  __device__ __forceinline__ void seed(u64 own) {
+    const uint32_t key = (uint32_t)(own >> 48);
+    uint32_t at = 0;
+#pragma unroll
+    for (int bit = 15; bit >= 0; bit--) {
+      const uint32_t t = at | 1u << bit;
+      if (__popcll(__ballot(key >= t)) >= n) at = t;
+    }
+    if (at) set(((u64)at << 48) - 1);        // (0: fewer than n lanes hold a value)
   }
 };
 
@@ -194,14 +232,14 @@ struct Part {
 
 // Merges the waves' statistics and lists; wave 0 returns the whole.
 template <bool TOP>
-__device__ __forceinline__ void block_merge(Stat &s, bool &bad, Top &top, u64 (*buf)[CAP],
-                                            Part *sh, int *counts) {
-  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+__device__ __forceinline__ void block_merge(Stat &s, bool &bad, Top &top, u64 (*buf)[CAP + PAD],
+                                            Part *sh, int *counts, u64 *thrs) {
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
   s = wave_merge(s);
-  if (TOP) top.cut();
   if (lane == 0) {
     sh[wave] = {s.m, s.z, s.w, bad};
     counts[wave] = TOP ? top.count : 0;
+    if (TOP) thrs[wave] = top.thr;
   }
   __syncthreads();
   if (wave != 0) return;
@@ -211,25 +249,115 @@ __device__ __forceinline__ void block_merge(Stat &s, bool &bad, Top &top, u64 (*
     b.m = sh[i].m; b.z = sh[i].z; b.w = sh[i].w;
     s = merge(s, b);
     bad |= sh[i].bad != 0;
-    if (TOP) top.push(lane < counts[i] ? buf[i][lane] : 0);
+    // n values of one wave lie above its threshold, so it holds for all
+    if (TOP) top.set(thrs[i]);
   }
-  if (TOP) top.cut();
+  if (TOP) {
+    // the lists' first 64 at once, over a threshold that n lanes' best reach
+    u64 c[LW], own = 0;
+#pragma unroll
+    for (int i = 0; i < LW; i++) {
+      c[i] = lane < counts[i] ? buf[i][lane] : 0;
+      own = c[i] > own ? c[i] : own;
+    }
+    const int mine = counts[0];
+    top.seed(own);
+    const uint32_t least = max((uint32_t)(top.thr >> 32), 1u);
+    u64 more[CAP / 64 - 1];                       // of the own list, which is written over
+#pragma unroll
+    for (int k = 0; k < CAP / 64 - 1; k++) more[k] = lane + 64 * (k + 1) < mine ? buf[0][lane + 64 * (k + 1)] : 0;
+    top.count = 0;
+    if (!top.push_all<LW>([&](int i) { return (uint32_t)(c[i] >> 32) >= least; },
+                          [&](int i) { return c[i]; })) {
+#pragma unroll 1
+      for (int i = 0; i < LW; i++) top.push(i == 0 ? c[0] : lane < counts[i] ? buf[i][lane] : 0);
+    }
+    if (mine > 64) {
+#pragma unroll
+      for (int k = 0; k < CAP / 64 - 1; k++) top.push(more[k]);
+    }
+#pragma unroll 1
+    for (int i = 1; i < LW; i++)
+#pragma unroll 1
+      for (int j = 64; j < counts[i]; j += 64) top.push(j + lane < counts[i] ? buf[i][j + lane] : 0);
+    top.cut();
+  }
+}
+
+// 4-byte words of a span's result.
+__host__ __device__ constexpr int part_words(int n) { return 4 + 2 * (n + (n & 1)); }
+
+// A row's S spans, each thread's in turn.
+template <bool TOP>
+__device__ __forceinline__ void join_spans(Rsrc rs, int words, const Out &o, int64_t t, int V, int n,
+                                           int S, u64 (*buf)[CAP + PAD], Part *sh, int *counts,
+                                           u64 *thrs) {
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  Stat s;
+  s.init();
+  bool bad = false;
+  Top top;
+  if (TOP) top.init(buf[wave], n);
+#pragma unroll 1
+  for (int s0 = wave * 64; s0 < S; s0 += LT) {
+    const bool in = s0 + lane < S;
+    const int at = min(s0 + lane, S - 1) * words;
+    const v4f q = shared4(rs, at);
+    u64 c[16];
+    if (TOP) {
+#pragma unroll
+      for (int j = 0; j < 16; j += 2) {          // (part_words rounds n up to even)
+        const v4u x = __builtin_bit_cast(v4u, shared4(rs, at + 4 + 2 * min(j, (n - 1) & ~1)));
+        c[j] = in && j < n ? (u64)x[1] << 32 | x[0] : 0;
+        c[j + 1] = in && j + 1 < n ? (u64)x[3] << 32 | x[2] : 0;
+      }
+    }
+    Stat b;
+    b.m = q[0]; b.z = q[1]; b.w = q[2];
+    if (in) {
+      s = merge(s, b);
+      bad |= q[3] != 0.0f;
+    }
+    if (TOP) {
+      if (S - s0 >= n) top.seed(c[0]);
+      // the candidates come in order: where the first 16 do not fit the list,
+      // or there are more, one by one until no lane's beats the threshold
+      const uint32_t least = max((uint32_t)(top.thr >> 32), 1u);
+      int j = top.push_all<16>([&](int i) { return (uint32_t)(c[i] >> 32) >= least; },
+                               [&](int i) { return c[i]; }) ? 16 : 0;
+#pragma unroll 1
+      for (; j < n; j++) {
+        const u64 x = __builtin_bit_cast(u64, shared2(rs, at + 4 + 2 * j));
+        if (!__ballot(in && x > top.thr)) break;
+        top.push(in ? x : 0);
+      }
+    }
+  }
+  bad = __ballot(bad) != 0;
+  if (S > 64) {
+    block_merge<TOP>(s, bad, top, buf, sh, counts, thrs);
+  } else if (wave == 0) {                          // the other waves have had none
+    s = wave_merge(s);
+    if (TOP) top.cut();
+  }
+  if (wave == 0) write_row(o, t, V, n, s, bad, buf[0]);
 }
 
 // Workgroup: span blockIdx % S of row blockIdx / S.  Groups of four values
 // are counted from the 16-byte boundary at or below the row's start.
-template <bool TOP>
-__global__ __launch_bounds__(LT) void logprobs_kernel(const float *__restrict__ logits,
+template <bool TOP, bool SPLIT>
+__global__ __launch_bounds__(LT, 4) void logprobs_kernel(const float *__restrict__ logits,
                                                       int64_t stride, Out o, int64_t T, int V,
-                                                      int n, int S, uint8_t *__restrict__ ws,
-                                                      int64_t part_bytes) {
-  __shared__ u64 buf[TOP ? LW : 1][CAP];
+                                                      int n, int S, int *count, uint8_t *ws) {
+  __shared__ __align__(16) u64 buf[TOP ? LW : 1][CAP + PAD];
   __shared__ Part sh[LW];
   __shared__ int counts[LW];
+  __shared__ u64 thrs[LW];
+  __shared__ int flag;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
   for (int64_t item = blockIdx.x; item < T * S; item += gridDim.x) {
-    const int64_t t = item / S;
-    const int span = (int)(item - t * S);
+    const int64_t t = SPLIT ? item / S : item;
+    const int span = SPLIT ? (int)(item - t * S) : 0;
     const float *row = logits + t * stride;
     const int a = (int)((t * stride) & 3);         // elements before the row in its first group
     const float4 *base = reinterpret_cast<const float4 *>(row - a);
@@ -308,21 +436,31 @@ __global__ __launch_bounds__(LT) void logprobs_kernel(const float *__restrict__ 
       }
       if (TOP) {
         if (__ballot(odd || !(cm < top.thrf))) {
-          const auto comp = [&](int i) -> u64 {
-            const uint32_t e = (uint32_t)(4 * (c + (i / 4) * 64 + lane) + (i & 3) - a);
-            return here >> i & 1u ? comp_of(x[i], e) : 0;
-          };
+          const auto at = [&](int i) { return (uint32_t)(4 * (c + (i / 4) * 64 + lane) + (i & 3) - a); };
           if (first) {
             u64 own = 0;
 #pragma unroll
-            for (int i = 0; i < 4 * UG; i++) {
-              const u64 q = comp(i);
-              own = q > own ? q : own;
-            }
+            for (int i = 0; i < 4 * UG; i++)
+              if (here >> i & 1u) {
+                const u64 q = comp_of(x[i], at(i));
+                own = q > own ? q : own;
+              }
             top.seed(own);
           }
-#pragma unroll
-          for (int i = 0; i < 4 * UG; i++) top.push(comp(i));
+          // by the value alone: one more of the threshold's own value does no harm
+          const float least = top.thrf;
+          if (__ballot(odd) ||
+              !top.push_all<4 * UG>([&](int i) { return (here >> i & 1u) && x[i] >= least; },
+                                    [&](int i) { return comp_of(x[i], at(i)); })) {
+            // more than the list takes: one by one, read again (kept out of the
+            // unrolled code, which a short row is bound by fetching)
+#pragma unroll 1
+            for (int i = 0; i < 4 * UG; i++) {
+              const int g = c + (i / 4) * 64 + lane, e = 4 * g + (i & 3) - a;
+              const bool in = g < g1 && e >= 0 && e < V;
+              top.push(in ? comp_of(row[e], (uint32_t)e) : 0);
+            }
+          }
         }
         first = false;
       }
@@ -330,69 +468,26 @@ __global__ __launch_bounds__(LT) void logprobs_kernel(const float *__restrict__ 
       for (int u = 0; u < UG; u++) v[u] = nx[u];
     }
     bad = __ballot(bad) != 0;
-    block_merge<TOP>(s, bad, top, buf, sh, counts);
-    if (wave == 0) {
-      if (S == 1) {
-        Out r = o;
-        r.row = row;
-        write_row(r, t, V, n, s, bad, buf[0]);
-      } else {
-        uint8_t *p = ws + item * part_bytes;
-        if (lane == 0) *reinterpret_cast<Part *>(p) = {s.m, s.z, s.w, bad};
-        if (TOP && lane < n)
-          reinterpret_cast<u64 *>(p + sizeof(Part))[lane] = lane < top.count ? buf[0][lane] : 0;
+    block_merge<TOP>(s, bad, top, buf, sh, counts, thrs);
+    Out r = o;
+    r.row = row;
+    if constexpr (!SPLIT) {
+      if (wave == 0) write_row(r, t, V, n, s, bad, buf[0]);
+    } else {
+      // the last span of the row to get here joins them all
+      const int words = part_words(n);
+      const Rsrc rs = shared_at(ws + t * S * words * 4);
+      if (wave == 0) {
+        if (lane == 0)
+          share(rs, span * words, v4f{s.m, s.z, s.w, bad ? 1.0f : 0.0f});
+        if (TOP && lane < n) {
+          const u64 c = lane < top.count ? buf[0][lane] : 0;
+          share(rs, span * words + 4 + 2 * lane, __builtin_bit_cast(v2f, c));
+        }
       }
+      if (last_of(count + t, S, &flag)) join_spans<TOP>(rs, words, r, t, V, n, S, buf, sh, counts, thrs);
     }
     __syncthreads();
-  }
-}
-
-// One workgroup a row: its S spans' statistics and candidates.
-template <bool TOP>
-__global__ __launch_bounds__(LT) void combine_spans_kernel(const float *__restrict__ logits,
-                                                           int64_t stride, Out o, int V, int n,
-                                                           int S, const uint8_t *__restrict__ ws,
-                                                           int64_t part_bytes) {
-  __shared__ u64 buf[TOP ? LW : 1][CAP];
-  __shared__ Part sh[LW];
-  __shared__ int counts[LW];
-  const int64_t t = blockIdx.x;
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
-  const uint8_t *p = ws + t * S * part_bytes;
-  Stat s;
-  s.init();
-  bool bad = false;
-  for (int i = threadIdx.x; i < S; i += LT) {
-    const Part q = *reinterpret_cast<const Part *>(p + i * part_bytes);
-    Stat b;
-    b.m = q.m; b.z = q.z; b.w = q.w;
-    s = merge(s, b);
-    bad |= q.bad != 0;
-  }
-  bad = __ballot(bad) != 0;
-  Top top;
-  if (TOP) {
-    top.init(buf[wave], n);
-    const auto cand = [&](int span, int j) -> u64 {
-      return span < S ? reinterpret_cast<const u64 *>(p + span * part_bytes + sizeof(Part))[j] : 0;
-    };
-    // lane: a span; its candidates come in order, so once no lane's next one
-    // beats the threshold the rest does not either
-    for (int s0 = wave * 64; s0 < S; s0 += LT) {
-      u64 c = cand(s0 + lane, 0);
-      if (S - s0 >= n) top.seed(c);
-      for (int j = 0; j < n; j++) {
-        if (!__ballot(c > top.thr)) break;
-        top.push(c);
-        c = j + 1 < n ? cand(s0 + lane, j + 1) : 0;
-      }
-    }
-  }
-  block_merge<TOP>(s, bad, top, buf, sh, counts);
-  if (wave == 0) {
-    Out r = o;
-    r.row = logits + t * stride;
-    write_row(r, t, V, n, s, bad, buf[0]);
   }
 }
 
@@ -402,7 +497,7 @@ int spans(int64_t T, int64_t V) {
   const int64_t want = (512 + T - 1) / T, most = (V + 3 + 4 * CHUNK * LW - 1) / (4 * CHUNK * LW);
   return (int)std::max<int64_t>(1, std::min(want, most));
 }
-int64_t part_bytes(int64_t n) { return (int64_t)sizeof(Part) + 8 * n + (n & 1) * 8; }
+constexpr int64_t COUNTERS = 512 * 4;            // an arrival count a row, before the parts
 
 }  // namespace
 }  // namespace w4a8
@@ -418,8 +513,8 @@ static int logprobs_sizes(int64_t T, int64_t V, int64_t n_top) {
 
 extern "C" size_t token_logprobs_workspace_size(int64_t T, int64_t V, int64_t n_top) {
   if (logprobs_sizes(T, V, n_top) != W4A8_OK) return 0;
-  if (T == 0) return 16;
-  return (size_t)std::max<int64_t>(16, T * spans(T, V) * part_bytes(n_top));
+  const int64_t S = T == 0 ? 1 : spans(T, V);
+  return S == 1 ? 16 : (size_t)(COUNTERS + T * S * part_words((int)n_top) * 4);
 }
 
 extern "C" int token_logprobs(const float *logits, int64_t stride, const int32_t *targets,
@@ -440,20 +535,17 @@ extern "C" int token_logprobs(const float *logits, int64_t stride, const int32_t
   if (T == 0) return W4A8_OK;
   if (int rc = check_device(); rc != W4A8_OK) return rc;
   const int S = spans(T, V);
-  const int64_t pb = part_bytes(n_top);
   const Out o = {nullptr, targets, logprob, entropy, top_ids, top_logprobs};
   const dim3 grid((unsigned)std::min<int64_t>(T * S, 1 << 22));
-  uint8_t *ws = reinterpret_cast<uint8_t *>(workspace);
-  const hipStream_t st = as_stream(stream);
-  const auto go = [&](auto top) {
-    constexpr bool TOP = decltype(top)::value;
-    logprobs_kernel<TOP><<<grid, dim3(LT), 0, st>>>(logits, stride, o, T, (int)V, (int)n_top, S,
-                                                    ws, pb);
-    int rc = check_launch();
-    if (rc != W4A8_OK || S == 1) return rc;
-    combine_spans_kernel<TOP><<<dim3((unsigned)T), dim3(LT), 0, st>>>(
-        logits, stride, o, (int)V, (int)n_top, S, ws, pb);
+  int *count = reinterpret_cast<int *>(workspace);
+  uint8_t *ws = reinterpret_cast<uint8_t *>(workspace) + COUNTERS;
+  const auto go = [&](auto top, auto split) {
+    logprobs_kernel<decltype(top)::value, decltype(split)::value>
+        <<<grid, dim3(LT), 0, as_stream(stream)>>>(logits, stride, o, T, (int)V, (int)n_top, S, count, ws);
     return check_launch();
   };
-  return n_top > 0 ? go(std::true_type{}) : go(std::false_type{});
+  const std::true_type yes;
+  const std::false_type no;
+  if (n_top > 0) return S > 1 ? go(yes, yes) : go(yes, no);
+  return S > 1 ? go(no, yes) : go(no, no);
 }

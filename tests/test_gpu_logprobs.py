@@ -127,6 +127,17 @@ def test_rows_with_nan_or_infinity(bad):
     check(x, t, n, w4.token_logprobs(dev(x), dev(t), n))
 
 
+def test_one_workspace_for_calls_of_several_shapes():
+    """Its arrival counters are zero after each call."""
+    g = synth.rng(13)
+    shapes = [(1, 151936, 20), (3, 9000, 32), (400, 9001, 1), (7, 50, 5), (2, 70000, 0)]
+    ws = torch.zeros(max(w4.logprobs_workspace(*s).numel() for s in shapes), dtype=torch.uint8, device="cuda")
+    for T, V, n in shapes + shapes[::-1]:
+        x, t = synth.normal_f32(g, (T, V), 3.0), g.integers(0, V, T).astype(np.int32)
+        check(x, t, n, w4.token_logprobs(dev(x), dev(t), n, workspace=ws), (T, V, n))
+        assert not bool(ws[:2048].any())
+
+
 def test_parts_of_the_result():
     """Each output on its own gives the same bits; nothing else is needed."""
     g = synth.rng(12)
