@@ -238,7 +238,7 @@ int gdn_chunked_scan(const float *q, const float *k, const float *v, const float
  * with (a, b) = (i, i + n_rot / 2) in W4A8_ROPE_HALF and (2i, 2i + 1) in
  * W4A8_ROPE_INTERLEAVED; elements from n_rot on pass through unchanged.  The
  * angle, its cosine and sine and the rotation are taken in fp64 and rounded
- * once to fp32, so far positions lose nothing.
+ * once to fp32, so far positions lose nothing (angles below 2^52).
  *   inv_freq  [n_rot / 2] fp64, radians per position (rope_frequencies, or
  *             the caller's own);  pos [T] int32, any sign;  mscale finite.
  * As the `rope` of another entry point NULL means no rotation.  Errors (there
@@ -296,10 +296,11 @@ int rope_rotate(const w4a8_rope *rope, const float *x, int64_t x_stride, float *
  * head's rows of one page in 4-bit blocks of 32 elements along D (NB = D/32
  * blocks a row): W4A8_KV_Q4_0 (the Q4_0 quantizer, fp16 scales) or
  * W4A8_KV_Q4_SYM (the Q4_SYM quantizer with d = amax * fl(1/7), the binary32
- * product with the rounded reciprocal, in place of the quotient; fp32 scales).  kv_q4_tile_bytes(D,
- * format) bytes each: NB * 1024 of codes, then the scales.  With t the token
- * of the page, b the block, payload byte j as in the block formats (element j
- * in the low nibble, element j + 16 in the high one):
+ * product with the rounded reciprocal, in place of the quotient; fp32
+ * scales).  kv_q4_tile_bytes(D, format) bytes each: NB * 1024 of codes, then
+ * the scales.  With t the token of the page, b the block, payload byte j as in
+ * the block formats (element j in the low nibble, element j + 16 in the high
+ * one):
  *   K codes   dword b*256 + c*64 + (t%16)*4 + t/16: payload bytes 4c .. 4c+3,
  *             each nibble code - 8 in two's complement;
  *   V codes   byte b*1024 + ((t%16)/4)*256 + j*16 + (t/16)*4 + p(t%4),
@@ -319,10 +320,10 @@ int rope_rotate(const w4a8_rope *rope, const float *x, int64_t x_stride, float *
  * may share pages that neither writes in the call.
  * Errors of every entry point that takes a plan: NULL plan, or a NULL pointer
  * to something its sizes say is there (pools with n_pages > 0, arrays with
- * B > 0, page_table with max_pages > 0 too) -> W4A8_ENULL; D not 64, 128 or 256, NKV < 1, B < 0, n_pages < 0, max_pages
- * < 0 or an unknown format -> W4A8_ESHAPE; NKV >= 2^16, B >= 2^20, n_pages
- * >= 2^31 or max_pages >= 2^24 -> W4A8_ERANGE; pools not 16-byte, arrays not
- * 4-byte aligned -> W4A8_EALIGN.
+ * B > 0, page_table with max_pages > 0 too) -> W4A8_ENULL; D not 64, 128 or
+ * 256, NKV < 1, B < 0, n_pages < 0, max_pages < 0 or an unknown format ->
+ * W4A8_ESHAPE; NKV >= 2^16, B >= 2^20, n_pages >= 2^31 or max_pages >= 2^24 ->
+ * W4A8_ERANGE; pools not 16-byte, arrays not 4-byte aligned -> W4A8_EALIGN.
  */
 #define W4A8_KV_PAGE   64
 #define W4A8_KV_Q4_0   0
@@ -350,9 +351,10 @@ size_t kv_q4_tile_bytes(int64_t D, int32_t format);   /* 0: invalid */
  * sequence are rotated too.
  *   k, v [T][NKV][D], q [T][NH][D] fp32, row r at r * stride elements, heads
  *   contiguous; q_out contiguous, may be q itself if q is.
- * Each stored block is bit-identical to its definition for the fp32 row.  Errors beside the plan's and rope's: T < 0, a stride below heads * D
- * or not a multiple of 4, q without rope, NH < 1 -> W4A8_ESHAPE; T >= 2^31,
- * NH >= 2^16 or a stride >= 2^31 -> W4A8_ERANGE; k, v or q_out NULL ->
+ * Each stored block is bit-identical to its definition for the fp32 row.
+ * Errors beside the plan's and rope's: T < 0, a stride below heads * D or not
+ * a multiple of 4, q without rope, NH < 1 -> W4A8_ESHAPE; T >= 2^31, NH >=
+ * 2^16 or a stride >= 2^31 -> W4A8_ERANGE; k, v or q_out NULL ->
  * W4A8_ENULL; k, v, q or q_out not 16-byte aligned -> W4A8_EALIGN; q_out
  * equal to k, v, or to q with a q_stride other than NH * D -> W4A8_EALIAS.
  * T == 0 or B == 0 is a no-op (with q and B == 0 only q is rotated).
@@ -386,8 +388,8 @@ int kv_q4_read(const w4a8_kv *kv, float *k_out, float *v_out, int64_t T, void *s
  * Keys that a row does not see cannot change its result, whatever their
  * codes and scales hold.
  *   q [T][NH][D] fp32 with row stride q_stride, out [T][NH][D], lse [T][NH]
- *   (NULL: not written).  One launch.  workspace >= attn_q4_workspace_size
- *   bytes, zero-filled before its first use (moe_w4a8_workspace_init does
+ *   (NULL: not written).  One launch, or two (long sequences, few rows).
+ *   workspace >= attn_q4_workspace_size bytes, zero-filled before its first use (moe_w4a8_workspace_init does
  *   that); each call leaves it ready for later ones of any sizes it suffices
  *   for.  The result does not depend on timing, and a sequence's does not on
  *   the values of the others'.

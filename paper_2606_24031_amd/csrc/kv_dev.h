@@ -90,7 +90,7 @@ __device__ __forceinline__ int kv_find(const KvPlan &p, int64_t T, int64_t r, in
   const int lane = threadIdx.x & 63;
   int lo = 0, n = p.B;
   token = -1;
-  while (n > 1) {
+  while (n > 64) {
     const int step = (n + 63) / 64, at = lane * step;
     const bool ok = at < n && kv_clamp_row(p.cu[lo + at], T) <= r;
     const int k = __popcll(__ballot(ok)) - 1;
@@ -98,11 +98,20 @@ __device__ __forceinline__ int kv_find(const KvPlan &p, int64_t T, int64_t r, in
     lo += k * step;
     n = min(step, n - k * step);
   }
-  const int64_t r0 = kv_clamp_row(p.cu[lo], T), r1 = kv_clamp_row(p.cu[lo + 1], T);
+  int c0 = 0, c1 = 0, len = 0;
+  if (lane < n) {
+    c0 = p.cu[lo + lane];
+    c1 = p.cu[lo + lane + 1];
+    len = p.len[lo + lane];
+  }
+  const int k = __popcll(__ballot(lane < n && kv_clamp_row(c0, T) <= r)) - 1;
+  if (k < 0) return -1;
+  const int64_t r0 = kv_clamp_row(__builtin_amdgcn_readlane(c0, k), T);
+  const int64_t r1 = kv_clamp_row(__builtin_amdgcn_readlane(c1, k), T);
   if (r < r0 || r >= r1) return -1;
-  const int64_t t = (int64_t)p.len[lo] - (r1 - r);
+  const int64_t t = (int64_t)__builtin_amdgcn_readlane(len, k) - (r1 - r);
   token = t < 0 || t >= (int64_t)p.max_pages * KV_PAGE ? -1 : (int)t;
-  return lo;
+  return lo + k;
 }
 
 }  // namespace w4a8
