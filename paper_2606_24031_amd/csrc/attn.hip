@@ -667,7 +667,8 @@ __global__ __launch_bounds__(AT, (NB * NT > 8 ? 2 : NT > 1 || NB > 4 ? 3 : 4)) v
       if (__ballot(grow)) {
 #pragma unroll
         for (int nt = 0; nt < NT; nt++) {
-          const float mkn = mn[nt] * a.k;
+          // (a row without keys so far has no product to take: it could overflow)
+          const float mkn = mn[nt] == -FLT_MAX ? -FLT_MAX : mn[nt] * a.k;
           const float al = m[nt] == -FLT_MAX ? 0.0f : exp2_f(mk[nt] - mkn);
           m[nt] = mn[nt];
           mk[nt] = mkn;

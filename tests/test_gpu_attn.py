@@ -211,3 +211,12 @@ def test_empty_calls():
     kv = attn_cases.on_gpu(c)
     o, l = w4.attn_forward(kv, dev(q[:0]), 0.1)
     assert o.shape == (0, 2, 64) and l.shape == (0, 2)
+
+
+@pytest.mark.parametrize("fmt", ["q4_0", "q4_sym"])
+def test_rows_without_keys_at_a_large_scale(fmt):
+    # rows before token 0 beside rows that see keys, with a scale at which the
+    # lowest running maximum times it would overflow
+    c, q = case(77, [5, 40], [9, 60], 4, 2, 64, fmt)
+    r = check(c, q, 20.0, what=f"rows before token 0 at scale 20, {fmt}")
+    assert np.isneginf(r.lse).any() and np.isfinite(r.lse).any()
