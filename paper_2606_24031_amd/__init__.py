@@ -455,82 +455,72 @@ def moe_forward_noalloc(hidden, topk_ids, topk_w, w_gate_up, w_down, ws_gate_up,
 
 
 # ------------------------------------------------------------------ attention and logits
-class _On:
-    """Makes a GPU the current one for a call (the library launches on the
-    current device; streams belong to one)."""
-
-    def __init__(self, index):
-        self.index = index
-
-    def __enter__(self):
-        import torch
-        self.back = torch.cuda.current_device()
-        torch.cuda.set_device(self.index)
-
-    def __exit__(self, *exc):
-        import torch
-        torch.cuda.set_device(self.back)
-
-
-class _Here:
-    def __enter__(self):
-        pass
-
-    def __exit__(self, *exc):
-        pass
-
-
-_HERE = _Here()
-
-
-def _on(*tensors):
-    """A context in which the tensors' device (one GPU for all) is current."""
-    import torch
-    dev = tensors[0].device
+# These calls are short (a token's rotation takes 4 us on the GPU), so their
+# checks are written for few Python operations each.
+def _call(what, stream, tensors, *args):
+    """Entry point `what` with `args` and a stream (None: the current one) on
+    the GPU that all of `tensors` are on, made current for the call."""
+    from torch import _C
+    dev = tensors[0].get_device()
     for t in tensors:
-        if t is not None and t.device != dev:
-            raise ValueError(f"tensors on {dev} and {t.device} in one call")
-    if dev.type != "cuda":
-        raise ValueError(f"tensors on {dev}: a GPU's are needed")
-    return _HERE if dev.index == torch.cuda.current_device() else _On(dev.index)
-
-
-def _raw(stream):
-    """The raw handle of `stream`, or of the current one."""
-    import torch
-    if stream is not None:
-        return stream.cuda_stream
-    return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
+        if t is not None and t.get_device() != dev:
+            raise ValueError(f"tensors on {tensors[0].device} and {t.device} in one call")
+    if dev < 0:
+        raise ValueError(f"tensors on {tensors[0].device}: a GPU's are needed")
+    here = _C._cuda_getDevice()
+    if here != dev:
+        _C._cuda_setDevice(dev)
+    try:
+        rc = getattr(lib(), what)(*args, stream.cuda_stream if stream is not None
+                                  else _C._cuda_getCurrentRawStream(dev))
+    finally:
+        if here != dev:
+            _C._cuda_setDevice(here)
+    if rc != OK:
+        raise W4A8Error(rc, what)
 
 
 def _ptr(t):
     return None if t is None else t.data_ptr()
 
 
+def _zeros(n, device, stream=None):
+    """A workspace, zero-filled and held on the stream that uses it."""
+    import torch
+    with torch.cuda.stream(stream):
+        return torch.zeros(n, dtype=torch.uint8, device=device)
+
+
 def _is(t, dtype, shape, what):
     """A contiguous tensor of this type and shape (None: any size)."""
-    if t.dtype is not dtype or not t.is_contiguous() or t.dim() != len(shape) or \
-            any(n is not None and n != m for n, m in zip(shape, t.shape)):
-        raise ValueError(f"{what}: a contiguous {dtype} tensor of shape {shape} is needed, "
-                         f"got {t.dtype} {tuple(t.shape)} with strides {t.stride()}")
+    if t.dtype is dtype and t.is_contiguous():
+        if t.shape == shape or \
+                None in shape and t.dim() == len(shape) and all(n in (None, m) for n, m in zip(shape, t.shape)):
+            return
+    raise ValueError(f"{what}: a contiguous {dtype} tensor of shape {shape} is needed, "
+                     f"got {t.dtype} {tuple(t.shape)} with strides {t.stride()}")
 
 
-def _heads(x, what):
-    """[rows, heads, D] fp32 with contiguous heads; returns the row stride."""
+def _heads(x, shape, what):
+    """[rows, heads, D] fp32 of this shape with contiguous heads; returns the
+    row stride."""
     import torch
-    if x.dtype is torch.float32 and x.dim() == 3:
-        T, NH, D = x.shape
+    if x.dtype is torch.float32 and x.shape == shape and len(shape) == 3:
+        T, NH, D = shape
         s0, s1, s2 = x.stride()
+        if s1 == D and s2 == 1 and T > 1:
+            return s0
         if T * NH * D == 0 or (s2 == 1 and (NH == 1 or s1 == D)):
             return s0 if T > 1 else max(s0, NH * D)
-    raise ValueError(f"{what}: fp32 [rows, heads, D] with contiguous heads is needed, "
+    raise ValueError(f"{what}: fp32 [rows, heads, D] = {tuple(shape)} with contiguous heads is needed, "
                      f"got {x.dtype} {tuple(x.shape)} with strides {x.stride()}")
 
 
 def _rope(pos, inv_freq, layout, mscale, T):
     import torch
     _is(pos, torch.int32, (T,), "pos")
-    _is(inv_freq, torch.float64, (None,), "inv_freq")
+    if inv_freq.dtype is not torch.float64 or inv_freq.dim() != 1 or not inv_freq.is_contiguous():
+        _is(inv_freq, torch.float64, (None,), "inv_freq")
     if layout not in ROPE_LAYOUTS:
         raise ValueError(f"layout {layout!r}: one of {sorted(ROPE_LAYOUTS)}")
     return _RopeArgs(inv_freq.data_ptr(), pos.data_ptr(), 2 * inv_freq.numel(),
@@ -548,9 +538,8 @@ def rope_frequencies(n_rot, base=10000.0, kind="none", factor=1.0, orig_len=0, b
     if out is None:
         out = torch.empty(max(0, n_rot // 2), dtype=torch.float64, device=device)
     _is(out, torch.float64, (n_rot // 2,), "out")
-    with _on(out):
-        _check(lib().rope_frequencies(_ptr(out), n_rot, base, ROPE_KINDS[kind], factor, orig_len,
-                                      beta_fast, beta_slow, _raw(stream)), "rope_frequencies")
+    _call("rope_frequencies", stream, (out,), _ptr(out), n_rot, base, ROPE_KINDS[kind], factor,
+          orig_len, beta_fast, beta_slow)
     return out
 
 
@@ -558,19 +547,16 @@ def rope_rotate(x, pos, inv_freq, layout="half", mscale=1.0, out=None, stream=No
     """The heads of x [T, NH, D] turned by their rows' positions pos [T] (the
     first 2 * len(inv_freq) elements; out may be x)."""
     import torch
-    T, NH, D = x.shape
-    xs = _heads(x, "x")
+    shape = x.shape
+    xs = _heads(x, shape, "x")
+    T, NH, D = shape
     r = _rope(pos, inv_freq, layout, mscale, T)
     if out is None:
-        out = torch.empty((T, NH, D), dtype=torch.float32, device=x.device)
-    if out.shape != x.shape:
-        raise ValueError(f"out: shape {tuple(x.shape)} is needed, got {tuple(out.shape)}")
-    os_ = _heads(out, "out")
-    if T == 0:
-        return out
-    with _on(x, pos, inv_freq, out):
-        _check(lib().rope_rotate(ctypes.byref(r), _ptr(x), xs, _ptr(out), os_, T, NH, D,
-                                 _raw(stream)), "rope_rotate")
+        out = torch.empty(shape, dtype=torch.float32, device=x.device)
+    os_ = _heads(out, shape, "out")
+    if T:
+        _call("rope_rotate", stream, (x, pos, inv_freq, out), ctypes.byref(r), x.data_ptr(), xs,
+              out.data_ptr(), os_, T, NH, D)
     return out
 
 
@@ -614,6 +600,7 @@ class KVCache:
         self.NKV, self.D, self.device = k_pages.shape[1], D, k_pages.device
         self.args = _KvArgs(*(t.data_ptr() for t in self.tensors), k_pages.shape[0], max_pages, B,
                             self.NKV, D, KV_FORMATS[fmt])
+        self.ref = ctypes.byref(self.args)
 
 
 def kv_append(kv, k, v, pos=None, inv_freq=None, layout="half", mscale=1.0, q=None, q_out=None,
@@ -624,28 +611,24 @@ def kv_append(kv, k, v, pos=None, inv_freq=None, layout="half", mscale=1.0, q=No
     import torch
     T = k.shape[0]
     shape = (T, kv.NKV, kv.D)
-    ks, vs = _heads(k, "k"), _heads(v, "v")
-    if k.shape != shape or v.shape != shape:
-        raise ValueError(f"k, v: shape {shape} is needed, got {tuple(k.shape)}, {tuple(v.shape)}")
+    ks, vs = _heads(k, shape, "k"), _heads(v, shape, "v")
     if (pos is None) != (inv_freq is None):
         raise ValueError("pos and inv_freq go together")
     r = None if pos is None else _rope(pos, inv_freq, layout, mscale, T)
     NH = qs = 0
     if q is not None:
-        qs, NH = _heads(q, "q"), q.shape[1]
-        if q.shape[0] != T or q.shape[2] != kv.D:
-            raise ValueError(f"q: shape ({T}, heads, {kv.D}) is needed, got {tuple(q.shape)}")
+        NH = q.shape[1] if q.dim() == 3 else 0
+        shape = (T, NH, kv.D)
+        qs = _heads(q, shape, "q")
         if q_out is None:
-            q_out = torch.empty((T, NH, kv.D), dtype=torch.float32, device=q.device)
-        _is(q_out, torch.float32, (T, NH, kv.D), "q_out")
+            q_out = torch.empty(shape, dtype=torch.float32, device=q.device)
+        _is(q_out, torch.float32, shape, "q_out")
     else:
         q_out = None
-    if T == 0:
-        return q_out
-    with _on(kv.tensors[0], k, v, pos, inv_freq, q, q_out):
-        _check(lib().kv_q4_append(ctypes.byref(kv.args), None if r is None else ctypes.byref(r),
-                                  _ptr(k), ks, _ptr(v), vs, _ptr(q), qs, _ptr(q_out), NH, T,
-                                  _raw(stream)), "kv_q4_append")
+    if T:
+        _call("kv_q4_append", stream, (kv.tensors[0], k, v, pos, inv_freq, q, q_out), kv.ref,
+              None if r is None else ctypes.byref(r), k.data_ptr(), ks, v.data_ptr(), vs, _ptr(q), qs,
+              _ptr(q_out), NH, T)
     return q_out
 
 
@@ -653,27 +636,25 @@ def kv_read(kv, T, k_out=None, v_out=None, stream=None):
     """The T rows of kv's sequences as fp32 (k, v) [T, NKV, D]."""
     import torch
     shape = (T, kv.NKV, kv.D)
-    new = lambda: torch.empty(shape, dtype=torch.float32, device=kv.device)
-    k_out = new() if k_out is None else k_out
-    v_out = new() if v_out is None else v_out
+    if k_out is None:
+        k_out = torch.empty(shape, dtype=torch.float32, device=kv.device)
+    if v_out is None:
+        v_out = torch.empty(shape, dtype=torch.float32, device=kv.device)
     _is(k_out, torch.float32, shape, "k_out")
     _is(v_out, torch.float32, shape, "v_out")
-    if T == 0:
-        return k_out, v_out
-    with _on(kv.tensors[0], k_out, v_out):
-        _check(lib().kv_q4_read(ctypes.byref(kv.args), _ptr(k_out), _ptr(v_out), T, _raw(stream)),
-               "kv_q4_read")
+    if T:
+        _call("kv_q4_read", stream, (kv.tensors[0], k_out, v_out), kv.ref, k_out.data_ptr(),
+              v_out.data_ptr(), T)
     return k_out, v_out
 
 
-def attn_workspace(kv, T, NH):
+def attn_workspace(kv, T, NH, stream=None):
     """A workspace for attn_forward with T rows of NH heads on kv's plan
-    (zero-filled; each call leaves it ready for the next)."""
-    import torch
-    n = int(lib().attn_q4_workspace_size(ctypes.byref(kv.args), T, NH))
+    (zero-filled on the stream; each call leaves it ready for the next)."""
+    n = int(lib().attn_q4_workspace_size(kv.ref, T, NH))
     if n == 0:
         raise W4A8Error(ESHAPE, "attn_q4_workspace_size")
-    return torch.zeros(n, dtype=torch.uint8, device=kv.device)
+    return _zeros(n, kv.device, stream)
 
 
 def attn_forward(kv, q, scale, window=0, out=None, lse=None, want_lse=True, workspace=None,
@@ -681,37 +662,34 @@ def attn_forward(kv, q, scale, window=0, out=None, lse=None, want_lse=True, work
     """Softmax attention of q [T, NH, D] (kv's rows) over the 4-bit cache;
     returns (out [T, NH, D], lse [T, NH] or None)."""
     import torch
-    qs = _heads(q, "q")
-    T, NH, D = q.shape
-    if D != kv.D:
-        raise ValueError(f"q: heads of {kv.D} are needed, got {D}")
+    T, NH = q.shape[:2] if q.dim() == 3 else (0, 0)
+    shape = (T, NH, kv.D)
+    qs = _heads(q, shape, "q")
     if out is None:
-        out = torch.empty((T, NH, D), dtype=torch.float32, device=q.device)
-    _is(out, torch.float32, (T, NH, D), "out")
+        out = torch.empty(shape, dtype=torch.float32, device=q.device)
+    _is(out, torch.float32, shape, "out")
     if lse is None and want_lse:
         lse = torch.empty((T, NH), dtype=torch.float32, device=q.device)
     if lse is not None:
         _is(lse, torch.float32, (T, NH), "lse")
-    if T == 0:
-        return out, lse
-    with _on(kv.tensors[0], q, out, lse, workspace):
+    if T:
         if workspace is None:
-            workspace = attn_workspace(kv, T, NH)
-        _check(lib().attn_q4_forward(ctypes.byref(kv.args), _ptr(q), qs, _ptr(out), _ptr(lse), T, NH,
-                                     scale, window, _ptr(workspace),
-                                     workspace.numel() * workspace.element_size(),
-                                     _raw(stream)), "attn_q4_forward")
+            workspace = attn_workspace(kv, T, NH, stream)
+        elif not workspace.is_contiguous():
+            raise ValueError("workspace: a contiguous tensor is needed")
+        _call("attn_q4_forward", stream, (kv.tensors[0], q, out, lse, workspace), kv.ref, q.data_ptr(),
+              qs, out.data_ptr(), _ptr(lse), T, NH, scale, window, workspace.data_ptr(),
+              workspace.numel() * workspace.element_size())
     return out, lse
 
 
-def logprobs_workspace(T, V, n_top=0, device="cuda"):
-    """A workspace for token_logprobs (zero-filled; each call leaves it ready
-    for the next)."""
-    import torch
+def logprobs_workspace(T, V, n_top=0, device="cuda", stream=None):
+    """A workspace for token_logprobs (zero-filled on the stream; each call
+    leaves it ready for the next)."""
     n = int(lib().token_logprobs_workspace_size(T, V, n_top))
     if n == 0:
         raise W4A8Error(ERANGE, "token_logprobs_workspace_size")
-    return torch.zeros(n, dtype=torch.uint8, device=device)
+    return _zeros(n, device, stream)
 
 
 def token_logprobs(logits, targets=None, n_top=0, want_entropy=True, logprob=None, entropy=None,
@@ -725,32 +703,40 @@ def token_logprobs(logits, targets=None, n_top=0, want_entropy=True, logprob=Non
         raise ValueError(f"logits: fp32 [T, V] with contiguous rows is needed, got {logits.dtype} "
                          f"{tuple(logits.shape)} with strides {logits.stride()}")
     T, V = logits.shape
-    stride = logits.stride(0) if T > 1 else max(V, logits.stride(0))
-    new = lambda *s, dt=torch.float32: torch.empty(s, dtype=dt, device=logits.device)
+    stride = logits.stride(0)
+    if T == 1 and stride < V:
+        stride = V
+    new = logits.new_empty
     if targets is not None:
         _is(targets, torch.int32, (T,), "targets")
-        logprob = new(T) if logprob is None else logprob
-        _is(logprob, torch.float32, (T,), "logprob")
+        if logprob is None:
+            logprob = new((T,))
+        else:
+            _is(logprob, torch.float32, (T,), "logprob")
     else:
         logprob = None
-    if want_entropy and entropy is None:
-        entropy = new(T)
     if entropy is not None:
         _is(entropy, torch.float32, (T,), "entropy")
+    elif want_entropy:
+        entropy = new((T,))
     if n_top > 0:
-        top_ids = new(T, n_top, dt=torch.int32) if top_ids is None else top_ids
-        top_logprobs = new(T, n_top) if top_logprobs is None else top_logprobs
-        _is(top_ids, torch.int32, (T, n_top), "top_ids")
-        _is(top_logprobs, torch.float32, (T, n_top), "top_logprobs")
+        if top_ids is None:
+            top_ids = new((T, n_top), dtype=torch.int32)
+        else:
+            _is(top_ids, torch.int32, (T, n_top), "top_ids")
+        if top_logprobs is None:
+            top_logprobs = new((T, n_top))
+        else:
+            _is(top_logprobs, torch.float32, (T, n_top), "top_logprobs")
     else:
         top_ids = top_logprobs = None
-    if T == 0:
-        return logprob, entropy, top_ids, top_logprobs
-    with _on(logits, targets, logprob, entropy, top_ids, top_logprobs, workspace):
+    if T:
         if workspace is None:
-            workspace = logprobs_workspace(T, V, n_top, logits.device)
-        _check(lib().token_logprobs(_ptr(logits), stride, _ptr(targets), _ptr(logprob), _ptr(entropy),
-                                    _ptr(top_ids), _ptr(top_logprobs), T, V, n_top, _ptr(workspace),
-                                    workspace.numel() * workspace.element_size(),
-                                    _raw(stream)), "token_logprobs")
+            workspace = logprobs_workspace(T, V, n_top, logits.device, stream)
+        elif not workspace.is_contiguous():
+            raise ValueError("workspace: a contiguous tensor is needed")
+        _call("token_logprobs", stream,
+              (logits, targets, logprob, entropy, top_ids, top_logprobs, workspace), logits.data_ptr(),
+              stride, _ptr(targets), _ptr(logprob), _ptr(entropy), _ptr(top_ids), _ptr(top_logprobs),
+              T, V, n_top, workspace.data_ptr(), workspace.numel() * workspace.element_size())
     return logprob, entropy, top_ids, top_logprobs

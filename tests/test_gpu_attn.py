@@ -220,3 +220,24 @@ def test_rows_without_keys_at_a_large_scale(fmt):
     c, q = case(77, [5, 40], [9, 60], 4, 2, 64, fmt)
     r = check(c, q, 20.0, what=f"rows before token 0 at scale 20, {fmt}")
     assert np.isneginf(r.lse).any() and np.isfinite(r.lse).any()
+
+
+def test_a_workspace_of_its_own_on_another_stream():
+    """Without a workspace the call's own is zero-filled on its stream, not
+    behind the current stream's work."""
+    c, q = case(31, [700, 90], [3, 2], 8, 2, 64, "q4_0")
+    kv, qd = attn_cases.on_gpu(c), dev(q)
+    want = w4.attn_forward(kv, qd, 0.125)
+    n = w4.attn_workspace(kv, c.T, 8).numel()
+    st, out, lse = torch.cuda.Stream(), torch.empty_like(want[0]), torch.empty_like(want[1])
+    x = torch.ones(4096, 4096, device="cuda")
+    for _ in range(3):
+        dirty = [torch.full((n,), 255, dtype=torch.uint8, device="cuda") for _ in range(4)]
+        torch.cuda.synchronize()
+        del dirty
+        st.wait_stream(torch.cuda.current_stream())
+        for _ in range(20):
+            x = torch.tanh(x)                     # the current stream is busy
+        w4.attn_forward(kv, qd, 0.125, out=out, lse=lse, stream=st)
+        torch.cuda.synchronize()
+        assert torch.equal(out, want[0]) and torch.equal(lse, want[1])
