@@ -507,10 +507,10 @@ def _heads(x, shape, what):
     import torch
     if x.dtype is torch.float32 and x.shape == shape and len(shape) == 3:
         T, NH, D = shape
+        if x.is_contiguous():
+            return NH * D
         s0, s1, s2 = x.stride()
-        if s1 == D and s2 == 1 and T > 1:
-            return s0
-        if T * NH * D == 0 or (s2 == 1 and (NH == 1 or s1 == D)):
+        if (s2 == 1 and (NH == 1 or s1 == D)):
             return s0 if T > 1 else max(s0, NH * D)
     raise ValueError(f"{what}: fp32 [rows, heads, D] = {tuple(shape)} with contiguous heads is needed, "
                      f"got {x.dtype} {tuple(x.shape)} with strides {x.stride()}")
