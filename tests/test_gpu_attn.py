@@ -241,3 +241,39 @@ def test_a_workspace_of_its_own_on_another_stream():
         w4.attn_forward(kv, qd, 0.125, out=out, lse=lse, stream=st)
         torch.cuda.synchronize()
         assert torch.equal(out, want[0]) and torch.equal(lse, want[1])
+
+
+@pytest.mark.parametrize("fmt", ["q4_0", "q4_sym"])
+def test_a_prompt_and_what_its_rows_do_not_see(fmt):
+    """NaN and infinite scales of a few keys: rows that do not see them (others
+    of their tile do) keep their results."""
+    D, NH = 128, 12
+    c, q = case(7, [1300], [1300], NH, 1, D, fmt)
+    clean = ref.attention(c, q, 0.09, 100)
+    ft = np.float16 if fmt == "q4_0" else np.float32
+    at = lambda t: (t % 16) // 4 * 16 + t // 16 * 4 + t % 4
+    bad = {400: np.nan, 801: np.inf, 1190: -np.inf}
+    for pool in (c.k_pool, c.v_pool):
+        for tok, x in bad.items():
+            sc = pool[c.table[0, tok // 64], 0, D // 32 * 1024:].view(ft)
+            sc[at(tok % 64)] = x
+            sc[3 * 64 + at(tok % 64)] = x
+    got = w4.attn_forward(attn_cases.on_gpu(c), dev(q), 0.09, 100)
+    o, l = got[0].cpu().numpy(), got[1].cpu().numpy()
+    t = np.arange(c.T)
+    see = np.any([(t >= k) & (t - 100 < k) for k in bad], axis=0)
+    assert see.sum() == 300
+    bo, bl = ref.attention_bounds(clean)
+    assert np.all(np.abs(o[~see] - clean.out[~see]) <= bo[~see])
+    assert np.all(np.abs(l[~see] - clean.lse[~see]) <= bl[~see])
+    # only values bad: scores are as they were, and the other columns too
+    c2, _ = case(7, [1300], [1300], NH, 1, D, fmt)
+    for tok, x in bad.items():
+        sc = c2.v_pool[c2.table[0, tok // 64], 0, D // 32 * 1024:].view(ft)
+        sc[at(tok % 64)] = x
+    got = w4.attn_forward(attn_cases.on_gpu(c2), dev(q), 0.09, 100)
+    o, l = got[0].cpu().numpy(), got[1].cpu().numpy()
+    assert np.all(np.abs(l - clean.lse) <= bl)
+    assert np.all(np.abs(o[~see] - clean.out[~see]) <= bo[~see])
+    assert np.all(np.abs(o[see][..., 32:] - clean.out[see][..., 32:]) <= bo[see][..., 32:])
+    assert not np.isfinite(o[see][..., :32]).any()
