@@ -915,12 +915,20 @@ template <int NB, int ROWS> __global__ __launch_bounds__(JT) void join_kernel(At
   if (c4 == 0 && a.lse) a.lse[o] = l != 0.0f ? (R + log2f(l)) * 0.693147180559945f : -INFINITY;
 }
 
-// Rows of a tile by the rows a sequence has of a KV head on average: 4 or 8
-// packed (a decode step of few heads a group), the 16 of one product, or 32,
-// which share the page's loads and decoded codes.
+// Rows of a tile: 4 or 8 packed where a sequence has no more of a KV head on
+// average (a decode step of few heads a group), the 16 of one product, or 32,
+// which share the page's loads and decoded codes.  More rows a tile are less
+// work in all but fewer workgroups, and longer ones: 32 only where they number
+// 1024 and more (2048 tokens of 32 heads of 128: 108 us against 121 with 16;
+// 512 tokens of 16 heads of 256, 256 tiles: 25.6 against 18.4), 8 where
+// tiles of 16 would number less than 64, at 256 columns 256 (128 tokens of 16
+// heads of 256: 10.1 us against 11.2; one token of 16 heads of 128 over 8000
+// keys: 15 against 21; past it 2 % to 10 % slower).
 int tile_rows(const w4a8_kv *kv, int64_t T, int64_t NH) {
   const int64_t rows = T * (NH / kv->NKV), B = std::max<int64_t>(1, kv->B);
-  return rows <= 4 * B ? 4 : rows <= 8 * B ? 8 : rows <= 16 * B ? 16 : 32;
+  if (rows <= 4 * B) return 4;
+  if (rows <= 8 * B || T * NH < (kv->D == 256 ? 4096 : 1024)) return 8;
+  return T * NH >= 32 * 1024 && rows > 16 * B ? 32 : 16;
 }
 
 // Bounds on the call's items, and on the partial results it can need: a
@@ -939,13 +947,16 @@ int64_t slots_bound(const w4a8_kv *kv, int64_t T, int64_t NH) {
 
 // Whether the last workgroups join the runs.  They read past the L2 caches,
 // some 30 KB a round trip: right for a few runs an item, which they join while
-// others still work, in place of a launch (4 sequences' 4 .. 5 runs an item:
-// 12.5 us a call against 15.0), but one row over 131072 keys, 256 runs an
-// item, takes 37 us so and 30 with a launch that puts 1024 threads on a row.
+// others still work, in place of a launch (one row of 32 heads of 128 over 2000
+// keys, 8 runs: 11 us against 13; 16 runs: 13.5 against 13).  A launch puts
+// 1024 threads on a row: better from a group of runs, or 2048 columns of a
+// row's, on (16 heads of 256 over 4000 keys, 16 runs: 14.9 us against 20.5; over
+// 131072, 256 runs: 30 against 37).  (An average: a long sequence among short
+// ones may have more runs, and is joined in two levels.)
 bool joins_fused(const w4a8_kv *kv, int64_t T, int64_t NH) {
   const int64_t runs = std::min<int64_t>((kv->max_pages + AW - 1) / AW,
                                          TARGET / std::max<int64_t>(1, items_bound(kv, T, NH)));
-  return runs <= 2 * GROUP;
+  return runs <= GROUP && runs * kv->D < 2048;
 }
 
 int attn_sizes(const w4a8_kv *kv, int64_t T, int64_t NH) {

@@ -277,3 +277,30 @@ def test_a_prompt_and_what_its_rows_do_not_see(fmt):
     assert np.all(np.abs(o[~see] - clean.out[~see]) <= bo[~see])
     assert np.all(np.abs(o[see][..., 32:] - clean.out[see][..., 32:]) <= bo[see][..., 32:])
     assert not np.isfinite(o[see][..., :32]).any()
+
+
+@pytest.mark.parametrize("D,fmt,lens,rows,NH,NKV,window", [
+    (64, "q4_0", [500], [500], 66, 2, 0),            # 33 heads a group: tiles end inside a token's
+    (128, "q4_sym", [500], [500], 66, 2, 0),
+    (256, "q4_0", [270, 30], [260, 7], 126, 2, 0),
+    (128, "q4_0", [321, 700], [321, 191], 64, 1, 90),
+    (64, "q4_sym", [3, 600, 0], [40, 470, 2], 64, 1, 0),   # rows before token 0, no tokens
+    (256, "q4_0", [300], [300], 16, 2, 0), (256, "q4_sym", [70, 600], [70, 200], 16, 1, 100),
+])
+def test_prompts_of_many_rows(D, fmt, lens, rows, NH, NKV, window):
+    """The tiles of large calls: 32 rows, and 16 of 256 columns (the last two)."""
+    c, q = case(D + sum(lens), lens, rows, NH, NKV, D, fmt)
+    check(c, q, D ** -0.5, window, what=f"many rows {lens} {NH}/{NKV} D={D} {fmt} window {window}")
+
+
+@pytest.mark.parametrize("D,lens,rows", [(256, [4000], [1]), (64, [9000, 5], [1, 1]), (128, [2500, 3100], [2, 1])])
+def test_joins_by_a_launch_and_without(D, lens, rows):
+    """Sequences whose runs the last workgroups join in one call and a second
+    launch in another (more pages in the plan's tables): the same results."""
+    c, q = case(D + len(lens), lens, rows, 4, 2, D, "q4_0")
+    check(c, q, D ** -0.5, what=f"joins {lens} D={D}")
+    wide = attn_cases.random_plan(synth.rng(1), lens, rows, 2, D, "q4_0", capacity=700)
+    wide.k_pool, wide.v_pool = c.k_pool, c.v_pool
+    wide.table[:, :c.table.shape[1]] = c.table
+    wide.table[:, c.table.shape[1]:] = -1
+    check(wide, q, D ** -0.5, what=f"joins, wide tables, {lens} D={D}")
