@@ -387,12 +387,15 @@ int kv_q4_read(const w4a8_kv *kv, float *k_out, float *v_out, int64_t T, void *s
  * (about 22 bits).  A row that sees no key gives out 0 and lse -infinity.
  * Keys that a row does not see cannot change its result, whatever their
  * codes and scales hold.
+ * Scores are to stay within fp32's range.
  *   q [T][NH][D] fp32 with row stride q_stride, out [T][NH][D], lse [T][NH]
  *   (NULL: not written).  One launch, or two (long sequences, few rows).
- *   workspace >= attn_q4_workspace_size bytes, zero-filled before its first use (moe_w4a8_workspace_init does
- *   that); each call leaves it ready for later ones of any sizes it suffices
- *   for.  The result does not depend on timing, and a sequence's does not on
- *   the values of the others'.
+ *   workspace >= attn_q4_workspace_size bytes, zero-filled before its first
+ *   use (moe_w4a8_workspace_init does that); each call leaves it ready for
+ *   later ones of this entry point of any sizes it suffices for.  Other entry
+ *   points would leave it in another state, and calls that overlap in time
+ *   would mix their results: neither may share it.  The result does not depend
+ *   on timing, and a sequence's does not on the values of the others'.
  * Errors beside the plan's: NH < 1, NH % NKV != 0, T < 0, window < 0,
  * q_stride < NH * D or not a multiple of 4, scale not finite -> W4A8_ESHAPE;
  * T * NH >= 2^31 or q_stride >= 2^31 -> W4A8_ERANGE; q, out or workspace NULL
@@ -425,7 +428,9 @@ int attn_q4_forward(const w4a8_kv *kv, const float *q, int64_t q_stride, float *
  *   NULL when n_top is 0).  One launch.  workspace >=
  *   token_logprobs_workspace_size bytes, zero-filled before its first use
  *   (moe_w4a8_workspace_init does that); each call leaves it ready for later
- *   ones of any sizes it suffices for.
+ *   ones of this entry point of any sizes it suffices for.  As for
+ *   attn_q4_forward, neither other entry points nor calls that overlap in time
+ *   may share it.
  * Errors: T < 0, V < 1, stride < V -> W4A8_ESHAPE; V >= 2^24, T >= 2^31,
  * n_top < 0, n_top > 32, n_top > V, T * stride >= 2^40 -> W4A8_ERANGE; logits,
  * only one of a pair, or the workspace NULL -> W4A8_ENULL; logits or the

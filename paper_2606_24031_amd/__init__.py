@@ -650,7 +650,8 @@ def kv_read(kv, T, k_out=None, v_out=None, stream=None):
 
 def attn_workspace(kv, T, NH, stream=None):
     """A workspace for attn_forward with T rows of NH heads on kv's plan
-    (zero-filled on the stream; each call leaves it ready for the next)."""
+    (zero-filled on the stream; each call of attn_forward leaves it ready for
+    the next)."""
     n = int(lib().attn_q4_workspace_size(kv.ref, T, NH))
     if n == 0:
         raise W4A8Error(ESHAPE, "attn_q4_workspace_size")
@@ -684,8 +685,8 @@ def attn_forward(kv, q, scale, window=0, out=None, lse=None, want_lse=True, work
 
 
 def logprobs_workspace(T, V, n_top=0, device="cuda", stream=None):
-    """A workspace for token_logprobs (zero-filled on the stream; each call
-    leaves it ready for the next)."""
+    """A workspace for token_logprobs (zero-filled on the stream; each call of
+    it leaves it ready for the next)."""
     n = int(lib().token_logprobs_workspace_size(T, V, n_top))
     if n == 0:
         raise W4A8Error(ERANGE, "token_logprobs_workspace_size")

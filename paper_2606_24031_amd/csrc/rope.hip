@@ -32,7 +32,7 @@ __global__ void frequencies_kernel(double *__restrict__ f, int half, double base
 // Workgroup (x, y): rows x * rows .. + rows - 1, heads y * heads .. + heads - 1.
 // Bound by HBM for a prompt (8 bytes an element; the fp64 work of a row's
 // cosines is shared by its heads): 5120 rows of 32 heads of 128 in 35 us, 4.8
-// TB/s, as a copy.  One row takes 4 us, the launch and the loads of the position
+// TB/s, as a copy.  One row takes 3 us, the launch and the loads of the position
 // and the frequencies.
 __global__ __launch_bounds__(RT) void rope_kernel(RopeArgs r, const float *x, int64_t xs, float *y,
                                                   int64_t ys, int64_t T, int NH, int D, int rows,
