@@ -317,7 +317,8 @@ int rope_rotate(const w4a8_rope *rope, const float *x, int64_t x_stride, float *
  * The arrays are read on the device and may change between replays of a
  * captured graph.  Tokens before 0 or past max_pages * W4A8_KV_PAGE do not
  * exist; rows outside every sequence are left as they were.  Two sequences
- * may share pages that neither writes in the call.
+ * may share pages that neither writes in the call; a page that a call writes
+ * stands once in its tables.
  * Errors of every entry point that takes a plan: NULL plan, or a NULL pointer
  * to something its sizes say is there (pools with n_pages > 0, arrays with
  * B > 0, page_table with max_pages > 0 too) -> W4A8_ENULL; D not 64, 128 or

@@ -149,9 +149,9 @@ def test_on_another_stream():
     x = torch.randn(T, 3000, device="cuda")
     torch.cuda.synchronize()
     q = w4.kv_append(kv, b[:, NH:NH + NKV], b[:, NH + NKV:], pos=pos, inv_freq=s.f, q=b[:, :NH], stream=st)
-    ws = w4.attn_workspace(kv, T, NH)
+    ws = w4.attn_workspace(kv, T, NH, stream=st)
     o, lse = w4.attn_forward(kv, q, D ** -0.5, workspace=ws, stream=st)
-    lw = w4.logprobs_workspace(T, 3000, 3)
+    lw = w4.logprobs_workspace(T, 3000, 3, stream=st)
     r = w4.token_logprobs(x, None, 3, workspace=lw, stream=st)
     st.synchronize()
     want, bound = s.want()
@@ -181,3 +181,40 @@ def test_two_calls_at_once_with_their_own_workspaces():
     torch.cuda.synchronize()
     for i in range(2):
         assert torch.equal(out[i], alone[i][0]) and torch.equal(lse[i], alone[i][1])
+
+
+def test_graphs_that_share_a_workspace():
+    """Graphs of calls of several shapes (runs joined within the launch, by a
+    second one, not split) on one workspace, replayed in turn with eager calls
+    on it between; log probabilities on theirs."""
+    g = synth.rng(8)
+    shapes = [([700, 30], [1, 2]), ([9000], [1]), ([130], [130])]
+    calls = []
+    for lens, rows in shapes:
+        c = attn_cases.random_plan(g, lens, rows, 2, 128, "q4_0")
+        q = dev(2 * synth.normal_f32(g, (c.T, 8, 128)))
+        calls.append((attn_cases.on_gpu(c), q, w4.attn_workspace(attn_cases.on_gpu(c), c.T, 8).numel()))
+    ws = torch.zeros(max(n for *_, n in calls), dtype=torch.uint8, device="cuda")
+    xs = [torch.randn(t, 20000, device="cuda") for t in (1, 5)]
+    lw = torch.zeros(max(w4.logprobs_workspace(x.shape[0], 20000, 7).numel() for x in xs),
+                     dtype=torch.uint8, device="cuda")
+    run = [lambda kv=kv, q=q: w4.attn_forward(kv, q, 0.09, workspace=ws) for kv, q, _ in calls] + \
+          [lambda x=x: w4.token_logprobs(x, None, 7, workspace=lw)[1:] for x in xs]
+    want = [[y.clone() for y in f()] for f in run]
+    torch.cuda.synchronize()
+    graphs, got = [], []
+    for f in run:
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1]):
+            got.append(f())
+    for i in range(4):
+        for k in (range(len(run)) if i % 2 else reversed(range(len(run)))):
+            for y in got[k]:
+                y.fill_(3)
+            graphs[k].replay()
+            other = run[(k + i) % len(run)]()
+            torch.cuda.synchronize()
+            for a, b in zip(got[k], want[k]):
+                assert torch.equal(a, b), (i, k)
+            for a, b in zip(other, want[(k + i) % len(run)]):
+                assert torch.equal(a, b), (i, k)
