@@ -399,10 +399,10 @@ int kv_q4_read(const w4a8_kv *kv, float *k_out, float *v_out, int64_t T, void *s
  *   on timing, and a sequence's does not on the values of the others'.
  * Errors beside the plan's: NH < 1, NH % NKV != 0, T < 0, window < 0,
  * q_stride < NH * D or not a multiple of 4, scale not finite -> W4A8_ESHAPE;
- * T * NH >= 2^31 or q_stride >= 2^31 -> W4A8_ERANGE; q, out or workspace NULL
- * -> W4A8_ENULL; q, out or workspace not 16-, lse not 4-byte aligned ->
- * W4A8_EALIGN; out equal to q -> W4A8_EALIAS; workspace too small ->
- * W4A8_EWORKSPACE.  T == 0 or B == 0 is a no-op.  attn_q4_workspace_size
+ * NH / NKV >= 2^16, T * NH >= 2^31 or q_stride >= 2^31 -> W4A8_ERANGE; q, out
+ * or workspace NULL -> W4A8_ENULL; q, out or workspace not 16-, lse not 4-byte
+ * aligned -> W4A8_EALIGN; out equal to q -> W4A8_EALIAS; workspace too small
+ * -> W4A8_EWORKSPACE.  T == 0 or B == 0 is a no-op.  attn_q4_workspace_size
  * returns 0 for invalid sizes; it reads only the plan's sizes and format.
  */
 size_t attn_q4_workspace_size(const w4a8_kv *kv, int64_t T, int64_t NH);

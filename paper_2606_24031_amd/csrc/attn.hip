@@ -438,8 +438,7 @@ __global__ __launch_bounds__(AT, (NB * NT > 8 ? 2 : NT > 1 || NB > 4 ? 3 : 4)) v
     if (a.window > 0) key0 = max((int64_t)0, (int64_t)pos0 - a.window + 1);
     const int per = f.runs == 1 ? sq.pages : (sq.pages + f.runs - 1) / f.runs;
     const int plo = max((int)(key0 / KV_PAGE), sq.lo + run * per);
-    int phi = min(sq.lo + min(sq.pages, (run + 1) * per), pos1 < 0 ? 0 : pos1 / KV_PAGE + 1);
-    if (a.p.n_pages == 0) phi = plo;
+    const int phi = min(sq.lo + min(sq.pages, (run + 1) * per), pos1 < 0 ? 0 : pos1 / KV_PAGE + 1);
 
     // page ids of a step: lane j < AW has page at0 + j's (-1: none)
     const int32_t *table = a.p.pages + (int64_t)f.s * a.p.max_pages;
@@ -920,6 +919,19 @@ template <int NB, int ROWS> __global__ __launch_bounds__(JT) void join_kernel(At
   if (c4 == 0 && a.lse) a.lse[o] = l != 0.0f ? (R + log2f(l)) * 0.693147180559945f : -INFINITY;
 }
 
+// The rows of a plan without any page (the kernels above load page 0 in an
+// absent one's place): a workgroup a row.
+__global__ __launch_bounds__(AT) void no_keys_kernel(AttnArgs a, int D) {
+  for (int64_t r = blockIdx.x; r < a.T; r += gridDim.x) {
+    int token;
+    if (kv_find(a.p, a.T, r, token) < 0) continue;
+    for (int i = threadIdx.x; i < a.NH * D / 4; i += AT)
+      reinterpret_cast<v4f *>(a.out + r * a.NH * D)[i] = v4f{0.f, 0.f, 0.f, 0.f};
+    if (a.lse)
+      for (int i = threadIdx.x; i < a.NH; i += AT) a.lse[r * a.NH + i] = -INFINITY;
+  }
+}
+
 // Rows of a tile: 4 or 8 packed where a sequence has no more of a KV head on
 // average (a decode step of few heads a group), the 16 of one product, or 32,
 // which share the page's loads and decoded codes.  More rows a tile are less
@@ -967,7 +979,7 @@ bool joins_fused(const w4a8_kv *kv, int64_t T, int64_t NH) {
 int attn_sizes(const w4a8_kv *kv, int64_t T, int64_t NH) {
   if (int rc = kv_check_sizes(kv); rc != W4A8_OK) return rc;
   if (NH < 1 || NH % kv->NKV != 0 || T < 0) return W4A8_ESHAPE;
-  if (NH >= ((int64_t)1 << 31) || T >= ((int64_t)1 << 31) || T * NH >= ((int64_t)1 << 31))
+  if (NH / kv->NKV >= (1 << 16) || T >= ((int64_t)1 << 31) || T * NH >= ((int64_t)1 << 31))
     return W4A8_ERANGE;
   return W4A8_OK;
 }
@@ -1013,7 +1025,8 @@ extern "C" int attn_q4_forward(const w4a8_kv *kv, const float *q, int64_t q_stri
   if (int rc = attn_sizes(kv, T, NH); rc != W4A8_OK) return rc;
   if (window < 0 || !std::isfinite(scale) || q_stride < NH * kv->D || q_stride % 4 != 0)
     return W4A8_ESHAPE;
-  if (q_stride >= ((int64_t)1 << 31)) return W4A8_ERANGE;
+  const int64_t lim = (int64_t)1 << 31;
+  if (q_stride >= lim) return W4A8_ERANGE;
   if (!aligned16(q) || !aligned16(out) || !aligned16(workspace) ||
       (reinterpret_cast<uintptr_t>(lse) & 3u))
     return W4A8_EALIGN;
@@ -1024,7 +1037,8 @@ extern "C" int attn_q4_forward(const w4a8_kv *kv, const float *q, int64_t q_stri
   AttnArgs a = {kv_plan(kv), q, q_stride, out, lse, T, (int)NH, (int)(NH / kv->NKV),
                 // a factor of 0 goes to Q, so that a masked score's -infinity stays one
                 scale != 0.0f ? std::fabs(scale) * 1.44269504f / 16.0f : 1.0f,
-                scale < 0.0f ? -1.0f : scale == 0.0f ? 0.0f : 1.0f, window,
+                scale < 0.0f ? -1.0f : scale == 0.0f ? 0.0f : 1.0f,
+                window < lim ? window : 0,       // wider than any sequence
                 reinterpret_cast<int *>(workspace),
                 reinterpret_cast<float *>(reinterpret_cast<uint8_t *>(workspace) + COUNTERS), (int)slots_bound(kv, T, NH),
                 joins_fused(kv, T, NH),
@@ -1033,6 +1047,10 @@ extern "C" int attn_q4_forward(const w4a8_kv *kv, const float *q, int64_t q_stri
   const bool sym = kv->format == W4A8_KV_Q4_SYM;
   const int rows = tile_rows(kv, T, NH);
   const hipStream_t s = as_stream(stream);
+  if (kv->n_pages == 0) {
+    no_keys_kernel<<<dim3((unsigned)std::min<int64_t>(T, 1 << 16)), dim3(AT), 0, s>>>(a, (int)kv->D);
+    return check_launch();
+  }
   if (kv->D == 64) return sym ? launch_rows<2, true>(a, rows, items, s) : launch_rows<2, false>(a, rows, items, s);
   if (kv->D == 128) return sym ? launch_rows<4, true>(a, rows, items, s) : launch_rows<4, false>(a, rows, items, s);
   return sym ? launch_rows<8, true>(a, rows, items, s) : launch_rows<8, false>(a, rows, items, s);

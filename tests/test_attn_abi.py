@@ -139,6 +139,17 @@ def test_attention_errors():
     assert call(T=0) == w4.OK and call(kv=plan(B=0, max_pages=4096)) == w4.OK
 
 
+def test_attention_refuses_very_large_groups():
+    """From 2^16 heads a group on the rows of a tile are not told apart."""
+    L = w4.lib()
+    kv = plan(max_pages=4096)
+    assert kv.NKV == 2
+    for NH, rc in ((2 << 16, w4.ERANGE), ((2 << 16) - 2, w4.EWORKSPACE)):
+        assert (L.attn_q4_workspace_size(ctypes.byref(kv), 1, NH) == 0) == (rc == w4.ERANGE)
+        assert L.attn_q4_forward(ctypes.byref(kv), P(A), NH * 128, P(A + 0x8000), None, 1, NH, 0.1, 0,
+                                 P(A + 0x10000), 0, None) == rc
+
+
 def test_logprobs_errors():
     L = w4.lib()
     S = L.token_logprobs_workspace_size

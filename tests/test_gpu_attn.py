@@ -73,6 +73,15 @@ def test_window(window):
     check(c, q, 0.125, window, what=f"window {window}")
 
 
+def test_a_window_wider_than_any_sequence():
+    c, q = case(3, [4, 333], [9, 5], 4, 2, 64, "q4_0")      # with rows before token 0
+    kv = attn_cases.on_gpu(c)
+    want = w4.attn_forward(kv, dev(q), 0.125)
+    for window in (2 ** 31 - 1, 2 ** 31, 2 ** 63 - 1):
+        got = w4.attn_forward(kv, dev(q), 0.125, window)
+        assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1]), window
+
+
 @pytest.mark.parametrize("D,NH,NKV,lens,rows", [
     (128, 8, 1, [20000], [1]), (256, 16, 2, [9000], [2]), (64, 2, 2, [15000, 40, 7000], [1, 1, 3]),
     (128, 16, 1, [6000, 2500], [4, 1])])
@@ -211,6 +220,27 @@ def test_empty_calls():
     kv = attn_cases.on_gpu(c)
     o, l = w4.attn_forward(kv, dev(q[:0]), 0.1)
     assert o.shape == (0, 2, 64) and l.shape == (0, 2)
+
+
+@pytest.mark.parametrize("rows", [1, 30])
+def test_a_pool_without_pages(rows):
+    """No page is present: rows give zeros and -infinity, stores go nowhere."""
+    D, fmt = 64, "q4_0"
+    kp, vp = w4.kv_pools(0, 2, D, fmt)
+    i32 = lambda a: dev(np.array(a, np.int32))
+    kv = w4.KVCache(kp, vp, i32([[0, 1], [-1, 7]]), i32([100, 40]), i32([0, rows, rows + 1]), D, fmt)
+    T = rows + 1
+    q = torch.randn(T, 4, D, device="cuda")
+    out, lse = w4.attn_forward(kv, q, 0.125)
+    assert bool((out == 0).all()) and bool(torch.isneginf(lse).all())
+    w4.kv_append(kv, q[:, :2].contiguous(), q[:, 2:].contiguous())
+    k, v = w4.kv_read(kv, T)
+    assert bool((k == 0).all()) and bool((v == 0).all())
+    # tables without columns
+    kv = w4.KVCache(kp, vp, torch.empty(2, 0, dtype=torch.int32, device="cuda"), i32([100, 40]),
+                    i32([0, rows, rows + 1]), D, fmt)
+    out, lse = w4.attn_forward(kv, q, 0.125)
+    assert bool((out == 0).all()) and bool(torch.isneginf(lse).all())
 
 
 @pytest.mark.parametrize("fmt", ["q4_0", "q4_sym"])
