@@ -45,6 +45,7 @@
 #include <algorithm>
 #include <cfloat>
 #include <cmath>
+#include <numeric>
 
 #include "kv_dev.h"
 #include "share_dev.h"
@@ -82,6 +83,7 @@ struct AttnArgs {
   int *count;       // arrivals: [SLOTS_MAX] of a group of runs, [SLOTS_MAX] of an item's groups
   float *part;      // partial results, `slots` of them
   int slots;
+  int64_t ids;      // runs at most
   int fused;        // the last workgroups join, not a second launch
   float inv_G;      // 1 / G
 };
@@ -416,7 +418,7 @@ __global__ __launch_bounds__(AT, (NB * NT > 8 ? 2 : NT > 1 || NB > 4 ? 3 : 4)) v
   constexpr int64_t TILE = kv_tile_bytes(D, SYM);
   constexpr int SB = kv_scale_bytes(SYM), SW = NB * SB / 4;   // words of scales a lane stages
   __shared__ Lds<NB, SYM, NT, PK> lds;
-  for (int id = blockIdx.x;; id += gridDim.x) {
+  for (int id = blockIdx.x; id < a.ids; id += gridDim.x) {
     // (taken anew each time round: what depends on it alone would otherwise
     // move out of this loop, that few go round twice, and hold registers)
     int tid = threadIdx.x;
@@ -949,12 +951,13 @@ int tile_rows(const w4a8_kv *kv, int64_t T, int64_t NH) {
 }
 
 // Bounds on the call's items, and on the partial results it can need: a
-// sequence is split only into runs of more than half of C >= total / TARGET
-// pages, so the runs of split items number at most 2 TARGET.
+// sequence's rows are a multiple of G, so its last tile holds gcd(G, rows of a
+// tile) at least; a sequence is split only into runs of more than half of C >=
+// total / TARGET pages, so the runs of split items number at most 2 TARGET.
 int64_t items_bound(const w4a8_kv *kv, int64_t T, int64_t NH) {
   const int rt = tile_rows(kv, T, NH);
   const int64_t G = NH / kv->NKV;
-  return ((T * G) / rt + std::min(kv->B, T)) * kv->NKV;
+  return (T * G + std::min(kv->B, T) * (rt - std::gcd(G, (int64_t)rt))) / rt * kv->NKV;
 }
 int64_t slots_bound(const w4a8_kv *kv, int64_t T, int64_t NH) {
   if (kv->max_pages <= AW || kv->B == 0) return 0;
@@ -986,7 +989,7 @@ int attn_sizes(const w4a8_kv *kv, int64_t T, int64_t NH) {
 
 template <int NB, bool SYM, int NT, int PK>
 int launch(const AttnArgs &a, int64_t items, hipStream_t s) {
-  const int64_t grid = std::min<int64_t>(items + a.slots, 1 << 20);
+  const int64_t grid = std::min<int64_t>(a.ids, 1 << 20);
   attn_kernel<NB, SYM, NT, PK><<<dim3((unsigned)grid), dim3(AT), 0, s>>>(a);
   if (int rc = check_launch(); rc != W4A8_OK || a.slots == 0 || a.fused) return rc;
   constexpr int ROWS = 16 * NT / PK;
@@ -1034,6 +1037,7 @@ extern "C" int attn_q4_forward(const w4a8_kv *kv, const float *q, int64_t q_stri
   if (ws_bytes < attn_q4_workspace_size(kv, T, NH)) return W4A8_EWORKSPACE;
   if (T == 0 || kv->B == 0) return W4A8_OK;
   if (int rc = check_device(); rc != W4A8_OK) return rc;
+  const int64_t items = items_bound(kv, T, NH);
   AttnArgs a = {kv_plan(kv), q, q_stride, out, lse, T, (int)NH, (int)(NH / kv->NKV),
                 // a factor of 0 goes to Q, so that a masked score's -infinity stays one
                 scale != 0.0f ? std::fabs(scale) * 1.44269504f / 16.0f : 1.0f,
@@ -1041,9 +1045,9 @@ extern "C" int attn_q4_forward(const w4a8_kv *kv, const float *q, int64_t q_stri
                 window < lim ? window : 0,       // wider than any sequence
                 reinterpret_cast<int *>(workspace),
                 reinterpret_cast<float *>(reinterpret_cast<uint8_t *>(workspace) + COUNTERS), (int)slots_bound(kv, T, NH),
-                joins_fused(kv, T, NH),
+                // a split item's runs beyond the first are C pages each
+                items + std::min<int64_t>(slots_bound(kv, T, NH), TARGET), joins_fused(kv, T, NH),
                 1.0f / (float)(NH / kv->NKV)};
-  const int64_t items = items_bound(kv, T, NH);
   const bool sym = kv->format == W4A8_KV_Q4_SYM;
   const int rows = tile_rows(kv, T, NH);
   const hipStream_t s = as_stream(stream);
