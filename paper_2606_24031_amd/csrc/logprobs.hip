@@ -5,10 +5,13 @@
 // compute units), and the last of them to finish joins their results, in their
 // order; every wave streams its share of a span in chunks of 16
 // values a lane, the next chunk's loads under way, and keeps
-//   - per lane the softmax statistics (m, z, w): the maximum so far, the sum
-//     of exp(l - m) WITHOUT the maximum's own 1, and sum exp(l - m) (l - m).
-//     With z kept apart from the 1, log Z = log1p(z) is accurate to fp32 for a
-//     confident row too, whose log Z may be 1e-6;
+//   - the softmax statistics (m, z, w): the maximum so far, the sum of
+//     exp(l - m) WITHOUT the maximum's own 1, and sum exp(l - m) (l - m), each
+//     lane its share of the sums.  With z kept apart from the 1, log Z =
+//     log1p(z) is accurate to fp32 for a confident row too, whose log Z may be
+//     1e-6.  One maximum for the wave: chunks that raise it are few, and in the
+//     others every value, its equal too, is one difference, exponential and
+//     two sums (a maximum a lane had its 1 to look for in every chunk);
 //   - per wave the n largest logits: a list in LDS of candidates that beat a
 //     threshold, cut back to the n best (by counting, for each candidate, the
 //     larger ones) when it fills.  The first threshold is a value that n of
@@ -60,7 +63,14 @@ struct Stat {
   __device__ void init() { m = -FLT_MAX; z = -1.0f; w = 0.0f; }   // 1 + z = 0: nothing seen
 };
 
-__device__ __forceinline__ float exp_f(float d) { return __builtin_amdgcn_exp2f(d * 1.44269504f); }
+// exp(d), FAR <= d <= 0.  exp2 of the rounded product t = d log2(e) alone would
+// be off by |d| 2^-24, which a confident row, whose sum hangs on a few values,
+// shows in full (3e-7 in its log probability; so 5e-8): what t leaves out of d
+// comes in to first order.
+__device__ __forceinline__ float exp_f(float d) {
+  const float t = d * 1.44269502f, e = __builtin_amdgcn_exp2f(t);
+  return fmaf(e, fmaf(t, -0.693147181f, d), e);
+}
 
 // a and b over disjoint values; the larger maximum's 1 stays out of the sum.
 __device__ __forceinline__ Stat merge(Stat a, Stat b) {
@@ -237,7 +247,6 @@ template <bool TOP>
 __device__ __forceinline__ void block_merge(Stat &s, bool &bad, Top &top, u64 (*buf)[CAP + PAD],
                                             Part *sh, int *counts, u64 *thrs) {
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
-  s = wave_merge(s);
   if (lane == 0) {
     sh[wave] = {s.m, s.z, s.w, bad};
     counts[wave] = TOP ? top.count : 0;
@@ -336,10 +345,10 @@ __device__ __forceinline__ void join_spans(Rsrc rs, int words, const Out &o, int
     }
   }
   bad = __ballot(bad) != 0;
+  s = wave_merge(s);
   if (S > 64) {
     block_merge<TOP>(s, bad, top, buf, sh, counts, thrs);
   } else if (wave == 0) {                          // the other waves have had none
-    s = wave_merge(s);
     if (TOP) top.cut();
   }
   if (wave == 0) write_row(o, t, V, n, s, bad, buf[0]);
@@ -366,8 +375,7 @@ __global__ __launch_bounds__(LT, 4) void logprobs_kernel(const float *__restrict
     const int G = (a + V + 3) / 4;
     const int per = ((G + CHUNK - 1) / CHUNK + S - 1) / S * CHUNK;
     const int g0 = min(span * per, G), g1 = min(g0 + per, G);
-    Stat s;
-    s.init();
+    float m = -INFINITY, z = 0.0f, w = 0.0f;       // m is the wave's, z and w are the lane's shares
     bool bad = false;
     Top top;
     if (TOP) top.init(buf[wave], n);
@@ -416,26 +424,6 @@ __global__ __launch_bounds__(LT, 4) void logprobs_kernel(const float *__restrict
         odd |= !(x[i] < INFINITY);
       }
       bad |= odd;
-      const float mn = fmaxf(s.m, cm);
-      const float dm = fmaxf(s.m - mn, FAR), f = exp_f(dm), t1 = 1.0f + s.z;
-      float zs = 0.0f, wsum = 0.0f;
-      int same = 0;
-#pragma unroll
-      for (int i = 0; i < 4 * UG; i++) {
-        const float d = x[i] - mn, e = exp_f(d);
-        const bool eq = x[i] == mn;
-        same += eq ? 1 : 0;
-        zs += eq ? 0.0f : e;
-        wsum = fmaf(e, fmaxf(d, FAR), wsum);
-      }
-      if (mn > s.m) {                              // the maximum's own 1 stays out
-        s.w = fmaf(f, fmaf(dm, t1, s.w), wsum);
-        s.z = fmaf(t1, f, zs + (float)(same - 1));
-        s.m = mn;
-      } else {
-        s.w += wsum;
-        s.z += zs + (float)same;
-      }
       if (TOP) {
         if (__ballot(odd || !(cm < top.thrf))) {
           const auto at = [&](int i) { return (uint32_t)(4 * (c + (i / 4) * 64 + lane) + (i & 3) - a); };
@@ -466,10 +454,46 @@ __global__ __launch_bounds__(LT, 4) void logprobs_kernel(const float *__restrict
         }
         first = false;
       }
+      if (__ballot(cm > m)) {                      // a new maximum: its own 1 stays out
+        float mn = cm;
+#pragma unroll
+        for (int k = 32; k > 0; k >>= 1) mn = fmaxf(mn, __shfl_xor(mn, k));
+        const float dm = fmaxf(m - mn, FAR), f = exp_f(dm);
+        const float t1 = lane == 0 && m > -INFINITY ? z + 1.0f : z;     // the former one's goes in
+        w = f * fmaf(dm, t1, w);
+        z = f * t1;
+        m = mn;
+        bool out = lane == __ffsll((long long)__ballot(cm == mn)) - 1;
+#pragma unroll
+        for (int i = 0; i < 4 * UG; i++) {
+          const bool eq = out && x[i] == mn;
+          if (eq) x[i] = -INFINITY;
+          out = out && !eq;
+        }
+      }
+      float zs = 0.0f, wsum = 0.0f;
+#pragma unroll
+      for (int i = 0; i < 4 * UG; i++) {
+        const float d = fmaxf(x[i] - m, FAR), e = exp_f(d);
+        zs += e;
+        wsum = fmaf(e, d, wsum);
+      }
+      z += zs;
+      w += wsum;
 #pragma unroll
       for (int u = 0; u < UG; u++) v[u] = nx[u];
     }
     bad = __ballot(bad) != 0;
+#pragma unroll
+    for (int k = 32; k > 0; k >>= 1) {
+      z += __shfl_xor(z, k);
+      w += __shfl_xor(w, k);
+    }
+    Stat s;
+    s.init();
+    if (m > -INFINITY) {
+      s.m = m; s.z = z; s.w = w;
+    }
     block_merge<TOP>(s, bad, top, buf, sh, counts, thrs);
     Out r = o;
     r.row = row;

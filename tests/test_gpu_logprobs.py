@@ -148,3 +148,19 @@ def test_parts_of_the_result():
     assert b[1] is None and b[2] is None and c[0] is None
     assert torch.equal(a[0], b[0]) and torch.equal(a[2], c[2]) and torch.equal(a[3], c[3])
     assert w4.token_logprobs(x[:0], t[:0], 4)[2].shape == (0, 4)
+
+
+@pytest.mark.parametrize("V", [7, 40000])
+def test_a_confident_rows_small_log_probability(V):
+    """Two values, the rest -infinity: log p of the larger is -log1p(exp(-d)),
+    to 2^-21 relative.  d is exact; exp's first-order term takes log(2) as fp32,
+    2^-28 |d| off (2^-22.4 at 45), exp2 is off by 2^-23, the correction's, the
+    sums' and log1p's roundings by 2^-24, 2^-24 and 2^-23: 6.5 2^-24 in all."""
+    d = np.array([0.5, 3.3, 7.9, 13.1, 19.7, 23.7, 31.3, 44.9], np.float32)
+    x = np.full((len(d), V), -np.inf, np.float32)
+    x[:, V - 2] = 1.0
+    x[np.arange(len(d)), np.arange(len(d)) % (V - 3)] = np.float32(1.0) - d
+    gap = 1.0 - x[np.arange(len(d)), np.arange(len(d)) % (V - 3)].astype(np.float64)
+    want = -np.log1p(np.exp(-gap))
+    got = w4.token_logprobs(dev(x), dev(np.full(len(d), V - 2, np.int32)))[0].cpu().numpy().astype(np.float64)
+    assert np.all(np.abs(got - want) <= 2.0 ** -21 * np.abs(want)), (got, want)
