@@ -41,7 +41,7 @@
 // by VALU issue, 93 % of a large one's cycles (2 x 2048 rows over 8192 keys, 32
 // heads of 128: 808 us, 427 TFLOP/s): the two scaling operations a score and
 // block and the three that make W's halves.  Short calls by their chain of
-// launch, plan, page ids, pages and join (one row over 948 keys: 13 us).
+// launch, plan, page ids, pages and join (one row over 948 keys: 12 us).
 #include <algorithm>
 #include <cfloat>
 #include <cmath>
