@@ -11,6 +11,11 @@ from __future__ import annotations
 import ctypes
 import os
 
+try:
+    import torch
+except ImportError:                   # building needs none
+    torch = None
+
 HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(HERE, "libw4a8.so")
 
@@ -455,27 +460,27 @@ def moe_forward_noalloc(hidden, topk_ids, topk_w, w_gate_up, w_down, ws_gate_up,
 
 
 # ------------------------------------------------------------------ attention and logits
-# These calls are short (a token's rotation takes 4 us on the GPU), so their
+# These calls are short (a token's rotation takes 3 us on the GPU), so their
 # checks are written for few Python operations each.
 def _call(what, stream, tensors, *args):
     """Entry point `what` with `args` and a stream (None: the current one) on
     the GPU that all of `tensors` are on, made current for the call."""
-    from torch import _C
     dev = tensors[0].get_device()
     for t in tensors:
         if t is not None and t.get_device() != dev:
             raise ValueError(f"tensors on {tensors[0].device} and {t.device} in one call")
     if dev < 0:
         raise ValueError(f"tensors on {tensors[0].device}: a GPU's are needed")
-    here = _C._cuda_getDevice()
-    if here != dev:
-        _C._cuda_setDevice(dev)
-    try:
-        rc = getattr(lib(), what)(*args, stream.cuda_stream if stream is not None
-                                  else _C._cuda_getCurrentRawStream(dev))
-    finally:
-        if here != dev:
-            _C._cuda_setDevice(here)
+    C, f = torch._C, getattr(_lib or lib(), what)
+    here = C._cuda_getDevice()
+    if here == dev:
+        rc = f(*args, stream.cuda_stream if stream is not None else C._cuda_getCurrentRawStream(dev))
+    else:
+        C._cuda_setDevice(dev)
+        try:
+            rc = f(*args, stream.cuda_stream if stream is not None else C._cuda_getCurrentRawStream(dev))
+        finally:
+            C._cuda_setDevice(here)
     if rc != OK:
         raise W4A8Error(rc, what)
 
@@ -486,7 +491,6 @@ def _ptr(t):
 
 def _zeros(n, device, stream=None):
     """A workspace, zero-filled and held on the stream that uses it."""
-    import torch
     with torch.cuda.stream(stream):
         return torch.zeros(n, dtype=torch.uint8, device=device)
 
@@ -504,20 +508,18 @@ def _is(t, dtype, shape, what):
 def _heads(x, shape, what):
     """[rows, heads, D] fp32 of this shape with contiguous heads; returns the
     row stride."""
-    import torch
     if x.dtype is torch.float32 and x.shape == shape and len(shape) == 3:
-        T, NH, D = shape
         if x.is_contiguous():
-            return NH * D
+            return shape[1] * shape[2]
+        T, NH, D = shape
         s0, s1, s2 = x.stride()
-        if (s2 == 1 and (NH == 1 or s1 == D)):
+        if s2 == 1 and (NH == 1 or s1 == D):
             return s0 if T > 1 else max(s0, NH * D)
     raise ValueError(f"{what}: fp32 [rows, heads, D] = {tuple(shape)} with contiguous heads is needed, "
                      f"got {x.dtype} {tuple(x.shape)} with strides {x.stride()}")
 
 
 def _rope(pos, inv_freq, layout, mscale, T):
-    import torch
     _is(pos, torch.int32, (T,), "pos")
     if inv_freq.dtype is not torch.float64 or inv_freq.dim() != 1 or not inv_freq.is_contiguous():
         _is(inv_freq, torch.float64, (None,), "inv_freq")
@@ -532,7 +534,6 @@ def rope_frequencies(n_rot, base=10000.0, kind="none", factor=1.0, orig_len=0, b
     """Frequencies of the n_rot / 2 rotated pairs, fp64 radians per position:
     base^(-2i / n_rot), as they are ("none"), over factor ("linear"), or mixed
     by how often a pair turns within orig_len positions ("parts")."""
-    import torch
     if kind not in ROPE_KINDS:
         raise ValueError(f"kind {kind!r}: one of {sorted(ROPE_KINDS)}")
     if out is None:
@@ -546,7 +547,6 @@ def rope_frequencies(n_rot, base=10000.0, kind="none", factor=1.0, orig_len=0, b
 def rope_rotate(x, pos, inv_freq, layout="half", mscale=1.0, out=None, stream=None):
     """The heads of x [T, NH, D] turned by their rows' positions pos [T] (the
     first 2 * len(inv_freq) elements; out may be x)."""
-    import torch
     shape = x.shape
     xs = _heads(x, shape, "x")
     T, NH, D = shape
@@ -566,7 +566,6 @@ def kv_tile_bytes(D, fmt="q4_0") -> int:
 
 def kv_pools(n_pages, NKV, D, fmt="q4_0", device="cuda"):
     """Key and value pools of n_pages pages (any contents) for NKV heads."""
-    import torch
     n = kv_tile_bytes(D, fmt)
     if n == 0:
         raise W4A8Error(ESHAPE, "kv_q4_tile_bytes")
@@ -581,7 +580,6 @@ class KVCache:
     on the device at each call: update them in place between steps."""
 
     def __init__(self, k_pages, v_pages, page_table, kv_len, cu_rows, D, fmt="q4_0"):
-        import torch
         if fmt not in KV_FORMATS:
             raise ValueError(f"format {fmt!r}: one of {sorted(KV_FORMATS)}")
         n = kv_tile_bytes(D, fmt)
@@ -608,7 +606,6 @@ def kv_append(kv, k, v, pos=None, inv_freq=None, layout="half", mscale=1.0, q=No
     """Stores the rows k, v [T, NKV, D] as the last tokens of kv's sequences,
     the keys rotated when pos [T] and inv_freq are given; with q [T, NH, D] the
     same launch rotates the queries, which are returned."""
-    import torch
     T = k.shape[0]
     shape = (T, kv.NKV, kv.D)
     ks, vs = _heads(k, shape, "k"), _heads(v, shape, "v")
@@ -634,7 +631,6 @@ def kv_append(kv, k, v, pos=None, inv_freq=None, layout="half", mscale=1.0, q=No
 
 def kv_read(kv, T, k_out=None, v_out=None, stream=None):
     """The T rows of kv's sequences as fp32 (k, v) [T, NKV, D]."""
-    import torch
     shape = (T, kv.NKV, kv.D)
     if k_out is None:
         k_out = torch.empty(shape, dtype=torch.float32, device=kv.device)
@@ -662,7 +658,6 @@ def attn_forward(kv, q, scale, window=0, out=None, lse=None, want_lse=True, work
                  stream=None):
     """Softmax attention of q [T, NH, D] (kv's rows) over the 4-bit cache;
     returns (out [T, NH, D], lse [T, NH] or None)."""
-    import torch
     T, NH = q.shape[:2] if q.dim() == 3 else (0, 0)
     shape = (T, NH, kv.D)
     qs = _heads(q, shape, "q")
@@ -698,7 +693,6 @@ def token_logprobs(logits, targets=None, n_top=0, want_entropy=True, logprob=Non
     """From fp32 logits [T, V] (rows may be strided): (log probability of
     targets [T] int32, entropy [T], the n_top largest logits' ids int32 and log
     probabilities [T, n_top]); None where not asked for."""
-    import torch
     if logits.dtype is not torch.float32 or logits.dim() != 2 or \
             (logits.shape[1] != 1 and logits.stride(1) != 1):
         raise ValueError(f"logits: fp32 [T, V] with contiguous rows is needed, got {logits.dtype} "
