@@ -149,3 +149,22 @@ def test_no_sequences_still_rotates_queries():
     r = w4.kv_append(kv, dev(x), dev(x), pos=dev(pos), inv_freq=dev(f), q=dev(q))
     assert np.allclose(r.cpu().numpy(), ref.rotate(q, pos, f), atol=1e-6)
     assert torch.equal(kp, before)
+
+
+@pytest.mark.parametrize("layout,n", [("half", 128), ("half", 58), ("interleaved", 64), ("interleaved", 58)])
+@pytest.mark.parametrize("T", [1, 3, 1100])
+def test_queries_rotated_in_place(T, layout, n):
+    """q_out as q itself: the bits of a call with a buffer of its own, a row on
+    one workgroup and on several."""
+    NH, NKV, D = 24, 1, 128
+    g = synth.rng(T + n)
+    c = attn_cases.random_plan(g, [T], [T], NKV, D, "q4_0")
+    kv = attn_cases.on_gpu(c)
+    q, k, v = (dev(synth.normal_f32(g, (T, h, D))) for h in (NH, NKV, NKV))
+    pos, f = torch.arange(T, dtype=torch.int32, device="cuda"), w4.rope_frequencies(n)
+    want = w4.kv_append(kv, k, v, pos=pos, inv_freq=f, layout=layout, q=q)
+    assert torch.equal(want, w4.rope_rotate(q, pos, f, layout))
+    pages = [t.clone() for t in kv.tensors[:2]]
+    got = w4.kv_append(kv, k, v, pos=pos, inv_freq=f, layout=layout, q=q, q_out=q)
+    assert got.data_ptr() == q.data_ptr() and torch.equal(q, want)
+    assert all(torch.equal(a, b) for a, b in zip(pages, kv.tensors[:2]))
