@@ -100,7 +100,7 @@ __device__ __forceinline__ Stat wave_merge(Stat s) {
 // A wave's list of candidates (wave-uniform fields; buf in LDS, CAP entries).
 struct Top {
   u64 *buf;
-  u64 thr;        // a candidate has to be larger
+  u64 thr;        // a candidate has to be larger; 0, or n values met are
   float thrf;     // thr's value (-infinity before there is one)
   int n, count;
 
@@ -151,7 +151,9 @@ struct Top {
       if (e[k] && rank[k] < n) buf[rank[k]] = e[k];
     __builtin_amdgcn_wave_barrier();
     count = min(count, n);
-    if (count == n) set(buf[n - 1]);
+    // below the n-th, so that n values lie above it in a list filled anew too
+    // (no borrow from the value: an index is below 2^24, its part not 0)
+    if (count == n) set(buf[n - 1] - 1);
   }
   __device__ __forceinline__ void cut() {
     if (count <= 64) cut_of<1>();
