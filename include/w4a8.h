@@ -385,9 +385,11 @@ int kv_q4_read(const w4a8_kv *kv, float *k_out, float *v_out, int64_t T, void *s
  * amax / 127 taken as the binary32 product amax * fl(1/127)), so the block
  * dots are exact integers; the softmax and every sum are fp32, and each
  * probability times value scale enters the matrix cores as two fp16 halves
- * (about 22 bits).  A row that sees no key gives out 0 and lse -infinity.
- * Keys that a row does not see cannot change its result, whatever their
- * codes and scales hold.
+ * (about 22 bits; with the largest score's probability as 1, to no less than
+ * 2^-27 of the least value scale met, or 2^-39 of the row's largest such
+ * product).  A row that sees no key gives out 0 and lse -infinity.  Keys that
+ * a row does not see, or gives next to no probability, change its result by no
+ * more than that rounding, whatever their codes and scales hold.
  * Scores are to stay within fp32's range.
  *   q [T][NH][D] fp32 with row stride q_stride, out [T][NH][D], lse [T][NH]
  *   (NULL: not written).  One launch, or two (long sequences, few rows).

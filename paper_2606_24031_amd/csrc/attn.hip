@@ -25,9 +25,13 @@
 //            goes in as hi + lo, two fp16 halves (22 bits; one fp16 or bf16
 //            would be off by 2^-12 or 2^-9, more than everything else here
 //            together).  d_v is scaled by a power of two, kept per wave, to
-//            put the largest value scale met so far just below 2^15: halves
-//            neither overflow nor lose bits unless a key's scale lies 2^17
-//            and more below it.
+//            put the largest value scale met so far just below 2^15, so halves
+//            do not overflow; fp16's smallest step is then 2^-26 of any scale's
+//            as long as the scales lie within 2^13 of each other.  Where they
+//            do not, a key of a huge scale that a row does not see, or gives no
+//            probability, would push the row's other products off fp16's end:
+//            from that step on the wave takes each row's products by a power
+//            of two of the row's own (vexp WIDE).
 // Scores by keys and values by columns: a wave's sums are 32 columns, not D,
 // so registers leave room for two and more waves a SIMD, the code stays small
 // (a short decode is bound by fetching it once) and no sums are exchanged at
@@ -61,6 +65,9 @@ constexpr int AW = 4, AT = 64 * AW;   // waves of a workgroup; pages of a step
 constexpr int GROUP = 16;             // runs joined at a time
 constexpr int JT = 1024;              // threads of the joining kernel
 constexpr int SLOTS_MAX = 2 * TARGET; // most runs of split items
+// Value scales that a wave's two halves serve: from 2^-UNDER to 2^OVER times
+// the first step's largest.
+constexpr int UNDER = 8, OVER = 5, WIDE = 1 << 10;
 constexpr int64_t COUNTERS = (2 * SLOTS_MAX * 4 + 255) / 256 * 256;   // bytes before the partial results
 static_assert(SLOTS_MAX / GROUP / GROUP <= GROUP, "two levels of joins");
 
@@ -231,15 +238,22 @@ __device__ __forceinline__ float mul_zero(float x, float y) {
 
 __device__ __forceinline__ float exp2_f(float x) { return __builtin_amdgcn_exp2f(x); }
 
-// W = p d of four keys as the sum of two fp16 halves.  (0 times anything is 0:
-// a key that the row does not see may have any scale.)
-__device__ __forceinline__ void make_w(v4f p, const float *d, float minus, h4 &hi, h4 &lo) {
+// p d of four keys.  (0 times anything is 0: a key that the row does not see
+// may have any scale.)
+__device__ __forceinline__ v4f products(v4f p, const float *d) {
   const v4f dv = *reinterpret_cast<const v4f *>(d);
+  v4f w;
+#pragma unroll
+  for (int e = 0; e < 4; e++) w[e] = mul_zero(p[e], dv[e]);
+  return w;
+}
+// The same, W, as the sum of two fp16 halves.
+__device__ __forceinline__ void halves(v4f x, float minus, h4 &hi, h4 &lo) {
 #pragma unroll
   for (int e = 0; e < 4; e += 2) {
     v2f w, z;
-    w[0] = mul_zero(p[e], dv[e]);
-    w[1] = mul_zero(p[e + 1], dv[e + 1]);
+    w[0] = x[e];
+    w[1] = x[e + 1];
     const h2 y = __builtin_convertvector(w, h2);
     z[0] = fmaf((float)y[0], minus, w[0]);
     z[1] = fmaf((float)y[1], minus, w[1]);
@@ -247,6 +261,28 @@ __device__ __forceinline__ void make_w(v4f p, const float *d, float minus, h4 &h
     hi[e] = y[0]; hi[e + 1] = y[1];
     lo[e] = y2[0]; lo[e + 1] = y2[1];
   }
+}
+__device__ __forceinline__ void make_w(v4f p, const float *d, float minus, h4 &hi, h4 &lo) {
+  halves(products(p, d), minus, hi, lo);
+}
+__device__ __forceinline__ float max_finite(float m, v4f w) {
+#pragma unroll
+  for (int e = 0; e < 4; e++) {
+    const float y = fabsf(w[e]);
+    m = fmaxf(m, y < INFINITY ? y : 0.0f);
+  }
+  return m;
+}
+// Magnitudes in order, 0 above all others; that of 2^e, and e again.
+__device__ __forceinline__ uint32_t order_of(float x) {
+  return (__builtin_bit_cast(uint32_t, x) << 1) - 1;
+}
+__device__ __forceinline__ uint32_t limit_of(int e) { return ((uint32_t)(e + 127) << 24) - 1; }
+__device__ __forceinline__ int exponent_of(uint32_t limit) { return (int)(limit >> 24) - 126; }
+__device__ __forceinline__ v4f ldexp4(v4f x, int by) {
+#pragma unroll
+  for (int e = 0; e < 4; e++) x[e] = ldexpf(x[e], by);
+  return x;
 }
 __device__ __forceinline__ void put(h8 &v, int i, h4 x) {
 #pragma unroll
@@ -534,8 +570,11 @@ __global__ __launch_bounds__(AT, (NB * NT > 8 ? 2 : NT > 1 || NB > 4 ? 3 : 4)) v
 #pragma unroll
       for (int b = 0; b < BW; b++) acc[nt][b][0] = acc[nt][b][1] = v4f{0.f, 0.f, 0.f, 0.f};
     }
-    // value scales are below 2^vexp and enter the product times 2^(15 - vexp)
+    // value scales are below 2^vexp, none below `limit` (0: none so far), and
+    // enter the product times 2^(15 - vexp); once wide, scales and sums stand
+    // as they are
     int vexp = -126;
+    uint32_t limit = 0;
     sc_t *ks = lds.ks[wave];
     float *vs = lds.vs[wave];
     float minus = -1.0f;               // opaque, so that the halves' difference is one mixed FMA
@@ -544,6 +583,23 @@ __global__ __launch_bounds__(AT, (NB * NT > 8 ? 2 : NT > 1 || NB > 4 ? 3 : 4)) v
     uint32_t low4 = 0x000F000Fu, high4 = 0x00F000F0u, bias = 0x64006400u;
     asm("" : "+v"(low4), "+v"(high4), "+v"(bias));
     const v4i c0 = {0x4B400000, 0x4B400000, 0x4B400000, 0x4B400000};
+    // the value codes of 32 keys, of words 2 hh and + 1
+    const auto value_codes = [&](const v4u &word4, int hh, h8 (&c)[2]) {
+#pragma unroll
+      for (int i = 0; i < 2; i++) {
+        // a nibble n in an fp16 number's low bits: 1024 + n or 1024 + 16 n
+        const uint32_t y = word4[2 * hh + i], z = y >> 8;
+        const h2 off = {(_Float16)-1032.0f, (_Float16)-1032.0f};
+        const h2 six = {(_Float16)0.0625f, (_Float16)0.0625f};
+        const h2 off2 = {(_Float16)-72.0f, (_Float16)-72.0f};
+        const h2 a0 = __builtin_bit_cast(h2, (y & low4) | bias) + off;
+        const h2 a1 = __builtin_bit_cast(h2, (z & low4) | bias) + off;
+        const h2 b0 = __builtin_elementwise_fma(__builtin_bit_cast(h2, (y & high4) | bias), six, off2);
+        const h2 b1 = __builtin_elementwise_fma(__builtin_bit_cast(h2, (z & high4) | bias), six, off2);
+        c[0][4 * i] = a0[0]; c[0][4 * i + 1] = a0[1]; c[0][4 * i + 2] = a1[0]; c[0][4 * i + 3] = a1[1];
+        c[1][4 * i] = b0[0]; c[1][4 * i + 1] = b0[1]; c[1][4 * i + 2] = b1[0]; c[1][4 * i + 3] = b1[1];
+      }
+    };
     for (int at0 = plo; at0 < phi; at0 += AW) {
       const bool more = at0 + AW < phi;
       const int raw_next = raw_ids(at0 + AW);
@@ -628,6 +684,7 @@ __global__ __launch_bounds__(AT, (NB * NT > 8 ? 2 : NT > 1 || NB > 4 ? 3 : 4)) v
         const int vkey = (at0 + spg) * KV_PAGE + vtok;
         const bool vhere = __shfl(ids, spg) >= 0;
         float dv[NB], vmax = 0.0f;
+        uint32_t least = 0xFFFFFFFFu;
 #pragma unroll
         for (int i = 0; i < NB; i++) {
           dv[i] = scale_of<SYM>(vsr, i);
@@ -635,23 +692,29 @@ __global__ __launch_bounds__(AT, (NB * NT > 8 ? 2 : NT > 1 || NB > 4 ? 3 : 4)) v
           if (!vhere || kk > pos1 || kk < key0) dv[i] = 0.0f;
           const float y = fabsf(dv[i]);
           vmax = fmaxf(vmax, y < INFINITY ? y : 0.0f);
+          least = min(least, order_of(dv[i]));
         }
-        if (__ballot(vmax >= ldexpf(1.0f, vexp))) {
+        if (__ballot(vmax >= ldexpf(1.0f, vexp) || least < limit)) {
 #pragma unroll
           for (int o = 32; o > 0; o >>= 1) vmax = fmaxf(vmax, __shfl_xor(vmax, o));
-          const int e = __builtin_amdgcn_readfirstlane(ilogbf(vmax) + 1);
+          int to = max(vexp, __builtin_amdgcn_readfirstlane(ilogbf(vmax) + 1));
+          if (limit == 0) limit = limit_of(max(to - UNDER, -126));
+          if (to > exponent_of(limit) + UNDER + OVER || __ballot(least < limit)) {
+            to = WIDE;
+            limit = 0;
+          }
+          const int by = vexp - (to == WIDE ? 15 : to);
 #pragma unroll
           for (int nt = 0; nt < NT; nt++)
 #pragma unroll
             for (int b = 0; b < BW; b++)
 #pragma unroll
-              for (int s = 0; s < 2; s++)
-#pragma unroll
-                for (int y = 0; y < 4; y++) acc[nt][b][s][y] = ldexpf(acc[nt][b][s][y], vexp - e);
-          vexp = e;
+              for (int s = 0; s < 2; s++) acc[nt][b][s] = ldexp4(acc[nt][b][s], by);
+          vexp = to;
         }
+        const int up = vexp == WIDE ? 0 : 15 - vexp;
 #pragma unroll
-        for (int i = 0; i < NB; i++) vs[lane * NB + i] = ldexpf(dv[i], 15 - vexp);
+        for (int i = 0; i < NB; i++) vs[lane * NB + i] = ldexpf(dv[i], up);
       }
       const int next = checked(raw_next);
       const uint8_t *const kt = k_tile(next);
@@ -703,67 +766,118 @@ __global__ __launch_bounds__(AT, (NB * NT > 8 ? 2 : NT > 1 || NB > 4 ? 3 : 4)) v
       __syncthreads();
 
       // ---- values of the wave's columns
-#pragma unroll
-      for (int j = 0; j < NP; j++) {
-        const int pgj = sub * NP + j;
-        if (at0 + pgj < phi) {
+      if (vexp == WIDE) {
+        // each row's products by a power of two of their own, into sums as they
+        // are; codes read again, so that this stays a loop (and places found
+        // again, so that none holds a register outside).  1.3 to 1.6 times the
+        // time (48 rows over 6000 keys 79 us, 2 x 2048 over 8192 1316)
+        int ln = lane;
+        asm volatile("" : "+v"(ln));
+        const auto at = [&] { return (ln >> 4) * 16 + (PK > 1 ? (ln & 15) / ROWS * 4 : 0); };
+#pragma unroll 1
+        for (int j = 0; j < NP && at0 + sub * NP + j < phi; j++) {
+          const int pgj = sub * NP + j;
+          const int64_t page = max(__builtin_amdgcn_readlane(ids, pgj), 0);
 #pragma unroll
           for (int bb = 0; bb < BW; bb++) {
-            const int pc = j * BW + bb;
-            // W of the lane's keys, as two halves
-            h4 whi[NT][CH], wlo[NT][CH];
-            if (PK > 1) make_w(lds.p[pgj][0][lane], vs + pc * 64 + g * 16 + 4 * grp, minus, whi[0][0], wlo[0][0]);
-            if (PK == 2) make_w(lds.p[pgj][CH - 1][lane], vs + pc * 64 + g * 16 + 4 * grp + 8, minus, whi[0][CH - 1], wlo[0][CH - 1]);
+            const v4u y4 = reinterpret_cast<const v4u *>(a.p.v + page * stride + head + (blk + bb) * 1024)[ln];
+            const float *const d = vs + (j * BW + bb) * 64;
 #pragma unroll
-            for (int hh = 0; hh < 2; hh++) {         // 32 keys at a time
-              h8 c[2];                               // elements l % 16 and + 16
-#pragma unroll
-              for (int i = 0; i < 2; i++) {
-                // a nibble n in an fp16 number's low bits: 1024 + n or 1024 + 16 n
-                const uint32_t y = buf[pc][2 * hh + i], z = y >> 8;
-                const h2 off = {(_Float16)-1032.0f, (_Float16)-1032.0f};
-                const h2 six = {(_Float16)0.0625f, (_Float16)0.0625f};
-                const h2 off2 = {(_Float16)-72.0f, (_Float16)-72.0f};
-                const h2 a0 = __builtin_bit_cast(h2, (y & low4) | bias) + off;
-                const h2 a1 = __builtin_bit_cast(h2, (z & low4) | bias) + off;
-                const h2 b0 = __builtin_elementwise_fma(__builtin_bit_cast(h2, (y & high4) | bias), six, off2);
-                const h2 b1 = __builtin_elementwise_fma(__builtin_bit_cast(h2, (z & high4) | bias), six, off2);
-                c[0][4 * i] = a0[0]; c[0][4 * i + 1] = a0[1]; c[0][4 * i + 2] = a1[0]; c[0][4 * i + 3] = a1[1];
-                c[1][4 * i] = b0[0]; c[1][4 * i + 1] = b0[1]; c[1][4 * i + 2] = b1[0]; c[1][4 * i + 3] = b1[1];
-              }
+            for (int hh = 0; hh < 2; hh++) {
+              h8 c[2];
+              value_codes(y4, hh, c);
 #pragma unroll
               for (int nt = 0; nt < NT; nt++) {
+                constexpr int N = PK == 1 ? 2 : CH;
+                v4f w[N];
+                float most = 0.0f;
+#pragma unroll
+                for (int i = 0; i < N; i++) {
+                  w[i] = products(lds.p[pgj][4 * nt + (PK == 1 ? 2 * hh : 0) + i][ln],
+                                  d + at() + (PK == 1 ? 8 * hh : 0) + 4 * PK * i);
+                  most = max_finite(most, w[i]);
+                }
+                const int up = 15 - __builtin_amdgcn_frexp_expf(max_row<PK>(most));
+                h4 x[N], y[N];
+#pragma unroll
+                for (int i = 0; i < N; i++) halves(ldexp4(w[i], up), minus, x[i], y[i]);
                 h8 hi, lo;
-                if constexpr (PK == 1) {
 #pragma unroll
-                  for (int i = 0; i < 2; i++) {
-                    h4 x, y;
-                    make_w(lds.p[pgj][4 * nt + 2 * hh + i][lane], vs + pc * 64 + g * 16 + 8 * hh + 4 * i, minus, x, y);
-                    put(hi, i, x);
-                    put(lo, i, y);
-                  }
-                } else {
-#pragma unroll
-                  for (int i = 0; i < 2; i++) {        // key group 2 hh + i
-                    const int ch = (2 * hh + i) / PK, z = (2 * hh + i) % PK;
-                    put(hi, i, from_col<PK>(whi[0][ch], z));
-                    put(lo, i, from_col<PK>(wlo[0][ch], z));
+                for (int i = 0; i < 2; i++) {
+                  if constexpr (PK == 1) {
+                    put(hi, i, x[i]);
+                    put(lo, i, y[i]);
+                  } else {
+                    put(hi, i, from_col<PK>(x[(2 * hh + i) / PK], (2 * hh + i) % PK));
+                    put(lo, i, from_col<PK>(y[(2 * hh + i) / PK], (2 * hh + i) % PK));
                   }
                 }
 #pragma unroll
                 for (int s = 0; s < 2; s++) {
-                  acc[nt][bb][s] = __builtin_amdgcn_mfma_f32_16x16x32_f16(c[s], hi, acc[nt][bb][s], 0, 0, 0);
-                  acc[nt][bb][s] = __builtin_amdgcn_mfma_f32_16x16x32_f16(c[s], lo, acc[nt][bb][s], 0, 0, 0);
+                  v4f t = __builtin_amdgcn_mfma_f32_16x16x32_f16(c[s], hi, v4f{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
+                  t = __builtin_amdgcn_mfma_f32_16x16x32_f16(c[s], lo, t, 0, 0, 0);
+                  acc[nt][bb][s] += ldexp4(t, -up);
                 }
+                asm volatile("" : "+v"(acc[nt][bb][0]), "+v"(acc[nt][bb][1]), "+v"(ln));
               }
-#pragma unroll
-              for (int nt = 0; nt < NT; nt++) asm volatile("" : "+v"(acc[nt][bb][0]), "+v"(acc[nt][bb][1]));
             }
           }
         }
-        if (more) {
 #pragma unroll
-          for (int bb = 0; bb < BW; bb++) load_k(kt, j * BW + bb);
+        for (int b = 0; b < NB; b++) {
+          buf[b] = v4u{0, 0, 0, 0};
+          if (more) load_k(kt, b);
+        }
+      } else {
+#pragma unroll
+        for (int j = 0; j < NP; j++) {
+          const int pgj = sub * NP + j;
+          if (at0 + pgj < phi) {
+#pragma unroll
+            for (int bb = 0; bb < BW; bb++) {
+              const int pc = j * BW + bb;
+              // W of the lane's keys, as two halves
+              h4 whi[NT][CH], wlo[NT][CH];
+              if (PK > 1) make_w(lds.p[pgj][0][lane], vs + pc * 64 + g * 16 + 4 * grp, minus, whi[0][0], wlo[0][0]);
+              if (PK == 2) make_w(lds.p[pgj][CH - 1][lane], vs + pc * 64 + g * 16 + 4 * grp + 8, minus, whi[0][CH - 1], wlo[0][CH - 1]);
+#pragma unroll
+              for (int hh = 0; hh < 2; hh++) {         // 32 keys at a time
+                h8 c[2];                               // elements l % 16 and + 16
+                value_codes(buf[pc], hh, c);
+#pragma unroll
+                for (int nt = 0; nt < NT; nt++) {
+                  h8 hi, lo;
+                  if constexpr (PK == 1) {
+#pragma unroll
+                    for (int i = 0; i < 2; i++) {
+                      h4 x, y;
+                      make_w(lds.p[pgj][4 * nt + 2 * hh + i][lane], vs + pc * 64 + g * 16 + 8 * hh + 4 * i, minus, x, y);
+                      put(hi, i, x);
+                      put(lo, i, y);
+                    }
+                  } else {
+#pragma unroll
+                    for (int i = 0; i < 2; i++) {        // key group 2 hh + i
+                      const int ch = (2 * hh + i) / PK, z = (2 * hh + i) % PK;
+                      put(hi, i, from_col<PK>(whi[0][ch], z));
+                      put(lo, i, from_col<PK>(wlo[0][ch], z));
+                    }
+                  }
+#pragma unroll
+                  for (int s = 0; s < 2; s++) {
+                    acc[nt][bb][s] = __builtin_amdgcn_mfma_f32_16x16x32_f16(c[s], hi, acc[nt][bb][s], 0, 0, 0);
+                    acc[nt][bb][s] = __builtin_amdgcn_mfma_f32_16x16x32_f16(c[s], lo, acc[nt][bb][s], 0, 0, 0);
+                  }
+                }
+#pragma unroll
+                for (int nt = 0; nt < NT; nt++) asm volatile("" : "+v"(acc[nt][bb][0]), "+v"(acc[nt][bb][1]));
+              }
+            }
+          }
+          if (more) {
+#pragma unroll
+            for (int bb = 0; bb < BW; bb++) load_k(kt, j * BW + bb);
+          }
         }
       }
       ids = next;
@@ -780,7 +894,7 @@ __global__ __launch_bounds__(AT, (NB * NT > 8 ? 2 : NT > 1 || NB > 4 ? 3 : 4)) v
         for (int s = 0; s < 2; s++)
 #pragma unroll
           for (int y = 0; y < 4; y++)
-            acc[nt][b][s][y] = ldexpf(acc[nt][b][s][y], vexp - 15);
+            acc[nt][b][s][y] = ldexpf(acc[nt][b][s][y], vexp == WIDE ? 0 : vexp - 15);
     }
     if constexpr (PS > 1) {
       __syncthreads();                 // the last step's probabilities have been read
