@@ -390,7 +390,8 @@ int kv_q4_read(const w4a8_kv *kv, float *k_out, float *v_out, int64_t T, void *s
  * product).  A row that sees no key gives out 0 and lse -infinity.  Keys that
  * a row does not see, or gives next to no probability, change its result by no
  * more than that rounding, whatever their codes and scales hold.
- * Scores are to stay within fp32's range.
+ * Twice the scores, and 16 times what they are before `scale`, are to stay
+ * within fp32's range.
  *   q [T][NH][D] fp32 with row stride q_stride, out [T][NH][D], lse [T][NH]
  *   (NULL: not written).  One launch, or two (long sequences, few rows).
  *   workspace >= attn_q4_workspace_size bytes, zero-filled before its first

@@ -68,6 +68,7 @@ constexpr int SLOTS_MAX = 2 * TARGET; // most runs of split items
 // Value scales that a wave's two halves serve: from 2^-UNDER to 2^OVER times
 // the first step's largest.
 constexpr int UNDER = 8, OVER = 5, WIDE = 1 << 10;
+constexpr float FAR = 4194304.0f;     // 2^22: half a unit in the last place is 2^-3 below it
 constexpr int64_t COUNTERS = (2 * SLOTS_MAX * 4 + 255) / 256 * 256;   // bytes before the partial results
 static_assert(SLOTS_MAX / GROUP / GROUP <= GROUP, "two levels of joins");
 
@@ -575,6 +576,7 @@ __global__ __launch_bounds__(AT, (NB * NT > 8 ? 2 : NT > 1 || NB > 4 ? 3 : 4)) v
     // as they are
     int vexp = -126;
     uint32_t limit = 0;
+    bool far = false;                  // some row's maximum is FAR from 0
     sc_t *ks = lds.ks[wave];
     float *vs = lds.vs[wave];
     float minus = -1.0f;               // opaque, so that the halves' difference is one mixed FMA
@@ -734,6 +736,7 @@ __global__ __launch_bounds__(AT, (NB * NT > 8 ? 2 : NT > 1 || NB > 4 ? 3 : 4)) v
         grow |= mn[nt] > m[nt];
       }
       if (__ballot(grow)) {
+        bool f = false;
 #pragma unroll
         for (int nt = 0; nt < NT; nt++) {
           // (a row without keys so far has no product to take: it could overflow)
@@ -741,12 +744,28 @@ __global__ __launch_bounds__(AT, (NB * NT > 8 ? 2 : NT > 1 || NB > 4 ? 3 : 4)) v
           const float al = m[nt] == -FLT_MAX ? 0.0f : exp2_f(mk[nt] - mkn);
           m[nt] = mn[nt];
           mk[nt] = mkn;
+          f |= fabsf(mkn) >= FAR && mkn != -FLT_MAX;
           l[nt] *= al;
 #pragma unroll
           for (int b = 0; b < BW; b++) {
             acc[nt][b][0] *= al;
             acc[nt][b][1] *= al;
           }
+        }
+        far = __ballot(f) != 0;
+      }
+      // Below FAR the product's rounding in mk makes the largest probability
+      // 2^(1/8) at most, in sums and halves alike; from there on scores are taken
+      // less the maximum first, so that it is 1.
+      float ref[NT];
+#pragma unroll
+      for (int nt = 0; nt < NT; nt++) ref[nt] = mk[nt];
+      if (far) {
+#pragma unroll
+        for (int nt = 0; nt < NT; nt++) {
+          ref[nt] = 0.0f;
+#pragma unroll
+          for (int i = 0; i < 4 * CH; i++) S[nt][i] -= m[nt];
         }
       }
       // ---- probabilities (a masked score's is exp2(-infinity) = 0)
@@ -757,7 +776,7 @@ __global__ __launch_bounds__(AT, (NB * NT > 8 ? 2 : NT > 1 || NB > 4 ? 3 : 4)) v
         for (int c = 0; c < CH; c++) {
           v4f p;
 #pragma unroll
-          for (int e = 0; e < 4; e++) p[e] = exp2_f(fmaf(S[nt][4 * c + e], a.k, -mk[nt]));
+          for (int e = 0; e < 4; e++) p[e] = exp2_f(fmaf(S[nt][4 * c + e], a.k, -ref[nt]));
           lds.p[wave][CH * nt + c][lane] = p;
           s += p;
         }
