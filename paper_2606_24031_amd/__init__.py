@@ -489,6 +489,15 @@ def _ptr(t):
     return None if t is None else t.data_ptr()
 
 
+def _empty(shape, dtype, device, stream):
+    """A call's own output, of the memory of the stream that writes it: the
+    current stream's pending work may still use what it has freed."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
 def _zeros(n, device, stream=None):
     """A workspace, zero-filled and held on the stream that uses it."""
     with torch.cuda.stream(stream):
@@ -537,7 +546,7 @@ def rope_frequencies(n_rot, base=10000.0, kind="none", factor=1.0, orig_len=0, b
     if kind not in ROPE_KINDS:
         raise ValueError(f"kind {kind!r}: one of {sorted(ROPE_KINDS)}")
     if out is None:
-        out = torch.empty(max(0, n_rot // 2), dtype=torch.float64, device=device)
+        out = _empty(max(0, n_rot // 2), torch.float64, device, stream)
     _is(out, torch.float64, (n_rot // 2,), "out")
     _call("rope_frequencies", stream, (out,), _ptr(out), n_rot, base, ROPE_KINDS[kind], factor,
           orig_len, beta_fast, beta_slow)
@@ -552,7 +561,7 @@ def rope_rotate(x, pos, inv_freq, layout="half", mscale=1.0, out=None, stream=No
     T, NH, D = shape
     r = _rope(pos, inv_freq, layout, mscale, T)
     if out is None:
-        out = torch.empty(shape, dtype=torch.float32, device=x.device)
+        out = _empty(shape, torch.float32, x.device, stream)
     os_ = _heads(out, shape, "out")
     if T:
         _call("rope_rotate", stream, (x, pos, inv_freq, out), ctypes.byref(r), x.data_ptr(), xs,
@@ -618,7 +627,7 @@ def kv_append(kv, k, v, pos=None, inv_freq=None, layout="half", mscale=1.0, q=No
         shape = (T, NH, kv.D)
         qs = _heads(q, shape, "q")
         if q_out is None:
-            q_out = torch.empty(shape, dtype=torch.float32, device=q.device)
+            q_out = _empty(shape, torch.float32, q.device, stream)
         _is(q_out, torch.float32, shape, "q_out")
     else:
         q_out = None
@@ -633,9 +642,9 @@ def kv_read(kv, T, k_out=None, v_out=None, stream=None):
     """The T rows of kv's sequences as fp32 (k, v) [T, NKV, D]."""
     shape = (T, kv.NKV, kv.D)
     if k_out is None:
-        k_out = torch.empty(shape, dtype=torch.float32, device=kv.device)
+        k_out = _empty(shape, torch.float32, kv.device, stream)
     if v_out is None:
-        v_out = torch.empty(shape, dtype=torch.float32, device=kv.device)
+        v_out = _empty(shape, torch.float32, kv.device, stream)
     _is(k_out, torch.float32, shape, "k_out")
     _is(v_out, torch.float32, shape, "v_out")
     if T:
@@ -662,10 +671,10 @@ def attn_forward(kv, q, scale, window=0, out=None, lse=None, want_lse=True, work
     shape = (T, NH, kv.D)
     qs = _heads(q, shape, "q")
     if out is None:
-        out = torch.empty(shape, dtype=torch.float32, device=q.device)
+        out = _empty(shape, torch.float32, q.device, stream)
     _is(out, torch.float32, shape, "out")
     if lse is None and want_lse:
-        lse = torch.empty((T, NH), dtype=torch.float32, device=q.device)
+        lse = _empty((T, NH), torch.float32, q.device, stream)
     if lse is not None:
         _is(lse, torch.float32, (T, NH), "lse")
     if T:
@@ -701,7 +710,8 @@ def token_logprobs(logits, targets=None, n_top=0, want_entropy=True, logprob=Non
     stride = logits.stride(0)
     if T == 1 and stride < V:
         stride = V
-    new = logits.new_empty
+    new = logits.new_empty if stream is None else \
+        lambda shape, dtype=torch.float32: _empty(shape, dtype, logits.device, stream)
     if targets is not None:
         _is(targets, torch.int32, (T,), "targets")
         if logprob is None:
