@@ -157,6 +157,15 @@ def _stream(stream):
     return ctypes.c_void_p(s.cuda_stream)
 
 
+def _empty(shape, dtype, device, stream):
+    """A call's own output, of the memory of the stream that writes it: the
+    current stream's pending work may still use what it has freed."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
 def _p(t):
     return None if t is None else ctypes.c_void_p(t.data_ptr())
 
@@ -174,7 +183,7 @@ def q8_0_quantize(x, out=None, stream=None):
     assert x.dtype == torch.float32 and x.is_contiguous()
     rows, K = (1, x.numel()) if x.dim() == 1 else (x.numel() // x.shape[-1], x.shape[-1])
     if out is None:
-        out = torch.empty((rows, K // 32 * Q8_0_BLOCK_BYTES), dtype=torch.uint8, device=x.device)
+        out = _empty((rows, K // 32 * Q8_0_BLOCK_BYTES), torch.uint8, x.device, stream)
     _check(lib().q8_0_quantize(_p(x), _p(_u8(out)), rows, K, _stream(stream)), "q8_0_quantize")
     return out
 
@@ -185,7 +194,7 @@ def q4_0_quantize(w, out=None, stream=None):
     assert w.dtype == torch.float32 and w.is_contiguous()
     rows, K = (1, w.numel()) if w.dim() == 1 else (w.numel() // w.shape[-1], w.shape[-1])
     if out is None:
-        out = torch.empty((rows, K // 32 * Q4_0_BLOCK_BYTES), dtype=torch.uint8, device=w.device)
+        out = _empty((rows, K // 32 * Q4_0_BLOCK_BYTES), torch.uint8, w.device, stream)
     _check(lib().q4_0_quantize(_p(w), _p(_u8(out)), rows, K, _stream(stream)), "q4_0_quantize")
     return out
 
@@ -194,27 +203,27 @@ def q4q8_gemv(w, xq, N, K, y=None, stream=None):
     """y[N] = W4A8(w [N, K/32 Q4_0 blocks], xq [K/32 Q8_0 blocks]) in fp32."""
     import torch
     if y is None:
-        y = torch.empty(N, dtype=torch.float32, device=w.device)
+        y = _empty(N, torch.float32, w.device, stream)
     _check(lib().q4q8_gemv(_p(_u8(w)), _p(_u8(xq)), _p(y), N, K, _stream(stream)), "q4q8_gemv")
     return y
 
 
-def gemm_workspace(M, K, device="cuda"):
+def gemm_workspace(M, K, device="cuda", stream=None):
     """A workspace for q4q8_gemm with M activation rows of length K."""
     import torch
     n = int(lib().q4q8_gemm_workspace_size(M, K))
     if n == 0:
         raise W4A8Error(ESHAPE, "q4q8_gemm_workspace_size")
-    return torch.empty(n, dtype=torch.uint8, device=device)
+    return _empty(n, torch.uint8, device, stream)
 
 
 def q4q8_gemm(w, xq, M, N, K, y=None, workspace=None, stream=None):
     """y[M, N] = W4A8(xq [M, K/32 Q8_0 blocks], w [N, K/32 Q4_0 blocks]) in fp32."""
     import torch
     if y is None:
-        y = torch.empty((M, N), dtype=torch.float32, device=w.device)
+        y = _empty((M, N), torch.float32, w.device, stream)
     if workspace is None and M > 1:
-        workspace = gemm_workspace(M, K, device=w.device)
+        workspace = gemm_workspace(M, K, w.device, stream)
     nbytes = 0 if workspace is None else workspace.numel()
     _check(lib().q4q8_gemm(_p(_u8(w)), _p(_u8(xq)), _p(y), M, N, K, _p(workspace), nbytes,
                            _stream(stream)), "q4q8_gemm")
@@ -246,7 +255,7 @@ def moe_sym_forward(hidden, topk_ids, topk_w, w_gate_up, w_down, ws_gate_up, ws_
     assert topk_ids.dtype == torch.int32 and topk_ids.is_contiguous()
     assert topk_w.dtype == torch.float32 and topk_w.is_contiguous()
     if out is None:
-        out = torch.empty((T, H), dtype=torch.float32, device=hidden.device)
+        out = _empty((T, H), torch.float32, hidden.device, stream)
     rc = lib().moe_sym_forward(_p(hidden), _p(topk_ids), _p(topk_w), _p(_u8(w_gate_up)),
                                _p(_u8(w_down)), _p(ws_gate_up), _p(ws_down), _p(out),
                                T, H, I, E, k, _p(workspace), workspace.numel(), _stream(stream))
@@ -264,14 +273,14 @@ def gdn_scan(q, k, v, g, beta, s0=None, out=None, s_out=None, workspace=None, st
     for t in (q, k, v, g, beta, s0):
         assert t is None or (t.dtype == torch.float32 and t.is_contiguous())
     if out is None:
-        out = torch.empty((T, NH, DV), dtype=torch.float32, device=k.device)
+        out = _empty((T, NH, DV), torch.float32, k.device, stream)
     if s_out is None:
-        s_out = torch.empty((NH, DK, DV), dtype=torch.float32, device=k.device)
+        s_out = _empty((NH, DK, DV), torch.float32, k.device, stream)
     if workspace is None:
         n = int(lib().gdn_workspace_size(T, NH, DK, DV))
         if n == 0:
             raise W4A8Error(ESHAPE, "gdn_workspace_size")
-        workspace = torch.empty(n, dtype=torch.uint8, device=k.device)
+        workspace = _empty(n, torch.uint8, k.device, stream)
     _check(lib().gdn_chunked_scan(_p(q), _p(k), _p(v), _p(g), _p(beta), _p(s0), _p(out),
                                   _p(s_out), T, NH, DK, DV, _p(workspace), workspace.numel(),
                                   _stream(stream)), "gdn_chunked_scan")
@@ -285,7 +294,7 @@ def q4_sym_quantize(w, out=None, stream=None):
     assert w.dtype == torch.float32 and w.is_contiguous()
     rows, K = (1, w.numel()) if w.dim() == 1 else (w.numel() // w.shape[-1], w.shape[-1])
     if out is None:
-        out = torch.empty((rows, K // 32 * Q4_SYM_BLOCK_BYTES), dtype=torch.uint8, device=w.device)
+        out = _empty((rows, K // 32 * Q4_SYM_BLOCK_BYTES), torch.uint8, w.device, stream)
     _check(lib().q4_sym_quantize(_p(w), _p(_u8(out)), rows, K, _stream(stream)), "q4_sym_quantize")
     return out
 
@@ -297,7 +306,7 @@ def q8_f32_quantize(x, out=None, stream=None):
     assert x.dtype == torch.float32 and x.is_contiguous()
     rows, K = (1, x.numel()) if x.dim() == 1 else (x.numel() // x.shape[-1], x.shape[-1])
     if out is None:
-        out = torch.empty((rows, K // 32 * Q8_F32_BLOCK_BYTES), dtype=torch.uint8, device=x.device)
+        out = _empty((rows, K // 32 * Q8_F32_BLOCK_BYTES), torch.uint8, x.device, stream)
     _check(lib().q8_f32_quantize(_p(x), _p(_u8(out)), rows, K, _stream(stream)), "q8_f32_quantize")
     return out
 
@@ -306,7 +315,7 @@ def q4sym_q8f32_gemv(w, xq, N, K, y=None, stream=None):
     """y[N] = product of w [N, K/32 Q4_SYM blocks] and xq [K/32 Q8_F32 blocks]."""
     import torch
     if y is None:
-        y = torch.empty(N, dtype=torch.float32, device=w.device)
+        y = _empty(N, torch.float32, w.device, stream)
     _check(lib().q4sym_q8f32_gemv(_p(_u8(w)), _p(_u8(xq)), _p(y), N, K, _stream(stream)),
            "q4sym_q8f32_gemv")
     return y
@@ -320,9 +329,9 @@ def router_topk(logits, k, ids=None, weights=None, stream=None):
     assert logits.dtype == torch.float32 and logits.is_contiguous() and logits.dim() == 2
     T, E = logits.shape
     if ids is None:
-        ids = torch.empty((T, k), dtype=torch.int32, device=logits.device)
+        ids = _empty((T, k), torch.int32, logits.device, stream)
     if weights is None:
-        weights = torch.empty((T, k), dtype=torch.float32, device=logits.device)
+        weights = _empty((T, k), torch.float32, logits.device, stream)
     _check(lib().moe_router_topk(_p(logits), _p(ids), _p(weights), T, E, k, _stream(stream)),
            "moe_router_topk")
     return ids, weights
@@ -338,7 +347,7 @@ def moe_workspace(T, H, I, E, k, device="cuda", stream=None):
     n = moe_workspace_size(T, H, I, E, k)
     if n == 0:
         raise W4A8Error(ESHAPE, "moe_workspace_size")
-    ws = torch.empty(n, dtype=torch.uint8, device=device)
+    ws = _empty(n, torch.uint8, device, stream)
     _check(lib().moe_w4a8_workspace_init(_p(ws), n, _stream(stream)), "moe_w4a8_workspace_init")
     return ws
 
@@ -360,7 +369,7 @@ def moe_forward(hidden, topk_ids, topk_w, w_gate_up, w_down, ws_gate_up, ws_down
     assert topk_ids.dtype == torch.int32 and topk_ids.is_contiguous()
     assert topk_w.dtype == torch.float32 and topk_w.is_contiguous()
     if out is None:
-        out = torch.empty((T, H), dtype=torch.float32, device=hidden.device)
+        out = _empty((T, H), torch.float32, hidden.device, stream)
     rc = lib().moe_w4a8_forward(_p(hidden), _p(topk_ids), _p(topk_w), _p(_u8(w_gate_up)),
                                 _p(_u8(w_down)), _p(ws_gate_up), _p(ws_down), _p(out),
                                 T, H, I, E, k, _p(workspace), workspace.numel(),
@@ -377,9 +386,9 @@ def rmsnorm_residual(x, y, gamma, eps=1e-6, x_out=None, xn=None, want_norm=True,
     for t in (x, y, gamma):
         assert t is None or (t.dtype == torch.float32 and t.is_contiguous())
     if x_out is None:
-        x_out = torch.empty_like(x)
+        x_out = _empty(x.shape, x.dtype, x.device, stream)
     if want_norm and xn is None:
-        xn = torch.empty_like(x)
+        xn = _empty(x.shape, x.dtype, x.device, stream)
     rc = lib().rmsnorm_residual(_p(x), _p(y), _p(gamma if want_norm else None), _p(x_out),
                                 _p(xn if want_norm else None), T, H, float(eps), _stream(stream))
     _check(rc, "rmsnorm_residual")
@@ -396,9 +405,9 @@ def moe_layer(x, y_prev, gamma, topk_ids, topk_w, w_gate_up, w_down, ws_gate_up,
         assert t is None or (t.dtype == torch.float32 and t.is_contiguous())
     assert topk_ids.dtype == torch.int32 and topk_ids.is_contiguous()
     if x_out is None:
-        x_out = torch.empty_like(x)
+        x_out = _empty(x.shape, x.dtype, x.device, stream)
     if out is None:
-        out = torch.empty_like(x)
+        out = _empty(x.shape, x.dtype, x.device, stream)
     rc = lib().moe_w4a8_layer(_p(x), _p(y_prev), _p(gamma), float(eps), _p(x_out), _p(topk_ids),
                               _p(topk_w), _p(_u8(w_gate_up)), _p(_u8(w_down)), _p(ws_gate_up),
                               _p(ws_down), _p(out), T, H, I, E, k, _p(workspace),
@@ -418,13 +427,13 @@ def moe_layer_routed(x, y_prev, gamma, router_logits, w_gate_up, w_down, ws_gate
     for t in (x, y_prev, gamma, router_logits, shared_gate):
         assert t is None or (t.dtype == torch.float32 and t.is_contiguous())
     if x_out is None:
-        x_out = torch.empty_like(x)
+        x_out = _empty(x.shape, x.dtype, x.device, stream)
     if out is None:
-        out = torch.empty_like(x)
+        out = _empty(x.shape, x.dtype, x.device, stream)
     if topk_ids is None:
-        topk_ids = torch.empty((T, k), dtype=torch.int32, device=x.device)
+        topk_ids = _empty((T, k), torch.int32, x.device, stream)
     if topk_w is None:
-        topk_w = torch.empty((T, k), dtype=torch.float32, device=x.device)
+        topk_w = _empty((T, k), torch.float32, x.device, stream)
     rc = lib().moe_w4a8_layer_routed(_p(x), _p(y_prev), _p(gamma), float(eps), _p(x_out),
                                      _p(router_logits), _p(shared_gate), _p(_u8(w_gate_up)),
                                      _p(_u8(w_down)), _p(ws_gate_up), _p(ws_down), _p(out),
@@ -451,7 +460,7 @@ def moe_forward_noalloc(hidden, topk_ids, topk_w, w_gate_up, w_down, ws_gate_up,
     assert topk_ids.dtype == torch.int32 and topk_ids.is_contiguous()
     assert topk_w.dtype == torch.float32 and topk_w.is_contiguous()
     if out is None:
-        out = torch.empty((T, H), dtype=torch.float32, device=hidden.device)
+        out = _empty((T, H), torch.float32, hidden.device, stream)
     rc = lib().moe_w4a8_forward_noalloc(_p(hidden), _p(topk_ids), _p(topk_w), _p(_u8(w_gate_up)),
                                         _p(_u8(w_down)), _p(ws_gate_up), _p(ws_down), _p(out),
                                         T, H, I, E, k, _stream(stream))
@@ -487,15 +496,6 @@ def _call(what, stream, tensors, *args):
 
 def _ptr(t):
     return None if t is None else t.data_ptr()
-
-
-def _empty(shape, dtype, device, stream):
-    """A call's own output, of the memory of the stream that writes it: the
-    current stream's pending work may still use what it has freed."""
-    if stream is None:
-        return torch.empty(shape, dtype=dtype, device=device)
-    with torch.cuda.stream(stream):
-        return torch.empty(shape, dtype=dtype, device=device)
 
 
 def _zeros(n, device, stream=None):
