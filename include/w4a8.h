@@ -313,7 +313,8 @@ int rope_rotate(const w4a8_rope *rope, const float *x, int64_t x_stride, float *
  *   kv_len     [B] int32: tokens of each sequence, this call's included;
  *   cu_rows    [B + 1] int32, not decreasing: sequence s has the rows
  *              cu_rows[s] .. cu_rows[s+1] - 1 of this call, its last tokens:
- *              row r is token kv_len[s] - (cu_rows[s+1] - r).
+ *              row r is token kv_len[s] - (cu_rows[s+1] - r).  cu_rows[B] may
+ *              lie past the T of a call, which then has the first T rows.
  * The arrays are read on the device and may change between replays of a
  * captured graph.  Tokens before 0 or past max_pages * W4A8_KV_PAGE do not
  * exist; rows outside every sequence are left as they were.  Two sequences

@@ -99,7 +99,7 @@ struct AttnArgs {
 // What a sequence asks for.
 struct Seq {
   int64_t r0;       // its first row
-  int qlen, len;    // rows, tokens (as given)
+  int qlen, pos;    // rows, the first one's token
   int lo, pages;    // first page any row sees, pages from there on
   int tiles;
 };
@@ -107,13 +107,15 @@ struct Seq {
 template <int RT_>
 __device__ __forceinline__ Seq seq_of(const AttnArgs &a, int s) {
   Seq r;
-  const int64_t r0 = kv_clamp_row(a.p.cu[s], a.T), r1 = kv_clamp_row(a.p.cu[s + 1], a.T);
+  const int c1 = a.p.cu[s + 1];
+  const int64_t r0 = kv_clamp_row(a.p.cu[s], a.T), r1 = kv_clamp_row(c1, a.T);
   r.r0 = r0;
   r.qlen = r1 > r0 ? (int)(r1 - r0) : 0;
-  r.len = a.p.len[s];
-  const int64_t hi = min((int64_t)r.len, (int64_t)a.p.max_pages * KV_PAGE);
+  // (no call has the 2^30 rows that would lead from below to token 0)
+  r.pos = (int)max((int64_t)a.p.len[s] - (c1 - r0), -((int64_t)1 << 30));
+  const int64_t hi = min((int64_t)r.pos + r.qlen, (int64_t)a.p.max_pages * KV_PAGE);
   int64_t lo = 0;
-  if (a.window > 0) lo = max((int64_t)0, (int64_t)r.len - r.qlen - a.window + 1);
+  if (a.window > 0) lo = max((int64_t)0, (int64_t)r.pos - a.window + 1);
   r.lo = (int)(lo / KV_PAGE);
   const int64_t end = (hi + KV_PAGE - 1) / KV_PAGE;
   r.pages = r.qlen > 0 && hi > 0 && end > r.lo ? (int)(end - r.lo) : 0;
@@ -470,8 +472,7 @@ __global__ __launch_bounds__(AT, (NB * NT > 8 ? 2 : NT > 1 || NB > 4 ? 3 : 4)) v
     const int tl = it / a.p.NKV, h = it - tl * a.p.NKV, tile = sq.tiles - 1 - tl;  // longest first
     const int f0 = tile * ROWS, fn = min(ROWS, sq.qlen * a.G - f0);  // rows of the tile
     const RowMap rm(a, f0);
-    const int base_pos = sq.len - sq.qlen;
-    const int pos0 = base_pos + rm.token(0), pos1 = base_pos + rm.token(fn - 1);
+    const int pos0 = sq.pos + rm.token(0), pos1 = sq.pos + rm.token(fn - 1);
     // the tile's pages within this run
     int64_t key0 = 0;
     if (a.window > 0) key0 = max((int64_t)0, (int64_t)pos0 - a.window + 1);
@@ -554,7 +555,7 @@ __global__ __launch_bounds__(AT, (NB * NT > 8 ? 2 : NT > 1 || NB > 4 ? 3 : 4)) v
     int hi_key[NT], lo_key[NT];
 #pragma unroll
     for (int nt = 0; nt < NT; nt++) {
-      const int pos = base_pos + rm.token(min(16 * nt + (PK > 1 ? col % ROWS : col), fn - 1));
+      const int pos = sq.pos + rm.token(min(16 * nt + (PK > 1 ? col % ROWS : col), fn - 1));
       hi_key[nt] = pos - kbase;
       lo_key[nt] = (a.window > 0 && a.window <= pos ? (int)(pos - a.window) : -1) - kbase;
     }

@@ -109,7 +109,9 @@ __device__ __forceinline__ int kv_find(const KvPlan &p, int64_t T, int64_t r, in
   const int64_t r0 = kv_clamp_row(__builtin_amdgcn_readlane(c0, k), T);
   const int64_t r1 = kv_clamp_row(__builtin_amdgcn_readlane(c1, k), T);
   if (r < r0 || r >= r1) return -1;
-  const int64_t t = (int64_t)__builtin_amdgcn_readlane(len, k) - (r1 - r);
+  // counted from the sequence's own end, which may lie past the call's rows
+  const int64_t t = (int64_t)__builtin_amdgcn_readlane(len, k) -
+                    ((int64_t)__builtin_amdgcn_readlane(c1, k) - r);
   token = t < 0 || t >= (int64_t)p.max_pages * KV_PAGE ? -1 : (int)t;
   return lo + k;
 }
