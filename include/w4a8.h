@@ -315,6 +315,8 @@ int rope_rotate(const w4a8_rope *rope, const float *x, int64_t x_stride, float *
  *              cu_rows[s] .. cu_rows[s+1] - 1 of this call, its last tokens:
  *              row r is token kv_len[s] - (cu_rows[s+1] - r).  cu_rows[B] may
  *              lie past the T of a call, which then has the first T rows.
+ *              Where they decrease attention writes nothing, and which rows
+ *              are stored or read is open.
  * The arrays are read on the device and may change between replays of a
  * captured graph.  Tokens before 0 or past max_pages * W4A8_KV_PAGE do not
  * exist; rows outside every sequence are left as they were.  Two sequences
@@ -399,7 +401,10 @@ int kv_q4_read(const w4a8_kv *kv, float *k_out, float *v_out, int64_t T, void *s
  *   use (moe_w4a8_workspace_init does that); each call leaves it ready for
  *   later ones of this entry point of any sizes it suffices for.  Other entry
  *   points would leave it in another state, and calls that overlap in time
- *   would mix their results: neither may share it.  The result does not depend
+ *   would mix their results: neither may share it.  (It holds counts that are
+ *   0 between calls.  Where they are not, this call and later ones join too
+ *   early or never, and rows of long sequences are wrong or not written, until
+ *   it is zero-filled again.)  The result does not depend
  *   on timing, and a sequence's does not on the values of the others'.
  * Errors beside the plan's: NH < 1, NH % NKV != 0, T < 0, window < 0,
  * q_stride < NH * D or not a multiple of 4, scale not finite -> W4A8_ESHAPE;
@@ -435,7 +440,8 @@ int attn_q4_forward(const w4a8_kv *kv, const float *q, int64_t q_stride, float *
  *   (moe_w4a8_workspace_init does that); each call leaves it ready for later
  *   ones of this entry point of any sizes it suffices for.  As for
  *   attn_q4_forward, neither other entry points nor calls that overlap in time
- *   may share it.
+ *   may share it, and one with other contents makes rows wrong or unwritten
+ *   until it is zero-filled again.
  * Errors: T < 0, V < 1, stride < V -> W4A8_ESHAPE; V >= 2^24, T >= 2^31,
  * n_top < 0, n_top > 32, n_top > V, T * stride >= 2^40 -> W4A8_ERANGE; logits,
  * only one of a pair, or the workspace NULL -> W4A8_ENULL; logits or the

@@ -102,13 +102,15 @@ struct Seq {
   int qlen, pos;    // rows, the first one's token
   int lo, pages;    // first page any row sees, pages from there on
   int tiles;
+  bool falls;       // cu_rows decrease here
 };
 
 template <int RT_>
 __device__ __forceinline__ Seq seq_of(const AttnArgs &a, int s) {
   Seq r;
-  const int c1 = a.p.cu[s + 1];
-  const int64_t r0 = kv_clamp_row(a.p.cu[s], a.T), r1 = kv_clamp_row(c1, a.T);
+  const int c0 = a.p.cu[s], c1 = a.p.cu[s + 1];
+  const int64_t r0 = kv_clamp_row(c0, a.T), r1 = kv_clamp_row(c1, a.T);
+  r.falls = c1 < c0;
   r.r0 = r0;
   r.qlen = r1 > r0 ? (int)(r1 - r0) : 0;
   // (no call has the 2^30 rows that would lead from below to token 0)
@@ -143,7 +145,10 @@ template <typename T_> __device__ __forceinline__ T_ wave_scan(T_ x) {
 // partial slot of the sequence's runs.  A sequence's items fall into runs of
 // at most C pages, C such that the call has about TARGET runs (of several
 // tiles, whose first see half the pages of the last on average, only from 2 C
-// on).  SPLIT: item `id` of those with several runs.  False past the end.
+// on).  SPLIT: item `id` of those with several runs.  False past the end, and
+// for every id where cu_rows decrease: sequences' rows could then number more
+// than T, and runs more than the call has, so that some would never arrive at
+// their counter and leave it for later calls.
 struct Found {
   int s, local, runs, slot0;
 };
@@ -151,6 +156,7 @@ template <int RT_, bool SPLIT = false>
 __device__ __forceinline__ bool plan_find(const AttnArgs &a, int id, Found &f) {
   const int lane = threadIdx.x & 63, B = a.p.B;
   int tiles = 0, items = 0, pages = 0;          // of sequence lane
+  bool falls = false;                           // of any so far
   const auto look = [&](int s) {
     tiles = items = pages = 0;
     if (s < B) {
@@ -158,6 +164,7 @@ __device__ __forceinline__ bool plan_find(const AttnArgs &a, int id, Found &f) {
       tiles = q.tiles;
       items = tiles * a.p.NKV;
       pages = q.pages;
+      falls |= q.falls;
     }
   };
   float total = 0.0f;
@@ -165,6 +172,7 @@ __device__ __forceinline__ bool plan_find(const AttnArgs &a, int id, Found &f) {
     look(s0 + lane);
     total += (float)items * (float)pages;
   }
+  if (__ballot(falls)) return false;
   total = __builtin_bit_cast(
       float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, wave_scan(total)), 63));
   // (rounded up past the sum's own rounding: the partial slots are counted on C)
@@ -929,7 +937,7 @@ __global__ __launch_bounds__(AT, (NB * NT > 8 ? 2 : NT > 1 || NB > 4 ? 3 : 4)) v
     const bool whole = f.runs == 1;
     const int first = f.slot0 + it * f.runs;              // slot of the item's run 0
     const Rsrc pr = shared_at(a.part + (int64_t)(whole ? 0 : first + run) * (ROWS * (D + 2)));
-    // (an item whose slots do not fit, as rows that overlap could make one, is left out)
+    // (every item's do, by slots_bound; no write hangs on it)
     const bool fits = whole || first + f.runs <= a.slots;
     if (sub == 0 && col < ROWS && fits) {
 #pragma unroll
