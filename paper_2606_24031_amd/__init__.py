@@ -13,7 +13,7 @@ import os
 
 try:
     import torch
-except ImportError:                   # building needs none
+except (ImportError, OSError):        # (its libraries may not load) building needs none
     torch = None
 
 HERE = os.path.dirname(os.path.abspath(__file__))
