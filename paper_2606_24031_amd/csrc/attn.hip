@@ -66,8 +66,8 @@ constexpr int GROUP = 16;             // runs joined at a time
 constexpr int JT = 1024;              // threads of the joining kernel
 constexpr int SLOTS_MAX = 2 * TARGET; // most runs of split items
 // Value scales that a wave's two halves serve: from 2^-UNDER to 2^OVER times
-// the first step's largest.
-constexpr int UNDER = 8, OVER = 5, WIDE = 1 << 10;
+// the first step's largest, none of 2^127 and more; others are wide.
+constexpr int UNDER = 8, OVER = 5, WIDE = 128;
 constexpr float FAR = 4194304.0f;     // 2^22: half a unit in the last place is 2^-3 below it
 constexpr int64_t COUNTERS = (2 * SLOTS_MAX * 4 + 255) / 256 * 256;   // bytes before the partial results
 static_assert(SLOTS_MAX / GROUP / GROUP <= GROUP, "two levels of joins");
@@ -87,7 +87,7 @@ struct AttnArgs {
   int NH, G;
   float k;          // |scale| * log2(e) / 16, 1 for 0
   float sign;       // of scale: -1, 0 or 1
-  int64_t window;
+  int window;       // 0: none
   int *count;       // arrivals: [SLOTS_MAX] of a group of runs, [SLOTS_MAX] of an item's groups
   float *part;      // partial results, `slots` of them
   int slots;
@@ -98,7 +98,7 @@ struct AttnArgs {
 
 // What a sequence asks for.
 struct Seq {
-  int64_t r0;       // its first row
+  int r0;           // its first row
   int qlen, pos;    // rows, the first one's token
   int lo, pages;    // first page any row sees, pages from there on
   int tiles;
@@ -108,20 +108,20 @@ struct Seq {
 template <int RT_>
 __device__ __forceinline__ Seq seq_of(const AttnArgs &a, int s) {
   Seq r;
-  const int c0 = a.p.cu[s], c1 = a.p.cu[s + 1];
-  const int64_t r0 = kv_clamp_row(c0, a.T), r1 = kv_clamp_row(c1, a.T);
+  const int c0 = a.p.cu[s], c1 = a.p.cu[s + 1], T = (int)a.T;
+  const int r0 = min(max(c0, 0), T), r1 = min(max(c1, 0), T);
   r.falls = c1 < c0;
   r.r0 = r0;
-  r.qlen = r1 > r0 ? (int)(r1 - r0) : 0;
-  // (no call has the 2^30 rows that would lead from below to token 0)
-  r.pos = (int)max((int64_t)a.p.len[s] - (c1 - r0), -((int64_t)1 << 30));
-  const int64_t hi = min((int64_t)r.pos + r.qlen, (int64_t)a.p.max_pages * KV_PAGE);
-  int64_t lo = 0;
-  if (a.window > 0) lo = max((int64_t)0, (int64_t)r.pos - a.window + 1);
-  r.lo = (int)(lo / KV_PAGE);
-  const int64_t end = (hi + KV_PAGE - 1) / KV_PAGE;
-  r.pages = r.qlen > 0 && hi > 0 && end > r.lo ? (int)(end - r.lo) : 0;
-  r.tiles = (int)(((int64_t)r.qlen * a.G + RT_ - 1) / RT_);
+  r.qlen = max(r1 - r0, 0);
+  // (no tokens are as good as fewer than none, and no call has the 2^30 rows
+  // that would lead from below to token 0: nothing here or in a row's keys
+  // leaves 32 bits where cu_rows do not decrease)
+  r.pos = max(max(a.p.len[s], 0) - (int)((uint32_t)c1 - (uint32_t)r0), -(1 << 30));
+  const int hi = min(r.pos + r.qlen, a.p.max_pages * KV_PAGE);
+  r.lo = a.window > 0 && r.pos >= a.window ? (r.pos - a.window + 1) / KV_PAGE : 0;
+  const int end = (hi + KV_PAGE - 1) / KV_PAGE;
+  r.pages = r.qlen > 0 && hi > 0 && end > r.lo ? end - r.lo : 0;
+  r.tiles = (int)(((uint32_t)r.qlen * a.G + RT_ - 1) / RT_);
   return r;
 }
 
@@ -172,7 +172,7 @@ __device__ __forceinline__ bool plan_find(const AttnArgs &a, int id, Found &f) {
     look(s0 + lane);
     total += (float)items * (float)pages;
   }
-  if (__ballot(falls)) return false;
+  if (__ballot(falls)) [[unlikely]] return false;
   total = __builtin_bit_cast(
       float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, wave_scan(total)), 63));
   // (rounded up past the sum's own rounding: the partial slots are counted on C)
@@ -284,12 +284,8 @@ __device__ __forceinline__ float max_finite(float m, v4f w) {
   }
   return m;
 }
-// Magnitudes in order, 0 above all others; that of 2^e, and e again.
-__device__ __forceinline__ uint32_t order_of(float x) {
-  return (__builtin_bit_cast(uint32_t, x) << 1) - 1;
-}
-__device__ __forceinline__ uint32_t limit_of(int e) { return ((uint32_t)(e + 127) << 24) - 1; }
-__device__ __forceinline__ int exponent_of(uint32_t limit) { return (int)(limit >> 24) - 126; }
+// 2^e's bits without the sign, -126 <= e <= 128 (infinity's).
+__device__ __forceinline__ uint32_t bits_of_2(int e) { return (uint32_t)(e + 127) << 24; }
 __device__ __forceinline__ v4f ldexp4(v4f x, int by) {
 #pragma unroll
   for (int e = 0; e < 4; e++) x[e] = ldexpf(x[e], by);
@@ -482,10 +478,10 @@ __global__ __launch_bounds__(AT, (NB * NT > 8 ? 2 : NT > 1 || NB > 4 ? 3 : 4)) v
     const RowMap rm(a, f0);
     const int pos0 = sq.pos + rm.token(0), pos1 = sq.pos + rm.token(fn - 1);
     // the tile's pages within this run
-    int64_t key0 = 0;
-    if (a.window > 0) key0 = max((int64_t)0, (int64_t)pos0 - a.window + 1);
+    const int key0 = a.window > 0 && pos0 >= a.window ? pos0 - a.window + 1 : 0;
+    const int behind = a.window > 0 && pos1 >= a.window ? pos1 - a.window : -1;   // a row's window
     const int per = f.runs == 1 ? sq.pages : (sq.pages + f.runs - 1) / f.runs;
-    const int plo = max((int)(key0 / KV_PAGE), sq.lo + run * per);
+    const int plo = max(key0 / KV_PAGE, sq.lo + run * per);
     const int phi = min(sq.lo + min(sq.pages, (run + 1) * per), pos1 < 0 ? 0 : pos1 / KV_PAGE + 1);
 
     // page ids of a step: lane j < AW has page at0 + j's (-1: none)
@@ -565,7 +561,7 @@ __global__ __launch_bounds__(AT, (NB * NT > 8 ? 2 : NT > 1 || NB > 4 ? 3 : 4)) v
     for (int nt = 0; nt < NT; nt++) {
       const int pos = sq.pos + rm.token(min(16 * nt + (PK > 1 ? col % ROWS : col), fn - 1));
       hi_key[nt] = pos - kbase;
-      lo_key[nt] = (a.window > 0 && a.window <= pos ? (int)(pos - a.window) : -1) - kbase;
+      lo_key[nt] = (a.window > 0 && a.window <= pos ? pos - a.window : -1) - kbase;
     }
     // first token of the lane's NB value scales within its page, as kv_scale_at has them
     const int vtok = sof / 16 * 4 + sof / 4 % 4 * 16 + sof % 4;
@@ -580,9 +576,9 @@ __global__ __launch_bounds__(AT, (NB * NT > 8 ? 2 : NT > 1 || NB > 4 ? 3 : 4)) v
 #pragma unroll
       for (int b = 0; b < BW; b++) acc[nt][b][0] = acc[nt][b][1] = v4f{0.f, 0.f, 0.f, 0.f};
     }
-    // value scales are below 2^vexp, none below `limit` (0: none so far), and
-    // enter the product times 2^(15 - vexp); once wide, scales and sums stand
-    // as they are
+    // value scales are below 2^vexp, their bits above `limit` (0: none so far),
+    // and enter the product times 2^(15 - vexp); once wide, scales and sums
+    // stand as they are
     int vexp = -126;
     uint32_t limit = 0;
     bool far = false;                  // some row's maximum is FAR from 0
@@ -672,7 +668,7 @@ __global__ __launch_bounds__(AT, (NB * NT > 8 ? 2 : NT > 1 || NB > 4 ? 3 : 4)) v
         load_v(ids, b);
       }
       // keys that not every row sees; an absent page's are seen by none
-      if (!here || key + KV_PAGE - 1 > pos0 || (a.window > 0 && key <= pos1 - a.window)) {
+      if (!here || key + KV_PAGE - 1 > pos0 || key <= behind) {
 #pragma unroll
         for (int nt = 0; nt < NT; nt++) {
           const int last = here ? hi_key[nt] - key : -100, before = lo_key[nt] - key;
@@ -694,27 +690,31 @@ __global__ __launch_bounds__(AT, (NB * NT > 8 ? 2 : NT > 1 || NB > 4 ? 3 : 4)) v
       {
         const int vkey = (at0 + spg) * KV_PAGE + vtok;
         const bool vhere = __shfl(ids, spg) >= 0;
-        float dv[NB], vmax = 0.0f;
-        uint32_t least = 0xFFFFFFFFu;
+        // (magnitudes by their bits without the sign; a 0 less 1 is above all)
+        float dv[NB];
+        uint32_t most = 0, least = 0xFFFFFFFFu;
 #pragma unroll
         for (int i = 0; i < NB; i++) {
           dv[i] = scale_of<SYM>(vsr, i);
           const int kk = vkey + (i >> 2) * 16 + (i & 3);
           if (!vhere || kk > pos1 || kk < key0) dv[i] = 0.0f;
-          const float y = fabsf(dv[i]);
-          vmax = fmaxf(vmax, y < INFINITY ? y : 0.0f);
-          least = min(least, order_of(dv[i]));
+          const uint32_t y = __builtin_bit_cast(uint32_t, dv[i]) << 1;
+          most = max(most, y);
+          least = min(least, y - 1);
         }
-        if (__ballot(vmax >= ldexpf(1.0f, vexp) || least < limit)) {
+        if (__ballot(most >= bits_of_2(vexp) || least < limit)) {
+          float vmax = 0.0f;
+#pragma unroll
+          for (int i = 0; i < NB; i++) vmax = fmaxf(vmax, fabsf(dv[i]) < INFINITY ? fabsf(dv[i]) : 0.0f);
 #pragma unroll
           for (int o = 32; o > 0; o >>= 1) vmax = fmaxf(vmax, __shfl_xor(vmax, o));
           int to = max(vexp, __builtin_amdgcn_readfirstlane(ilogbf(vmax) + 1));
-          if (limit == 0) limit = limit_of(max(to - UNDER, -126));
-          if (to > exponent_of(limit) + UNDER + OVER || __ballot(least < limit)) {
+          if (limit == 0 && vexp != WIDE) limit = bits_of_2(max(to - UNDER, -126)) - 1;
+          if (to == WIDE || to > (int)(limit >> 24) - 126 + UNDER + OVER || __ballot(least < limit)) {
             to = WIDE;
             limit = 0;
           }
-          const int by = vexp - (to == WIDE ? 15 : to);
+          const int by = (vexp == WIDE ? 15 : vexp) - (to == WIDE ? 15 : to);
 #pragma unroll
           for (int nt = 0; nt < NT; nt++)
 #pragma unroll
@@ -769,7 +769,7 @@ __global__ __launch_bounds__(AT, (NB * NT > 8 ? 2 : NT > 1 || NB > 4 ? 3 : 4)) v
       float ref[NT];
 #pragma unroll
       for (int nt = 0; nt < NT; nt++) ref[nt] = mk[nt];
-      if (far) {
+      if (far) [[unlikely]] {
 #pragma unroll
         for (int nt = 0; nt < NT; nt++) {
           ref[nt] = 0.0f;
@@ -794,7 +794,7 @@ __global__ __launch_bounds__(AT, (NB * NT > 8 ? 2 : NT > 1 || NB > 4 ? 3 : 4)) v
       __syncthreads();
 
       // ---- values of the wave's columns
-      if (vexp == WIDE) {
+      if (vexp == WIDE) [[unlikely]] {
         // each row's products by a power of two of their own, into sums as they
         // are; codes read again, so that this stays a loop (and places found
         // again, so that none holds a register outside).  1.3 to 1.6 times the
@@ -1184,7 +1184,7 @@ extern "C" int attn_q4_forward(const w4a8_kv *kv, const float *q, int64_t q_stri
                 // a factor of 0 goes to Q, so that a masked score's -infinity stays one
                 scale != 0.0f ? std::fabs(scale) * 1.44269504f / 16.0f : 1.0f,
                 scale < 0.0f ? -1.0f : scale == 0.0f ? 0.0f : 1.0f,
-                window < lim ? window : 0,       // wider than any sequence
+                window < lim ? (int)window : 0,  // wider than any sequence
                 reinterpret_cast<int *>(workspace),
                 reinterpret_cast<float *>(reinterpret_cast<uint8_t *>(workspace) + COUNTERS), (int)slots_bound(kv, T, NH),
                 // a split item's runs beyond the first are C pages each
