@@ -388,8 +388,8 @@ int kv_q4_read(const w4a8_kv *kv, float *k_out, float *v_out, int64_t T, void *s
  * amax / 127 taken as the binary32 product amax * fl(1/127)), so the block
  * dots are exact integers; the softmax and every sum are fp32, and each
  * probability times value scale enters the matrix cores as two fp16 halves
- * (about 22 bits; with the largest score's probability as 1, to no less than
- * 2^-27 of the least value scale met, or 2^-39 of the row's largest such
+ * (about 22 bits; small ones, with the largest score's probability as 1, to
+ * 2^-27 of the least value scale met or 2^-39 of the row's largest such
  * product).  A row that sees no key gives out 0 and lse -infinity.  Keys that
  * a row does not see, or gives next to no probability, change its result by no
  * more than that rounding, whatever their codes and scales hold.
@@ -397,6 +397,8 @@ int kv_q4_read(const w4a8_kv *kv, float *k_out, float *v_out, int64_t T, void *s
  * within fp32's range.
  *   q [T][NH][D] fp32 with row stride q_stride, out [T][NH][D], lse [T][NH]
  *   (NULL: not written).  One launch, or two (long sequences, few rows).
+ *   (Every workgroup looks through the plan's sequences: from some thousand
+ *   on, a call's time grows with their number's square; 8192 take 0.6 ms.)
  *   workspace >= attn_q4_workspace_size bytes, zero-filled before its first
  *   use (moe_w4a8_workspace_init does that); each call leaves it ready for
  *   later ones of this entry point of any sizes it suffices for.  Other entry
@@ -404,8 +406,8 @@ int kv_q4_read(const w4a8_kv *kv, float *k_out, float *v_out, int64_t T, void *s
  *   would mix their results: neither may share it.  (It holds counts that are
  *   0 between calls.  Where they are not, this call and later ones join too
  *   early or never, and rows of long sequences are wrong or not written, until
- *   it is zero-filled again.)  The result does not depend
- *   on timing, and a sequence's does not on the values of the others'.
+ *   it is zero-filled again.)  The result does not depend on timing, and a
+ *   sequence's does not on the values of the others'.
  * Errors beside the plan's: NH < 1, NH % NKV != 0, T < 0, window < 0,
  * q_stride < NH * D or not a multiple of 4, scale not finite -> W4A8_ESHAPE;
  * NH / NKV >= 2^16, T * NH >= 2^31 or q_stride >= 2^31 -> W4A8_ERANGE; q, out

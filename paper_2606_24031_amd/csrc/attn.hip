@@ -39,12 +39,13 @@
 // 4 (l / 16) + e + 16 i) is the one the value product wants for W, so a lane
 // reads back from LDS what the same lane of another wave wrote.
 // Bound: long decodes by HBM (36 bytes a key and 32 columns of K and V, read
-// once for all G heads of a group) and by VALU issue, which is close behind: 48
-// rows of 32 heads of 128 over up to 6000 keys take 52 us, 3.9 TB/s; one of 16
-// heads of 256 over 131072 keys 28 us, 19 of them the runs, 4.0 TB/s.  Prompts
-// by VALU issue, 93 % of a large one's cycles (2 x 2048 rows over 8192 keys, 32
-// heads of 128: 808 us, 427 TFLOP/s): the two scaling operations a score and
-// block and the three that make W's halves.  Short calls by their chain of
+// once for a tile's rows: for a group's heads up to 8 in small calls, 16 or 32
+// in larger ones, again for the rest) and by VALU issue, which is close behind:
+// 48 rows of 32 heads of 128 over up to 6000 keys take 52 us, 3.9 TB/s; one of
+// 16 heads of 256 over 131072 keys 28 us, 19 of them the runs, 4.0 TB/s.
+// Prompts by VALU issue, 94 % of a large one's cycles (2 x 2048 rows over 8192
+// keys, 32 heads of 128: 803 us, 430 TFLOP/s): the two scaling operations a
+// score and block and the three that make W's halves.  Short calls by their chain of
 // launch, plan, page ids, pages and join (one row over 948 keys: 12 us).
 #include <algorithm>
 #include <cfloat>
@@ -148,7 +149,10 @@ template <typename T_> __device__ __forceinline__ T_ wave_scan(T_ x) {
 // on).  SPLIT: item `id` of those with several runs.  False past the end, and
 // for every id where cu_rows decrease: sequences' rows could then number more
 // than T, and runs more than the call has, so that some would never arrive at
-// their counter and leave it for later calls.
+// their counter and leave it for later calls.  Every workgroup goes over all
+// sequences: not to be seen up to some hundred (1024 of one page and 4 heads:
+// 22 us a call), but the square of their number counts later (4096: 184 us,
+// 8192: 638).
 struct Found {
   int s, local, runs, slot0;
 };
@@ -798,7 +802,7 @@ __global__ __launch_bounds__(AT, (NB * NT > 8 ? 2 : NT > 1 || NB > 4 ? 3 : 4)) v
         // each row's products by a power of two of their own, into sums as they
         // are; codes read again, so that this stays a loop (and places found
         // again, so that none holds a register outside).  1.3 to 1.6 times the
-        // time (48 rows over 6000 keys 79 us, 2 x 2048 over 8192 1316)
+        // time (48 rows over 6000 keys 77 us, 2 x 2048 over 8192 1320)
         int ln = lane;
         asm volatile("" : "+v"(ln));
         const auto at = [&] { return (ln >> 4) * 16 + (PK > 1 ? (ln & 15) / ROWS * 4 : 0); };
