@@ -19,7 +19,7 @@
 //     the n best.  After that a random row sends a candidate every few hundred
 //     values.
 // Bound by HBM: 4 bytes a logit, read once, about 13 VALU ops a value.  947
-// rows of 151936 logits with 5 alternatives take 129 us (4.5 TB/s); one row
+// rows of 151936 logits with 5 alternatives take 130 us (4.4 TB/s); one row
 // with 20 takes 13 us, a chain of launch, one pass of its spans and their join.
 #include <algorithm>
 #include <cfloat>
