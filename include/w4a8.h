@@ -456,6 +456,143 @@ int token_logprobs(const float *logits, int64_t stride, const int32_t *targets, 
                    int64_t n_top, void *workspace, size_t ws_bytes, void *stream);
 
 /*
+ * 8-bit rows: the projections around a layer's mixing step, which the paper
+ * leaves in more than 4 bits (Sec. 2.3 quantizes the experts), as int8 codes
+ * with one fp32 scale for each row (a token's, or an output channel's).
+ *   Q8_ROW matrix of `rows` rows of K: codes [rows][q8_row_bytes(K)] int8,
+ *   rows of K rounded up to W4A8_Q8_ROW_PAD codes, and scales d [rows] fp32;
+ *   value = code * d.  Quantizer: d = amax * fl(1/127) (the binary32 product
+ *   with the rounded reciprocal, as the cache's scales), code =
+ *   clamp(round_half_away(x * (1/d)), -127, 127), every step one binary32
+ *   operation; a zero scale, or one whose reciprocal overflows fp32 (below
+ *   2^-128), gives zero codes; the codes past K are zero.  A row with a NaN or
+ *   an infinity has d = NaN and zero codes: its products are NaN, those of
+ *   other rows what they are without it.
+ * q8_row_quantize: x fp32, row r at r * x_stride elements (a slice of wider
+ *   rows works), x 4-byte aligned.  Bit-identical to the definition.
+ * Errors: rows < 0, K < 1, x_stride < K -> W4A8_ESHAPE; K >= 2^17, rows >=
+ * 2^31 or x_stride >= 2^31 -> W4A8_ERANGE; a NULL pointer -> W4A8_ENULL; q not
+ * 16-, x or d not 4-byte aligned -> W4A8_EALIGN.  rows == 0 is a no-op.
+ * q8_row_bytes returns 0 for an invalid K.
+ */
+#define W4A8_Q8_ROW_PAD 128
+size_t q8_row_bytes(int64_t K);
+int q8_row_quantize(const float *x, int64_t x_stride, int8_t *q, float *d, int64_t rows,
+                    int64_t K, void *stream);
+
+/*
+ * Product of M 8-bit activation rows with N 8-bit weight rows:
+ *   y[m][n] = (float)s[m][n] * (xd[m] * wd[n]) + bias[n],
+ *   s[m][n] = sum_k xq[m][k] * wq[n][k]
+ * with s exact in int32 and every operation on it one binary32 operation (the
+ * scales' product first; bias NULL: none is added).
+ *   xq [M], wq [N] rows of q8_row_bytes(K) codes, any int8 values (codes past K
+ *   are multiplied too: they are zero in at least one of the two, as the
+ *   quantizer writes them); xd [M], wd [N], bias [N] fp32; y fp32, row m at
+ *   m * y_stride elements, written.  One launch, no workspace.
+ * Errors: M < 0, N < 1, K < 1, y_stride < N -> W4A8_ESHAPE; K >= 2^17, M or N
+ * >= 2^31, y_stride >= 2^31 -> W4A8_ERANGE; a NULL pointer (but bias) ->
+ * W4A8_ENULL; xq or wq not 16-, xd, wd, bias or y not 4-byte aligned ->
+ * W4A8_EALIGN; y equal to an operand -> W4A8_EALIAS.  M == 0 is a no-op.
+ */
+int q8q8_gemm(const int8_t *xq, const float *xd, const int8_t *wq, const float *wd,
+              const float *bias, float *y, int64_t y_stride, int64_t M, int64_t N, int64_t K,
+              void *stream);
+
+/*
+ * The sequences of a call of the recurrent operators, and where their states
+ * stand in a pool of n_slots slots.
+ *   cu_rows [B + 1] int32, not decreasing: sequence s has the rows cu_rows[s]
+ *           .. cu_rows[s+1] - 1 of the call.  cu_rows[B] may lie past the T of
+ *           a call, which then has the first T rows.  Where they decrease,
+ *           which rows and slots are written, and what with, is open.
+ *   src     [B] int32: the slot that a sequence's state is read from; outside
+ *           [0, n_slots) the sequence begins with a state of zeros.  NULL:
+ *           sequence s reads slot s.
+ *   dst     [B] int32: the slot that its state after its last row goes to;
+ *           outside the pool it is not kept.  NULL: the slot it was read from.
+ * The arrays are read on the device and may change between replays of a
+ * captured graph.  Rows outside every sequence are left as they were;
+ * a sequence without rows writes nothing.  A slot that one sequence of a call
+ * writes is neither read nor written by another (those sequences' results are
+ * open where it is); several may read one.
+ * Errors of every entry point that takes a plan: NULL plan, or cu_rows NULL
+ * with B > 0 -> W4A8_ENULL; B < 0 or n_slots < 0 -> W4A8_ESHAPE; B >= 2^20 or
+ * n_slots >= 2^31 -> W4A8_ERANGE; an array not 4-byte aligned -> W4A8_EALIGN.
+ */
+typedef struct w4a8_seqs {
+  const int32_t *cu_rows;
+  const int32_t *src;
+  const int32_t *dst;
+  int64_t n_slots;
+  int64_t B;
+} w4a8_seqs;
+
+/*
+ * The short causal convolution in front of a recurrence (gdn_chunked_scan,
+ * ssm_scan): per channel c, row t of a sequence and its W - 1 rows before,
+ *   y[t][c] = act(bias[c] + sum_{i < W} w[i][c] * x[t - W + 1 + i][c]),
+ * fp32, the sum in order of i from the oldest row, bias last (bias NULL: none),
+ * act W4A8_CONV_NONE or W4A8_CONV_SILU (v / (1 + exp(-v))).  Rows before a
+ * sequence's first are its state, the last W - 1 inputs, oldest first.
+ *   x fp32, row t at t * x_stride; out the same with out_stride; w [W][CH],
+ *   bias [CH]; state [n_slots][W-1][CH] fp32, read and written as the plan
+ *   says (NULL if the plan has no slots).  One launch.  A NaN or an infinity
+ *   reaches the W rows that it is an input of and the state.
+ * Errors beside the plan's: T < 0, CH < 4, CH % 4 != 0, W not 2, 3 or 4, act
+ * unknown, a stride below CH or not a multiple of 4 -> W4A8_ESHAPE; T >= 2^31,
+ * CH >= 2^24 or a stride >= 2^31 -> W4A8_ERANGE; x, w, out, or state with
+ * n_slots > 0, NULL -> W4A8_ENULL; a pointer not 16-byte aligned ->
+ * W4A8_EALIGN; out or state equal to x or to each other -> W4A8_EALIAS.
+ * T == 0 or B == 0 is a no-op.
+ */
+#define W4A8_CONV_NONE 0
+#define W4A8_CONV_SILU 1
+int short_conv(const w4a8_seqs *seqs, const float *x, int64_t x_stride, const float *w,
+               const float *bias, float *state, float *out, int64_t out_stride, int64_t T,
+               int64_t CH, int64_t W, int32_t act, void *stream);
+
+/*
+ * The selective state space scan, the recurrence of the state space layers of
+ * hybrid models (beside the gated delta rule of gdn_chunked_scan): per head h
+ * of NH, with its group's B and C (group h / (NH / NG)) and a state S in
+ * R^{N x P}, row by row of a sequence, fp32:
+ *   delta = dt[t][h] + dt_bias[h],  log(1 + exp(delta)) of it if softplus
+ *   S     = exp(delta * A[h]) * S + delta * B[t] x[t]^T
+ *   y[t]  = C[t]^T S + D[h] * x[t],  times z[t] / (1 + exp(-z[t])) if z
+ * computed as a chunked scan (chunks of 64 rows: products within a chunk and a
+ * group in parallel, then the chunks in order per head and columns of P);
+ * sequences of up to 8 rows row by row.  Sums and states are fp32; logarithms
+ * of decays are summed in fp64.
+ *   x, z [T][NH][P], b, c [T][NG][N], dt [T][NH] fp32, row t at t times the
+ *   row's stride in elements, heads and groups contiguous; A [NH]; D, dt_bias
+ *   [NH], z: NULL for none; state [n_slots][NH][N][P] fp32, read and written as
+ *   the plan says (NULL if it has no slots); y [T][NH][P], row stride y_stride.
+ *   workspace >= ssm_workspace_size bytes, no initialisation.
+ *   Inputs are finite.  (A value that is not reaches rows of its own sequence
+ *   and head, or group, only: from its 64-row chunk on.)
+ * Errors beside the plan's: NULL ssm -> W4A8_ENULL; T < 0, NH or NG < 1,
+ * NH % NG != 0, N not 64, 128 or 256, P < 16, P % 16 != 0, a stride below its
+ * row's elements, or (but for dt's) not a multiple of 4 -> W4A8_ESHAPE; T >=
+ * 2^31, NH >= 2^16, P > 4096 or a stride >= 2^31 -> W4A8_ERANGE; x, dt, b, c,
+ * A, y or workspace, or state with n_slots > 0, NULL -> W4A8_ENULL; dt, A, D or
+ * dt_bias not 4-, another pointer not 16-byte aligned -> W4A8_EALIGN; y or
+ * state equal to an input or to each other -> W4A8_EALIAS; workspace too small
+ * -> W4A8_EWORKSPACE.  T == 0 or B == 0 is a no-op.  ssm_workspace_size returns
+ * 0 for invalid sizes; it reads only sizes.
+ */
+typedef struct w4a8_ssm {
+  const float *x, *dt, *b, *c, *z;
+  const float *A, *D, *dt_bias;
+  int64_t x_stride, dt_stride, b_stride, c_stride, z_stride;
+  int64_t NH, NG, N, P;
+  int32_t softplus;
+} w4a8_ssm;
+size_t ssm_workspace_size(const w4a8_seqs *seqs, const w4a8_ssm *ssm, int64_t T);
+int ssm_scan(const w4a8_seqs *seqs, const w4a8_ssm *ssm, float *state, float *y,
+             int64_t y_stride, int64_t T, void *workspace, size_t ws_bytes, void *stream);
+
+/*
  * Bytes of device workspace moe_w4a8_forward needs for these sizes, or 0 if
  * the sizes are invalid.  The workspace must be zero-filled once before its
  * first use (moe_w4a8_workspace_init does that); the library leaves its

@@ -32,6 +32,8 @@ KV_PAGE = 64
 KV_FORMATS = {"q4_0": 0, "q4_sym": 1}
 ROPE_LAYOUTS = {"half": 0, "interleaved": 1}
 ROPE_KINDS = {"none": 0, "linear": 1, "parts": 2}
+Q8_ROW_PAD = 128
+CONV_ACTS = {"none": 0, "silu": 1}
 
 EXPORTS = ("w4a8_strerror", "q8_0_quantize", "q4_0_quantize", "q4q8_gemv",
            "moe_w4a8_workspace_size", "moe_w4a8_workspace_init",
@@ -42,7 +44,9 @@ EXPORTS = ("w4a8_strerror", "q8_0_quantize", "q4_0_quantize", "q4q8_gemv",
            "q4q8_gemm", "moe_sym_workspace_size", "moe_sym_workspace_layout", "moe_sym_forward",
            "gdn_workspace_size", "gdn_chunked_scan", "rope_frequencies", "rope_rotate",
            "kv_q4_tile_bytes", "kv_q4_append", "kv_q4_read", "attn_q4_workspace_size",
-           "attn_q4_forward", "token_logprobs_workspace_size", "token_logprobs")
+           "attn_q4_forward", "token_logprobs_workspace_size", "token_logprobs",
+           "q8_row_bytes", "q8_row_quantize", "q8q8_gemm", "short_conv", "ssm_workspace_size",
+           "ssm_scan")
 
 _lib = None
 
@@ -58,6 +62,17 @@ class _KvArgs(ctypes.Structure):       # w4a8_kv
                 ("cu_rows", ctypes.c_void_p), ("n_pages", ctypes.c_int64),
                 ("max_pages", ctypes.c_int64), ("B", ctypes.c_int64), ("NKV", ctypes.c_int64),
                 ("D", ctypes.c_int64), ("format", ctypes.c_int32)]
+
+
+class _SeqArgs(ctypes.Structure):      # w4a8_seqs
+    _fields_ = [("cu_rows", ctypes.c_void_p), ("src", ctypes.c_void_p), ("dst", ctypes.c_void_p),
+                ("n_slots", ctypes.c_int64), ("B", ctypes.c_int64)]
+
+
+class _SsmArgs(ctypes.Structure):      # w4a8_ssm
+    _fields_ = [(n, ctypes.c_void_p) for n in ("x", "dt", "b", "c", "z", "A", "D", "dt_bias")] + \
+               [(n, ctypes.c_int64) for n in ("x_stride", "dt_stride", "b_stride", "c_stride", "z_stride",
+                                              "NH", "NG", "N", "P")] + [("softplus", ctypes.c_int32)]
 
 
 class W4A8Error(RuntimeError):
@@ -135,8 +150,18 @@ def lib() -> ctypes.CDLL:
     L.token_logprobs_workspace_size.argtypes = [I64, I64, I64]
     L.token_logprobs_workspace_size.restype = SZ
     L.token_logprobs.argtypes = [P, I64, P, P, P, P, P, I64, I64, I64, P, SZ, P]
+    SEQ, SSM = ctypes.POINTER(_SeqArgs), ctypes.POINTER(_SsmArgs)
+    L.q8_row_bytes.argtypes = [I64]
+    L.q8_row_bytes.restype = SZ
+    L.q8_row_quantize.argtypes = [P, I64, P, P, I64, I64, P]
+    L.q8q8_gemm.argtypes = [P, P, P, P, P, P, I64, I64, I64, I64, P]
+    L.short_conv.argtypes = [SEQ, P, I64, P, P, P, P, I64, I64, I64, I64, ctypes.c_int32, P]
+    L.ssm_workspace_size.argtypes = [SEQ, SSM, I64]
+    L.ssm_workspace_size.restype = SZ
+    L.ssm_scan.argtypes = [SEQ, SSM, P, P, I64, I64, P, SZ, P]
     for name in ("rope_frequencies", "rope_rotate", "kv_q4_append", "kv_q4_read",
-                 "attn_q4_forward", "token_logprobs"):
+                 "attn_q4_forward", "token_logprobs", "q8_row_quantize", "q8q8_gemm", "short_conv",
+                 "ssm_scan"):
         getattr(L, name).restype = INT
     _lib = L
     return L
@@ -745,3 +770,160 @@ def token_logprobs(logits, targets=None, n_top=0, want_entropy=True, logprob=Non
               stride, _ptr(targets), _ptr(logprob), _ptr(entropy), _ptr(top_ids), _ptr(top_logprobs),
               T, V, n_top, workspace.data_ptr(), workspace.numel() * workspace.element_size())
     return logprob, entropy, top_ids, top_logprobs
+
+
+# ------------------------------------------------------------------ around a layer's recurrence
+def _rows(x, shape, what):
+    """fp32 [rows, n] of this shape with contiguous rows; returns the row
+    stride."""
+    if x.dtype is torch.float32 and x.shape == shape and len(shape) == 2:
+        T, n = shape
+        s0, s1 = x.stride()
+        if s1 == 1 or n == 1:
+            return s0 if T > 1 else max(s0, n)
+    raise ValueError(f"{what}: fp32 [rows, n] = {tuple(shape)} with contiguous rows is needed, "
+                     f"got {x.dtype} {tuple(x.shape)} with strides {x.stride()}")
+
+
+def q8_row_bytes(K) -> int:
+    return int(lib().q8_row_bytes(K))
+
+
+def q8_row_quantize(x, q=None, d=None, stream=None):
+    """8-bit rows of fp32 x [rows, K] (rows may be strided): codes int8 [rows,
+    K rounded up to 128] and scales fp32 [rows], of activations or weights."""
+    xs = _rows(x, x.shape, "x")
+    M, K = x.shape
+    KP = (K + Q8_ROW_PAD - 1) // Q8_ROW_PAD * Q8_ROW_PAD
+    if q is None:
+        q = _empty((M, KP), torch.int8, x.device, stream)
+    else:
+        _is(q, torch.int8, (M, KP), "q")
+    if d is None:
+        d = _empty((M,), torch.float32, x.device, stream)
+    else:
+        _is(d, torch.float32, (M,), "d")
+    if M:
+        _call("q8_row_quantize", stream, (x, q, d), x.data_ptr(), xs, q.data_ptr(), d.data_ptr(), M, K)
+    return q, d
+
+
+def q8q8_gemm(xq, xd, wq, wd, bias=None, out=None, stream=None):
+    """out [M, N] fp32 (rows may be strided) = the product of 8-bit rows xq [M,
+    KP] with scales xd [M] and weight rows wq [N, KP] with scales wd [N], plus
+    bias [N]."""
+    _is(xq, torch.int8, (None, None), "xq")
+    M, KP = xq.shape
+    _is(wq, torch.int8, (None, KP), "wq")
+    N = wq.shape[0]
+    if KP % Q8_ROW_PAD:
+        raise ValueError(f"xq: rows of a multiple of {Q8_ROW_PAD} codes are needed, got {KP}")
+    _is(xd, torch.float32, (M,), "xd")
+    _is(wd, torch.float32, (N,), "wd")
+    if bias is not None:
+        _is(bias, torch.float32, (N,), "bias")
+    if out is None:
+        out = _empty((M, N), torch.float32, xq.device, stream)
+    ys = _rows(out, (M, N), "out")
+    if M:
+        _call("q8q8_gemm", stream, (xq, xd, wq, wd, bias, out), xq.data_ptr(), xd.data_ptr(),
+              wq.data_ptr(), wd.data_ptr(), _ptr(bias), out.data_ptr(), ys, M, N, KP - (KP == 1 << 17))
+    return out
+
+
+class SeqPlan:
+    """The sequences of a call of the recurrent operators (w4a8_seqs): cu_rows
+    [B + 1], and the slots of a pool of n_slots states that each reads (src
+    [B], default its number; outside the pool: none, zeros) and writes (dst
+    [B], default the one it reads; outside the pool: not kept).  It keeps the
+    tensors, int32, which are read on the device at each call."""
+
+    def __init__(self, cu_rows, n_slots, src=None, dst=None):
+        _is(cu_rows, torch.int32, (None,), "cu_rows")
+        B = cu_rows.shape[0] - 1
+        if B < 0:
+            raise ValueError("cu_rows: [B + 1] is needed, got an empty tensor")
+        for t, what in ((src, "src"), (dst, "dst")):
+            if t is not None:
+                _is(t, torch.int32, (B,), what)
+                if t.device != cu_rows.device:
+                    raise ValueError(f"tensors on {cu_rows.device} and {t.device} in one plan")
+        self.tensors = (cu_rows, src, dst)
+        self.B, self.n_slots, self.device = B, n_slots, cu_rows.device
+        self.args = _SeqArgs(cu_rows.data_ptr(), _ptr(src), _ptr(dst), n_slots, B)
+        self.ref = ctypes.byref(self.args)
+
+
+def short_conv(plan, x, w, state, bias=None, act="silu", out=None, stream=None):
+    """The causal convolution of x [T, CH] (rows may be strided) with w [W, CH]
+    along plan's sequences, and its activation ("silu" or "none"); state
+    [n_slots, W - 1, CH] holds the sequences' last inputs (None without slots).
+    Returns out [T, CH]."""
+    xs = _rows(x, x.shape, "x")
+    T, CH = x.shape
+    _is(w, torch.float32, (None, CH), "w")
+    W = w.shape[0]
+    if state is not None:
+        _is(state, torch.float32, (plan.n_slots, W - 1, CH), "state")
+    elif plan.n_slots > 0:
+        raise ValueError("state: the plan has slots")
+    if bias is not None:
+        _is(bias, torch.float32, (CH,), "bias")
+    if act not in CONV_ACTS:
+        raise ValueError(f"act {act!r}: one of {sorted(CONV_ACTS)}")
+    if out is None:
+        out = _empty((T, CH), torch.float32, x.device, stream)
+    os_ = _rows(out, (T, CH), "out")
+    if T:
+        _call("short_conv", stream, (plan.tensors[0], x, w, state, bias, out), plan.ref, x.data_ptr(), xs,
+              w.data_ptr(), _ptr(bias), _ptr(state), out.data_ptr(), os_, T, CH, W, CONV_ACTS[act])
+    return out
+
+
+def _ssm_sizes(plan, T, NH, NG, N, P):
+    a = _SsmArgs(NH=NH, NG=NG, N=N, P=P)
+    return int(lib().ssm_workspace_size(plan.ref, ctypes.byref(a), T))
+
+
+def ssm_workspace(plan, T, NH, NG, N, P, stream=None):
+    """A workspace for ssm_scan with T rows on plan's sequences."""
+    n = _ssm_sizes(plan, T, NH, NG, N, P)
+    if n == 0:
+        raise W4A8Error(ESHAPE, "ssm_workspace_size")
+    return _empty(n, torch.uint8, plan.device, stream)
+
+
+def ssm_scan(plan, x, dt, A, B, C, state, D=None, z=None, dt_bias=None, softplus=True, out=None,
+             workspace=None, stream=None):
+    """The selective state space scan of x [T, NH, P] with steps dt [T, NH],
+    decays A [NH], B and C [T, NG, N] (rows of all may be strided) along plan's
+    sequences; state [n_slots, NH, N, P] (None without slots).  Optional: D and
+    dt_bias [NH], the gate z [T, NH, P].  Returns out [T, NH, P]."""
+    xs = _heads(x, x.shape, "x")
+    T, NH, P = x.shape
+    ds = _rows(dt, (T, NH), "dt")
+    NG, N = B.shape[1:] if B.dim() == 3 else (0, 0)
+    bs, cs = _heads(B, (T, NG, N), "B"), _heads(C, (T, NG, N), "C")
+    zs = 0 if z is None else _heads(z, (T, NH, P), "z")
+    _is(A, torch.float32, (NH,), "A")
+    for t, what in ((D, "D"), (dt_bias, "dt_bias")):
+        if t is not None:
+            _is(t, torch.float32, (NH,), what)
+    if state is not None:
+        _is(state, torch.float32, (plan.n_slots, NH, N, P), "state")
+    elif plan.n_slots > 0:
+        raise ValueError("state: the plan has slots")
+    if out is None:
+        out = _empty((T, NH, P), torch.float32, x.device, stream)
+    os_ = _heads(out, (T, NH, P), "out")
+    if T:
+        if workspace is None:
+            workspace = ssm_workspace(plan, T, NH, NG, N, P, stream)
+        elif not workspace.is_contiguous():
+            raise ValueError("workspace: a contiguous tensor is needed")
+        a = _SsmArgs(x.data_ptr(), dt.data_ptr(), B.data_ptr(), C.data_ptr(), _ptr(z), A.data_ptr(), _ptr(D),
+                     _ptr(dt_bias), xs, ds, bs, cs, zs, NH, NG, N, P, 1 if softplus else 0)
+        _call("ssm_scan", stream, (plan.tensors[0], x, dt, A, B, C, state, D, z, dt_bias, out, workspace),
+              plan.ref, ctypes.byref(a), _ptr(state), out.data_ptr(), os_, T, workspace.data_ptr(),
+              workspace.numel() * workspace.element_size())
+    return out
