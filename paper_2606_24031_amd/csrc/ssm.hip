@@ -10,14 +10,16 @@ namespace w4a8 {
 namespace {
 
 constexpr int SC = 64;              // rows of a chunk
-constexpr int STEP_NT = 256;        // threads of a step workgroup
+constexpr int SNT = 512;            // threads of a scan workgroup: eight waves
+constexpr int STEP_NT = 256;        // ... of a step workgroup
+constexpr int STEP_T = 8;           // sequences of up to this many rows go row by row
 
 typedef float v4f __attribute__((ext_vector_type(4)));
 
 struct ScanArgs {
   Seqs q;
   const float *x, *dt, *b, *c, *z, *A, *D, *bias;
-  float *state, *y;
+  float *state, *y, *gram;
   int64_t xs, ds, bs, cs, zs, ys;
   int NH, G, NG, P, nsl;            // heads, heads of a group, groups, columns, slices of columns
   int softplus;
@@ -99,6 +101,282 @@ __global__ __launch_bounds__(STEP_NT) void step_kernel(ScanArgs a) {
   step_rows<N, COLS, STEP_NT>(a, b, h, sl * COLS, begin, end, red);
 }
 
+// ---------------------------------------------------------------- chunked scan
+// Chunk c of sequence b has its products C B^T in the workspace at record
+// cu[b] / 64 + b + c: a sequence of n rows has ceil(n / 64) of them, which never
+// reach the next sequence's first.
+__device__ __forceinline__ int record_of(int begin, int b) { return begin / SC + b; }
+
+// A record holds the ten 16 x 16 tiles (r, j <= r) of a chunk's C B^T, each as a
+// lane of a product takes it: four neighbouring columns 4 (l / 16) .. + 3 of row
+// l % 16.
+constexpr int REC = 10 * 256;       // floats
+__device__ __forceinline__ int tile_at(int r, int j) { return (r * (r + 1) / 2 + j) * 256; }
+
+// Four products of 16 x 16 x 4 of a 16-byte piece of either operand, in two
+// sums: lane l's pieces are k = 4 (l / 16) .. + 3 of row (A) and column (B) l % 16
+// of 16 k in all; element e of a sum is row 4 (l / 16) + e, column l % 16.
+__device__ __forceinline__ void mm4(v4f x, v4f y, v4f &c0, v4f &c1) {
+  c0 = __builtin_amdgcn_mfma_f32_16x16x4f32(x.x, y.x, c0, 0, 0, 0);
+  c1 = __builtin_amdgcn_mfma_f32_16x16x4f32(x.y, y.y, c1, 0, 0, 0);
+  c0 = __builtin_amdgcn_mfma_f32_16x16x4f32(x.z, y.z, c0, 0, 0, 0);
+  c1 = __builtin_amdgcn_mfma_f32_16x16x4f32(x.w, y.w, c1, 0, 0, 0);
+}
+__device__ __forceinline__ v4f quad(const float *p) { return *reinterpret_cast<const v4f *>(p); }
+
+// C B^T of one chunk and group, a wave per 16 rows of C.  The rows of B are the A
+// operand, so that a lane's sums are neighbouring columns of one row.  Rows past
+// the sequence's last repeat it (their steps are 0 where they are used).
+template <int N>
+__global__ __launch_bounds__(256) void gram_kernel(ScanArgs a) {
+  const int rec = blockIdx.x / a.NG, g = blockIdx.x % a.NG;
+  int lo = 0, hi = a.q.B;           // the last sequence whose first record is not past rec
+  while (hi - lo > 1) {
+    const int m = (lo + hi) >> 1;
+    if (record_of(seq_begin(a.q, m), m) <= rec) lo = m; else hi = m;
+  }
+  const int begin = seq_begin(a.q, lo), end = seq_begin(a.q, lo + 1);
+  const int t0 = begin + (rec - record_of(begin, lo)) * SC;
+  if (t0 < begin || t0 >= end || end - begin <= STEP_T) return;
+  const int r = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  const int l16 = lane & 15, lq = lane >> 4;
+  const float *cp = a.c + min(t0 + 16 * r + l16, end - 1) * a.cs + (int64_t)g * N + 4 * lq;
+  v4f c[N / 16];
+#pragma unroll
+  for (int s = 0; s < N / 16; s++) c[s] = quad(cp + 16 * s);
+  for (int j = 0; j <= r; j++) {
+    const float *bp = a.b + min(t0 + 16 * j + l16, end - 1) * a.bs + (int64_t)g * N + 4 * lq;
+    v4f s0 = {0.f, 0.f, 0.f, 0.f}, s1 = s0;
+#pragma unroll
+    for (int s = 0; s < N / 16; s++) mm4(quad(bp + 16 * s), c[s], s0, s1);
+    *reinterpret_cast<v4f *>(a.gram + ((int64_t)rec * a.NG + g) * REC + tile_at(r, j) + 4 * lane) =
+        s0 + s1;
+  }
+}
+
+// Inclusive sum over the wave's lanes.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ double dpp_add(double v) {
+  const uint64_t u = __builtin_bit_cast(uint64_t, v);
+  const uint32_t l = __builtin_amdgcn_update_dpp(0, (int)(uint32_t)u, CTRL, ROWS, 0xF, false);
+  const uint32_t h = __builtin_amdgcn_update_dpp(0, (int)(uint32_t)(u >> 32), CTRL, ROWS, 0xF, false);
+  return v + __builtin_bit_cast(double, (uint64_t)h << 32 | l);
+}
+__device__ __forceinline__ double scan64(double v) {
+  v = dpp_add<0x111, 0xF>(v);       // from 1, 2, 4 and 8 lanes before in a row of 16
+  v = dpp_add<0x112, 0xF>(v);
+  v = dpp_add<0x114, 0xF>(v);
+  v = dpp_add<0x118, 0xF>(v);
+  v = dpp_add<0x142, 0xA>(v);       // the row before's last lane, into rows 1 and 3
+  return dpp_add<0x143, 0xC>(v);    // lane 31, into rows 2 and 3
+}
+
+// What a lane has in registers of a chunk, loaded a chunk ahead.
+template <int CF, int BF, int GF>
+struct ChunkRegs {
+  v4f c[CF], g[GF], x, z;           // pieces of C, of C B^T; four columns of a row of x and z
+  float b[BF][16];                  // B of 16 rows for a column of each of its tiles
+  float dt;
+};
+
+template <int N, int PS>
+struct ScanLds {
+  float xt[2][PS][SC + 4];          // x by column
+  float st[2][PS][N + 4];           // the state before the chunk by column
+  float yl[2][2][SC][PS + 4];       // sums of y: of either half of the state's rows
+  float lh[2][SC], ll[2][SC];       // logarithms (base 2) of the decay up to a row: two halves
+  float dl[2][SC], wj[2][SC];       // steps; steps times the decay from a row to the chunk's end
+  float el[2][SC];                  // decay up to a row; the last is the chunk's
+  float red[SNT / 64][PS];
+};
+
+// The chunks of a sequence in order, for one head and PS columns; the state's
+// tiles of 16 x 16 in the accumulators of eight waves.  With L the sums of the
+// logarithms of the decays, within a chunk
+//   y = diag(e^L) C S + (C B^T o e^{L_i - L_j} o d_j) x   (j <= i)
+//   S <- e^{L_C} S + B^T diag(d e^{L_C - L}) x.
+template <int N, int PS>
+__global__ __launch_bounds__(SNT) void scan_kernel(ScanArgs a) {
+  constexpr int NT = N / 16, PT = PS / 16, TPW = NT * PT / 8, KH = 2 / PT;
+  constexpr int CF = N / KH / 16, GF = KH == 2 ? 2 : 4;
+  static_assert(TPW * 8 == NT * PT && KH * PT == 2, "tiles over the waves");
+  __shared__ __align__(16) ScanLds<N, PS> L;
+  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
+  const int l16 = lane & 15, lq = lane >> 4;
+  // all slices of a head on one XCD (workgroup w runs on XCD w mod 8)
+  const int k = blockIdx.x >> 3, bh = (k / a.nsl) * 8 + (blockIdx.x & 7);
+  if (bh >= a.q.B * a.NH) return;
+  const int b = bh / a.NH, h = bh % a.NH, g = h / a.G, c0 = (k % a.nsl) * PS;
+  const int begin = seq_begin(a.q, b), end = seq_begin(a.q, b + 1);
+  if (begin >= end) return;
+  if (end - begin <= STEP_T) {
+    step_rows<N, PS, SNT>(a, b, h, c0, begin, end, L.red);
+    return;
+  }
+  const int nch = (end - begin + SC - 1) / SC;
+  const float bias = a.bias ? a.bias[h] : 0.0f, D = a.D ? a.D[h] : 0.0f;
+  const double A = (double)a.A[h] * 1.4426950408889634;
+
+  // roles: sums of y of rows 16 r .. + 15, column tile ct, half kh of the
+  // state's rows (waves w and w + 4, of one SIMD, take r and 3 - r); the tiles
+  // of S; row xr and columns xc .. + 3 of x, z and y
+  const int hi = wave >> 2, r = hi ? 3 - (wave & 3) : wave & 3;
+  const int kh = KH == 2 ? hi : 0, ct = KH == 2 ? 0 : hi;
+  int nt[TPW], sct[TPW];
+#pragma unroll
+  for (int i = 0; i < TPW; i++) { nt[i] = (wave + 8 * i) % NT; sct[i] = (wave + 8 * i) / NT; }
+  const int xr = tid / (PS / 4), xc = 4 * (tid % (PS / 4));
+  const bool xlive = xr < SC && c0 + xc < a.P;
+
+  using Regs = ChunkRegs<CF, TPW, GF>;
+  const auto load = [&](int c, Regs &q) {
+    const int t0 = begin + c * SC, last = end - 1;
+    const float *cp = a.c + min(t0 + 16 * r + l16, last) * a.cs + (int64_t)g * N + kh * (N / KH) + 4 * lq;
+#pragma unroll
+    for (int s = 0; s < CF; s++) q.c[s] = quad(cp + 16 * s);
+    const float *gp = a.gram + ((int64_t)(record_of(begin, b) + c) * a.NG + g) * REC + 4 * lane;
+#pragma unroll
+    for (int s = 0; s < GF; s++) q.g[s] = quad(gp + tile_at(r, min(KH == 2 ? kh + 2 * s : s, r)));
+#pragma unroll
+    for (int i = 0; i < TPW; i++)
+#pragma unroll
+      for (int e = 0; e < 16; e++)
+        q.b[i][e] = a.b[min(t0 + 16 * (e >> 2) + 4 * lq + (e & 3), last) * a.bs + (int64_t)g * N +
+                        16 * nt[i] + l16];
+    const int tx = min(t0 + min(xr, SC - 1), last), cx = min(c0 + xc, a.P - 4);
+    q.x = quad(a.x + tx * a.xs + (int64_t)h * a.P + cx);
+    if (a.z) q.z = quad(a.z + tx * a.zs + (int64_t)h * a.P + cx);
+    q.dt = a.dt[min(t0 + lane, last) * a.ds + h];
+  };
+  // x by column, and the decays of a chunk (one wave, the one without products of
+  // C B^T): logarithms are summed in fp64 and kept in two halves, so that
+  // differences of long sums keep their precision
+  const auto stage = [&](int c, const Regs &q) {
+    const int p = c & 1;
+    if (xr < SC)
+#pragma unroll
+      for (int e = 0; e < 4; e++) L.xt[p][xc + e][xr] = q.x[e];
+    if (wave == 7) {
+      const bool in = begin + c * SC + lane < end;
+      const float d = in ? step_of(q.dt, bias, a.softplus) : 0.0f;
+      const double s = scan64(in ? (double)d * A : 0.0);
+      const uint64_t u = __builtin_bit_cast(uint64_t, s);
+      const double sc = __builtin_bit_cast(
+          double, (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(u >> 32), 63) << 32 |
+                      (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)u, 63));
+      const float lh = (float)s;
+      L.lh[p][lane] = lh;
+      L.ll[p][lane] = (float)(s - (double)lh);
+      L.dl[p][lane] = d;
+      L.wj[p][lane] = d * __builtin_amdgcn_exp2f((float)(sc - s));
+      L.el[p][lane] = __builtin_amdgcn_exp2f(lh);
+    }
+  };
+
+  const int64_t src = seq_src(a.q, b), dst = seq_dst(a.q, b);
+  v4f S[TPW];
+#pragma unroll
+  for (int i = 0; i < TPW; i++) {
+    const int col = c0 + 16 * sct[i] + l16;
+#pragma unroll
+    for (int e = 0; e < 4; e++)
+      S[i][e] = src >= 0 && col < a.P
+                    ? a.state[((src * a.NH + h) * N + 16 * nt[i] + 4 * lq + e) * a.P + col]
+                    : 0.0f;
+  }
+  const auto put_state = [&](int p) {
+#pragma unroll
+    for (int i = 0; i < TPW; i++)
+      *reinterpret_cast<v4f *>(&L.st[p][16 * sct[i] + l16][16 * nt[i] + 4 * lq]) = S[i];
+  };
+
+  // chunk c: its registers in `q`, its x, decays and state in LDS; `nx` the next one's
+  const auto step = [&](int c, Regs &q, Regs &nx) {
+    const int p = c & 1;
+    if (c + 1 < nch) load(c + 1, nx);
+    v4f xt[4];
+#pragma unroll
+    for (int s = 0; s < 4; s++) xt[s] = quad(&L.xt[p][16 * ct + l16][16 * s + 4 * lq]);
+    // C S
+    v4f y0 = {0.f, 0.f, 0.f, 0.f}, y1 = y0;
+#pragma unroll
+    for (int s = 0; s < CF; s++)
+      mm4(q.c[s], quad(&L.st[p][16 * ct + l16][kh * (N / KH) + 16 * s + 4 * lq]), y0, y1);
+    // S
+    const float eC = L.el[p][SC - 1];
+#pragma unroll
+    for (int i = 0; i < TPW; i++) {
+      v4f s1 = {0.f, 0.f, 0.f, 0.f};
+      S[i] *= eC;
+#pragma unroll
+      for (int s = 0; s < 4; s++) {
+        const v4f w = quad(&L.wj[p][16 * s + 4 * lq]);
+        mm4(v4f{q.b[i][4 * s], q.b[i][4 * s + 1], q.b[i][4 * s + 2], q.b[i][4 * s + 3]}, w * xt[s], S[i], s1);
+      }
+      S[i] += s1;
+    }
+    y0 = (y0 + y1) * quad(&L.el[p][16 * r + 4 * lq]);
+    // (C B^T o decays) x
+    const float lhi = L.lh[p][16 * r + l16], lli = L.ll[p][16 * r + l16];
+    y1 = v4f{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int s = 0; s < GF; s++) {
+      const int j = KH == 2 ? kh + 2 * s : s;
+      if (j > r) continue;
+      const v4f lh = quad(&L.lh[p][16 * j + 4 * lq]), ll = quad(&L.ll[p][16 * j + 4 * lq]);
+      const v4f dl = quad(&L.dl[p][16 * j + 4 * lq]);
+      v4f w;
+#pragma unroll
+      for (int e = 0; e < 4; e++) {
+        w[e] = q.g[s][e] * (dl[e] * __builtin_amdgcn_exp2f((lhi - lh[e]) + (lli - ll[e])));
+        if (16 * j + 4 * lq + e > 16 * r + l16) w[e] = 0.0f;
+      }
+      v4f xs = xt[0];
+#pragma unroll
+      for (int m = 1; m < 4; m++)
+        if (m == j) xs = xt[m];
+      mm4(w, xs, y0, y1);
+    }
+    y0 += y1;
+#pragma unroll
+    for (int e = 0; e < 4; e++) L.yl[p][kh][16 * r + 4 * lq + e][16 * ct + l16] = y0[e];
+    if (c + 1 < nch) {
+      put_state(p ^ 1);
+      stage(c + 1, nx);
+    }
+    __syncthreads();
+    if (xlive && begin + c * SC + xr < end) {
+      v4f o = quad(&L.yl[p][0][xr][xc]);
+      if (KH == 2) o += quad(&L.yl[p][1][xr][xc]);
+      o += D * q.x;
+      if (a.z) o *= v4f{silu_f32(q.z.x), silu_f32(q.z.y), silu_f32(q.z.z), silu_f32(q.z.w)};
+      *reinterpret_cast<v4f *>(a.y + (int64_t)(begin + c * SC + xr) * a.ys + (int64_t)h * a.P + c0 + xc) = o;
+    }
+  };
+  Regs ra, rb;
+  load(0, ra);
+  put_state(0);
+  stage(0, ra);
+  __syncthreads();
+  for (int c = 0;;) {
+    step(c, ra, rb);
+    if (++c >= nch) break;
+    step(c, rb, ra);
+    if (++c >= nch) break;
+  }
+  if (dst >= 0)
+#pragma unroll
+    for (int i = 0; i < TPW; i++) {
+      const int col = c0 + 16 * sct[i] + l16;
+      if (col < a.P)
+#pragma unroll
+        for (int e = 0; e < 4; e++)
+          a.state[((dst * a.NH + h) * N + 16 * nt[i] + 4 * lq + e) * a.P + col] = S[i][e];
+    }
+}
+
+int64_t records(const Seqs &q) { return (int64_t)q.T / SC + q.B + 1; }
+
 int ssm_sizes(const w4a8_seqs *q, const w4a8_ssm *m, int64_t T) {
   if (!m) return W4A8_ENULL;
   int rc = seqs_sizes(q, T);
@@ -115,8 +393,17 @@ int ssm_sizes(const w4a8_seqs *q, const w4a8_ssm *m, int64_t T) {
 
 template <int N>
 int launch_ssm(ScanArgs a, hipStream_t s) {
-  a.nsl = (a.P + 63) / 64;
-  step_kernel<N, 64><<<dim3((unsigned)(a.q.B * a.NH * a.nsl)), dim3(STEP_NT), 0, s>>>(a);
+  if (a.q.T <= STEP_T || a.q.T <= a.q.B) {
+    a.nsl = (a.P + 63) / 64;
+    step_kernel<N, 64><<<dim3((unsigned)(a.q.B * a.NH * a.nsl)), dim3(STEP_NT), 0, s>>>(a);
+    return check_launch();
+  }
+  gram_kernel<N><<<dim3((unsigned)(records(a.q) * a.NG)), dim3(256), 0, s>>>(a);
+  if (int rc = check_launch(); rc != W4A8_OK) return rc;
+  constexpr int PS = N == 64 ? 32 : 16;
+  a.nsl = (a.P + PS - 1) / PS;
+  const unsigned pairs = (unsigned)((a.q.B * a.NH + 7) / 8 * 8);
+  scan_kernel<N, PS><<<dim3(pairs * a.nsl), dim3(SNT), 0, s>>>(a);
   return check_launch();
 }
 
@@ -128,7 +415,7 @@ using namespace w4a8;
 
 extern "C" size_t ssm_workspace_size(const w4a8_seqs *seqs, const w4a8_ssm *ssm, int64_t T) {
   if (ssm_sizes(seqs, ssm, T) != W4A8_OK) return 0;
-  return 256;
+  return ((size_t)(T / SC + seqs->B + 1) * ssm->NG * REC + 64) * sizeof(float);
 }
 
 extern "C" int ssm_scan(const w4a8_seqs *seqs, const w4a8_ssm *m, float *state, float *y,
@@ -160,7 +447,7 @@ extern "C" int ssm_scan(const w4a8_seqs *seqs, const w4a8_ssm *m, float *state, 
   a.q = seqs_args(seqs, T);
   a.x = m->x; a.dt = m->dt; a.b = m->b; a.c = m->c; a.z = m->z;
   a.A = m->A; a.D = m->D; a.bias = m->dt_bias;
-  a.state = state; a.y = y;
+  a.state = state; a.y = y; a.gram = reinterpret_cast<float *>(workspace);
   a.xs = m->x_stride; a.ds = m->dt_stride; a.bs = m->b_stride; a.cs = m->c_stride;
   a.zs = m->z_stride; a.ys = y_stride;
   a.NH = (int)m->NH; a.NG = (int)m->NG; a.G = (int)(m->NH / m->NG); a.P = (int)m->P;
