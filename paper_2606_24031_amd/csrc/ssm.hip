@@ -19,7 +19,7 @@ typedef float v4f __attribute__((ext_vector_type(4)));
 struct ScanArgs {
   Seqs q;
   const float *x, *dt, *b, *c, *z, *A, *D, *bias;
-  float *state, *y, *gram;
+  float *state, *y, *gram, *dec;    // gram, dec: the workspace
   int64_t xs, ds, bs, cs, zs, ys;
   int NH, G, NG, P, nsl;            // heads, heads of a group, groups, columns, slices of columns
   int softplus;
@@ -124,36 +124,6 @@ __device__ __forceinline__ void mm4(v4f x, v4f y, v4f &c0, v4f &c1) {
 }
 __device__ __forceinline__ v4f quad(const float *p) { return *reinterpret_cast<const v4f *>(p); }
 
-// C B^T of one chunk and group, a wave per 16 rows of C.  The rows of B are the A
-// operand, so that a lane's sums are neighbouring columns of one row.  Rows past
-// the sequence's last repeat it (their steps are 0 where they are used).
-template <int N>
-__global__ __launch_bounds__(256) void gram_kernel(ScanArgs a) {
-  const int rec = blockIdx.x / a.NG, g = blockIdx.x % a.NG;
-  int lo = 0, hi = a.q.B;           // the last sequence whose first record is not past rec
-  while (hi - lo > 1) {
-    const int m = (lo + hi) >> 1;
-    if (record_of(seq_begin(a.q, m), m) <= rec) lo = m; else hi = m;
-  }
-  const int begin = seq_begin(a.q, lo), end = seq_begin(a.q, lo + 1);
-  const int t0 = begin + (rec - record_of(begin, lo)) * SC;
-  if (t0 < begin || t0 >= end || end - begin <= STEP_T) return;
-  const int r = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
-  const int l16 = lane & 15, lq = lane >> 4;
-  const float *cp = a.c + min(t0 + 16 * r + l16, end - 1) * a.cs + (int64_t)g * N + 4 * lq;
-  v4f c[N / 16];
-#pragma unroll
-  for (int s = 0; s < N / 16; s++) c[s] = quad(cp + 16 * s);
-  for (int j = 0; j <= r; j++) {
-    const float *bp = a.b + min(t0 + 16 * j + l16, end - 1) * a.bs + (int64_t)g * N + 4 * lq;
-    v4f s0 = {0.f, 0.f, 0.f, 0.f}, s1 = s0;
-#pragma unroll
-    for (int s = 0; s < N / 16; s++) mm4(quad(bp + 16 * s), c[s], s0, s1);
-    *reinterpret_cast<v4f *>(a.gram + ((int64_t)rec * a.NG + g) * REC + tile_at(r, j) + 4 * lane) =
-        s0 + s1;
-  }
-}
-
 // Inclusive sum over the wave's lanes.
 template <int CTRL, int ROWS>
 __device__ __forceinline__ double dpp_add(double v) {
@@ -171,12 +141,76 @@ __device__ __forceinline__ double scan64(double v) {
   return dpp_add<0x143, 0xC>(v);    // lane 31, into rows 2 and 3
 }
 
+// What the scan takes of a chunk's steps, per head DEC arrays of 64 rows: the
+// logarithms (base 2) of the decay up to a row, in two halves, the steps, the
+// steps times the decay from a row to the chunk's end, and the decay up to a row.
+// Logarithms are summed in fp64 and kept in two halves so that differences of
+// long sums keep their precision: rows of strong decay (hundreds) may stand
+// beside rows of next to none.
+constexpr int DEC = 5, DEC_LH = 0, DEC_LL = 1, DEC_DL = 2, DEC_WJ = 3, DEC_EL = 4;
+
+// What the chunks need that does not wait for the one before, a workgroup per
+// chunk and group, then one per chunk and four heads:
+//   C B^T, a wave per 16 rows of C.  The rows of B are the A operand, so that a
+//   lane's sums are neighbouring columns of one row.  Rows past the sequence's
+//   last repeat it (their steps are 0 where they are used).
+//   the steps and decays, a wave per head, a row a lane.
+template <int N>
+__global__ __launch_bounds__(256) void prep_kernel(ScanArgs a, unsigned ngram) {
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  const bool gram = blockIdx.x < ngram;
+  const unsigned w = gram ? blockIdx.x : blockIdx.x - ngram, per = gram ? a.NG : (a.NH + 3) / 4;
+  const int rec = w / per, part = w % per;
+  int lo = 0, hi = a.q.B;           // the last sequence whose first record is not past rec
+  while (hi - lo > 1) {
+    const int m = (lo + hi) >> 1;
+    if (record_of(seq_begin(a.q, m), m) <= rec) lo = m; else hi = m;
+  }
+  const int begin = seq_begin(a.q, lo), end = seq_begin(a.q, lo + 1);
+  const int t0 = begin + (rec - record_of(begin, lo)) * SC;
+  if (t0 < begin || t0 >= end || end - begin <= STEP_T) return;
+  if (!gram) {
+    const int h = 4 * part + wave;
+    if (h >= a.NH) return;
+    const double A = (double)a.A[h] * 1.4426950408889634;
+    const int t = t0 + lane;
+    const float d = t < end ? step_of(a.dt[min(t, end - 1) * a.ds + h], a.bias ? a.bias[h] : 0.0f, a.softplus)
+                            : 0.0f;
+    const double s = scan64(t < end ? (double)d * A : 0.0);
+    const uint64_t u = __builtin_bit_cast(uint64_t, s);
+    const double all = __builtin_bit_cast(
+        double, (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(u >> 32), 63) << 32 |
+                    (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)u, 63));
+    const float lh = (float)s;
+    float *o = a.dec + ((int64_t)rec * a.NH + h) * (DEC * SC) + lane;
+    o[DEC_LH * SC] = lh;
+    o[DEC_LL * SC] = (float)(s - (double)lh);
+    o[DEC_DL * SC] = d;
+    o[DEC_WJ * SC] = d * __builtin_amdgcn_exp2f((float)(all - s));
+    o[DEC_EL * SC] = __builtin_amdgcn_exp2f(lh);
+    return;
+  }
+  const int r = wave, g = part, l16 = lane & 15, lq = lane >> 4;
+  const float *cp = a.c + min(t0 + 16 * r + l16, end - 1) * a.cs + (int64_t)g * N + 4 * lq;
+  v4f c[N / 16];
+#pragma unroll
+  for (int s = 0; s < N / 16; s++) c[s] = quad(cp + 16 * s);
+  for (int j = 0; j <= r; j++) {
+    const float *bp = a.b + min(t0 + 16 * j + l16, end - 1) * a.bs + (int64_t)g * N + 4 * lq;
+    v4f s0 = {0.f, 0.f, 0.f, 0.f}, s1 = s0;
+#pragma unroll
+    for (int s = 0; s < N / 16; s++) mm4(quad(bp + 16 * s), c[s], s0, s1);
+    *reinterpret_cast<v4f *>(a.gram + ((int64_t)rec * a.NG + g) * REC + tile_at(r, j) + 4 * lane) =
+        s0 + s1;
+  }
+}
+
 // What a lane has in registers of a chunk, loaded a chunk ahead.
 template <int CF, int BF, int GF>
 struct ChunkRegs {
   v4f c[CF], g[GF], x, z;           // pieces of C, of C B^T; four columns of a row of x and z
   float b[BF][16];                  // B of 16 rows for a column of each of its tiles
-  float dt;
+  float dec;                        // of one of the decay arrays (waves 0 .. 4) a row
 };
 
 template <int N, int PS>
@@ -184,9 +218,7 @@ struct ScanLds {
   float xt[2][PS][SC + 4];          // x by column
   float st[2][PS][N + 4];           // the state before the chunk by column
   float yl[2][2][SC][PS + 4];       // sums of y: of either half of the state's rows
-  float lh[2][SC], ll[2][SC];       // logarithms (base 2) of the decay up to a row: two halves
-  float dl[2][SC], wj[2][SC];       // steps; steps times the decay from a row to the chunk's end
-  float el[2][SC];                  // decay up to a row; the last is the chunk's
+  float dec[2][DEC][SC];
   float red[SNT / 64][PS];
 };
 
@@ -214,8 +246,7 @@ __global__ __launch_bounds__(SNT) void scan_kernel(ScanArgs a) {
     return;
   }
   const int nch = (end - begin + SC - 1) / SC;
-  const float bias = a.bias ? a.bias[h] : 0.0f, D = a.D ? a.D[h] : 0.0f;
-  const double A = (double)a.A[h] * 1.4426950408889634;
+  const float D = a.D ? a.D[h] : 0.0f;
 
   // roles: sums of y of rows 16 r .. + 15, column tile ct, half kh of the
   // state's rows (waves w and w + 4, of one SIMD, take r and 3 - r); the tiles
@@ -246,31 +277,15 @@ __global__ __launch_bounds__(SNT) void scan_kernel(ScanArgs a) {
     const int tx = min(t0 + min(xr, SC - 1), last), cx = min(c0 + xc, a.P - 4);
     q.x = quad(a.x + tx * a.xs + (int64_t)h * a.P + cx);
     if (a.z) q.z = quad(a.z + tx * a.zs + (int64_t)h * a.P + cx);
-    q.dt = a.dt[min(t0 + lane, last) * a.ds + h];
+    q.dec = a.dec[((int64_t)(record_of(begin, b) + c) * a.NH + h) * (DEC * SC) + min(wave, DEC - 1) * SC + lane];
   };
-  // x by column, and the decays of a chunk (one wave, the one without products of
-  // C B^T): logarithms are summed in fp64 and kept in two halves, so that
-  // differences of long sums keep their precision
+  // x by column, and the decays of a chunk
   const auto stage = [&](int c, const Regs &q) {
     const int p = c & 1;
     if (xr < SC)
 #pragma unroll
       for (int e = 0; e < 4; e++) L.xt[p][xc + e][xr] = q.x[e];
-    if (wave == 7) {
-      const bool in = begin + c * SC + lane < end;
-      const float d = in ? step_of(q.dt, bias, a.softplus) : 0.0f;
-      const double s = scan64(in ? (double)d * A : 0.0);
-      const uint64_t u = __builtin_bit_cast(uint64_t, s);
-      const double sc = __builtin_bit_cast(
-          double, (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(u >> 32), 63) << 32 |
-                      (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)u, 63));
-      const float lh = (float)s;
-      L.lh[p][lane] = lh;
-      L.ll[p][lane] = (float)(s - (double)lh);
-      L.dl[p][lane] = d;
-      L.wj[p][lane] = d * __builtin_amdgcn_exp2f((float)(sc - s));
-      L.el[p][lane] = __builtin_amdgcn_exp2f(lh);
-    }
+    if (wave < DEC) L.dec[p][wave][lane] = q.dec;
   };
 
   const int64_t src = seq_src(a.q, b), dst = seq_dst(a.q, b);
@@ -303,28 +318,29 @@ __global__ __launch_bounds__(SNT) void scan_kernel(ScanArgs a) {
     for (int s = 0; s < CF; s++)
       mm4(q.c[s], quad(&L.st[p][16 * ct + l16][kh * (N / KH) + 16 * s + 4 * lq]), y0, y1);
     // S
-    const float eC = L.el[p][SC - 1];
+    const auto &dec = L.dec[p];
+    const float eC = dec[DEC_EL][SC - 1];
 #pragma unroll
     for (int i = 0; i < TPW; i++) {
       v4f s1 = {0.f, 0.f, 0.f, 0.f};
       S[i] *= eC;
 #pragma unroll
       for (int s = 0; s < 4; s++) {
-        const v4f w = quad(&L.wj[p][16 * s + 4 * lq]);
+        const v4f w = quad(&dec[DEC_WJ][16 * s + 4 * lq]);
         mm4(v4f{q.b[i][4 * s], q.b[i][4 * s + 1], q.b[i][4 * s + 2], q.b[i][4 * s + 3]}, w * xt[s], S[i], s1);
       }
       S[i] += s1;
     }
-    y0 = (y0 + y1) * quad(&L.el[p][16 * r + 4 * lq]);
+    y0 = (y0 + y1) * quad(&dec[DEC_EL][16 * r + 4 * lq]);
     // (C B^T o decays) x
-    const float lhi = L.lh[p][16 * r + l16], lli = L.ll[p][16 * r + l16];
+    const float lhi = dec[DEC_LH][16 * r + l16], lli = dec[DEC_LL][16 * r + l16];
     y1 = v4f{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int s = 0; s < GF; s++) {
       const int j = KH == 2 ? kh + 2 * s : s;
       if (j > r) continue;
-      const v4f lh = quad(&L.lh[p][16 * j + 4 * lq]), ll = quad(&L.ll[p][16 * j + 4 * lq]);
-      const v4f dl = quad(&L.dl[p][16 * j + 4 * lq]);
+      const v4f lh = quad(&dec[DEC_LH][16 * j + 4 * lq]), ll = quad(&dec[DEC_LL][16 * j + 4 * lq]);
+      const v4f dl = quad(&dec[DEC_DL][16 * j + 4 * lq]);
       v4f w;
 #pragma unroll
       for (int e = 0; e < 4; e++) {
@@ -386,7 +402,7 @@ int ssm_sizes(const w4a8_seqs *q, const w4a8_ssm *m, int64_t T) {
     return W4A8_ESHAPE;
   // (a grid's threads are counted in 32 bits)
   if (m->NH >= (1 << 16) || m->P > 4096 || q->B * m->NH * m->P >= ((int64_t)1 << 27) ||
-      (T / SC + q->B + 1) * m->NG >= ((int64_t)1 << 23))
+      (T / SC + q->B + 1) * (m->NG + m->NH) >= ((int64_t)1 << 23))
     return W4A8_ERANGE;
   return W4A8_OK;
 }
@@ -398,7 +414,8 @@ int launch_ssm(ScanArgs a, hipStream_t s) {
     step_kernel<N, 64><<<dim3((unsigned)(a.q.B * a.NH * a.nsl)), dim3(STEP_NT), 0, s>>>(a);
     return check_launch();
   }
-  gram_kernel<N><<<dim3((unsigned)(records(a.q) * a.NG)), dim3(256), 0, s>>>(a);
+  const unsigned ngram = (unsigned)(records(a.q) * a.NG), ndec = (unsigned)(records(a.q) * ((a.NH + 3) / 4));
+  prep_kernel<N><<<dim3(ngram + ndec), dim3(256), 0, s>>>(a, ngram);
   if (int rc = check_launch(); rc != W4A8_OK) return rc;
   constexpr int PS = N == 64 ? 32 : 16;
   a.nsl = (a.P + PS - 1) / PS;
@@ -415,7 +432,7 @@ using namespace w4a8;
 
 extern "C" size_t ssm_workspace_size(const w4a8_seqs *seqs, const w4a8_ssm *ssm, int64_t T) {
   if (ssm_sizes(seqs, ssm, T) != W4A8_OK) return 0;
-  return ((size_t)(T / SC + seqs->B + 1) * ssm->NG * REC + 64) * sizeof(float);
+  return (size_t)(T / SC + seqs->B + 1) * (ssm->NG * REC + ssm->NH * DEC * SC) * sizeof(float);
 }
 
 extern "C" int ssm_scan(const w4a8_seqs *seqs, const w4a8_ssm *m, float *state, float *y,
@@ -448,6 +465,7 @@ extern "C" int ssm_scan(const w4a8_seqs *seqs, const w4a8_ssm *m, float *state, 
   a.x = m->x; a.dt = m->dt; a.b = m->b; a.c = m->c; a.z = m->z;
   a.A = m->A; a.D = m->D; a.bias = m->dt_bias;
   a.state = state; a.y = y; a.gram = reinterpret_cast<float *>(workspace);
+  a.dec = a.gram + records(a.q) * m->NG * REC;
   a.xs = m->x_stride; a.ds = m->dt_stride; a.bs = m->b_stride; a.cs = m->c_stride;
   a.zs = m->z_stride; a.ys = y_stride;
   a.NH = (int)m->NH; a.NG = (int)m->NG; a.G = (int)(m->NH / m->NG); a.P = (int)m->P;
