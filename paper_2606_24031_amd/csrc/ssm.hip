@@ -20,7 +20,7 @@ struct ScanArgs {
   Seqs q;
   const float *x, *dt, *b, *c, *z, *A, *D, *bias;
   float *state, *y, *gram, *dec;    // gram, dec: the workspace
-  int64_t xs, ds, bs, cs, zs, ys;
+  int xs, ds, bs, cs, zs, ys;       // strides
   int NH, G, NG, P, nsl;            // heads, heads of a group, groups, columns, slices of columns
   int softplus;
 };
@@ -52,10 +52,10 @@ __device__ __forceinline__ void step_rows(const ScanArgs &a, int b, int h, int c
                ? *reinterpret_cast<const v4f *>(a.state + ((src * a.NH + h) * N + r0 + RG * m) * a.P + c)
                : v4f{0.f, 0.f, 0.f, 0.f};
   for (int t = begin; t < end; t++) {
-    const float *bt = a.b + t * a.bs + (int64_t)g * N, *ct = a.c + t * a.cs + (int64_t)g * N;
-    const v4f x = live ? *reinterpret_cast<const v4f *>(a.x + t * a.xs + (int64_t)h * a.P + c)
+    const float *bt = a.b + (int64_t)t * a.bs + (int64_t)g * N, *ct = a.c + (int64_t)t * a.cs + (int64_t)g * N;
+    const v4f x = live ? *reinterpret_cast<const v4f *>(a.x + (int64_t)t * a.xs + (int64_t)h * a.P + c)
                        : v4f{0.f, 0.f, 0.f, 0.f};
-    const float d = step_of(a.dt[t * a.ds + h], bias, a.softplus);
+    const float d = step_of(a.dt[(int64_t)t * a.ds + h], bias, a.softplus);
     const float keep = expf(d * A);
     const v4f dx = d * x;
     v4f y = {0.f, 0.f, 0.f, 0.f};
@@ -79,10 +79,10 @@ __device__ __forceinline__ void step_rows(const ScanArgs &a, int b, int h, int c
 #pragma unroll
       for (int w = 0; w < NT / 64; w++) s += *reinterpret_cast<const v4f *>(&red[w][4 * tid]);
       if (a.z) {
-        const v4f z = *reinterpret_cast<const v4f *>(a.z + t * a.zs + (int64_t)h * a.P + c);
+        const v4f z = *reinterpret_cast<const v4f *>(a.z + (int64_t)t * a.zs + (int64_t)h * a.P + c);
         s *= v4f{silu_f32(z.x), silu_f32(z.y), silu_f32(z.z), silu_f32(z.w)};
       }
-      *reinterpret_cast<v4f *>(a.y + t * a.ys + (int64_t)h * a.P + c) = s;
+      *reinterpret_cast<v4f *>(a.y + (int64_t)t * a.ys + (int64_t)h * a.P + c) = s;
     }
     __syncthreads();                // red is rewritten for the next row
   }
@@ -174,7 +174,7 @@ __global__ __launch_bounds__(256) void prep_kernel(ScanArgs a, unsigned ngram) {
     if (h >= a.NH) return;
     const double A = (double)a.A[h] * 1.4426950408889634;
     const int t = t0 + lane;
-    const float d = t < end ? step_of(a.dt[min(t, end - 1) * a.ds + h], a.bias ? a.bias[h] : 0.0f, a.softplus)
+    const float d = t < end ? step_of(a.dt[(int64_t)min(t, end - 1) * a.ds + h], a.bias ? a.bias[h] : 0.0f, a.softplus)
                             : 0.0f;
     const double s = scan64(t < end ? (double)d * A : 0.0);
     const uint64_t u = __builtin_bit_cast(uint64_t, s);
@@ -191,12 +191,12 @@ __global__ __launch_bounds__(256) void prep_kernel(ScanArgs a, unsigned ngram) {
     return;
   }
   const int r = wave, g = part, l16 = lane & 15, lq = lane >> 4;
-  const float *cp = a.c + min(t0 + 16 * r + l16, end - 1) * a.cs + (int64_t)g * N + 4 * lq;
+  const float *cp = a.c + (int64_t)min(t0 + 16 * r + l16, end - 1) * a.cs + (int64_t)g * N + 4 * lq;
   v4f c[N / 16];
 #pragma unroll
   for (int s = 0; s < N / 16; s++) c[s] = quad(cp + 16 * s);
   for (int j = 0; j <= r; j++) {
-    const float *bp = a.b + min(t0 + 16 * j + l16, end - 1) * a.bs + (int64_t)g * N + 4 * lq;
+    const float *bp = a.b + (int64_t)min(t0 + 16 * j + l16, end - 1) * a.bs + (int64_t)g * N + 4 * lq;
     v4f s0 = {0.f, 0.f, 0.f, 0.f}, s1 = s0;
 #pragma unroll
     for (int s = 0; s < N / 16; s++) mm4(quad(bp + 16 * s), c[s], s0, s1);
@@ -204,14 +204,6 @@ __global__ __launch_bounds__(256) void prep_kernel(ScanArgs a, unsigned ngram) {
         s0 + s1;
   }
 }
-
-// What a lane has in registers of a chunk, loaded a chunk ahead.
-template <int CF, int BF, int GF>
-struct ChunkRegs {
-  v4f c[CF], g[GF], x, z;           // pieces of C, of C B^T; four columns of a row of x and z
-  float b[BF][16];                  // B of 16 rows for a column of each of its tiles
-  float dec;                        // of one of the decay arrays (waves 0 .. 4) a row
-};
 
 template <int N, int PS>
 struct ScanLds {
@@ -239,7 +231,8 @@ __global__ __launch_bounds__(SNT) void scan_kernel(ScanArgs a) {
   const int k = blockIdx.x >> 3, bh = (k / a.nsl) * 8 + (blockIdx.x & 7);
   if (bh >= a.q.B * a.NH) return;
   const int b = bh / a.NH, h = bh % a.NH, g = h / a.G, c0 = (k % a.nsl) * PS;
-  const int begin = seq_begin(a.q, b), end = seq_begin(a.q, b + 1);
+  const int begin = __builtin_amdgcn_readfirstlane(seq_begin(a.q, b)),
+            end = __builtin_amdgcn_readfirstlane(seq_begin(a.q, b + 1));
   if (begin >= end) return;
   if (end - begin <= STEP_T) {
     step_rows<N, PS, SNT>(a, b, h, c0, begin, end, L.red);
@@ -256,36 +249,65 @@ __global__ __launch_bounds__(SNT) void scan_kernel(ScanArgs a) {
   int nt[TPW], sct[TPW];
 #pragma unroll
   for (int i = 0; i < TPW; i++) { nt[i] = (wave + 8 * i) % NT; sct[i] = (wave + 8 * i) / NT; }
+  constexpr int XW = PS / 4;                     // waves that have a row of x
   const int xr = tid / (PS / 4), xc = 4 * (tid % (PS / 4));
-  const bool xlive = xr < SC && c0 + xc < a.P;
 
-  using Regs = ChunkRegs<CF, TPW, GF>;
-  const auto load = [&](int c, Regs &q) {
-    const int t0 = begin + c * SC, last = end - 1;
-    const float *cp = a.c + min(t0 + 16 * r + l16, last) * a.cs + (int64_t)g * N + kh * (N / KH) + 4 * lq;
+  // Rows of a chunk are read as buffers that end at the sequence's last row: past
+  // it, and past the last chunk, loads give zeros, so none needs a condition.
+  // (The number of rows by way of readfirstlane: a clamp is a VALU operation, and
+  // the buffer's words belong in scalar registers.)
+  const auto rows = [&](const float *p, int stride, int c, bool there = true) {
+    const int left = __builtin_amdgcn_readfirstlane(there ? min(max(end - begin - c * SC, 0), SC) : 0);
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<float *>(p + (begin + (int64_t)c * SC) * stride), 0,
+                                             (int)((uint32_t)left * (uint32_t)stride * 4u), 0x00027000);
+  };
+  const auto load4 = [](__amdgpu_buffer_rsrc_t q, uint32_t at, uint32_t more) {
+    return __builtin_bit_cast(v4f, __builtin_amdgcn_raw_buffer_load_b128(q, at, more, 0));
+  };
+  const uint32_t cat = 4u * ((16 * r + l16) * (uint32_t)a.cs + kh * (N / KH) + 4 * lq);
+  uint32_t bat[4];                               // (row e of four and the lane's column)
 #pragma unroll
-    for (int s = 0; s < CF; s++) q.c[s] = quad(cp + 16 * s);
-    const float *gp = a.gram + ((int64_t)(record_of(begin, b) + c) * a.NG + g) * REC + 4 * lane;
+  for (int e = 0; e < 4; e++) bat[e] = 4u * ((4 * lq + e) * (uint32_t)a.bs + 16 * (wave % NT) + l16);
+  const int xrow = min(xr, SC - 1), cx = min(xc, a.P - 4 - c0);
+  const uint32_t xat = 4u * (xrow * (uint32_t)a.xs + cx), zat = 4u * (xrow * (uint32_t)a.zs + cx);
+  const int rec0 = record_of(begin, b);
+  // A chunk's operands have one set of registers each: the next chunk's are
+  // loaded into them behind their last use, a step ahead of their own.
+  v4f cf[CF], gf[GF], xcur, xnext, z;
+  float bf[TPW][16], dec1;                       // B of 16 rows for a column of each tile; one of the decay arrays
+  const auto load_c = [&](int c) {
+    const auto q = rows(a.c + (int64_t)g * N, a.cs, c);
 #pragma unroll
-    for (int s = 0; s < GF; s++) q.g[s] = quad(gp + tile_at(r, min(KH == 2 ? kh + 2 * s : s, r)));
+    for (int s = 0; s < CF; s++) cf[s] = load4(q, cat, 64 * s);
+  };
+  const auto load_b = [&](int c) {
+    const auto q = rows(a.b + (int64_t)g * N, a.bs, c);
 #pragma unroll
     for (int i = 0; i < TPW; i++)
 #pragma unroll
       for (int e = 0; e < 16; e++)
-        q.b[i][e] = a.b[min(t0 + 16 * (e >> 2) + 4 * lq + (e & 3), last) * a.bs + (int64_t)g * N +
-                        16 * nt[i] + l16];
-    const int tx = min(t0 + min(xr, SC - 1), last), cx = min(c0 + xc, a.P - 4);
-    q.x = quad(a.x + tx * a.xs + (int64_t)h * a.P + cx);
-    if (a.z) q.z = quad(a.z + tx * a.zs + (int64_t)h * a.P + cx);
-    q.dec = a.dec[((int64_t)(record_of(begin, b) + c) * a.NH + h) * (DEC * SC) + min(wave, DEC - 1) * SC + lane];
+        bf[i][e] = __builtin_bit_cast(
+            float, __builtin_amdgcn_raw_buffer_load_b32(
+                       q, bat[e & 3], 64u * (e >> 2) * (uint32_t)a.bs + (TPW > 1 ? 512 * i : 0), 0));
   };
-  // x by column, and the decays of a chunk
-  const auto stage = [&](int c, const Regs &q) {
-    const int p = c & 1;
-    if (xr < SC)
+  const auto load_g = [&](int c) {
+    const float *const gp = a.gram + ((int64_t)(rec0 + min(c, nch - 1)) * a.NG + g) * REC;
 #pragma unroll
-      for (int e = 0; e < 4; e++) L.xt[p][xc + e][xr] = q.x[e];
-    if (wave < DEC) L.dec[p][wave][lane] = q.dec;
+    for (int s = 0; s < GF; s++) gf[s] = quad(gp + tile_at(r, min(KH == 2 ? kh + 2 * s : s, r)) + 4 * lane);
+  };
+  const auto load_x = [&](int c) {
+    xnext = load4(rows(a.x + (int64_t)h * a.P + c0, a.xs, c), xat, 0);
+    dec1 = a.dec[((int64_t)(rec0 + min(c, nch - 1)) * a.NH + h) * (DEC * SC) + min(wave, DEC - 1) * SC + lane];
+  };
+  const float *const zh = a.z ? a.z + (int64_t)h * a.P + c0 : a.x;
+  const auto load_z = [&](int c) { z = load4(rows(zh, a.zs, c, a.z != nullptr), zat, 0); };
+  // x by column, and the decays of a chunk
+  const auto stage = [&](int p) {
+    if (wave < XW)
+#pragma unroll
+      for (int e = 0; e < 4; e++) L.xt[p][xc + e][xr] = xnext[e];
+    if (wave < DEC) L.dec[p][wave][lane] = dec1;
+    xcur = xnext;
   };
 
   const int64_t src = seq_src(a.q, b), dst = seq_dst(a.q, b);
@@ -305,10 +327,19 @@ __global__ __launch_bounds__(SNT) void scan_kernel(ScanArgs a) {
       *reinterpret_cast<v4f *>(&L.st[p][16 * sct[i] + l16][16 * nt[i] + 4 * lq]) = S[i];
   };
 
-  // chunk c: its registers in `q`, its x, decays and state in LDS; `nx` the next one's
-  const auto step = [&](int c, Regs &q, Regs &nx) {
+  load_x(0);
+  load_c(0);
+  load_b(0);
+  load_g(0);
+  load_z(0);
+  put_state(0);
+  stage(0);
+  load_x(1);
+  v4f xe = xcur;                                 // x of the chunk whose outputs are written
+  __syncthreads();
+  for (int c = 0; c < nch; c++) {
     const int p = c & 1;
-    if (c + 1 < nch) load(c + 1, nx);
+    const auto &dec = L.dec[p];
     v4f xt[4];
 #pragma unroll
     for (int s = 0; s < 4; s++) xt[s] = quad(&L.xt[p][16 * ct + l16][16 * s + 4 * lq]);
@@ -316,9 +347,9 @@ __global__ __launch_bounds__(SNT) void scan_kernel(ScanArgs a) {
     v4f y0 = {0.f, 0.f, 0.f, 0.f}, y1 = y0;
 #pragma unroll
     for (int s = 0; s < CF; s++)
-      mm4(q.c[s], quad(&L.st[p][16 * ct + l16][kh * (N / KH) + 16 * s + 4 * lq]), y0, y1);
+      mm4(cf[s], quad(&L.st[p][16 * ct + l16][kh * (N / KH) + 16 * s + 4 * lq]), y0, y1);
+    load_c(c + 1);
     // S
-    const auto &dec = L.dec[p];
     const float eC = dec[DEC_EL][SC - 1];
 #pragma unroll
     for (int i = 0; i < TPW; i++) {
@@ -327,10 +358,11 @@ __global__ __launch_bounds__(SNT) void scan_kernel(ScanArgs a) {
 #pragma unroll
       for (int s = 0; s < 4; s++) {
         const v4f w = quad(&dec[DEC_WJ][16 * s + 4 * lq]);
-        mm4(v4f{q.b[i][4 * s], q.b[i][4 * s + 1], q.b[i][4 * s + 2], q.b[i][4 * s + 3]}, w * xt[s], S[i], s1);
+        mm4(v4f{bf[i][4 * s], bf[i][4 * s + 1], bf[i][4 * s + 2], bf[i][4 * s + 3]}, w * xt[s], S[i], s1);
       }
       S[i] += s1;
     }
+    load_b(c + 1);
     y0 = (y0 + y1) * quad(&dec[DEC_EL][16 * r + 4 * lq]);
     // (C B^T o decays) x
     const float lhi = dec[DEC_LH][16 * r + l16], lli = dec[DEC_LL][16 * r + l16];
@@ -344,41 +376,30 @@ __global__ __launch_bounds__(SNT) void scan_kernel(ScanArgs a) {
       v4f w;
 #pragma unroll
       for (int e = 0; e < 4; e++) {
-        w[e] = q.g[s][e] * (dl[e] * __builtin_amdgcn_exp2f((lhi - lh[e]) + (lli - ll[e])));
+        w[e] = gf[s][e] * (dl[e] * __builtin_amdgcn_exp2f((lhi - lh[e]) + (lli - ll[e])));
         if (16 * j + 4 * lq + e > 16 * r + l16) w[e] = 0.0f;
       }
-      v4f xs = xt[0];
-#pragma unroll
-      for (int m = 1; m < 4; m++)
-        if (m == j) xs = xt[m];
-      mm4(w, xs, y0, y1);
+      mm4(w, KH == 2 ? (kh ? xt[2 * s + 1] : xt[2 * s]) : xt[s], y0, y1);
     }
+    load_g(c + 1);
     y0 += y1;
 #pragma unroll
     for (int e = 0; e < 4; e++) L.yl[p][kh][16 * r + 4 * lq + e][16 * ct + l16] = y0[e];
-    if (c + 1 < nch) {
-      put_state(p ^ 1);
-      stage(c + 1, nx);
-    }
+    put_state(p ^ 1);
+    stage(p ^ 1);                                // (past the last chunk unused)
+    load_x(c + 2);
     __syncthreads();
-    if (xlive && begin + c * SC + xr < end) {
+    if (wave < XW) {
       v4f o = quad(&L.yl[p][0][xr][xc]);
       if (KH == 2) o += quad(&L.yl[p][1][xr][xc]);
-      o += D * q.x;
-      if (a.z) o *= v4f{silu_f32(q.z.x), silu_f32(q.z.y), silu_f32(q.z.z), silu_f32(q.z.w)};
-      *reinterpret_cast<v4f *>(a.y + (int64_t)(begin + c * SC + xr) * a.ys + (int64_t)h * a.P + c0 + xc) = o;
+      o += D * xe;
+      if (a.z) o *= v4f{silu_f32(z.x), silu_f32(z.y), silu_f32(z.z), silu_f32(z.w)};
+      const int t = begin + c * SC + xr;
+      if (t < end && c0 + xc < a.P)
+        *reinterpret_cast<v4f *>(a.y + (int64_t)t * a.ys + (int64_t)h * a.P + c0 + xc) = o;
     }
-  };
-  Regs ra, rb;
-  load(0, ra);
-  put_state(0);
-  stage(0, ra);
-  __syncthreads();
-  for (int c = 0;;) {
-    step(c, ra, rb);
-    if (++c >= nch) break;
-    step(c, rb, ra);
-    if (++c >= nch) break;
+    xe = xcur;
+    load_z(c + 1);
   }
   if (dst >= 0)
 #pragma unroll
@@ -439,11 +460,12 @@ extern "C" int ssm_scan(const w4a8_seqs *seqs, const w4a8_ssm *m, float *state, 
                         int64_t y_stride, int64_t T, void *workspace, size_t ws_bytes, void *stream) {
   int rc = ssm_sizes(seqs, m, T);
   if (rc != W4A8_OK) return rc;
-  const int64_t xrow = m->NH * m->P, brow = m->NG * m->N, top = (int64_t)1 << 31;
+  const int64_t xrow = m->NH * m->P, brow = m->NG * m->N, top = (int64_t)1 << 24;
   if (m->x_stride < xrow || m->x_stride % 4 != 0 || m->b_stride < brow || m->b_stride % 4 != 0 ||
       m->c_stride < brow || m->c_stride % 4 != 0 || m->dt_stride < m->NH || y_stride < xrow ||
       y_stride % 4 != 0 || (m->z && (m->z_stride < xrow || m->z_stride % 4 != 0)))
     return W4A8_ESHAPE;
+  // (a chunk's rows are addressed in 32 bits)
   if (m->x_stride >= top || m->b_stride >= top || m->c_stride >= top || m->dt_stride >= top ||
       y_stride >= top || (m->z && m->z_stride >= top))
     return W4A8_ERANGE;
@@ -466,8 +488,8 @@ extern "C" int ssm_scan(const w4a8_seqs *seqs, const w4a8_ssm *m, float *state, 
   a.A = m->A; a.D = m->D; a.bias = m->dt_bias;
   a.state = state; a.y = y; a.gram = reinterpret_cast<float *>(workspace);
   a.dec = a.gram + records(a.q) * m->NG * REC;
-  a.xs = m->x_stride; a.ds = m->dt_stride; a.bs = m->b_stride; a.cs = m->c_stride;
-  a.zs = m->z_stride; a.ys = y_stride;
+  a.xs = (int)m->x_stride; a.ds = (int)m->dt_stride; a.bs = (int)m->b_stride; a.cs = (int)m->c_stride;
+  a.zs = (int)m->z_stride; a.ys = (int)y_stride;
   a.NH = (int)m->NH; a.NG = (int)m->NG; a.G = (int)(m->NH / m->NG); a.P = (int)m->P;
   a.softplus = m->softplus;
   hipStream_t s = as_stream(stream);

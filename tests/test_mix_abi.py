@@ -119,11 +119,14 @@ def test_scan_errors():
                dict(c_stride=66), dict(z_stride=120), dict(z_stride=129), dict(dt_stride=1)):
         assert scan_call(m=ssm(**kw)) == w4.ESHAPE, kw
     assert scan_call(ys=124) == w4.ESHAPE and scan_call(ys=130) == w4.ESHAPE
-    for kw in (dict(NH=1 << 16), dict(P=4112), dict(x_stride=TOP), dict(b_stride=TOP), dict(c_stride=TOP),
-               dict(dt_stride=TOP), dict(z_stride=TOP)):
+    for kw in (dict(NH=1 << 16), dict(P=4112), dict(x_stride=1 << 24), dict(b_stride=1 << 24),
+               dict(c_stride=1 << 24), dict(dt_stride=1 << 24), dict(z_stride=1 << 24)):
         assert scan_call(m=ssm(**kw)) in (w4.ERANGE, w4.ESHAPE), kw
     assert scan_call(m=ssm(P=4112, x_stride=1 << 14, z_stride=1 << 14), ys=1 << 14) == w4.ERANGE
-    assert scan_call(ys=TOP) == w4.ERANGE
+    assert scan_call(ys=1 << 24) == w4.ERANGE
+    assert scan_call(q=seqs(B=(1 << 20) - 1), m=ssm(NH=4, x_stride=256, z_stride=256, dt_stride=4), ys=256) == w4.ERANGE
+    assert scan_call(T=1 << 29) == w4.ERANGE
+    assert w4.lib().ssm_workspace_size(ctypes.byref(seqs()), ctypes.byref(ssm()), 1 << 29) == 0
     for kw in (dict(x=A + 4), dict(b=A + 8), dict(c=A + 4), dict(z=A + 4), dict(dt=A + 2), dict(A=A + 1),
                dict(D=A + 3), dict(dt_bias=A + 2)):
         assert scan_call(m=ssm(**kw)) == w4.EALIGN, kw
