@@ -471,7 +471,7 @@ int token_logprobs(const float *logits, int64_t stride, const int32_t *targets, 
  * q8_row_quantize: x fp32, row r at r * x_stride elements (a slice of wider
  *   rows works), x 4-byte aligned.  Bit-identical to the definition.
  * Errors: rows < 0, K < 1, x_stride < K -> W4A8_ESHAPE; K >= 2^17, rows >=
- * 2^31 or x_stride >= 2^31 -> W4A8_ERANGE; a NULL pointer -> W4A8_ENULL; q not
+ * 2^24 or x_stride >= 2^31 -> W4A8_ERANGE; a NULL pointer -> W4A8_ENULL; q not
  * 16-, x or d not 4-byte aligned -> W4A8_EALIGN.  rows == 0 is a no-op.
  * q8_row_bytes returns 0 for an invalid K.
  */
@@ -490,8 +490,8 @@ int q8_row_quantize(const float *x, int64_t x_stride, int8_t *q, float *d, int64
  *   are multiplied too: they are zero in at least one of the two, as the
  *   quantizer writes them); xd [M], wd [N], bias [N] fp32; y fp32, row m at
  *   m * y_stride elements, written.  One launch, no workspace.
- * Errors: M < 0, N < 1, K < 1, y_stride < N -> W4A8_ESHAPE; K >= 2^17, M or N
- * >= 2^31, y_stride >= 2^31 -> W4A8_ERANGE; a NULL pointer (but bias) ->
+ * Errors: M < 0, N < 1, K < 1, y_stride < N -> W4A8_ESHAPE; K >= 2^17, y_stride
+ * >= 2^31 or 2^22 tiles of 64 rows by 128 channels or more -> W4A8_ERANGE; a NULL pointer (but bias) ->
  * W4A8_ENULL; xq or wq not 16-, xd, wd, bias or y not 4-byte aligned ->
  * W4A8_EALIGN; y equal to an operand -> W4A8_EALIAS.  M == 0 is a no-op.
  */

@@ -66,6 +66,7 @@
 // takes 132 and 80 us for gate/up and down of 947 tokens.
 #include <algorithm>
 
+#include "dma_dev.h"
 #include "w4a8_dev.h"
 #include "w4a8_host.h"
 
@@ -139,31 +140,6 @@ struct MLds {
   uint4 ring[RING_BYTES / 16];
   float dw[4][SB][32];             // weight-row scales of the current stage, [wave][block][row]
 };
-
-// Direct load of 16 bytes per active lane into LDS at dst + 16 * lane.
-// Written as an instruction the compiler does not model: through the builtin
-// it cannot tell a copy into one slot from reads of another, and waits for
-// every outstanding load before reading LDS.  The copies are ordered by the
-// explicit wait and barrier at the top of the stage that reads them.
-// M0 is named as clobbered; nothing else in these kernels keeps a value in it.
-#pragma clang diagnostic push
-#pragma clang diagnostic ignored "-Winline-asm"
-__device__ __forceinline__ void lds_dma16(const uint8_t *src, const void *dst) {
-  const uint32_t m0 =
-      (uint32_t)(uintptr_t)(const void __attribute__((address_space(3))) *)dst;
-  asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off"
-               :
-               : "v"(src), "s"(m0)
-               : "memory", "m0");
-}
-#pragma clang diagnostic pop
-
-// All but this wave's youngest N vector memory operations are done, its LDS
-// reads too, and so for every other wave of the workgroup.
-template <int N>
-__device__ __forceinline__ void wait_barrier() {
-  asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");
-}
 
 // Dwords of a weight row in a slot: block j's fp16 scale and payload.  A
 // stage of Q4_0 is half a 144-byte group: the first half is loaded as bytes

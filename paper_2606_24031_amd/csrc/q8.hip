@@ -1,5 +1,6 @@
 // 8-bit rows: int8 codes with one fp32 scale a row (the quantizer), and the
 // product of activation rows with weight rows in exact int32 sums.
+#include "dma_dev.h"
 #include "w4a8_dev.h"
 #include "w4a8_host.h"
 
@@ -9,98 +10,318 @@ namespace {
 
 constexpr int QNT = 256;            // threads of a quantizing workgroup: one row
 constexpr int TNT = 256;            // ... of a product tile: four waves
+constexpr int KNT = 512;            // ... of a product of few rows: eight waves
 constexpr int PAD = W4A8_Q8_ROW_PAD;
 
 typedef int v4i __attribute__((ext_vector_type(4)));
+typedef int v16i __attribute__((ext_vector_type(16)));
 typedef float v4f __attribute__((ext_vector_type(4)));
 
-// One row a workgroup: its largest magnitude, then the codes, four a thread.
-__global__ __launch_bounds__(QNT) void q8_row_kernel(const float *__restrict__ x, int64_t xs,
-                                                     int8_t *__restrict__ q, float *__restrict__ d,
-                                                     int K, int KP) {
+// ------------------------------------------------------------------ quantizer
+__device__ __forceinline__ int odd_value(float v) { return !(fabsf(v) < __builtin_inff()); }
+__device__ __forceinline__ uint32_t code(float v, float id) { return (uint32_t)round_clamp(v * id, 127) & 0xFFu; }
+
+// The row's scale and its inverse from each thread's largest magnitude and
+// whether it saw a NaN or an infinity.
+__device__ __forceinline__ float row_scale(float amax, int odd, float &id) {
   __shared__ float top[QNT / 64];
   __shared__ int bad[QNT / 64];
-  const int64_t r = blockIdx.x;
-  const float *xr = x + r * xs;
-  float amax = 0.0f;
-  int odd = 0;                      // a NaN or an infinity
-  for (int k = threadIdx.x; k < K; k += QNT) {
-    const float v = fabsf(xr[k]);
-    odd |= !(v < __builtin_inff());
-    amax = fmaxf(amax, v);
-  }
 #pragma unroll
-  for (int o = 32; o > 0; o >>= 1) {
-    amax = fmaxf(amax, __shfl_xor(amax, o));
-    odd |= __shfl_xor(odd, o);
-  }
+  for (int o = 32; o > 0; o >>= 1) amax = fmaxf(amax, __shfl_xor(amax, o));
+  odd = __any(odd);
   if ((threadIdx.x & 63) == 0) { top[threadIdx.x >> 6] = amax; bad[threadIdx.x >> 6] = odd; }
   __syncthreads();
 #pragma unroll
   for (int w = 0; w < QNT / 64; w++) { amax = fmaxf(amax, top[w]); odd |= bad[w]; }
-  const float dr = odd ? __builtin_nanf("") : amax * (1.0f / 127.0f);
-  const float id = odd ? 0.0f : sym_inverse(dr);
+  const float d = odd ? __builtin_nanf("") : amax * (1.0f / 127.0f);
+  id = odd ? 0.0f : sym_inverse(d);
+  return d;
+}
+
+// One row a workgroup, in registers: V times four values a thread, K a multiple
+// of 4 and rows 16-byte aligned.
+template <int V>
+__global__ __launch_bounds__(QNT) void q8_row_kernel(const float *__restrict__ x, int64_t xs,
+                                                     int8_t *__restrict__ q, float *__restrict__ d,
+                                                     int K, int KP) {
+  const int64_t r = blockIdx.x;
+  const float *xr = x + r * xs;
+  v4f v[V];
+  float amax = 0.0f;
+  int odd = 0;
+#pragma unroll
+  for (int i = 0; i < V; i++) {
+    const int k = 4 * (threadIdx.x + QNT * i);
+    v[i] = k < K ? *reinterpret_cast<const v4f *>(xr + k) : v4f{0.f, 0.f, 0.f, 0.f};
+  }
+#pragma unroll
+  for (int i = 0; i < V; i++)
+#pragma unroll
+    for (int e = 0; e < 4; e++) {
+      odd |= odd_value(v[i][e]);
+      amax = fmaxf(amax, fabsf(v[i][e]));
+    }
+  float id;
+  const float dr = row_scale(amax, odd, id);
+  if (threadIdx.x == 0) d[r] = dr;
+#pragma unroll
+  for (int i = 0; i < V; i++) {
+    const int k = 4 * (threadIdx.x + QNT * i);
+    if (k < KP)
+      *reinterpret_cast<uint32_t *>(q + r * KP + k) =
+          dr == dr ? code(v[i][0], id) | code(v[i][1], id) << 8 | code(v[i][2], id) << 16 | code(v[i][3], id) << 24
+                   : 0u;
+  }
+}
+
+// Rows of any length and alignment, read twice.
+__global__ __launch_bounds__(QNT) void q8_any_row_kernel(const float *__restrict__ x, int64_t xs,
+                                                         int8_t *__restrict__ q, float *__restrict__ d,
+                                                         int K, int KP) {
+  const int64_t r = blockIdx.x;
+  const float *xr = x + r * xs;
+  float amax = 0.0f;
+  int odd = 0;
+  for (int k = threadIdx.x; k < K; k += QNT) {
+    odd |= odd_value(xr[k]);
+    amax = fmaxf(amax, fabsf(xr[k]));
+  }
+  float id;
+  const float dr = row_scale(amax, odd, id);
   if (threadIdx.x == 0) d[r] = dr;
   for (int k = 4 * threadIdx.x; k < KP; k += 4 * QNT) {
     uint32_t packed = 0;
 #pragma unroll
     for (int i = 0; i < 4; i++)
-      if (k + i < K && !odd) packed |= ((uint32_t)round_clamp(xr[k + i] * id, 127) & 0xFFu) << (8 * i);
+      if (k + i < K && dr == dr) packed |= code(xr[k + i], id) << (8 * i);
     *reinterpret_cast<uint32_t *>(q + r * KP + k) = packed;
   }
 }
 
+// ------------------------------------------------------------------ product
 struct QArgs {
   const int8_t *xq, *wq;
   const float *xd, *wd, *bias;
   float *y;
-  int64_t ys, M, N;
-  int KP, nt;                       // bytes of a row; tiles of 64 channels
+  int64_t ys;
+  int M, N, KP;
+  int mt, nt;                       // tiles of rows and of channels
+  int vec;                          // rows of y start 16-byte aligned
 };
 
-// 64 rows by 64 channels a workgroup, 32 x 32 a wave, operands straight from
-// memory: the weights are the A operand, so a lane holds four neighbouring
-// channels of one row.
-__global__ __launch_bounds__(TNT) void q8_tile_kernel(QArgs a) {
-  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, l16 = lane & 15, lq = lane >> 4;
-  const int64_t n0 = (int64_t)(blockIdx.x % a.nt) * 64 + 32 * (wave & 1);
-  const int64_t m0 = (int64_t)(blockIdx.x / a.nt) * 64 + 32 * (wave >> 1);
-  const int8_t *wp[2], *xp[2];
+// Four neighbouring channels of a row: scaled, plus bias, stored.
+__device__ __forceinline__ void put4(const QArgs &a, int m, int n, v4i s, float xd, v4f wd, v4f bias) {
+  v4f y;
 #pragma unroll
-  for (int i = 0; i < 2; i++) {
-    wp[i] = a.wq + min(n0 + 16 * i + l16, a.N - 1) * a.KP + 16 * lq;
-    xp[i] = a.xq + min(m0 + 16 * i + l16, a.M - 1) * a.KP + 16 * lq;
+  for (int e = 0; e < 4; e++) {
+    y[e] = (float)s[e] * (xd * wd[e]);
+    if (a.bias) y[e] += bias[e];
   }
-  v4i acc[2][2] = {};
-  for (int k = 0; k < a.KP; k += 64) {
-    v4i wv[2], xv[2];
+  float *p = a.y + (int64_t)m * a.ys + n;
+  if (a.vec && n + 4 <= a.N) {
+    *reinterpret_cast<v4f *>(p) = y;
+  } else {
 #pragma unroll
-    for (int i = 0; i < 2; i++) {
-      wv[i] = *reinterpret_cast<const v4i *>(wp[i] + k);
-      xv[i] = *reinterpret_cast<const v4i *>(xp[i] + k);
+    for (int e = 0; e < 4; e++)
+      if (n + e < a.N) p[e] = y[e];
+  }
+}
+__device__ __forceinline__ v4f load_channels(const QArgs &a, const float *p, int n) {
+  v4f v;
+#pragma unroll
+  for (int e = 0; e < 4; e++) v[e] = p[min(n + e, a.N - 1)];
+  return v;
+}
+
+// Tiles of TN channels by TM rows, four waves of RN by RM on 32 x 32 x 32
+// products; the weights are the A operand, so that element e of a sum in lane l
+// is channel 8 (e / 4) + 4 (l / 32) + e % 4 and row l % 32.  64 codes of every row
+// a stage, by direct loads into a ring of NS slots; the 16-byte pieces of a row
+// stand XOR-swizzled by the row, so that 16 lanes that read one piece of 16
+// rows meet distinct banks.
+template <int TN, int TM, int WN, int WM, int NS>
+struct Tile {
+  static constexpr int RN = TN / WN, RM = TM / WM, BN = RN / 32, BM = RM / 32;
+  static constexpr int SLOT = (TN + TM) * 64, PER = (TN + TM) / 16 / 4;
+  static constexpr int OS = RN + 4;                // row stride of a wave's output in LDS
+  static constexpr int LDS = NS * SLOT > 4 * 32 * OS * 4 ? NS * SLOT : 4 * 32 * OS * 4;
+  static_assert(WN * WM == 4 && BN * 32 == RN && BM * 32 == RM && PER * 64 == TN + TM && NS >= 3, "tile");
+};
+
+template <int TN, int TM, int WN, int WM, int NS>
+__global__ __launch_bounds__(TNT, 2) void q8_tile_kernel(QArgs a) {
+  using T = Tile<TN, TM, WN, WM, NS>;
+  __shared__ __align__(16) uint8_t lds[T::LDS];
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  // Each XCD (workgroup b runs on XCD b mod 8) takes an even contiguous share of
+  // the tiles, in the order of groups of 8 row tiles, within a group channels by
+  // channels: what runs on it at once shares rows and channels in its L2.
+  const int total = a.mt * a.nt, x = blockIdx.x & 7;
+  int w = x * (total >> 3) + min(x, total & 7) + (blockIdx.x >> 3);
+  const int g = w / (8 * a.nt), gm = min(8, a.mt - 8 * g);
+  w -= g * 8 * a.nt;
+  const int m0 = (8 * g + w % gm) * TM, n0 = (w / gm) * TN;
+
+  // direct loads: 16 rows of 64 bytes an instruction, rows past the last repeat it
+  const uint8_t *src[T::PER];
+  uint32_t off[T::PER];
+  const uint32_t piece = 16 * ((lane & 3) ^ ((lane >> 4) & 3));
+#pragma unroll
+  for (int u = 0; u < T::PER; u++) {
+    const int r = 16 * (wave + 4 * u);             // of the tile's TN + TM
+    const bool is_w = r < TN;
+    const int first = is_w ? n0 : m0, last = (is_w ? a.N : a.M) - 1;
+    src[u] = reinterpret_cast<const uint8_t *>(is_w ? a.wq : a.xq) + (int64_t)first * a.KP;
+    off[u] = (uint32_t)(min(first + r - (is_w ? 0 : TN) + (lane >> 2), last) - first) * (uint32_t)a.KP + piece;
+  }
+  const int S = a.KP / 64;
+  const auto load_stage = [&](int t) {
+    uint8_t *const slot = lds + (t % NS) * T::SLOT;
+#pragma unroll
+    for (int u = 0; u < T::PER; u++) lds_dma16(src[u] + t * 64, off[u], slot + 1024 * (wave + 4 * u));
+  };
+  const int wn = wave % WN, wm = wave / WN, l32 = lane & 31, lh = lane >> 5;
+  const int nl = n0 + wn * T::RN + 4 * l32;        // this lane's channels when rows are stored
+  v4f wd, bias = {0.f, 0.f, 0.f, 0.f};
+  float xd[T::BM];
+  wd = load_channels(a, a.wd, nl);
+  if (a.bias) bias = load_channels(a, a.bias, nl);
+#pragma unroll
+  for (int j = 0; j < T::BM; j++) xd[j] = a.xd[min(m0 + wm * T::RM + 32 * j + l32, a.M - 1)];
+#pragma unroll
+  for (int t = 0; t < NS - 1; t++)
+    if (t < S) load_stage(t);
+
+  const uint32_t at = l32 * 64 + 16 * (lh ^ ((l32 >> 2) & 3));
+  v16i acc[T::BN][T::BM] = {};
+  for (int t = 0; t < S; t++) {
+    // stage t has landed (the younger NS - 2 may be under way), and every wave is
+    // done with stage t - 1, whose slot the next loads fill
+    if (t + NS - 2 < S)
+      wait_barrier<(NS - 2) * T::PER>();
+    else
+      wait_barrier<0>();
+    if (t + NS - 1 < S) load_stage(t + NS - 1);
+    const uint8_t *slot = lds + (t % NS) * T::SLOT;
+#pragma unroll
+    for (int k = 0; k < 2; k++) {
+      v4i wv[T::BN], xv[T::BM];
+#pragma unroll
+      for (int i = 0; i < T::BN; i++)
+        wv[i] = *reinterpret_cast<const v4i *>(slot + (wn * T::RN + 32 * i) * 64 + (at ^ (32 * k)));
+#pragma unroll
+      for (int j = 0; j < T::BM; j++)
+        xv[j] = *reinterpret_cast<const v4i *>(slot + (TN + wm * T::RM + 32 * j) * 64 + (at ^ (32 * k)));
+#pragma unroll
+      for (int i = 0; i < T::BN; i++)
+#pragma unroll
+        for (int j = 0; j < T::BM; j++)
+          acc[i][j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(wv[i], xv[j], acc[i][j], 0, 0, 0);
+    }
+  }
+  // the sums through LDS, a wave's 32 rows at a time, so that whole rows of its
+  // channels are stored
+  wait_barrier<0>();
+  int *const o = reinterpret_cast<int *>(lds) + wave * 32 * T::OS;
+#pragma unroll
+  for (int j = 0; j < T::BM; j++) {
+#pragma unroll
+    for (int i = 0; i < T::BN; i++)
+#pragma unroll
+      for (int q = 0; q < 4; q++)
+        *reinterpret_cast<v4i *>(o + l32 * T::OS + 32 * i + 8 * q + 4 * lh) =
+            v4i{acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
+    constexpr int LR = T::RN / 4, PR = 64 / LR;    // lanes of a row, rows an instruction
+    const int c = lane % LR, m = m0 + wm * T::RM + 32 * j;
+    const v4f wc = LR == 32 ? wd : load_channels(a, a.wd, n0 + wn * T::RN + 4 * c);
+    const v4f bc = LR == 32 || !a.bias ? bias : load_channels(a, a.bias, n0 + wn * T::RN + 4 * c);
+#pragma unroll 4
+    for (int u = 0; u < 32 / PR; u++) {
+      const int r = PR * u + lane / LR;
+      const v4i s = *reinterpret_cast<const v4i *>(o + r * T::OS + 4 * c);
+      const float d = __shfl(xd[j], r);
+      const int n = n0 + wn * T::RN + 4 * c;
+      if (m + r < a.M && n < a.N) put4(a, m + r, n, s, d, wc, bc);
+    }
+  }
+}
+
+// Few rows: 16 RN channels by 16 MT rows a workgroup, eight waves that split the
+// row length, operands straight from memory: the weights stream once, the rows'
+// codes come from the L2 cache.  The waves' sums (whole numbers: any order
+// gives the same) are added up in LDS.
+template <int MT, int RN>
+__global__ __launch_bounds__(KNT) void q8_few_kernel(QArgs a) {
+  constexpr int OS = 16 * RN + 4, U = RN * MT >= 8 ? 2 : 4;
+  __shared__ __align__(16) int o[16 * MT * OS];
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  const int l16 = lane & 15, lq = lane >> 4;
+  const int n0 = blockIdx.x * 16 * RN;
+  for (int i = threadIdx.x; i < 16 * MT * OS; i += KNT) o[i] = 0;
+  const int8_t *wp[RN], *xp[MT];
+#pragma unroll
+  for (int i = 0; i < RN; i++) wp[i] = a.wq + (int64_t)min(n0 + 16 * i + l16, a.N - 1) * a.KP + 16 * lq;
+#pragma unroll
+  for (int j = 0; j < MT; j++) xp[j] = a.xq + (int64_t)min(16 * j + l16, a.M - 1) * a.KP + 16 * lq;
+  // the wave's steps of 64 codes, two at least
+  const int steps = a.KP / 64, per = ((steps / 2 + KNT / 64 - 1) / (KNT / 64)) * 2;
+  const int s0 = wave * per, s1 = min(s0 + per, steps);
+  v4i acc[RN][MT] = {};
+  for (int s = s0; s < s1; s += U) {
+    v4i wv[U][RN], xv[U][MT];
+#pragma unroll
+    for (int u = 0; u < U; u++) {
+      const int k = 64 * min(s + u, s1 - 1);
+#pragma unroll
+      for (int i = 0; i < RN; i++) wv[u][i] = *reinterpret_cast<const v4i *>(wp[i] + k);
+#pragma unroll
+      for (int j = 0; j < MT; j++) xv[u][j] = *reinterpret_cast<const v4i *>(xp[j] + k);
     }
 #pragma unroll
-    for (int i = 0; i < 2; i++)
+    for (int u = 0; u < U; u++) {
+      if (u > 0 && s + u >= s1) break;
 #pragma unroll
-      for (int j = 0; j < 2; j++)
-        acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(wv[i], xv[j], acc[i][j], 0, 0, 0);
+      for (int i = 0; i < RN; i++)
+#pragma unroll
+        for (int j = 0; j < MT; j++)
+          acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(wv[u][i], xv[u][j], acc[i][j], 0, 0, 0);
+    }
   }
+  __syncthreads();
+  if (s0 < s1)
 #pragma unroll
-  for (int j = 0; j < 2; j++) {
-    const int64_t m = m0 + 16 * j + l16;
-    if (m >= a.M) continue;
-    const float xd = a.xd[m];
+    for (int i = 0; i < RN; i++)
 #pragma unroll
-    for (int i = 0; i < 2; i++)
+      for (int j = 0; j < MT; j++)
 #pragma unroll
-      for (int e = 0; e < 4; e++) {
-        const int64_t n = n0 + 16 * i + 4 * lq + e;
-        if (n >= a.N) continue;
-        float y = (float)acc[i][j][e] * (xd * a.wd[n]);
-        if (a.bias) y += a.bias[n];
-        a.y[m * a.ys + n] = y;
-      }
+        for (int e = 0; e < 4; e++) atomicAdd(&o[(16 * j + l16) * OS + 16 * i + 4 * lq + e], acc[i][j][e]);
+  __syncthreads();
+  for (int i = threadIdx.x; i < 16 * MT * 4 * RN; i += KNT) {
+    const int m = i / (4 * RN), c = 4 * (i % (4 * RN)), n = n0 + c;
+    if (m < a.M && n < a.N)
+      put4(a, m, n, *reinterpret_cast<const v4i *>(&o[m * OS + c]), a.xd[m], load_channels(a, a.wd, n),
+           a.bias ? load_channels(a, a.bias, n) : v4f{0.f, 0.f, 0.f, 0.f});
   }
+}
+
+template <int TN, int TM, int WN, int WM, int NS>
+int launch_tiles(QArgs a, hipStream_t s) {
+  a.nt = (a.N + TN - 1) / TN;
+  a.mt = (a.M + TM - 1) / TM;
+  q8_tile_kernel<TN, TM, WN, WM, NS><<<dim3((unsigned)(a.nt * a.mt)), dim3(TNT), 0, s>>>(a);
+  return check_launch();
+}
+
+template <int MT>
+int launch_few(const QArgs &a, hipStream_t s) {
+  const int n16 = (a.N + 15) / 16, cus = device_cus();
+  if (n16 >= 8 * cus)
+    q8_few_kernel<MT, 4><<<dim3((n16 + 3) / 4), dim3(KNT), 0, s>>>(a);
+  else if (n16 >= 4 * cus)
+    q8_few_kernel<MT, 2><<<dim3((n16 + 1) / 2), dim3(KNT), 0, s>>>(a);
+  else
+    q8_few_kernel<MT, 1><<<dim3(n16), dim3(KNT), 0, s>>>(a);
+  return check_launch();
 }
 
 inline bool aligned4(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
@@ -119,13 +340,25 @@ extern "C" size_t q8_row_bytes(int64_t K) {
 extern "C" int q8_row_quantize(const float *x, int64_t x_stride, int8_t *q, float *d, int64_t rows,
                                int64_t K, void *stream) {
   if (rows < 0 || K < 1 || x_stride < K) return W4A8_ESHAPE;
-  if (K >= KTOP || rows >= TOP || x_stride >= TOP) return W4A8_ERANGE;
+  if (K >= KTOP || rows >= (1 << 24) || x_stride >= TOP) return W4A8_ERANGE;
   if (!x || !q || !d) return W4A8_ENULL;
   if (!aligned4(x) || !aligned16(q) || !aligned4(d)) return W4A8_EALIGN;
   if (rows == 0) return W4A8_OK;
   if (int rc = check_device(); rc != W4A8_OK) return rc;
-  q8_row_kernel<<<dim3((unsigned)rows), dim3(QNT), 0, as_stream(stream)>>>(x, x_stride, q, d, (int)K,
-                                                                         (int)q8_row_bytes(K));
+  const int KP = (int)q8_row_bytes(K);
+  const dim3 grid((unsigned)rows), nt(QNT);
+  hipStream_t s = as_stream(stream);
+  const bool vec = K % 4 == 0 && x_stride % 4 == 0 && aligned16(x);
+  if (vec && K <= 4 * QNT)
+    q8_row_kernel<1><<<grid, nt, 0, s>>>(x, x_stride, q, d, (int)K, KP);
+  else if (vec && K <= 8 * QNT)
+    q8_row_kernel<2><<<grid, nt, 0, s>>>(x, x_stride, q, d, (int)K, KP);
+  else if (vec && K <= 16 * QNT)
+    q8_row_kernel<4><<<grid, nt, 0, s>>>(x, x_stride, q, d, (int)K, KP);
+  else if (vec && K <= 32 * QNT)
+    q8_row_kernel<8><<<grid, nt, 0, s>>>(x, x_stride, q, d, (int)K, KP);
+  else
+    q8_any_row_kernel<<<grid, nt, 0, s>>>(x, x_stride, q, d, (int)K, KP);
   return check_launch();
 }
 
@@ -133,9 +366,9 @@ extern "C" int q8q8_gemm(const int8_t *xq, const float *xd, const int8_t *wq, co
                          const float *bias, float *y, int64_t y_stride, int64_t M, int64_t N,
                          int64_t K, void *stream) {
   if (M < 0 || N < 1 || K < 1 || y_stride < N) return W4A8_ESHAPE;
-  if (K >= KTOP || M >= TOP || N >= TOP || y_stride >= TOP) return W4A8_ERANGE;
-  const int64_t nt = (N + 63) / 64, mt = (M + 63) / 64;
-  if (nt * mt >= (1 << 23)) return W4A8_ERANGE;
+  // (a grid's threads are counted in 32 bits)
+  if (K >= KTOP || M >= TOP || N >= TOP || y_stride >= TOP || ((M + 63) / 64) * ((N + 127) / 128) >= (1 << 22))
+    return W4A8_ERANGE;
   if (!xq || !xd || !wq || !wd || !y) return W4A8_ENULL;
   if (!aligned16(xq) || !aligned16(wq) || !aligned4(xd) || !aligned4(wd) || !aligned4(bias) || !aligned4(y))
     return W4A8_EALIGN;
@@ -143,7 +376,13 @@ extern "C" int q8q8_gemm(const int8_t *xq, const float *xd, const int8_t *wq, co
     if (p == y) return W4A8_EALIAS;
   if (M == 0) return W4A8_OK;
   if (int rc = check_device(); rc != W4A8_OK) return rc;
-  QArgs a{xq, wq, xd, wd, bias, y, y_stride, M, N, (int)q8_row_bytes(K), (int)nt};
-  q8_tile_kernel<<<dim3((unsigned)(nt * mt)), dim3(TNT), 0, as_stream(stream)>>>(a);
-  return check_launch();
+  QArgs a{xq, wq, xd, wd, bias, y, y_stride, (int)M, (int)N, (int)q8_row_bytes(K), 0, 0,
+          y_stride % 4 == 0 && aligned16(y)};
+  hipStream_t s = as_stream(stream);
+  if (M <= 16) return launch_few<1>(a, s);
+  if (M <= 32) return launch_few<2>(a, s);
+  if (M <= 48) return launch_few<3>(a, s);
+  if (M <= 64) return launch_few<4>(a, s);
+  if (((M + 127) / 128) * ((N + 255) / 256) >= device_cus()) return launch_tiles<256, 128, 2, 2, 3>(a, s);
+  return launch_tiles<128, 64, 2, 2, 4>(a, s);
 }
