@@ -189,35 +189,55 @@ __global__ __launch_bounds__(TNT, 2) void q8_tile_kernel(QArgs a) {
 #pragma unroll
   for (int j = 0; j < T::BM; j++) xd[j] = a.xd[min(m0 + wm * T::RM + 32 * j + l32, a.M - 1)];
 #pragma unroll
-  for (int t = 0; t < NS - 1; t++)
+  for (int t = 0; t < NS; t++)
     if (t < S) load_stage(t);
 
+  // Half a stage's operands are read while the products of the half before run: a
+  // stage's second half behind its first, the next stage's first behind the
+  // barrier that says it has landed (the younger NS - 2 may be under way) and
+  // that every wave has read the stage before, whose slot the next loads fill.
   const uint32_t at = l32 * 64 + 16 * (lh ^ ((l32 >> 2) & 3));
   v16i acc[T::BN][T::BM] = {};
-  for (int t = 0; t < S; t++) {
-    // stage t has landed (the younger NS - 2 may be under way), and every wave is
-    // done with stage t - 1, whose slot the next loads fill
+  v4i w0[T::BN], x0[T::BM], w1[T::BN], x1[T::BM];
+  const auto read = [&](int t, int k, v4i (&wv)[T::BN], v4i (&xv)[T::BM]) {
+    const uint8_t *slot = lds + (t % NS) * T::SLOT;
+#pragma unroll
+    for (int j = 0; j < T::BM; j++)
+      xv[j] = *reinterpret_cast<const v4i *>(slot + (TN + wm * T::RM + 32 * j) * 64 + (at ^ (32 * k)));
+#pragma unroll
+    for (int i = 0; i < T::BN; i++)
+      wv[i] = *reinterpret_cast<const v4i *>(slot + (wn * T::RN + 32 * i) * 64 + (at ^ (32 * k)));
+  };
+  const auto products = [&](const v4i (&wv)[T::BN], const v4i (&xv)[T::BM]) {
+#pragma unroll
+    for (int i = 0; i < T::BN; i++)
+#pragma unroll
+      for (int j = 0; j < T::BM; j++)
+        acc[i][j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(wv[i], xv[j], acc[i][j], 0, 0, 0);
+  };
+  const auto landed = [&](int t) {
     if (t + NS - 2 < S)
       wait_barrier<(NS - 2) * T::PER>();
     else
       wait_barrier<0>();
-    if (t + NS - 1 < S) load_stage(t + NS - 1);
-    const uint8_t *slot = lds + (t % NS) * T::SLOT;
-#pragma unroll
-    for (int k = 0; k < 2; k++) {
-      v4i wv[T::BN], xv[T::BM];
-#pragma unroll
-      for (int i = 0; i < T::BN; i++)
-        wv[i] = *reinterpret_cast<const v4i *>(slot + (wn * T::RN + 32 * i) * 64 + (at ^ (32 * k)));
-#pragma unroll
-      for (int j = 0; j < T::BM; j++)
-        xv[j] = *reinterpret_cast<const v4i *>(slot + (TN + wm * T::RM + 32 * j) * 64 + (at ^ (32 * k)));
-#pragma unroll
-      for (int i = 0; i < T::BN; i++)
-#pragma unroll
-        for (int j = 0; j < T::BM; j++)
-          acc[i][j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(wv[i], xv[j], acc[i][j], 0, 0, 0);
+  };
+  if (S > NS - 1)
+    wait_barrier<(NS - 1) * T::PER>();
+  else
+    wait_barrier<0>();
+  read(0, 0, w0, x0);
+  for (int t = 0; t < S; t++) {
+    read(t, 1, w1, x1);
+    __builtin_amdgcn_sched_barrier(0);
+    products(w0, x0);
+    __builtin_amdgcn_sched_barrier(0);
+    if (t + 1 < S) {
+      landed(t + 1);
+      if (t + NS < S) load_stage(t + NS);
+      read(t + 1, 0, w0, x0);
     }
+    __builtin_amdgcn_sched_barrier(0);
+    products(w1, x1);
   }
   // the sums through LDS, a wave's 32 rows at a time, so that whole rows of its
   // channels are stored
