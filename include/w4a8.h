@@ -491,7 +491,7 @@ int q8_row_quantize(const float *x, int64_t x_stride, int8_t *q, float *d, int64
  *   quantizer writes them); xd [M], wd [N], bias [N] fp32; y fp32, row m at
  *   m * y_stride elements, written.  One launch, no workspace.
  * Errors: M < 0, N < 1, K < 1, y_stride < N -> W4A8_ESHAPE; K >= 2^17, y_stride
- * >= 2^31 or 2^22 tiles of 64 rows by 128 channels or more -> W4A8_ERANGE; a NULL pointer (but bias) ->
+ * >= 2^31 or 2^23 tiles of 64 rows by 64 channels or more -> W4A8_ERANGE; a NULL pointer (but bias) ->
  * W4A8_ENULL; xq or wq not 16-, xd, wd, bias or y not 4-byte aligned ->
  * W4A8_EALIGN; y equal to an operand -> W4A8_EALIAS.  M == 0 is a no-op.
  */

@@ -792,15 +792,17 @@ def q8_row_bytes(K) -> int:
 def q8_row_quantize(x, q=None, d=None, stream=None):
     """8-bit rows of fp32 x [rows, K] (rows may be strided): codes int8 [rows,
     K rounded up to 128] and scales fp32 [rows], of activations or weights."""
-    xs = _rows(x, x.shape, "x")
-    M, K = x.shape
+    shape = x.shape
+    xs = _rows(x, shape, "x")
+    M, K = shape
     KP = (K + Q8_ROW_PAD - 1) // Q8_ROW_PAD * Q8_ROW_PAD
     if q is None:
-        q = _empty((M, KP), torch.int8, x.device, stream)
+        q = x.new_empty((M, KP), dtype=torch.int8) if stream is None else \
+            _empty((M, KP), torch.int8, x.device, stream)
     else:
         _is(q, torch.int8, (M, KP), "q")
     if d is None:
-        d = _empty((M,), torch.float32, x.device, stream)
+        d = x.new_empty(M) if stream is None else _empty((M,), torch.float32, x.device, stream)
     else:
         _is(d, torch.float32, (M,), "d")
     if M:
@@ -826,6 +828,7 @@ def q8q8_gemm(xq, xd, wq, wd, bias=None, out=None, stream=None):
         out = _empty((M, N), torch.float32, xq.device, stream)
     ys = _rows(out, (M, N), "out")
     if M:
+        # (rows of 2^17 codes end with at least one of the padding: K is below 2^17)
         _call("q8q8_gemm", stream, (xq, xd, wq, wd, bias, out), xq.data_ptr(), xd.data_ptr(),
               wq.data_ptr(), wd.data_ptr(), _ptr(bias), out.data_ptr(), ys, M, N, KP - (KP == 1 << 17))
     return out

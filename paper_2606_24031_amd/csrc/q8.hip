@@ -9,7 +9,6 @@ namespace w4a8 {
 namespace {
 
 constexpr int QNT = 256;            // threads of a quantizing workgroup: one row
-constexpr int TNT = 256;            // ... of a product tile: four waves
 constexpr int KNT = 512;            // ... of a product of few rows: eight waves
 constexpr int PAD = W4A8_Q8_ROW_PAD;
 
@@ -133,7 +132,7 @@ __device__ __forceinline__ v4f load_channels(const QArgs &a, const float *p, int
   return v;
 }
 
-// Tiles of TN channels by TM rows, four waves of RN by RM on 32 x 32 x 32
+// Tiles of TN channels by TM rows, waves of RN by RM on 32 x 32 x 32
 // products; the weights are the A operand, so that element e of a sum in lane l
 // is channel 8 (e / 4) + 4 (l / 32) + e % 4 and row l % 32.  64 codes of every row
 // a stage, by direct loads into a ring of NS slots; the 16-byte pieces of a row
@@ -142,14 +141,15 @@ __device__ __forceinline__ v4f load_channels(const QArgs &a, const float *p, int
 template <int TN, int TM, int WN, int WM, int NS>
 struct Tile {
   static constexpr int RN = TN / WN, RM = TM / WM, BN = RN / 32, BM = RM / 32;
-  static constexpr int SLOT = (TN + TM) * 64, PER = (TN + TM) / 16 / 4;
+  static constexpr int NW = WN * WM, NT = 64 * NW;
+  static constexpr int SLOT = (TN + TM) * 64, PER = (TN + TM) / 16 / NW;
   static constexpr int OS = RN + 4;                // row stride of a wave's output in LDS
-  static constexpr int LDS = NS * SLOT > 4 * 32 * OS * 4 ? NS * SLOT : 4 * 32 * OS * 4;
-  static_assert(WN * WM == 4 && BN * 32 == RN && BM * 32 == RM && PER * 64 == TN + TM && NS >= 3, "tile");
+  static constexpr int LDS = NS * SLOT > NW * 32 * OS * 4 ? NS * SLOT : NW * 32 * OS * 4;
+  static_assert(BN * 32 == RN && BM * 32 == RM && PER * 16 * NW == TN + TM && NS >= 3, "tile");
 };
 
 template <int TN, int TM, int WN, int WM, int NS>
-__global__ __launch_bounds__(TNT, 2) void q8_tile_kernel(QArgs a) {
+__global__ __launch_bounds__(64 * WN * WM, 2) void q8_tile_kernel(QArgs a) {
   using T = Tile<TN, TM, WN, WM, NS>;
   __shared__ __align__(16) uint8_t lds[T::LDS];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
@@ -168,7 +168,7 @@ __global__ __launch_bounds__(TNT, 2) void q8_tile_kernel(QArgs a) {
   const uint32_t piece = 16 * ((lane & 3) ^ ((lane >> 4) & 3));
 #pragma unroll
   for (int u = 0; u < T::PER; u++) {
-    const int r = 16 * (wave + 4 * u);             // of the tile's TN + TM
+    const int r = 16 * (wave + T::NW * u);         // of the tile's TN + TM
     const bool is_w = r < TN;
     const int first = is_w ? n0 : m0, last = (is_w ? a.N : a.M) - 1;
     src[u] = reinterpret_cast<const uint8_t *>(is_w ? a.wq : a.xq) + (int64_t)first * a.KP;
@@ -178,7 +178,7 @@ __global__ __launch_bounds__(TNT, 2) void q8_tile_kernel(QArgs a) {
   const auto load_stage = [&](int t) {
     uint8_t *const slot = lds + (t % NS) * T::SLOT;
 #pragma unroll
-    for (int u = 0; u < T::PER; u++) lds_dma16(src[u] + t * 64, off[u], slot + 1024 * (wave + 4 * u));
+    for (int u = 0; u < T::PER; u++) lds_dma16(src[u] + t * 64, off[u], slot + 1024 * (wave + T::NW * u));
   };
   const int wn = wave % WN, wm = wave / WN, l32 = lane & 31, lh = lane >> 5;
   const int nl = n0 + wn * T::RN + 4 * l32;        // this lane's channels when rows are stored
@@ -192,52 +192,56 @@ __global__ __launch_bounds__(TNT, 2) void q8_tile_kernel(QArgs a) {
   for (int t = 0; t < NS; t++)
     if (t < S) load_stage(t);
 
-  // Half a stage's operands are read while the products of the half before run: a
-  // stage's second half behind its first, the next stage's first behind the
-  // barrier that says it has landed (the younger NS - 2 may be under way) and
-  // that every wave has read the stage before, whose slot the next loads fill.
+  // Half a stage's operands are read between the products of the half before: a
+  // stage's second half among its first's, the next stage's first half, and the
+  // loads of the stage NS on, among its second's, behind the barrier that says the
+  // next stage has landed (the younger NS - 2 may be under way) and that every
+  // wave has read this one, whose slot the loads fill.  A product takes 32
+  // cycles and the two or three other instructions behind it are issued meanwhile.
   const uint32_t at = l32 * 64 + 16 * (lh ^ ((l32 >> 2) & 3));
   v16i acc[T::BN][T::BM] = {};
   v4i w0[T::BN], x0[T::BM], w1[T::BN], x1[T::BM];
-  const auto read = [&](int t, int k, v4i (&wv)[T::BN], v4i (&xv)[T::BM]) {
-    const uint8_t *slot = lds + (t % NS) * T::SLOT;
-#pragma unroll
-    for (int j = 0; j < T::BM; j++)
-      xv[j] = *reinterpret_cast<const v4i *>(slot + (TN + wm * T::RM + 32 * j) * 64 + (at ^ (32 * k)));
-#pragma unroll
-    for (int i = 0; i < T::BN; i++)
-      wv[i] = *reinterpret_cast<const v4i *>(slot + (wn * T::RN + 32 * i) * 64 + (at ^ (32 * k)));
-  };
-  const auto products = [&](const v4i (&wv)[T::BN], const v4i (&xv)[T::BM]) {
-#pragma unroll
-    for (int i = 0; i < T::BN; i++)
-#pragma unroll
-      for (int j = 0; j < T::BM; j++)
-        acc[i][j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(wv[i], xv[j], acc[i][j], 0, 0, 0);
-  };
-  const auto landed = [&](int t) {
-    if (t + NS - 2 < S)
-      wait_barrier<(NS - 2) * T::PER>();
+  constexpr int NP = T::BN * T::BM, NR = T::BN + T::BM;
+  const auto read = [&](const uint8_t *slot, int k, int u, v4i (&wv)[T::BN], v4i (&xv)[T::BM]) {
+    if (u < T::BM)
+      xv[u] = *reinterpret_cast<const v4i *>(slot + (TN + wm * T::RM + 32 * u) * 64 + (at ^ (32 * k)));
     else
-      wait_barrier<0>();
+      wv[u - T::BM] = *reinterpret_cast<const v4i *>(slot + (wn * T::RN + 32 * (u - T::BM)) * 64 + (at ^ (32 * k)));
   };
-  if (S > NS - 1)
+  // the products of (wv, xv) with the reads of half k of `next` into (wn, xn) and, if
+  // `dma`, the loads of stage t
+  const auto half = [&](const v4i (&wv)[T::BN], const v4i (&xv)[T::BM], const uint8_t *next, int k,
+                        v4i (&wnext)[T::BN], v4i (&xnext)[T::BM], bool dma, int t, uint8_t *slot) {
+#pragma unroll
+    for (int p = 0; p < NP; p++) {
+      const int i = p / T::BM, j = p % T::BM;
+      acc[i][j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(wv[i], xv[j], acc[i][j], 0, 0, 0);
+#pragma unroll
+      for (int u = p * NR / NP; u < (p + 1) * NR / NP; u++) read(next, k, u, wnext, xnext);
+      if (dma)
+#pragma unroll
+        for (int u = p * T::PER / NP; u < (p + 1) * T::PER / NP; u++)
+          lds_dma16(src[u] + t * 64, off[u], slot + 1024 * (wave + T::NW * u));
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  };
+  if (S >= NS)
     wait_barrier<(NS - 1) * T::PER>();
   else
     wait_barrier<0>();
-  read(0, 0, w0, x0);
-  for (int t = 0; t < S; t++) {
-    read(t, 1, w1, x1);
-    __builtin_amdgcn_sched_barrier(0);
-    products(w0, x0);
-    __builtin_amdgcn_sched_barrier(0);
-    if (t + 1 < S) {
-      landed(t + 1);
-      if (t + NS < S) load_stage(t + NS);
-      read(t + 1, 0, w0, x0);
-    }
-    __builtin_amdgcn_sched_barrier(0);
-    products(w1, x1);
+#pragma unroll
+  for (int u = 0; u < NR; u++) read(lds, 0, u, w0, x0);
+  for (int t = 0, sl = 0; t < S; t++) {            // the stage, its slot
+    const int sn = sl + 1 == NS ? 0 : sl + 1;
+    uint8_t *const slot = lds + sl * T::SLOT;
+    half(w0, x0, slot, 1, w1, x1, false, 0, nullptr);
+    if (t + NS - 1 < S)
+      wait_barrier<(NS - 2) * T::PER>();
+    else
+      wait_barrier<0>();
+    // (past the last stage what is read is not used)
+    half(w1, x1, lds + sn * T::SLOT, 0, w0, x0, t + NS < S, t + NS, slot);
+    sl = sn;
   }
   // the sums through LDS, a wave's 32 rows at a time, so that whole rows of its
   // channels are stored
@@ -328,19 +332,13 @@ template <int TN, int TM, int WN, int WM, int NS>
 int launch_tiles(QArgs a, hipStream_t s) {
   a.nt = (a.N + TN - 1) / TN;
   a.mt = (a.M + TM - 1) / TM;
-  q8_tile_kernel<TN, TM, WN, WM, NS><<<dim3((unsigned)(a.nt * a.mt)), dim3(TNT), 0, s>>>(a);
+  q8_tile_kernel<TN, TM, WN, WM, NS><<<dim3((unsigned)(a.nt * a.mt)), dim3(64 * WN * WM), 0, s>>>(a);
   return check_launch();
 }
 
-template <int MT>
+template <int MT, int RN>
 int launch_few(const QArgs &a, hipStream_t s) {
-  const int n16 = (a.N + 15) / 16, cus = device_cus();
-  if (n16 >= 8 * cus)
-    q8_few_kernel<MT, 4><<<dim3((n16 + 3) / 4), dim3(KNT), 0, s>>>(a);
-  else if (n16 >= 4 * cus)
-    q8_few_kernel<MT, 2><<<dim3((n16 + 1) / 2), dim3(KNT), 0, s>>>(a);
-  else
-    q8_few_kernel<MT, 1><<<dim3(n16), dim3(KNT), 0, s>>>(a);
+  q8_few_kernel<MT, RN><<<dim3((a.N + 16 * RN - 1) / (16 * RN)), dim3(KNT), 0, s>>>(a);
   return check_launch();
 }
 
@@ -387,7 +385,7 @@ extern "C" int q8q8_gemm(const int8_t *xq, const float *xd, const int8_t *wq, co
                          int64_t K, void *stream) {
   if (M < 0 || N < 1 || K < 1 || y_stride < N) return W4A8_ESHAPE;
   // (a grid's threads are counted in 32 bits)
-  if (K >= KTOP || M >= TOP || N >= TOP || y_stride >= TOP || ((M + 63) / 64) * ((N + 127) / 128) >= (1 << 22))
+  if (K >= KTOP || M >= TOP || N >= TOP || y_stride >= TOP || ((M + 63) / 64) * ((N + 63) / 64) >= (1 << 23))
     return W4A8_ERANGE;
   if (!xq || !xd || !wq || !wd || !y) return W4A8_ENULL;
   if (!aligned16(xq) || !aligned16(wq) || !aligned4(xd) || !aligned4(wd) || !aligned4(bias) || !aligned4(y))
@@ -399,10 +397,36 @@ extern "C" int q8q8_gemm(const int8_t *xq, const float *xd, const int8_t *wq, co
   QArgs a{xq, wq, xd, wd, bias, y, y_stride, (int)M, (int)N, (int)q8_row_bytes(K), 0, 0,
           y_stride % 4 == 0 && aligned16(y)};
   hipStream_t s = as_stream(stream);
-  if (M <= 16) return launch_few<1>(a, s);
-  if (M <= 32) return launch_few<2>(a, s);
-  if (M <= 48) return launch_few<3>(a, s);
-  if (M <= 64) return launch_few<4>(a, s);
-  if (((M + 127) / 128) * ((N + 255) / 256) >= device_cus()) return launch_tiles<256, 128, 2, 2, 3>(a, s);
-  return launch_tiles<128, 64, 2, 2, 4>(a, s);
+  // Up to 16 rows stream the weights; two tiles of channels a wave where there are
+  // several rows and enough channels for all compute units eight times (16 rows over
+  // 151936 x 2048 73 us against 89; one row 64 against 59).  Up to 64 rows do while
+  // one workgroup a compute unit covers the channels (48 over 4096 x 2048 7.5 us, 8.4
+  // on tiles; over 12288 x 2048 15, 9.2 on tiles).
+  const int n16 = (a.N + 15) / 16, cus = device_cus();
+  if (M <= 16) return M > 1 && n16 >= 8 * cus ? launch_few<1, 2>(a, s) : launch_few<1, 1>(a, s);
+  if (M <= 64 && n16 <= cus)
+    return M <= 32 ? launch_few<2, 1>(a, s) : M <= 48 ? launch_few<3, 1>(a, s) : launch_few<4, 1>(a, s);
+  // One tile a compute unit takes `one`, each further round `more` (us at K = 2048;
+  // longer rows in proportion): the kind whose rounds end first.  Measured there:
+  // 947 x 12288 37.5 on the largest tiles and 46, 45, 52, 62 on the others; 947 x
+  // 8192 34, 29.5, 30.5, 38, 43; 947 x 4096 28, 23, 17, 19, 21; 947 x 2048 27, 22, 15,
+  // 12, 12; 200 x 8192 27, 22, 15, 12, 11.5; 100 x 4096 26, 21, 14, 10.5, 8.4.
+  struct Kind { int tn, tm; float one, more; };
+  constexpr Kind kinds[] = {{256, 256, 30.f, 38.f}, {256, 128, 22.f, 25.f}, {128, 128, 14.f, 14.7f},
+                            {128, 64, 10.5f, 8.7f}, {64, 64, 8.f, 5.1f}};
+  int best = 0;
+  float least = 0.0f;
+  for (int i = 0; i < 5; i++) {
+    const Kind &k = kinds[i];
+    const int64_t tiles = ((N + k.tn - 1) / k.tn) * ((M + k.tm - 1) / k.tm);
+    const float t = k.one + k.more * (float)((tiles - 1) / device_cus());
+    if (i == 0 || t < least) { best = i; least = t; }
+  }
+  switch (best) {
+    case 0: return launch_tiles<256, 256, 2, 4, 4>(a, s);
+    case 1: return launch_tiles<256, 128, 2, 2, 3>(a, s);
+    case 2: return launch_tiles<128, 128, 2, 2, 4>(a, s);
+    case 3: return launch_tiles<128, 64, 2, 2, 4>(a, s);
+    default: return launch_tiles<64, 64, 2, 2, 4>(a, s);
+  }
 }
