@@ -107,10 +107,11 @@ __global__ __launch_bounds__(STEP_NT) void step_kernel(ScanArgs a) {
 // reach the next sequence's first.
 __device__ __forceinline__ int record_of(int begin, int b) { return begin / SC + b; }
 
-// A record holds the ten 16 x 16 tiles (r, j <= r) of a chunk's C B^T, each as a
-// lane of a product takes it: four neighbouring columns 4 (l / 16) .. + 3 of row
-// l % 16.
-constexpr int REC = 10 * 256;       // floats
+// A record holds the ten 16 x 16 tiles (r, j <= r) of a chunk's C B^T, then the
+// tiles (n, j) of B^T (16 entries by 16 rows of the chunk), each as a lane of a
+// product takes it: four neighbouring columns 4 (l / 16) .. + 3 of row l % 16.
+constexpr int GRAM = 10 * 256;      // floats
+constexpr int rec_floats(int N) { return GRAM + N * SC; }
 __device__ __forceinline__ int tile_at(int r, int j) { return (r * (r + 1) / 2 + j) * 256; }
 
 // Four products of 16 x 16 x 4 of a 16-byte piece of either operand, in two
@@ -153,7 +154,9 @@ constexpr int DEC = 5, DEC_LH = 0, DEC_LL = 1, DEC_DL = 2, DEC_WJ = 3, DEC_EL = 
 // chunk and group, then one per chunk and four heads:
 //   C B^T, a wave per 16 rows of C.  The rows of B are the A operand, so that a
 //   lane's sums are neighbouring columns of one row.  Rows past the sequence's
-//   last repeat it (their steps are 0 where they are used).
+//   last repeat it (their steps are 0 where they are used).  Then B^T, a lane's
+//   four numbers of a product together (the scan would gather them one by one:
+//   16384 rows of 64 heads of 64 took 718 us).
 //   the steps and decays, a wave per head, a row a lane.
 template <int N>
 __global__ __launch_bounds__(256) void prep_kernel(ScanArgs a, unsigned ngram) {
@@ -192,6 +195,7 @@ __global__ __launch_bounds__(256) void prep_kernel(ScanArgs a, unsigned ngram) {
   }
   const int r = wave, g = part, l16 = lane & 15, lq = lane >> 4;
   const float *cp = a.c + (int64_t)min(t0 + 16 * r + l16, end - 1) * a.cs + (int64_t)g * N + 4 * lq;
+  float *const out = a.gram + ((int64_t)rec * a.NG + g) * rec_floats(N);
   v4f c[N / 16];
 #pragma unroll
   for (int s = 0; s < N / 16; s++) c[s] = quad(cp + 16 * s);
@@ -200,9 +204,17 @@ __global__ __launch_bounds__(256) void prep_kernel(ScanArgs a, unsigned ngram) {
     v4f s0 = {0.f, 0.f, 0.f, 0.f}, s1 = s0;
 #pragma unroll
     for (int s = 0; s < N / 16; s++) mm4(quad(bp + 16 * s), c[s], s0, s1);
-    *reinterpret_cast<v4f *>(a.gram + ((int64_t)rec * a.NG + g) * REC + tile_at(r, j) + 4 * lane) =
-        s0 + s1;
+    *reinterpret_cast<v4f *>(out + tile_at(r, j) + 4 * lane) = s0 + s1;
   }
+  for (int n = r; n < N / 16; n += 4)
+#pragma unroll
+    for (int j = 0; j < 4; j++) {
+      v4f v;
+#pragma unroll
+      for (int e = 0; e < 4; e++)
+        v[e] = a.b[(int64_t)min(t0 + 16 * j + 4 * lq + e, end - 1) * a.bs + (int64_t)g * N + 16 * n + l16];
+      *reinterpret_cast<v4f *>(out + GRAM + (4 * n + j) * 256 + 4 * lane) = v;
+    }
 }
 
 template <int N, int PS>
@@ -265,35 +277,32 @@ __global__ __launch_bounds__(SNT) void scan_kernel(ScanArgs a) {
     return __builtin_bit_cast(v4f, __builtin_amdgcn_raw_buffer_load_b128(q, at, more, 0));
   };
   const uint32_t cat = 4u * ((16 * r + l16) * (uint32_t)a.cs + kh * (N / KH) + 4 * lq);
-  uint32_t bat[4];                               // (row e of four and the lane's column)
-#pragma unroll
-  for (int e = 0; e < 4; e++) bat[e] = 4u * ((4 * lq + e) * (uint32_t)a.bs + 16 * (wave % NT) + l16);
   const int xrow = min(xr, SC - 1), cx = min(xc, a.P - 4 - c0);
   const uint32_t xat = 4u * (xrow * (uint32_t)a.xs + cx), zat = 4u * (xrow * (uint32_t)a.zs + cx);
   const int rec0 = record_of(begin, b);
   // A chunk's operands have one set of registers each: the next chunk's are
   // loaded into them behind their last use, a step ahead of their own.
-  v4f cf[CF], gf[GF], xcur, xnext, z;
-  float bf[TPW][16], dec1;                       // B of 16 rows for a column of each tile; one of the decay arrays
+  v4f cf[CF], gf[GF], bf[TPW][4], xcur, xnext, z;
+  float dec1;                                    // of one of the decay arrays
   const auto load_c = [&](int c) {
     const auto q = rows(a.c + (int64_t)g * N, a.cs, c);
 #pragma unroll
     for (int s = 0; s < CF; s++) cf[s] = load4(q, cat, 64 * s);
   };
+  const auto record = [&](int c) {
+    return a.gram + ((int64_t)(rec0 + min(c, nch - 1)) * a.NG + g) * rec_floats(N) + 4 * lane;
+  };
   const auto load_b = [&](int c) {
-    const auto q = rows(a.b + (int64_t)g * N, a.bs, c);
+    const float *const q = record(c) + GRAM;
 #pragma unroll
     for (int i = 0; i < TPW; i++)
 #pragma unroll
-      for (int e = 0; e < 16; e++)
-        bf[i][e] = __builtin_bit_cast(
-            float, __builtin_amdgcn_raw_buffer_load_b32(
-                       q, bat[e & 3], 64u * (e >> 2) * (uint32_t)a.bs + (TPW > 1 ? 512 * i : 0), 0));
+      for (int s = 0; s < 4; s++) bf[i][s] = quad(q + (4 * nt[i] + s) * 256);
   };
   const auto load_g = [&](int c) {
-    const float *const gp = a.gram + ((int64_t)(rec0 + min(c, nch - 1)) * a.NG + g) * REC;
+    const float *const q = record(c);
 #pragma unroll
-    for (int s = 0; s < GF; s++) gf[s] = quad(gp + tile_at(r, min(KH == 2 ? kh + 2 * s : s, r)) + 4 * lane);
+    for (int s = 0; s < GF; s++) gf[s] = quad(q + tile_at(r, min(KH == 2 ? kh + 2 * s : s, r)));
   };
   const auto load_x = [&](int c) {
     xnext = load4(rows(a.x + (int64_t)h * a.P + c0, a.xs, c), xat, 0);
@@ -358,7 +367,7 @@ __global__ __launch_bounds__(SNT) void scan_kernel(ScanArgs a) {
 #pragma unroll
       for (int s = 0; s < 4; s++) {
         const v4f w = quad(&dec[DEC_WJ][16 * s + 4 * lq]);
-        mm4(v4f{bf[i][4 * s], bf[i][4 * s + 1], bf[i][4 * s + 2], bf[i][4 * s + 3]}, w * xt[s], S[i], s1);
+        mm4(bf[i][s], w * xt[s], S[i], s1);
       }
       S[i] += s1;
     }
@@ -453,7 +462,8 @@ using namespace w4a8;
 
 extern "C" size_t ssm_workspace_size(const w4a8_seqs *seqs, const w4a8_ssm *ssm, int64_t T) {
   if (ssm_sizes(seqs, ssm, T) != W4A8_OK) return 0;
-  return (size_t)(T / SC + seqs->B + 1) * (ssm->NG * REC + ssm->NH * DEC * SC) * sizeof(float);
+  return (size_t)(T / SC + seqs->B + 1) * (ssm->NG * rec_floats((int)ssm->N) + ssm->NH * DEC * SC) *
+         sizeof(float);
 }
 
 extern "C" int ssm_scan(const w4a8_seqs *seqs, const w4a8_ssm *m, float *state, float *y,
@@ -487,7 +497,7 @@ extern "C" int ssm_scan(const w4a8_seqs *seqs, const w4a8_ssm *m, float *state, 
   a.x = m->x; a.dt = m->dt; a.b = m->b; a.c = m->c; a.z = m->z;
   a.A = m->A; a.D = m->D; a.bias = m->dt_bias;
   a.state = state; a.y = y; a.gram = reinterpret_cast<float *>(workspace);
-  a.dec = a.gram + records(a.q) * m->NG * REC;
+  a.dec = a.gram + records(a.q) * m->NG * rec_floats((int)m->N);
   a.xs = (int)m->x_stride; a.ds = (int)m->dt_stride; a.bs = (int)m->b_stride; a.cs = (int)m->c_stride;
   a.zs = (int)m->z_stride; a.ys = (int)y_stride;
   a.NH = (int)m->NH; a.NG = (int)m->NG; a.G = (int)(m->NH / m->NG); a.P = (int)m->P;
