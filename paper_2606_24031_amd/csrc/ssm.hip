@@ -108,10 +108,11 @@ __global__ __launch_bounds__(STEP_NT) void step_kernel(ScanArgs a) {
 __device__ __forceinline__ int record_of(int begin, int b) { return begin / SC + b; }
 
 // A record holds the ten 16 x 16 tiles (r, j <= r) of a chunk's C B^T, then the
-// tiles (n, j) of B^T (16 entries by 16 rows of the chunk), each as a lane of a
-// product takes it: four neighbouring columns 4 (l / 16) .. + 3 of row l % 16.
+// tiles (n, j) of B^T (16 entries by 16 rows of the chunk) and (r, n) of C, each as
+// a lane of a product takes it: four neighbouring columns 4 (l / 16) .. + 3 of
+// row l % 16.
 constexpr int GRAM = 10 * 256;      // floats
-constexpr int rec_floats(int N) { return GRAM + N * SC; }
+constexpr int rec_floats(int N) { return GRAM + 2 * N * SC; }
 __device__ __forceinline__ int tile_at(int r, int j) { return (r * (r + 1) / 2 + j) * 256; }
 
 // Four products of 16 x 16 x 4 of a 16-byte piece of either operand, in two
@@ -154,9 +155,9 @@ constexpr int DEC = 5, DEC_LH = 0, DEC_LL = 1, DEC_DL = 2, DEC_WJ = 3, DEC_EL = 
 // chunk and group, then one per chunk and four heads:
 //   C B^T, a wave per 16 rows of C.  The rows of B are the A operand, so that a
 //   lane's sums are neighbouring columns of one row.  Rows past the sequence's
-//   last repeat it (their steps are 0 where they are used).  Then B^T, a lane's
-//   four numbers of a product together (the scan would gather them one by one:
-//   16384 rows of 64 heads of 64 took 718 us).
+//   last repeat it (their steps are 0 where they are used).  Then B^T and C, a lane's
+//   four numbers of a product together and 1 KB an instruction (gathered by the
+//   scan 16384 rows of 64 heads of 64 took 718 us, B^T here 631).
 //   the steps and decays, a wave per head, a row a lane.
 template <int N>
 __global__ __launch_bounds__(256) void prep_kernel(ScanArgs a, unsigned ngram) {
@@ -198,7 +199,10 @@ __global__ __launch_bounds__(256) void prep_kernel(ScanArgs a, unsigned ngram) {
   float *const out = a.gram + ((int64_t)rec * a.NG + g) * rec_floats(N);
   v4f c[N / 16];
 #pragma unroll
-  for (int s = 0; s < N / 16; s++) c[s] = quad(cp + 16 * s);
+  for (int s = 0; s < N / 16; s++) {
+    c[s] = quad(cp + 16 * s);
+    *reinterpret_cast<v4f *>(out + GRAM + N * SC + (r * (N / 16) + s) * 256 + 4 * lane) = c[s];
+  }
   for (int j = 0; j <= r; j++) {
     const float *bp = a.b + (int64_t)min(t0 + 16 * j + l16, end - 1) * a.bs + (int64_t)g * N + 4 * lq;
     v4f s0 = {0.f, 0.f, 0.f, 0.f}, s1 = s0;
@@ -276,7 +280,6 @@ __global__ __launch_bounds__(SNT) void scan_kernel(ScanArgs a) {
   const auto load4 = [](__amdgpu_buffer_rsrc_t q, uint32_t at, uint32_t more) {
     return __builtin_bit_cast(v4f, __builtin_amdgcn_raw_buffer_load_b128(q, at, more, 0));
   };
-  const uint32_t cat = 4u * ((16 * r + l16) * (uint32_t)a.cs + kh * (N / KH) + 4 * lq);
   const int xrow = min(xr, SC - 1), cx = min(xc, a.P - 4 - c0);
   const uint32_t xat = 4u * (xrow * (uint32_t)a.xs + cx), zat = 4u * (xrow * (uint32_t)a.zs + cx);
   const int rec0 = record_of(begin, b);
@@ -284,13 +287,13 @@ __global__ __launch_bounds__(SNT) void scan_kernel(ScanArgs a) {
   // loaded into them behind their last use, a step ahead of their own.
   v4f cf[CF], gf[GF], bf[TPW][4], xcur, xnext, z;
   float dec1;                                    // of one of the decay arrays
-  const auto load_c = [&](int c) {
-    const auto q = rows(a.c + (int64_t)g * N, a.cs, c);
-#pragma unroll
-    for (int s = 0; s < CF; s++) cf[s] = load4(q, cat, 64 * s);
-  };
   const auto record = [&](int c) {
     return a.gram + ((int64_t)(rec0 + min(c, nch - 1)) * a.NG + g) * rec_floats(N) + 4 * lane;
+  };
+  const auto load_c = [&](int c) {
+    const float *const q = record(c) + GRAM + N * SC + (r * NT + kh * CF) * 256;
+#pragma unroll
+    for (int s = 0; s < CF; s++) cf[s] = quad(q + 256 * s);
   };
   const auto load_b = [&](int c) {
     const float *const q = record(c) + GRAM;
