@@ -124,6 +124,8 @@ __device__ __forceinline__ void mm4(v4f x, v4f y, v4f &c0, v4f &c1) {
   c0 = __builtin_amdgcn_mfma_f32_16x16x4f32(x.z, y.z, c0, 0, 0, 0);
   c1 = __builtin_amdgcn_mfma_f32_16x16x4f32(x.w, y.w, c1, 0, 0, 0);
 }
+// A value is computed by here.
+__device__ __forceinline__ void pin(v4f &v) { asm volatile("" : "+v"(v)); }
 __device__ __forceinline__ v4f quad(const float *p) { return *reinterpret_cast<const v4f *>(p); }
 
 // Inclusive sum over the wave's lanes.
@@ -284,8 +286,10 @@ __global__ __launch_bounds__(SNT) void scan_kernel(ScanArgs a) {
   const uint32_t xat = 4u * (xrow * (uint32_t)a.xs + cx), zat = 4u * (xrow * (uint32_t)a.zs + cx);
   const int rec0 = record_of(begin, b);
   // A chunk's operands have one set of registers each: the next chunk's are
-  // loaded into them behind their last use, a step ahead of their own.
-  v4f cf[CF], gf[GF], bf[TPW][4], xcur, xnext, z;
+  // loaded into them behind their last use, a step ahead of their own.  (A
+  // scheduling barrier before each load: moved up, it would need other registers,
+  // and copies at the loop's end that wait for it: 616 us.)
+  v4f cf[CF], gf[GF], bf[TPW][4], x, z;
   float dec1;                                    // of one of the decay arrays
   const auto record = [&](int c) {
     return a.gram + ((int64_t)(rec0 + min(c, nch - 1)) * a.NG + g) * rec_floats(N) + 4 * lane;
@@ -308,7 +312,7 @@ __global__ __launch_bounds__(SNT) void scan_kernel(ScanArgs a) {
     for (int s = 0; s < GF; s++) gf[s] = quad(q + tile_at(r, min(KH == 2 ? kh + 2 * s : s, r)));
   };
   const auto load_x = [&](int c) {
-    xnext = load4(rows(a.x + (int64_t)h * a.P + c0, a.xs, c), xat, 0);
+    x = load4(rows(a.x + (int64_t)h * a.P + c0, a.xs, c), xat, 0);
     dec1 = a.dec[((int64_t)(rec0 + min(c, nch - 1)) * a.NH + h) * (DEC * SC) + min(wave, DEC - 1) * SC + lane];
   };
   const float *const zh = a.z ? a.z + (int64_t)h * a.P + c0 : a.x;
@@ -317,9 +321,8 @@ __global__ __launch_bounds__(SNT) void scan_kernel(ScanArgs a) {
   const auto stage = [&](int p) {
     if (wave < XW)
 #pragma unroll
-      for (int e = 0; e < 4; e++) L.xt[p][xc + e][xr] = xnext[e];
+      for (int e = 0; e < 4; e++) L.xt[p][xc + e][xr] = x[e];
     if (wave < DEC) L.dec[p][wave][lane] = dec1;
-    xcur = xnext;
   };
 
   const int64_t src = seq_src(a.q, b), dst = seq_dst(a.q, b);
@@ -347,7 +350,6 @@ __global__ __launch_bounds__(SNT) void scan_kernel(ScanArgs a) {
   put_state(0);
   stage(0);
   load_x(1);
-  v4f xe = xcur;                                 // x of the chunk whose outputs are written
   __syncthreads();
   for (int c = 0; c < nch; c++) {
     const int p = c & 1;
@@ -360,6 +362,9 @@ __global__ __launch_bounds__(SNT) void scan_kernel(ScanArgs a) {
 #pragma unroll
     for (int s = 0; s < CF; s++)
       mm4(cf[s], quad(&L.st[p][16 * ct + l16][kh * (N / KH) + 16 * s + 4 * lq]), y0, y1);
+    pin(y0);
+    pin(y1);
+    __builtin_amdgcn_sched_barrier(0);
     load_c(c + 1);
     // S
     const float eC = dec[DEC_EL][SC - 1];
@@ -373,7 +378,9 @@ __global__ __launch_bounds__(SNT) void scan_kernel(ScanArgs a) {
         mm4(bf[i][s], w * xt[s], S[i], s1);
       }
       S[i] += s1;
+      pin(S[i]);
     }
+    __builtin_amdgcn_sched_barrier(0);
     load_b(c + 1);
     y0 = (y0 + y1) * quad(&dec[DEC_EL][16 * r + 4 * lq]);
     // (C B^T o decays) x
@@ -391,14 +398,21 @@ __global__ __launch_bounds__(SNT) void scan_kernel(ScanArgs a) {
         w[e] = gf[s][e] * (dl[e] * __builtin_amdgcn_exp2f((lhi - lh[e]) + (lli - ll[e])));
         if (16 * j + 4 * lq + e > 16 * r + l16) w[e] = 0.0f;
       }
-      mm4(w, KH == 2 ? (kh ? xt[2 * s + 1] : xt[2 * s]) : xt[s], y0, y1);
+      mm4(w, quad(&L.xt[p][16 * ct + l16][16 * j + 4 * lq]), y0, y1);
     }
-    load_g(c + 1);
     y0 += y1;
+    pin(y0);
+    __builtin_amdgcn_sched_barrier(0);
+    load_g(c + 1);
 #pragma unroll
     for (int e = 0; e < 4; e++) L.yl[p][kh][16 * r + 4 * lq + e][16 * ct + l16] = y0[e];
+    v4f xe = {0.f, 0.f, 0.f, 0.f};               // x of the outputs
+    if (wave < XW)
+#pragma unroll
+      for (int e = 0; e < 4; e++) xe[e] = L.xt[p][xc + e][xr];
     put_state(p ^ 1);
     stage(p ^ 1);                                // (past the last chunk unused)
+    __builtin_amdgcn_sched_barrier(0);
     load_x(c + 2);
     __syncthreads();
     if (wave < XW) {
@@ -410,8 +424,9 @@ __global__ __launch_bounds__(SNT) void scan_kernel(ScanArgs a) {
       if (t < end && c0 + xc < a.P)
         *reinterpret_cast<v4f *>(a.y + (int64_t)t * a.ys + (int64_t)h * a.P + c0 + xc) = o;
     }
-    xe = xcur;
+    __builtin_amdgcn_sched_barrier(0);
     load_z(c + 1);
+    __builtin_amdgcn_sched_barrier(0);
   }
   if (dst >= 0)
 #pragma unroll
