@@ -151,7 +151,8 @@ __device__ __forceinline__ double scan64(double v) {
 // Logarithms are summed in fp64 and kept in two halves so that differences of
 // long sums keep their precision: rows of strong decay (hundreds) may stand
 // beside rows of next to none.
-constexpr int DEC = 5, DEC_LH = 0, DEC_LL = 1, DEC_DL = 2, DEC_WJ = 3, DEC_EL = 4;
+constexpr int DEC = 5, DEC_LH = 0, DEC_LL = 1, DEC_EL = 2, DEC_DL = 3, DEC_WJ = 4;
+constexpr int DEC_LDS = 3;          // the first ones go to LDS, the others into x
 
 // What the chunks need that does not wait for the one before, a workgroup per
 // chunk and group, then one per chunk and four heads:
@@ -225,10 +226,11 @@ __global__ __launch_bounds__(256) void prep_kernel(ScanArgs a, unsigned ngram) {
 
 template <int N, int PS>
 struct ScanLds {
-  float xt[2][PS][SC + 4];          // x by column
+  float xd[2][PS][SC + 4];          // x by column, times the steps
+  float xw[2][PS][SC + 4];          // ... and the decays to the chunk's end
   float st[2][PS][N + 4];           // the state before the chunk by column
-  float yl[2][2][SC][PS + 4];       // sums of y: of either half of the state's rows
-  float dec[2][DEC][SC];
+  float yl[2][2 / (PS / 16)][SC][PS + 4];   // sums of y (N > 64: of either half of the state's rows)
+  float dec[2][DEC_LDS][SC];
   float red[SNT / 64][PS];
 };
 
@@ -289,8 +291,8 @@ __global__ __launch_bounds__(SNT) void scan_kernel(ScanArgs a) {
   // loaded into them behind their last use, a step ahead of their own.  (A
   // scheduling barrier before each load: moved up, it would need other registers,
   // and copies at the loop's end that wait for it: 616 us.)
-  v4f cf[CF], gf[GF], bf[TPW][4], x, z;
-  float dec1;                                    // of one of the decay arrays
+  v4f cf[CF], gf[GF], bf[TPW][4], x, xe, z;            // (xe: x for the outputs)
+  float dec1, dl, wj;                            // of one of the decay arrays; of x's row
   const auto record = [&](int c) {
     return a.gram + ((int64_t)(rec0 + min(c, nch - 1)) * a.NG + g) * rec_floats(N) + 4 * lane;
   };
@@ -313,16 +315,25 @@ __global__ __launch_bounds__(SNT) void scan_kernel(ScanArgs a) {
   };
   const auto load_x = [&](int c) {
     x = load4(rows(a.x + (int64_t)h * a.P + c0, a.xs, c), xat, 0);
-    dec1 = a.dec[((int64_t)(rec0 + min(c, nch - 1)) * a.NH + h) * (DEC * SC) + min(wave, DEC - 1) * SC + lane];
+    const float *const q = a.dec + ((int64_t)(rec0 + min(c, nch - 1)) * a.NH + h) * (DEC * SC);
+    dec1 = q[min(wave, DEC_LDS - 1) * SC + lane];
+    dl = q[DEC_DL * SC + xrow];
+    wj = q[DEC_WJ * SC + xrow];
   };
   const float *const zh = a.z ? a.z + (int64_t)h * a.P + c0 : a.x;
-  const auto load_z = [&](int c) { z = load4(rows(zh, a.zs, c, a.z != nullptr), zat, 0); };
+  const auto load_out = [&](int c) {
+    xe = load4(rows(a.x + (int64_t)h * a.P + c0, a.xs, c), xat, 0);
+    z = load4(rows(zh, a.zs, c, a.z != nullptr), zat, 0);
+  };
   // x by column, and the decays of a chunk
   const auto stage = [&](int p) {
     if (wave < XW)
 #pragma unroll
-      for (int e = 0; e < 4; e++) L.xt[p][xc + e][xr] = x[e];
-    if (wave < DEC) L.dec[p][wave][lane] = dec1;
+      for (int e = 0; e < 4; e++) {
+        L.xd[p][xc + e][xr] = dl * x[e];
+        L.xw[p][xc + e][xr] = wj * x[e];
+      }
+    if (wave < DEC_LDS) L.dec[p][wave][lane] = dec1;
   };
 
   const int64_t src = seq_src(a.q, b), dst = seq_dst(a.q, b);
@@ -346,7 +357,7 @@ __global__ __launch_bounds__(SNT) void scan_kernel(ScanArgs a) {
   load_c(0);
   load_b(0);
   load_g(0);
-  load_z(0);
+  load_out(0);
   put_state(0);
   stage(0);
   load_x(1);
@@ -354,9 +365,6 @@ __global__ __launch_bounds__(SNT) void scan_kernel(ScanArgs a) {
   for (int c = 0; c < nch; c++) {
     const int p = c & 1;
     const auto &dec = L.dec[p];
-    v4f xt[4];
-#pragma unroll
-    for (int s = 0; s < 4; s++) xt[s] = quad(&L.xt[p][16 * ct + l16][16 * s + 4 * lq]);
     // C S
     v4f y0 = {0.f, 0.f, 0.f, 0.f}, y1 = y0;
 #pragma unroll
@@ -373,10 +381,7 @@ __global__ __launch_bounds__(SNT) void scan_kernel(ScanArgs a) {
       v4f s1 = {0.f, 0.f, 0.f, 0.f};
       S[i] *= eC;
 #pragma unroll
-      for (int s = 0; s < 4; s++) {
-        const v4f w = quad(&dec[DEC_WJ][16 * s + 4 * lq]);
-        mm4(bf[i][s], w * xt[s], S[i], s1);
-      }
+      for (int s = 0; s < 4; s++) mm4(bf[i][s], quad(&L.xw[p][16 * ct + l16][16 * s + 4 * lq]), S[i], s1);
       S[i] += s1;
       pin(S[i]);
     }
@@ -391,14 +396,13 @@ __global__ __launch_bounds__(SNT) void scan_kernel(ScanArgs a) {
       const int j = KH == 2 ? kh + 2 * s : s;
       if (j > r) continue;
       const v4f lh = quad(&dec[DEC_LH][16 * j + 4 * lq]), ll = quad(&dec[DEC_LL][16 * j + 4 * lq]);
-      const v4f dl = quad(&dec[DEC_DL][16 * j + 4 * lq]);
       v4f w;
 #pragma unroll
       for (int e = 0; e < 4; e++) {
-        w[e] = gf[s][e] * (dl[e] * __builtin_amdgcn_exp2f((lhi - lh[e]) + (lli - ll[e])));
+        w[e] = gf[s][e] * __builtin_amdgcn_exp2f((lhi - lh[e]) + (lli - ll[e]));
         if (16 * j + 4 * lq + e > 16 * r + l16) w[e] = 0.0f;
       }
-      mm4(w, quad(&L.xt[p][16 * ct + l16][16 * j + 4 * lq]), y0, y1);
+      mm4(w, quad(&L.xd[p][16 * ct + l16][16 * j + 4 * lq]), y0, y1);
     }
     y0 += y1;
     pin(y0);
@@ -406,10 +410,6 @@ __global__ __launch_bounds__(SNT) void scan_kernel(ScanArgs a) {
     load_g(c + 1);
 #pragma unroll
     for (int e = 0; e < 4; e++) L.yl[p][kh][16 * r + 4 * lq + e][16 * ct + l16] = y0[e];
-    v4f xe = {0.f, 0.f, 0.f, 0.f};               // x of the outputs
-    if (wave < XW)
-#pragma unroll
-      for (int e = 0; e < 4; e++) xe[e] = L.xt[p][xc + e][xr];
     put_state(p ^ 1);
     stage(p ^ 1);                                // (past the last chunk unused)
     __builtin_amdgcn_sched_barrier(0);
@@ -425,7 +425,7 @@ __global__ __launch_bounds__(SNT) void scan_kernel(ScanArgs a) {
         *reinterpret_cast<v4f *>(a.y + (int64_t)t * a.ys + (int64_t)h * a.P + c0 + xc) = o;
     }
     __builtin_amdgcn_sched_barrier(0);
-    load_z(c + 1);
+    load_out(c + 1);
     __builtin_amdgcn_sched_barrier(0);
   }
   if (dst >= 0)
