@@ -224,11 +224,18 @@ __global__ __launch_bounds__(256) void prep_kernel(ScanArgs a, unsigned ngram) {
     }
 }
 
+// Matrices by column: 16-byte pieces of a column stand XOR-swizzled by the column,
+// so that lanes that read a piece of 16 columns, or different pieces of some, meet
+// distinct banks (with columns padded by 16 bytes half of the LDS cycles were
+// conflicts).
+template <int LEN>
+__device__ __forceinline__ int piece_at(int col, int piece) { return col * LEN + 4 * (piece ^ (col & 15)); }
+
 template <int N, int PS>
 struct ScanLds {
-  float xd[2][PS][SC + 4];          // x by column, times the steps
-  float xw[2][PS][SC + 4];          // ... and the decays to the chunk's end
-  float st[2][PS][N + 4];           // the state before the chunk by column
+  float xd[2][PS * SC];             // x by column, times the steps
+  float xw[2][PS * SC];             // ... and the decays to the chunk's end
+  float st[2][PS * N];              // the state before the chunk by column
   float yl[2][2 / (PS / 16)][SC][PS + 4];   // sums of y (N > 64: of either half of the state's rows)
   float dec[2][DEC_LDS][SC];
   float red[SNT / 64][PS];
@@ -330,8 +337,9 @@ __global__ __launch_bounds__(SNT) void scan_kernel(ScanArgs a) {
     if (wave < XW)
 #pragma unroll
       for (int e = 0; e < 4; e++) {
-        L.xd[p][xc + e][xr] = dl * x[e];
-        L.xw[p][xc + e][xr] = wj * x[e];
+        const int at = piece_at<SC>(xc + e, xr >> 2) + (xr & 3);
+        L.xd[p][at] = dl * x[e];
+        L.xw[p][at] = wj * x[e];
       }
     if (wave < DEC_LDS) L.dec[p][wave][lane] = dec1;
   };
@@ -350,7 +358,7 @@ __global__ __launch_bounds__(SNT) void scan_kernel(ScanArgs a) {
   const auto put_state = [&](int p) {
 #pragma unroll
     for (int i = 0; i < TPW; i++)
-      *reinterpret_cast<v4f *>(&L.st[p][16 * sct[i] + l16][16 * nt[i] + 4 * lq]) = S[i];
+      *reinterpret_cast<v4f *>(&L.st[p][piece_at<N>(16 * sct[i] + l16, 4 * nt[i] + lq)]) = S[i];
   };
 
   load_x(0);
@@ -369,7 +377,7 @@ __global__ __launch_bounds__(SNT) void scan_kernel(ScanArgs a) {
     v4f y0 = {0.f, 0.f, 0.f, 0.f}, y1 = y0;
 #pragma unroll
     for (int s = 0; s < CF; s++)
-      mm4(cf[s], quad(&L.st[p][16 * ct + l16][kh * (N / KH) + 16 * s + 4 * lq]), y0, y1);
+      mm4(cf[s], quad(&L.st[p][piece_at<N>(16 * ct + l16, 4 * (kh * CF + s) + lq)]), y0, y1);
     pin(y0);
     pin(y1);
     __builtin_amdgcn_sched_barrier(0);
@@ -381,7 +389,7 @@ __global__ __launch_bounds__(SNT) void scan_kernel(ScanArgs a) {
       v4f s1 = {0.f, 0.f, 0.f, 0.f};
       S[i] *= eC;
 #pragma unroll
-      for (int s = 0; s < 4; s++) mm4(bf[i][s], quad(&L.xw[p][16 * ct + l16][16 * s + 4 * lq]), S[i], s1);
+      for (int s = 0; s < 4; s++) mm4(bf[i][s], quad(&L.xw[p][piece_at<SC>(16 * ct + l16, 4 * s + lq)]), S[i], s1);
       S[i] += s1;
       pin(S[i]);
     }
@@ -402,7 +410,7 @@ __global__ __launch_bounds__(SNT) void scan_kernel(ScanArgs a) {
         w[e] = gf[s][e] * __builtin_amdgcn_exp2f((lhi - lh[e]) + (lli - ll[e]));
         if (16 * j + 4 * lq + e > 16 * r + l16) w[e] = 0.0f;
       }
-      mm4(w, quad(&L.xd[p][16 * ct + l16][16 * j + 4 * lq]), y0, y1);
+      mm4(w, quad(&L.xd[p][piece_at<SC>(16 * ct + l16, 4 * j + lq)]), y0, y1);
     }
     y0 += y1;
     pin(y0);
