@@ -15,6 +15,7 @@ constexpr int STEP_NT = 256;        // ... of a step workgroup
 constexpr int STEP_T = 8;           // sequences of up to this many rows go row by row
 
 typedef float v4f __attribute__((ext_vector_type(4)));
+typedef uint32_t v4u __attribute__((ext_vector_type(4)));
 
 struct ScanArgs {
   Seqs q;
@@ -279,58 +280,76 @@ __global__ __launch_bounds__(SNT) void scan_kernel(ScanArgs a) {
   constexpr int XW = PS / 4;                     // waves that have a row of x
   const int xr = tid / (PS / 4), xc = 4 * (tid % (PS / 4));
 
-  // Rows of a chunk are read as buffers that end at the sequence's last row: past
-  // it, and past the last chunk, loads give zeros, so none needs a condition.
-  // (The number of rows by way of readfirstlane: a clamp is a VALU operation, and
-  // the buffer's words belong in scalar registers.)
-  const auto rows = [&](const float *p, int stride, int c, bool there = true) {
-    const int left = __builtin_amdgcn_readfirstlane(there ? min(max(end - begin - c * SC, 0), SC) : 0);
-    return __builtin_amdgcn_make_buffer_rsrc(const_cast<float *>(p + (begin + (int64_t)c * SC) * stride), 0,
-                                             (int)((uint32_t)left * (uint32_t)stride * 4u), 0x00027000);
+  // Everything of a chunk is read as buffers, by offsets that stay, from bases that
+  // move on a chunk with each load: no address is computed by the lanes.  The rows'
+  // buffers end at the sequence's last row: past it loads give zeros and stores
+  // do nothing, so none needs a condition.
+  typedef __amdgpu_buffer_rsrc_t Rsrc;
+  const auto buffer = [](const float *p, uint32_t bytes) {
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<float *>(p), 0, (int)bytes, 0x00027000);
   };
-  const auto load4 = [](__amdgpu_buffer_rsrc_t q, uint32_t at, uint32_t more) {
+  const auto load4 = [](Rsrc q, uint32_t at, uint32_t more) {
     return __builtin_bit_cast(v4f, __builtin_amdgcn_raw_buffer_load_b128(q, at, more, 0));
+  };
+  const auto load1 = [](Rsrc q, uint32_t at, uint32_t more) {
+    return __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(q, at, more, 0));
+  };
+  struct Rows {                                  // a tensor's rows from the next chunk on
+    const float *p;
+    int stride, left;
+  };
+  const auto rows = [&](const float *p, int stride) {
+    return Rows{p + (int64_t)begin * stride, stride, end - begin};
+  };
+  const auto next = [&](Rows &q) {
+    const Rsrc b = buffer(q.p, (uint32_t)min(q.left, SC) * (uint32_t)q.stride * 4u);
+    q.p += (int64_t)SC * q.stride;
+    q.left = max(q.left - SC, 0);
+    return b;
   };
   const int xrow = min(xr, SC - 1), cx = min(xc, a.P - 4 - c0);
   const uint32_t xat = 4u * (xrow * (uint32_t)a.xs + cx), zat = 4u * (xrow * (uint32_t)a.zs + cx);
-  const int rec0 = record_of(begin, b);
+  const uint32_t yat = c0 + xc < a.P ? 4u * (xrow * (uint32_t)a.ys + xc) : 0xFFFFFFF0u;
+  const uint32_t lane16 = 16 * lane, row4 = 4 * xrow;
+  const int64_t hp = (int64_t)h * a.P + c0, rec0 = record_of(begin, b);
+  Rows xrows = rows(a.x + hp, a.xs), erows = xrows, yrows = rows(a.y + hp, a.ys),
+       zrows = rows((a.z ? a.z : a.x) + hp, a.zs);
+  constexpr int RF = rec_floats(N);
+  const float *recp = a.gram + (rec0 * a.NG + g) * RF, *decp = a.dec + (rec0 * a.NH + h) * (DEC * SC);
   // A chunk's operands have one set of registers each: the next chunk's are
   // loaded into them behind their last use, a step ahead of their own.  (A
   // scheduling barrier before each load: moved up, it would need other registers,
   // and copies at the loop's end that wait for it: 616 us.)
-  v4f cf[CF], gf[GF], bf[TPW][4], x, xe, z;            // (xe: x for the outputs)
+  v4f cf[CF], gf[GF], bf[TPW][4], x, xe, z;      // (xe: x for the outputs)
   float dec1, dl, wj;                            // of one of the decay arrays; of x's row
-  const auto record = [&](int c) {
-    return a.gram + ((int64_t)(rec0 + min(c, nch - 1)) * a.NG + g) * rec_floats(N) + 4 * lane;
-  };
-  const auto load_c = [&](int c) {
-    const float *const q = record(c) + GRAM + N * SC + (r * NT + kh * CF) * 256;
+  Rsrc rec;
+  const auto load_c = [&]() {
+    rec = buffer(recp, 4 * RF);
+    recp += (int64_t)a.NG * RF;
 #pragma unroll
-    for (int s = 0; s < CF; s++) cf[s] = quad(q + 256 * s);
+    for (int s = 0; s < CF; s++) cf[s] = load4(rec, lane16, 4 * (GRAM + N * SC + (r * NT + kh * CF + s) * 256));
   };
-  const auto load_b = [&](int c) {
-    const float *const q = record(c) + GRAM;
+  const auto load_b = [&]() {
 #pragma unroll
     for (int i = 0; i < TPW; i++)
 #pragma unroll
-      for (int s = 0; s < 4; s++) bf[i][s] = quad(q + (4 * nt[i] + s) * 256);
+      for (int s = 0; s < 4; s++) bf[i][s] = load4(rec, lane16, 4 * (GRAM + (4 * nt[i] + s) * 256));
   };
-  const auto load_g = [&](int c) {
-    const float *const q = record(c);
+  const auto load_g = [&]() {
 #pragma unroll
-    for (int s = 0; s < GF; s++) gf[s] = quad(q + tile_at(r, min(KH == 2 ? kh + 2 * s : s, r)));
+    for (int s = 0; s < GF; s++) gf[s] = load4(rec, lane16, 4 * tile_at(r, min(KH == 2 ? kh + 2 * s : s, r)));
   };
-  const auto load_x = [&](int c) {
-    x = load4(rows(a.x + (int64_t)h * a.P + c0, a.xs, c), xat, 0);
-    const float *const q = a.dec + ((int64_t)(rec0 + min(c, nch - 1)) * a.NH + h) * (DEC * SC);
-    dec1 = q[min(wave, DEC_LDS - 1) * SC + lane];
-    dl = q[DEC_DL * SC + xrow];
-    wj = q[DEC_WJ * SC + xrow];
+  const auto load_x = [&]() {
+    x = load4(next(xrows), xat, 0);
+    const Rsrc q = buffer(decp, 4 * DEC * SC);
+    decp += (int64_t)a.NH * (DEC * SC);
+    dec1 = load1(q, 4 * lane, 4 * min(wave, DEC_LDS - 1) * SC);
+    dl = load1(q, row4, 4 * DEC_DL * SC);
+    wj = load1(q, row4, 4 * DEC_WJ * SC);
   };
-  const float *const zh = a.z ? a.z + (int64_t)h * a.P + c0 : a.x;
-  const auto load_out = [&](int c) {
-    xe = load4(rows(a.x + (int64_t)h * a.P + c0, a.xs, c), xat, 0);
-    z = load4(rows(zh, a.zs, c, a.z != nullptr), zat, 0);
+  const auto load_out = [&]() {
+    xe = load4(next(erows), xat, 0);
+    z = load4(next(zrows), zat, 0);
   };
   // x by column, and the decays of a chunk
   const auto stage = [&](int p) {
@@ -361,14 +380,14 @@ __global__ __launch_bounds__(SNT) void scan_kernel(ScanArgs a) {
       *reinterpret_cast<v4f *>(&L.st[p][piece_at<N>(16 * sct[i] + l16, 4 * nt[i] + lq)]) = S[i];
   };
 
-  load_x(0);
-  load_c(0);
-  load_b(0);
-  load_g(0);
-  load_out(0);
+  load_x();
+  load_c();
+  load_b();
+  load_g();
+  load_out();
   put_state(0);
   stage(0);
-  load_x(1);
+  load_x();
   __syncthreads();
   for (int c = 0; c < nch; c++) {
     const int p = c & 1;
@@ -381,7 +400,7 @@ __global__ __launch_bounds__(SNT) void scan_kernel(ScanArgs a) {
     pin(y0);
     pin(y1);
     __builtin_amdgcn_sched_barrier(0);
-    load_c(c + 1);
+    load_c();
     // S
     const float eC = dec[DEC_EL][SC - 1];
 #pragma unroll
@@ -394,7 +413,7 @@ __global__ __launch_bounds__(SNT) void scan_kernel(ScanArgs a) {
       pin(S[i]);
     }
     __builtin_amdgcn_sched_barrier(0);
-    load_b(c + 1);
+    load_b();
     y0 = (y0 + y1) * quad(&dec[DEC_EL][16 * r + 4 * lq]);
     // (C B^T o decays) x
     const float lhi = dec[DEC_LH][16 * r + l16], lli = dec[DEC_LL][16 * r + l16];
@@ -415,25 +434,23 @@ __global__ __launch_bounds__(SNT) void scan_kernel(ScanArgs a) {
     y0 += y1;
     pin(y0);
     __builtin_amdgcn_sched_barrier(0);
-    load_g(c + 1);
+    load_g();
 #pragma unroll
     for (int e = 0; e < 4; e++) L.yl[p][kh][16 * r + 4 * lq + e][16 * ct + l16] = y0[e];
     put_state(p ^ 1);
     stage(p ^ 1);                                // (past the last chunk unused)
     __builtin_amdgcn_sched_barrier(0);
-    load_x(c + 2);
+    load_x();
     __syncthreads();
     if (wave < XW) {
       v4f o = quad(&L.yl[p][0][xr][xc]);
       if (KH == 2) o += quad(&L.yl[p][1][xr][xc]);
       o += D * xe;
       if (a.z) o *= v4f{silu_f32(z.x), silu_f32(z.y), silu_f32(z.z), silu_f32(z.w)};
-      const int t = begin + c * SC + xr;
-      if (t < end && c0 + xc < a.P)
-        *reinterpret_cast<v4f *>(a.y + (int64_t)t * a.ys + (int64_t)h * a.P + c0 + xc) = o;
+      __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(v4u, o), next(yrows), yat, 0, 0);
     }
     __builtin_amdgcn_sched_barrier(0);
-    load_out(c + 1);
+    load_out();
     __builtin_amdgcn_sched_barrier(0);
   }
   if (dst >= 0)
@@ -447,7 +464,8 @@ __global__ __launch_bounds__(SNT) void scan_kernel(ScanArgs a) {
     }
 }
 
-int64_t records(const Seqs &q) { return (int64_t)q.T / SC + q.B + 1; }
+// Records of a call; the scan's loads run two past a sequence's last.
+int64_t records(int64_t T, int64_t B) { return T / SC + B + 3; }
 
 int ssm_sizes(const w4a8_seqs *q, const w4a8_ssm *m, int64_t T) {
   if (!m) return W4A8_ENULL;
@@ -458,7 +476,7 @@ int ssm_sizes(const w4a8_seqs *q, const w4a8_ssm *m, int64_t T) {
     return W4A8_ESHAPE;
   // (a grid's threads are counted in 32 bits)
   if (m->NH >= (1 << 16) || m->P > 4096 || q->B * m->NH * m->P >= ((int64_t)1 << 27) ||
-      (T / SC + q->B + 1) * (m->NG + m->NH) >= ((int64_t)1 << 23))
+      (T / SC + q->B + 3) * (m->NG + m->NH) >= ((int64_t)1 << 23))
     return W4A8_ERANGE;
   return W4A8_OK;
 }
@@ -470,7 +488,7 @@ int launch_ssm(ScanArgs a, hipStream_t s) {
     step_kernel<N, 64><<<dim3((unsigned)(a.q.B * a.NH * a.nsl)), dim3(STEP_NT), 0, s>>>(a);
     return check_launch();
   }
-  const unsigned ngram = (unsigned)(records(a.q) * a.NG), ndec = (unsigned)(records(a.q) * ((a.NH + 3) / 4));
+  const unsigned ngram = (unsigned)(records(a.q.T, a.q.B) * a.NG), ndec = (unsigned)(records(a.q.T, a.q.B) * ((a.NH + 3) / 4));
   prep_kernel<N><<<dim3(ngram + ndec), dim3(256), 0, s>>>(a, ngram);
   if (int rc = check_launch(); rc != W4A8_OK) return rc;
   constexpr int PS = N == 64 ? 32 : 16;
@@ -488,7 +506,7 @@ using namespace w4a8;
 
 extern "C" size_t ssm_workspace_size(const w4a8_seqs *seqs, const w4a8_ssm *ssm, int64_t T) {
   if (ssm_sizes(seqs, ssm, T) != W4A8_OK) return 0;
-  return (size_t)(T / SC + seqs->B + 1) * (ssm->NG * rec_floats((int)ssm->N) + ssm->NH * DEC * SC) *
+  return (size_t)records(T, seqs->B) * (ssm->NG * rec_floats((int)ssm->N) + ssm->NH * DEC * SC) *
          sizeof(float);
 }
 
@@ -523,9 +541,9 @@ extern "C" int ssm_scan(const w4a8_seqs *seqs, const w4a8_ssm *m, float *state, 
   a.x = m->x; a.dt = m->dt; a.b = m->b; a.c = m->c; a.z = m->z;
   a.A = m->A; a.D = m->D; a.bias = m->dt_bias;
   a.state = state; a.y = y; a.gram = reinterpret_cast<float *>(workspace);
-  a.dec = a.gram + records(a.q) * m->NG * rec_floats((int)m->N);
+  a.dec = a.gram + records(a.q.T, a.q.B) * m->NG * rec_floats((int)m->N);
   a.xs = (int)m->x_stride; a.ds = (int)m->dt_stride; a.bs = (int)m->b_stride; a.cs = (int)m->c_stride;
-  a.zs = (int)m->z_stride; a.ys = (int)y_stride;
+  a.zs = m->z ? (int)m->z_stride : 0; a.ys = (int)y_stride;
   a.NH = (int)m->NH; a.NG = (int)m->NG; a.G = (int)(m->NH / m->NG); a.P = (int)m->P;
   a.softplus = m->softplus;
   hipStream_t s = as_stream(stream);
