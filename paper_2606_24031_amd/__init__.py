@@ -810,18 +810,27 @@ def q8_row_quantize(x, q=None, d=None, stream=None):
     return q, d
 
 
+def _q8_rows(q, d, what):
+    """8-bit rows: codes [rows, multiple of 128] and scales [rows]; returns
+    that shape."""
+    if q.dtype is torch.int8 and q.dim() == 2 and q.is_contiguous() and d.dtype is torch.float32 and \
+            d.dim() == 1 and d.is_contiguous():
+        rows, KP = q.shape
+        if KP % Q8_ROW_PAD == 0 and d.numel() == rows:
+            return rows, KP
+    raise ValueError(f"{what}: contiguous int8 codes [rows, multiple of {Q8_ROW_PAD}] and fp32 scales [rows] are "
+                     f"needed, got {q.dtype} {tuple(q.shape)} and {d.dtype} {tuple(d.shape)} with strides "
+                     f"{q.stride()} and {d.stride()}")
+
+
 def q8q8_gemm(xq, xd, wq, wd, bias=None, out=None, stream=None):
     """out [M, N] fp32 (rows may be strided) = the product of 8-bit rows xq [M,
     KP] with scales xd [M] and weight rows wq [N, KP] with scales wd [N], plus
     bias [N]."""
-    _is(xq, torch.int8, (None, None), "xq")
-    M, KP = xq.shape
-    _is(wq, torch.int8, (None, KP), "wq")
-    N = wq.shape[0]
-    if KP % Q8_ROW_PAD:
-        raise ValueError(f"xq: rows of a multiple of {Q8_ROW_PAD} codes are needed, got {KP}")
-    _is(xd, torch.float32, (M,), "xd")
-    _is(wd, torch.float32, (N,), "wd")
+    M, KP = _q8_rows(xq, xd, "xq, xd")
+    N, KW = _q8_rows(wq, wd, "wq, wd")
+    if KP != KW:
+        raise ValueError(f"xq and wq: rows of {KP} and {KW} codes")
     if bias is not None:
         _is(bias, torch.float32, (N,), "bias")
     if out is None:

@@ -127,8 +127,12 @@ extern "C" int short_conv(const w4a8_seqs *seqs, const float *x, int64_t x_strid
   a.x = x; a.w = w; a.bias = bias; a.state = state; a.out = out;
   a.xs = x_stride; a.os = out_stride; a.CH = (int)CH;
   a.nx = (int)((CH + 255) / 256);
+  // Runs of 16 rows, fewer while the call would leave a compute unit fewer than 32
+  // waves, so that a decode batch's sequences are not taken one behind the other;
+  // more where the grid would be too large (its threads are counted in 32 bits).
   int64_t grid, R = 16;
-  for (;; R *= 2) {                 // (a grid's threads are counted in 32 bits)
+  while (R > 1 && a.nx * T < 32 * R * device_cus()) R /= 2;
+  for (;; R *= 2) {
     grid = a.nx * ((T + R * (CNT / 64) - 1) / (R * (CNT / 64)));
     if (grid < (1 << 23)) break;
   }
