@@ -12,7 +12,7 @@ namespace {
 constexpr int SC = 64;              // rows of a chunk
 constexpr int SNT = 512;            // threads of a scan workgroup: eight waves
 constexpr int STEP_NT = 256;        // ... of a step workgroup
-constexpr int STEP_T = 8;           // sequences of up to this many rows go row by row
+constexpr int STEP_T = 8;           // sequences of up to this many rows may go row by row
 
 typedef float v4f __attribute__((ext_vector_type(4)));
 typedef uint32_t v4u __attribute__((ext_vector_type(4)));
@@ -24,6 +24,7 @@ struct ScanArgs {
   int xs, ds, bs, cs, zs, ys;       // strides
   int NH, G, NG, P, nsl;            // heads, heads of a group, groups, columns, slices of columns
   int softplus;
+  int done;                         // chunks: sequences of up to so many rows are another launch's
 };
 
 // The step of a row: dt + bias, and log(1 + exp(.)) of it.
@@ -34,58 +35,81 @@ __device__ __forceinline__ float step_of(float dt, float bias, int softplus) {
 
 // One sequence's rows for COLS columns of a head, the recurrence as written.
 // A lane holds four columns of every RG-th row of S, in registers from the
-// first row of the sequence to its last.
-template <int N, int COLS, int NT>
+// first row of the sequence to its last.  TB rows at a time: their inputs are
+// loaded together, and their outputs, sums over the lanes and waves, joined
+// behind one barrier.
+template <int COLS, int NT, int TB>
+struct StepLds {
+  float part[TB][NT / 64][COLS];
+};
+template <int N, int COLS, int NT, int TB>
 __device__ __forceinline__ void step_rows(const ScanArgs &a, int b, int h, int c0, int begin, int end,
-                                          float (*red)[COLS]) {
+                                          StepLds<COLS, NT, TB> &L) {
   constexpr int CL = COLS / 4, RG = NT / CL, RPT = N / RG;
-  static_assert(RPT >= 1 && RPT * RG == N && CL <= 64, "rows of S over the threads");
+  static_assert(RPT >= 1 && RPT * RG == N && CL <= 64 && TB * CL <= NT, "rows of S over the threads");
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int c = c0 + 4 * (tid % CL), r0 = tid / CL;
   const bool live = c < a.P;
-  const int64_t src = seq_src(a.q, b), dst = seq_dst(a.q, b);
+  const int cc = min(c, a.P - 4);
+  const int64_t src = seq_src(a.q, b), dst = seq_dst(a.q, b), hp = (int64_t)h * a.P;
   const float A = a.A[h], bias = a.bias ? a.bias[h] : 0.0f, D = a.D ? a.D[h] : 0.0f;
-  const int g = h / a.G;
+  const int64_t gn = (int64_t)(h / a.G) * N + r0;
   v4f S[RPT];
 #pragma unroll
   for (int m = 0; m < RPT; m++)
     S[m] = src >= 0 && live
                ? *reinterpret_cast<const v4f *>(a.state + ((src * a.NH + h) * N + r0 + RG * m) * a.P + c)
                : v4f{0.f, 0.f, 0.f, 0.f};
-  for (int t = begin; t < end; t++) {
-    const float *bt = a.b + (int64_t)t * a.bs + (int64_t)g * N, *ct = a.c + (int64_t)t * a.cs + (int64_t)g * N;
-    const v4f x = live ? *reinterpret_cast<const v4f *>(a.x + (int64_t)t * a.xs + (int64_t)h * a.P + c)
-                       : v4f{0.f, 0.f, 0.f, 0.f};
-    const float d = step_of(a.dt[(int64_t)t * a.ds + h], bias, a.softplus);
-    const float keep = expf(d * A);
-    const v4f dx = d * x;
-    v4f y = {0.f, 0.f, 0.f, 0.f};
+  for (int t0 = begin; t0 < end; t0 += TB) {
+    v4f x[TB], xo, zo;                           // (xo, zo: of the output that this thread joins)
+    float bn[TB][RPT], cn[TB][RPT], dt[TB];
 #pragma unroll
-    for (int m = 0; m < RPT; m++) {
-      const float bn = bt[r0 + RG * m], cn = ct[r0 + RG * m];
+    for (int u = 0; u < TB; u++) {
+      const int64_t t = min(t0 + u, end - 1);
+      x[u] = *reinterpret_cast<const v4f *>(a.x + t * a.xs + hp + cc);
+      dt[u] = a.dt[t * a.ds + h];
 #pragma unroll
-      for (int e = 0; e < 4; e++) {
-        S[m][e] = fmaf(keep, S[m][e], bn * dx[e]);
-        y[e] = fmaf(cn, S[m][e], y[e]);
+      for (int m = 0; m < RPT; m++) {
+        bn[u][m] = a.b[t * a.bs + gn + RG * m];
+        cn[u][m] = a.c[t * a.cs + gn + RG * m];
       }
     }
+    const int64_t to = min(t0 + tid / CL, end - 1);
+    const bool joins = tid < TB * CL && t0 + tid / CL < end && live;
+    if (joins) {
+      xo = *reinterpret_cast<const v4f *>(a.x + to * a.xs + hp + cc);
+      if (a.z) zo = *reinterpret_cast<const v4f *>(a.z + to * a.zs + hp + cc);
+    }
 #pragma unroll
-    for (int o = CL; o < 64; o <<= 1)
+    for (int u = 0; u < TB; u++) {
+      if (u > 0 && t0 + u >= end) break;
+      const float d = step_of(dt[u], bias, a.softplus);
+      const float keep = expf(d * A);
+      const v4f dx = d * x[u];
+      v4f y = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int e = 0; e < 4; e++) y[e] += __shfl_xor(y[e], o);
-    if (lane < CL) *reinterpret_cast<v4f *>(&red[wave][4 * lane]) = y;
+      for (int m = 0; m < RPT; m++)
+#pragma unroll
+        for (int e = 0; e < 4; e++) {
+          S[m][e] = fmaf(keep, S[m][e], bn[u][m] * dx[e]);
+          y[e] = fmaf(cn[u][m], S[m][e], y[e]);
+        }
+#pragma unroll
+      for (int o = CL; o < 64; o <<= 1)
+#pragma unroll
+        for (int e = 0; e < 4; e++) y[e] += __shfl_xor(y[e], o);
+      if (lane < CL) *reinterpret_cast<v4f *>(&L.part[u][wave][4 * lane]) = y;
+    }
     __syncthreads();
-    if (tid < CL && live) {
-      v4f s = D * x;
+    if (joins) {
+      v4f s = D * xo;
 #pragma unroll
-      for (int w = 0; w < NT / 64; w++) s += *reinterpret_cast<const v4f *>(&red[w][4 * tid]);
-      if (a.z) {
-        const v4f z = *reinterpret_cast<const v4f *>(a.z + (int64_t)t * a.zs + (int64_t)h * a.P + c);
-        s *= v4f{silu_f32(z.x), silu_f32(z.y), silu_f32(z.z), silu_f32(z.w)};
-      }
-      *reinterpret_cast<v4f *>(a.y + (int64_t)t * a.ys + (int64_t)h * a.P + c) = s;
+      for (int w = 0; w < NT / 64; w++)
+        s += *reinterpret_cast<const v4f *>(&L.part[tid / CL][w][4 * (tid % CL)]);
+      if (a.z) s *= v4f{silu_f32(zo.x), silu_f32(zo.y), silu_f32(zo.z), silu_f32(zo.w)};
+      *reinterpret_cast<v4f *>(a.y + to * a.ys + hp + c) = s;
     }
-    __syncthreads();                // red is rewritten for the next row
+    if (t0 + TB < end) __syncthreads();          // the partial sums are rewritten
   }
   if (dst >= 0 && live)
 #pragma unroll
@@ -93,13 +117,15 @@ __device__ __forceinline__ void step_rows(const ScanArgs &a, int b, int h, int c
       *reinterpret_cast<v4f *>(a.state + ((dst * a.NH + h) * N + r0 + RG * m) * a.P + c) = S[m];
 }
 
-template <int N, int COLS>
-__global__ __launch_bounds__(STEP_NT) void step_kernel(ScanArgs a) {
-  __shared__ __align__(16) float red[STEP_NT / 64][COLS];
+// Sequences row by row, 64 columns of a head a workgroup; with `most`, those of
+// up to that many rows.
+template <int N, int TB>
+__global__ __launch_bounds__(STEP_NT) void step_kernel(ScanArgs a, int most) {
+  __shared__ __align__(16) StepLds<64, STEP_NT, TB> L;
   const int sl = blockIdx.x % a.nsl, bh = blockIdx.x / a.nsl, h = bh % a.NH, b = bh / a.NH;
   const int begin = seq_begin(a.q, b), end = seq_begin(a.q, b + 1);
-  if (begin >= end) return;
-  step_rows<N, COLS, STEP_NT>(a, b, h, sl * COLS, begin, end, red);
+  if (begin >= end || (most && end - begin > most)) return;
+  step_rows<N, 64, STEP_NT, TB>(a, b, h, sl * 64, begin, end, L);
 }
 
 // ---------------------------------------------------------------- chunked scan
@@ -176,7 +202,7 @@ __global__ __launch_bounds__(256) void prep_kernel(ScanArgs a, unsigned ngram) {
   }
   const int begin = seq_begin(a.q, lo), end = seq_begin(a.q, lo + 1);
   const int t0 = begin + (rec - record_of(begin, lo)) * SC;
-  if (t0 < begin || t0 >= end || end - begin <= STEP_T) return;
+  if (t0 < begin || t0 >= end || end - begin <= a.done) return;
   if (!gram) {
     const int h = 4 * part + wave;
     if (h >= a.NH) return;
@@ -239,7 +265,6 @@ struct ScanLds {
   float st[2][PS * N];              // the state before the chunk by column
   float yl[2][2 / (PS / 16)][SC][PS + 4];   // sums of y (N > 64: of either half of the state's rows)
   float dec[2][DEC_LDS][SC];
-  float red[SNT / 64][PS];
 };
 
 // The chunks of a sequence in order, for one head and PS columns; the state's
@@ -261,11 +286,7 @@ __global__ __launch_bounds__(SNT) void scan_kernel(ScanArgs a) {
   const int b = bh / a.NH, h = bh % a.NH, g = h / a.G, c0 = (k % a.nsl) * PS;
   const int begin = __builtin_amdgcn_readfirstlane(seq_begin(a.q, b)),
             end = __builtin_amdgcn_readfirstlane(seq_begin(a.q, b + 1));
-  if (begin >= end) return;
-  if (end - begin <= STEP_T) {
-    step_rows<N, PS, SNT>(a, b, h, c0, begin, end, L.red);
-    return;
-  }
+  if (begin >= end || end - begin <= a.done) return;
   const int nch = (end - begin + SC - 1) / SC;
   const float D = a.D ? a.D[h] : 0.0f;
 
@@ -483,10 +504,21 @@ int ssm_sizes(const w4a8_seqs *q, const w4a8_ssm *m, int64_t T) {
 
 template <int N>
 int launch_ssm(ScanArgs a, hipStream_t s) {
-  if (a.q.T <= STEP_T || a.q.T <= a.q.B) {
-    a.nsl = (a.P + 63) / 64;
-    step_kernel<N, 64><<<dim3((unsigned)(a.q.B * a.NH * a.nsl)), dim3(STEP_NT), 0, s>>>(a);
+  // Row by row where no sequence can be long, or hardly one (as many sequences as
+  // rows).  Batches that may hold many short sequences beside long ones: the short
+  // ones in that launch too (16 of 4 rows, 64 heads of 64: 26 us), the others chunk
+  // by chunk; few short ones do not pay for a launch.
+  constexpr int TB = N == 256 ? 2 : 4;
+  const unsigned steps = (unsigned)(a.q.B * a.NH * ((a.P + 63) / 64));
+  a.nsl = (a.P + 63) / 64;
+  if (a.q.T <= a.q.B) {
+    step_kernel<N, 1><<<dim3(steps), dim3(STEP_NT), 0, s>>>(a, 0);
     return check_launch();
+  }
+  if (a.q.T <= STEP_T || a.q.T / 64 < a.q.B) {
+    a.done = a.q.T <= STEP_T ? 0 : STEP_T;
+    step_kernel<N, TB><<<dim3(steps), dim3(STEP_NT), 0, s>>>(a, a.done);
+    if (int rc = check_launch(); rc != W4A8_OK || a.q.T <= STEP_T) return rc;
   }
   const unsigned ngram = (unsigned)(records(a.q.T, a.q.B) * a.NG), ndec = (unsigned)(records(a.q.T, a.q.B) * ((a.NH + 3) / 4));
   prep_kernel<N><<<dim3(ngram + ndec), dim3(256), 0, s>>>(a, ngram);
