@@ -575,7 +575,7 @@ int short_conv(const w4a8_seqs *seqs, const float *x, int64_t x_stride, const fl
  * NH % NG != 0, N not 64, 128 or 256, P < 16, P % 16 != 0, a stride below its
  * row's elements, or (but for dt's) not a multiple of 4 -> W4A8_ESHAPE; T >=
  * 2^31, NH >= 2^16, P > 4096, a stride >= 2^24, B * NH * P >= 2^27 or (T / 64 + B + 3)
- * * (NG + NH) >= 2^23 -> W4A8_ERANGE; x, dt, b, c,
+ * * (NG + NH) >= 2^21 -> W4A8_ERANGE; x, dt, b, c,
  * A, y or workspace, or state with n_slots > 0, NULL -> W4A8_ENULL; dt, A, D or
  * dt_bias not 4-, another pointer not 16-byte aligned -> W4A8_EALIGN; y or
  * state equal to an input or to each other -> W4A8_EALIAS; workspace too small

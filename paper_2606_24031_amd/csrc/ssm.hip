@@ -181,19 +181,21 @@ __device__ __forceinline__ double scan64(double v) {
 constexpr int DEC = 5, DEC_LH = 0, DEC_LL = 1, DEC_EL = 2, DEC_DL = 3, DEC_WJ = 4;
 constexpr int DEC_LDS = 3;          // the first ones go to LDS, the others into x
 
-// What the chunks need that does not wait for the one before, a workgroup per
-// chunk and group, then one per chunk and four heads:
-//   C B^T, a wave per 16 rows of C.  The rows of B are the A operand, so that a
-//   lane's sums are neighbouring columns of one row.  Rows past the sequence's
-//   last repeat it (their steps are 0 where they are used).  Then B^T and C, a lane's
-//   four numbers of a product together and 1 KB an instruction (gathered by the
-//   scan 16384 rows of 64 heads of 64 took 718 us, B^T here 631).
-//   the steps and decays, a wave per head, a row a lane.
+// What the chunks need that does not wait for the one before: a record's pieces,
+// a wave each (one trip to memory; a workgroup of four waves for all of a record
+// took 12 us for a 947-token prompt), then the steps and decays, a wave per chunk and
+// head, a row a lane.
+//   C B^T: the rows of B are the A operand, so that a lane's sums are neighbouring
+//   columns of one row.  Rows past the sequence's last repeat it (their steps are 0
+//   where they are used).
+//   B^T and C: a lane's four numbers of a product together and 1 KB an instruction
+//   (gathered by the scan 16384 rows of 64 heads of 64 took 718 us, B^T here 631).
+constexpr int prep_parts(int N) { return (10 + N / 16 + 4 + 3) / 4; }
 template <int N>
 __global__ __launch_bounds__(256) void prep_kernel(ScanArgs a, unsigned ngram) {
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
   const bool gram = blockIdx.x < ngram;
-  const unsigned w = gram ? blockIdx.x : blockIdx.x - ngram, per = gram ? a.NG : (a.NH + 3) / 4;
+  const unsigned w = gram ? blockIdx.x : blockIdx.x - ngram, per = gram ? a.NG * prep_parts(N) : (a.NH + 3) / 4;
   const int rec = w / per, part = w % per;
   int lo = 0, hi = a.q.B;           // the last sequence whose first record is not past rec
   while (hi - lo > 1) {
@@ -224,31 +226,35 @@ __global__ __launch_bounds__(256) void prep_kernel(ScanArgs a, unsigned ngram) {
     o[DEC_EL * SC] = __builtin_amdgcn_exp2f(lh);
     return;
   }
-  const int r = wave, g = part, l16 = lane & 15, lq = lane >> 4;
-  const float *cp = a.c + (int64_t)min(t0 + 16 * r + l16, end - 1) * a.cs + (int64_t)g * N + 4 * lq;
-  float *const out = a.gram + ((int64_t)rec * a.NG + g) * rec_floats(N);
-  v4f c[N / 16];
-#pragma unroll
-  for (int s = 0; s < N / 16; s++) {
-    c[s] = quad(cp + 16 * s);
-    *reinterpret_cast<v4f *>(out + GRAM + N * SC + (r * (N / 16) + s) * 256 + 4 * lane) = c[s];
-  }
-  for (int j = 0; j <= r; j++) {
-    const float *bp = a.b + (int64_t)min(t0 + 16 * j + l16, end - 1) * a.bs + (int64_t)g * N + 4 * lq;
+  const int g = part / prep_parts(N), job = 4 * (part % prep_parts(N)) + wave;
+  const int l16 = lane & 15, lq = lane >> 4;
+  float *const out = a.gram + ((int64_t)rec * a.NG + g) * rec_floats(N) + 4 * lane;
+  const auto row = [&](const float *p, int stride, int i) {    // row i of the chunk
+    return p + (int64_t)min(t0 + i, end - 1) * stride + (int64_t)g * N;
+  };
+  if (job < 10) {
+    const int r = job >= 6 ? 3 : job >= 3 ? 2 : job >= 1 ? 1 : 0, j = job - r * (r + 1) / 2;
+    const float *const cp = row(a.c, a.cs, 16 * r + l16) + 4 * lq, *const bp = row(a.b, a.bs, 16 * j + l16) + 4 * lq;
     v4f s0 = {0.f, 0.f, 0.f, 0.f}, s1 = s0;
 #pragma unroll
-    for (int s = 0; s < N / 16; s++) mm4(quad(bp + 16 * s), c[s], s0, s1);
-    *reinterpret_cast<v4f *>(out + tile_at(r, j) + 4 * lane) = s0 + s1;
-  }
-  for (int n = r; n < N / 16; n += 4)
+    for (int s = 0; s < N / 16; s++) mm4(quad(bp + 16 * s), quad(cp + 16 * s), s0, s1);
+    *reinterpret_cast<v4f *>(out + tile_at(r, j)) = s0 + s1;
+  } else if (job < 10 + N / 16) {
+    const int n = job - 10;
 #pragma unroll
     for (int j = 0; j < 4; j++) {
       v4f v;
 #pragma unroll
-      for (int e = 0; e < 4; e++)
-        v[e] = a.b[(int64_t)min(t0 + 16 * j + 4 * lq + e, end - 1) * a.bs + (int64_t)g * N + 16 * n + l16];
-      *reinterpret_cast<v4f *>(out + GRAM + (4 * n + j) * 256 + 4 * lane) = v;
+      for (int e = 0; e < 4; e++) v[e] = row(a.b, a.bs, 16 * j + 4 * lq + e)[16 * n + l16];
+      *reinterpret_cast<v4f *>(out + GRAM + (4 * n + j) * 256) = v;
     }
+  } else if (job < 14 + N / 16) {
+    const int r = job - 10 - N / 16;
+    const float *const cp = row(a.c, a.cs, 16 * r + l16) + 4 * lq;
+#pragma unroll
+    for (int s = 0; s < N / 16; s++)
+      *reinterpret_cast<v4f *>(out + GRAM + N * SC + (r * (N / 16) + s) * 256) = quad(cp + 16 * s);
+  }
 }
 
 // Matrices by column: 16-byte pieces of a column stand XOR-swizzled by the column,
@@ -497,7 +503,7 @@ int ssm_sizes(const w4a8_seqs *q, const w4a8_ssm *m, int64_t T) {
     return W4A8_ESHAPE;
   // (a grid's threads are counted in 32 bits)
   if (m->NH >= (1 << 16) || m->P > 4096 || q->B * m->NH * m->P >= ((int64_t)1 << 27) ||
-      (T / SC + q->B + 3) * (m->NG + m->NH) >= ((int64_t)1 << 23))
+      (T / SC + q->B + 3) * (m->NG + m->NH) >= ((int64_t)1 << 21))
     return W4A8_ERANGE;
   return W4A8_OK;
 }
@@ -520,7 +526,7 @@ int launch_ssm(ScanArgs a, hipStream_t s) {
     step_kernel<N, TB><<<dim3(steps), dim3(STEP_NT), 0, s>>>(a, a.done);
     if (int rc = check_launch(); rc != W4A8_OK || a.q.T <= STEP_T) return rc;
   }
-  const unsigned ngram = (unsigned)(records(a.q.T, a.q.B) * a.NG), ndec = (unsigned)(records(a.q.T, a.q.B) * ((a.NH + 3) / 4));
+  const unsigned ngram = (unsigned)(records(a.q.T, a.q.B) * a.NG * prep_parts(N)), ndec = (unsigned)(records(a.q.T, a.q.B) * ((a.NH + 3) / 4));
   prep_kernel<N><<<dim3(ngram + ndec), dim3(256), 0, s>>>(a, ngram);
   if (int rc = check_launch(); rc != W4A8_OK) return rc;
   constexpr int PS = N == 64 ? 32 : 16;
