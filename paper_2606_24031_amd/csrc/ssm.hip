@@ -235,19 +235,23 @@ __global__ __launch_bounds__(256) void prep_kernel(ScanArgs a, unsigned ngram) {
   if (job < 10) {
     const int r = job >= 6 ? 3 : job >= 3 ? 2 : job >= 1 ? 1 : 0, j = job - r * (r + 1) / 2;
     const float *const cp = row(a.c, a.cs, 16 * r + l16) + 4 * lq, *const bp = row(a.b, a.bs, 16 * j + l16) + 4 * lq;
-    v4f s0 = {0.f, 0.f, 0.f, 0.f}, s1 = s0;
+    v4f s0 = {0.f, 0.f, 0.f, 0.f}, s1 = s0, cv[N / 16], bv[N / 16];
 #pragma unroll
-    for (int s = 0; s < N / 16; s++) mm4(quad(bp + 16 * s), quad(cp + 16 * s), s0, s1);
+    for (int s = 0; s < N / 16; s++) { bv[s] = quad(bp + 16 * s); cv[s] = quad(cp + 16 * s); }
+    __builtin_amdgcn_sched_barrier(0);           // (all loads under way)
+#pragma unroll
+    for (int s = 0; s < N / 16; s++) mm4(bv[s], cv[s], s0, s1);
     *reinterpret_cast<v4f *>(out + tile_at(r, j)) = s0 + s1;
   } else if (job < 10 + N / 16) {
     const int n = job - 10;
+    v4f v[4];
 #pragma unroll
-    for (int j = 0; j < 4; j++) {
-      v4f v;
+    for (int j = 0; j < 4; j++)
 #pragma unroll
-      for (int e = 0; e < 4; e++) v[e] = row(a.b, a.bs, 16 * j + 4 * lq + e)[16 * n + l16];
-      *reinterpret_cast<v4f *>(out + GRAM + (4 * n + j) * 256) = v;
-    }
+      for (int e = 0; e < 4; e++) v[j][e] = row(a.b, a.bs, 16 * j + 4 * lq + e)[16 * n + l16];
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int j = 0; j < 4; j++) *reinterpret_cast<v4f *>(out + GRAM + (4 * n + j) * 256) = v[j];
   } else if (job < 14 + N / 16) {
     const int r = job - 10 - N / 16;
     const float *const cp = row(a.c, a.cs, 16 * r + l16) + 4 * lq;
