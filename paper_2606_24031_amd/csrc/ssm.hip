@@ -273,7 +273,7 @@ struct ScanLds {
   float xd[2][PS * SC];             // x by column, times the steps
   float xw[2][PS * SC];             // ... and the decays to the chunk's end
   float st[2][PS * N];              // the state before the chunk by column
-  float yl[2][2 / (PS / 16)][SC][PS + 4];   // sums of y (N > 64: of either half of the state's rows)
+  float yl[2][N == 64 ? 1 : 2][SC][PS + 4]; // sums of y (N > 64: of either half of the state's rows)
   float dec[2][DEC_LDS][SC];
 };
 
@@ -284,9 +284,12 @@ struct ScanLds {
 //   S <- e^{L_C} S + B^T diag(d e^{L_C - L}) x.
 template <int N, int PS>
 __global__ __launch_bounds__(SNT) void scan_kernel(ScanArgs a) {
-  constexpr int NT = N / 16, PT = PS / 16, TPW = NT * PT / 8, KH = 2 / PT;
+  // tiles of S a wave: TN of its rows by TC of its columns; of y: CT of its columns, over
+  // one of KH parts of S's rows
+  constexpr int NT = N / 16, PT = PS / 16, KH = NT < 8 ? 1 : 2, CT = PT * KH / 2;
+  constexpr int TN = NT < 8 ? 1 : NT / 8, TC = NT < 8 ? PT * NT / 8 : PT;
   constexpr int CF = N / KH / 16, GF = KH == 2 ? 2 : 4;
-  static_assert(TPW * 8 == NT * PT && KH * PT == 2, "tiles over the waves");
+  static_assert(8 * CT == 4 * KH * PT && 8 * TN * TC == NT * PT, "tiles over the waves");
   __shared__ __align__(16) ScanLds<N, PS> L;
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
   const int l16 = lane & 15, lq = lane >> 4;
@@ -300,14 +303,15 @@ __global__ __launch_bounds__(SNT) void scan_kernel(ScanArgs a) {
   const int nch = (end - begin + SC - 1) / SC;
   const float D = a.D ? a.D[h] : 0.0f;
 
-  // roles: sums of y of rows 16 r .. + 15, column tile ct, half kh of the
-  // state's rows (waves w and w + 4, of one SIMD, take r and 3 - r); the tiles
-  // of S; row xr and columns xc .. + 3 of x, z and y
+  // roles: sums of y of rows 16 r .. + 15, column tiles from yct on, part kh of the
+  // state's rows (waves w and w + 4, of one SIMD, take r and 3 - r); rows of tiles
+  // nt[] and column tiles from sct on of S; row xr and columns xc .. + 3 of x, z
+  // and y
   const int hi = wave >> 2, r = hi ? 3 - (wave & 3) : wave & 3;
-  const int kh = KH == 2 ? hi : 0, ct = KH == 2 ? 0 : hi;
-  int nt[TPW], sct[TPW];
+  const int kh = KH == 2 ? hi : 0, yct = KH == 2 ? 0 : hi * CT, sct = NT < 8 ? wave / NT * TC : 0;
+  int nt[TN];
 #pragma unroll
-  for (int i = 0; i < TPW; i++) { nt[i] = (wave + 8 * i) % NT; sct[i] = (wave + 8 * i) / NT; }
+  for (int i = 0; i < TN; i++) nt[i] = (wave + 8 * i) % NT;
   constexpr int XW = PS / 4;                     // waves that have a row of x
   const int xr = tid / (PS / 4), xc = 4 * (tid % (PS / 4));
 
@@ -351,7 +355,7 @@ __global__ __launch_bounds__(SNT) void scan_kernel(ScanArgs a) {
   // loaded into them behind their last use, a step ahead of their own.  (A
   // scheduling barrier before each load: moved up, it would need other registers,
   // and copies at the loop's end that wait for it: 616 us.)
-  v4f cf[CF], gf[GF], bf[TPW][4], x, xe, z;      // (xe: x for the outputs)
+  v4f cf[CF], gf[GF], bf[TN][4], x, xe, z;      // (xe: x for the outputs)
   float dec1, dl, wj;                            // of one of the decay arrays; of x's row
   Rsrc rec;
   const auto load_c = [&]() {
@@ -362,7 +366,7 @@ __global__ __launch_bounds__(SNT) void scan_kernel(ScanArgs a) {
   };
   const auto load_b = [&]() {
 #pragma unroll
-    for (int i = 0; i < TPW; i++)
+    for (int i = 0; i < TN; i++)
 #pragma unroll
       for (int s = 0; s < 4; s++) bf[i][s] = load4(rec, lane16, 4 * (GRAM + (4 * nt[i] + s) * 256));
   };
@@ -395,20 +399,24 @@ __global__ __launch_bounds__(SNT) void scan_kernel(ScanArgs a) {
   };
 
   const int64_t src = seq_src(a.q, b), dst = seq_dst(a.q, b);
-  v4f S[TPW];
+  v4f S[TN][TC];
 #pragma unroll
-  for (int i = 0; i < TPW; i++) {
-    const int col = c0 + 16 * sct[i] + l16;
+  for (int i = 0; i < TN; i++)
 #pragma unroll
-    for (int e = 0; e < 4; e++)
-      S[i][e] = src >= 0 && col < a.P
-                    ? a.state[((src * a.NH + h) * N + 16 * nt[i] + 4 * lq + e) * a.P + col]
-                    : 0.0f;
-  }
+    for (int k = 0; k < TC; k++) {
+      const int col = c0 + 16 * (sct + k) + l16;
+#pragma unroll
+      for (int e = 0; e < 4; e++)
+        S[i][k][e] = src >= 0 && col < a.P
+                         ? a.state[((src * a.NH + h) * N + 16 * nt[i] + 4 * lq + e) * a.P + col]
+                         : 0.0f;
+    }
   const auto put_state = [&](int p) {
 #pragma unroll
-    for (int i = 0; i < TPW; i++)
-      *reinterpret_cast<v4f *>(&L.st[p][piece_at<N>(16 * sct[i] + l16, 4 * nt[i] + lq)]) = S[i];
+    for (int i = 0; i < TN; i++)
+#pragma unroll
+      for (int k = 0; k < TC; k++)
+        *reinterpret_cast<v4f *>(&L.st[p][piece_at<N>(16 * (sct + k) + l16, 4 * nt[i] + lq)]) = S[i][k];
   };
 
   load_x();
@@ -424,31 +432,42 @@ __global__ __launch_bounds__(SNT) void scan_kernel(ScanArgs a) {
     const int p = c & 1;
     const auto &dec = L.dec[p];
     // C S
-    v4f y0 = {0.f, 0.f, 0.f, 0.f}, y1 = y0;
+    v4f y0[CT], y1[CT];
+#pragma unroll
+    for (int k = 0; k < CT; k++) y0[k] = y1[k] = v4f{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int s = 0; s < CF; s++)
-      mm4(cf[s], quad(&L.st[p][piece_at<N>(16 * ct + l16, 4 * (kh * CF + s) + lq)]), y0, y1);
-    pin(y0);
-    pin(y1);
+#pragma unroll
+      for (int k = 0; k < CT; k++)
+        mm4(cf[s], quad(&L.st[p][piece_at<N>(16 * (yct + k) + l16, 4 * (kh * CF + s) + lq)]), y0[k], y1[k]);
+#pragma unroll
+    for (int k = 0; k < CT; k++) { pin(y0[k]); pin(y1[k]); }
     __builtin_amdgcn_sched_barrier(0);
     load_c();
     // S
     const float eC = dec[DEC_EL][SC - 1];
 #pragma unroll
-    for (int i = 0; i < TPW; i++) {
-      v4f s1 = {0.f, 0.f, 0.f, 0.f};
-      S[i] *= eC;
+    for (int i = 0; i < TN; i++)
 #pragma unroll
-      for (int s = 0; s < 4; s++) mm4(bf[i][s], quad(&L.xw[p][piece_at<SC>(16 * ct + l16, 4 * s + lq)]), S[i], s1);
-      S[i] += s1;
-      pin(S[i]);
-    }
+      for (int k = 0; k < TC; k++) {
+        v4f s1 = {0.f, 0.f, 0.f, 0.f};
+        S[i][k] *= eC;
+#pragma unroll
+        for (int s = 0; s < 4; s++)
+          mm4(bf[i][s], quad(&L.xw[p][piece_at<SC>(16 * (sct + k) + l16, 4 * s + lq)]), S[i][k], s1);
+        S[i][k] += s1;
+        pin(S[i][k]);
+      }
     __builtin_amdgcn_sched_barrier(0);
     load_b();
-    y0 = (y0 + y1) * quad(&dec[DEC_EL][16 * r + 4 * lq]);
+    const v4f el = quad(&dec[DEC_EL][16 * r + 4 * lq]);
+#pragma unroll
+    for (int k = 0; k < CT; k++) {
+      y0[k] = (y0[k] + y1[k]) * el;
+      y1[k] = v4f{0.f, 0.f, 0.f, 0.f};
+    }
     // (C B^T o decays) x
     const float lhi = dec[DEC_LH][16 * r + l16], lli = dec[DEC_LL][16 * r + l16];
-    y1 = v4f{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int s = 0; s < GF; s++) {
       const int j = KH == 2 ? kh + 2 * s : s;
@@ -460,14 +479,21 @@ __global__ __launch_bounds__(SNT) void scan_kernel(ScanArgs a) {
         w[e] = gf[s][e] * __builtin_amdgcn_exp2f((lhi - lh[e]) + (lli - ll[e]));
         if (16 * j + 4 * lq + e > 16 * r + l16) w[e] = 0.0f;
       }
-      mm4(w, quad(&L.xd[p][piece_at<SC>(16 * ct + l16, 4 * j + lq)]), y0, y1);
+#pragma unroll
+      for (int k = 0; k < CT; k++)
+        mm4(w, quad(&L.xd[p][piece_at<SC>(16 * (yct + k) + l16, 4 * j + lq)]), y0[k], y1[k]);
     }
-    y0 += y1;
-    pin(y0);
+#pragma unroll
+    for (int k = 0; k < CT; k++) {
+      y0[k] += y1[k];
+      pin(y0[k]);
+    }
     __builtin_amdgcn_sched_barrier(0);
     load_g();
 #pragma unroll
-    for (int e = 0; e < 4; e++) L.yl[p][kh][16 * r + 4 * lq + e][16 * ct + l16] = y0[e];
+    for (int k = 0; k < CT; k++)
+#pragma unroll
+      for (int e = 0; e < 4; e++) L.yl[p][kh][16 * r + 4 * lq + e][16 * (yct + k) + l16] = y0[k][e];
     put_state(p ^ 1);
     stage(p ^ 1);                                // (past the last chunk unused)
     __builtin_amdgcn_sched_barrier(0);
@@ -486,13 +512,15 @@ __global__ __launch_bounds__(SNT) void scan_kernel(ScanArgs a) {
   }
   if (dst >= 0)
 #pragma unroll
-    for (int i = 0; i < TPW; i++) {
-      const int col = c0 + 16 * sct[i] + l16;
-      if (col < a.P)
+    for (int i = 0; i < TN; i++)
 #pragma unroll
-        for (int e = 0; e < 4; e++)
-          a.state[((dst * a.NH + h) * N + 16 * nt[i] + 4 * lq + e) * a.P + col] = S[i][e];
-    }
+      for (int k = 0; k < TC; k++) {
+        const int col = c0 + 16 * (sct + k) + l16;
+        if (col < a.P)
+#pragma unroll
+          for (int e = 0; e < 4; e++)
+            a.state[((dst * a.NH + h) * N + 16 * nt[i] + 4 * lq + e) * a.P + col] = S[i][k][e];
+      }
 }
 
 // Records of a call; the scan's loads run two past a sequence's last.
@@ -510,6 +538,14 @@ int ssm_sizes(const w4a8_seqs *q, const w4a8_ssm *m, int64_t T) {
       (T / SC + q->B + 3) * (m->NG + m->NH) >= ((int64_t)1 << 21))
     return W4A8_ERANGE;
   return W4A8_OK;
+}
+
+template <int N, int PS>
+int launch_scan(ScanArgs a, hipStream_t s) {
+  a.nsl = (a.P + PS - 1) / PS;
+  const unsigned pairs = (unsigned)((a.q.B * a.NH + 7) / 8 * 8);
+  scan_kernel<N, PS><<<dim3(pairs * a.nsl), dim3(SNT), 0, s>>>(a);
+  return check_launch();
 }
 
 template <int N>
@@ -533,11 +569,9 @@ int launch_ssm(ScanArgs a, hipStream_t s) {
   const unsigned ngram = (unsigned)(records(a.q.T, a.q.B) * a.NG * prep_parts(N)), ndec = (unsigned)(records(a.q.T, a.q.B) * ((a.NH + 3) / 4));
   prep_kernel<N><<<dim3(ngram + ndec), dim3(256), 0, s>>>(a, ngram);
   if (int rc = check_launch(); rc != W4A8_OK) return rc;
-  constexpr int PS = N == 64 ? 32 : 16;
-  a.nsl = (a.P + PS - 1) / PS;
-  const unsigned pairs = (unsigned)((a.q.B * a.NH + 7) / 8 * 8);
-  scan_kernel<N, PS><<<dim3(pairs * a.nsl), dim3(SNT), 0, s>>>(a);
-  return check_launch();
+  if constexpr (N == 128)
+    if ((int64_t)a.q.B * a.NH * (a.P / 32) >= device_cus()) return launch_scan<N, 32>(a, s);
+  return launch_scan<N, N == 64 ? 32 : 16>(a, s);
 }
 
 }  // namespace

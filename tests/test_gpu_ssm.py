@@ -180,6 +180,15 @@ def test_whole_numbers_are_exact(lens, N, P, NH, NG):
     whole_numbers(Case([13, N, P, *lens], lens, N=N, P=P, NH=NH, NG=NG)).check(exact=True)
 
 
+@pytest.mark.parametrize("P,NH,lens", [(64, 128, [65, 9]), (80, 130, [70]), (32, 256, [20, 64]), (64, 128, [129])])
+def test_enough_heads_for_wider_slices(P, NH, lens):
+    """Calls with 32 columns for every compute unit: twice as many a workgroup;
+    columns that end inside them."""
+    whole_numbers(Case([26, P, *lens], lens, N=128, P=P, NH=NH, NG=2)).check(exact=True)
+    Case([27, P, *lens], lens, N=128, P=P, NH=NH, NG=2, n_slots=len(lens), src=range(len(lens)),
+         dst=range(len(lens))).check()
+
+
 @pytest.mark.parametrize("n", [6, 200])
 def test_strong_decay_forgets(n):
     """exp(-200) is 0 in fp32: a row's state is its own term."""
