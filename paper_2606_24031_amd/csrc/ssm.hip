@@ -10,8 +10,8 @@
 // before (prep: C B^T, decays, operands in the products' order), then a workgroup
 // per head and slice of columns with the chunks in order (scan), the state in the
 // accumulators of fp32 matrix products.  All arithmetic is fp32 (products of rounded
-// halves would be off by more than the rest together), so the products' rate, an
-// 8th of an int8 product's at most, is the bound: a chunk's products of a 16-column
+// halves would be off by more than the rest together), so the products' rate, a
+// 16th of bf16's, is a bound: a chunk's products of a 16-column
 // slice take 2370 cycles of each SIMD; a step takes 4500: the products do not overlap
 // with the SIMD's other work (1350 cycles: decays, addresses, the gate), and about 90
 // KB a step come from the L2 caches (14 TB/s in all).  16384 rows, 64 heads of 64:
