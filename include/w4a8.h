@@ -490,8 +490,8 @@ int q8_row_quantize(const float *x, int64_t x_stride, int8_t *q, float *d, int64
  *   are multiplied too: they are zero in at least one of the two, as the
  *   quantizer writes them); xd [M], wd [N], bias [N] fp32; y fp32, row m at
  *   m * y_stride elements, written.  One launch, no workspace.
- * Errors: M < 0, N < 1, K < 1, y_stride < N -> W4A8_ESHAPE; K >= 2^17, y_stride
- * >= 2^31 or 2^23 tiles of 64 rows by 64 channels or more -> W4A8_ERANGE; a NULL pointer (but bias) ->
+ * Errors: M < 0, N < 1, K < 1, y_stride < N -> W4A8_ESHAPE; K >= 2^17, M or N
+ * >= 2^26, y_stride >= 2^31 or 2^23 tiles of 64 rows by 64 channels or more -> W4A8_ERANGE; a NULL pointer (but bias) ->
  * W4A8_ENULL; xq or wq not 16-, xd, wd, bias or y not 4-byte aligned ->
  * W4A8_EALIGN; y equal to an operand -> W4A8_EALIAS.  M == 0 is a no-op.
  */
@@ -561,20 +561,23 @@ int short_conv(const w4a8_seqs *seqs, const float *x, int64_t x_stride, const fl
  *   S     = exp(delta * A[h]) * S + delta * B[t] x[t]^T
  *   y[t]  = C[t]^T S + D[h] * x[t],  times z[t] / (1 + exp(-z[t])) if z
  * computed as a chunked scan (chunks of 64 rows: products within a chunk and a
- * group in parallel, then the chunks in order per head and columns of P);
- * sequences of up to 8 rows row by row.  Sums and states are fp32; logarithms
- * of decays are summed in fp64.
+ * group in parallel, then the chunks in order per head and columns of P), or
+ * row by row where sequences are short.  Sums and states are fp32; logarithms
+ * of decays are summed in fp64.  A sequence's result does not depend on the
+ * values of others; which way it is computed, and so its last bits, may depend
+ * on the call's sizes.
  *   x, z [T][NH][P], b, c [T][NG][N], dt [T][NH] fp32, row t at t times the
  *   row's stride in elements, heads and groups contiguous; A [NH]; D, dt_bias
  *   [NH], z: NULL for none; state [n_slots][NH][N][P] fp32, read and written as
  *   the plan says (NULL if it has no slots); y [T][NH][P], row stride y_stride.
  *   workspace >= ssm_workspace_size bytes, no initialisation.
- *   Inputs are finite.  (A value that is not reaches rows of its own sequence
- *   and head, or group, only: from its 64-row chunk on.)
+ *   Inputs are finite, and so is the growth over 64 rows where delta * A > 0.
+ *   (A value that is not reaches rows of its own sequence and head, or group,
+ *   only: from its 64-row chunk on.)
  * Errors beside the plan's: NULL ssm -> W4A8_ENULL; T < 0, NH or NG < 1,
  * NH % NG != 0, N not 64, 128 or 256, P < 16, P % 16 != 0, a stride below its
  * row's elements, or (but for dt's) not a multiple of 4 -> W4A8_ESHAPE; T >=
- * 2^31, NH >= 2^16, P > 4096, a stride >= 2^24, B * NH * P >= 2^27 or (T / 64 + B + 3)
+ * 2^31, NH >= 2^16, P > 4096, a stride >= 2^24, B * NH * P >= 2^26 or (T / 64 + B + 3)
  * * (NG + NH) >= 2^21 -> W4A8_ERANGE; x, dt, b, c,
  * A, y or workspace, or state with n_slots > 0, NULL -> W4A8_ENULL; dt, A, D or
  * dt_bias not 4-, another pointer not 16-byte aligned -> W4A8_EALIGN; y or

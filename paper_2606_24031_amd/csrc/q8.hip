@@ -405,7 +405,7 @@ extern "C" int q8q8_gemm(const int8_t *xq, const float *xd, const int8_t *wq, co
                          int64_t K, void *stream) {
   if (M < 0 || N < 1 || K < 1 || y_stride < N) return W4A8_ESHAPE;
   // (a grid's threads are counted in 32 bits)
-  if (K >= KTOP || M >= TOP || N >= TOP || y_stride >= TOP || ((M + 63) / 64) * ((N + 63) / 64) >= (1 << 23))
+  if (K >= KTOP || M >= (1 << 26) || N >= (1 << 26) || y_stride >= TOP || ((M + 63) / 64) * ((N + 63) / 64) >= (1 << 23))
     return W4A8_ERANGE;
   if (!xq || !xd || !wq || !wd || !y) return W4A8_ENULL;
   if (!aligned16(xq) || !aligned16(wq) || !aligned4(xd) || !aligned4(wd) || !aligned4(bias) || !aligned4(y))

@@ -227,7 +227,8 @@ __global__ __launch_bounds__(256) void prep_kernel(ScanArgs a, unsigned ngram) {
     const int t = t0 + lane;
     const float d = t < end ? step_of(a.dt[(int64_t)min(t, end - 1) * a.ds + h], a.bias ? a.bias[h] : 0.0f, a.softplus)
                             : 0.0f;
-    const double s = scan64(t < end ? (double)d * A : 0.0);
+    // (past 2^20 either way a row's decay is 0 or infinite; kept there, sums stay finite)
+    const double s = scan64(t < end ? fmin(fmax((double)d * A, -1048576.0), 1048576.0) : 0.0);
     const uint64_t u = __builtin_bit_cast(uint64_t, s);
     const double all = __builtin_bit_cast(
         double, (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(u >> 32), 63) << 32 |
@@ -549,7 +550,7 @@ int ssm_sizes(const w4a8_seqs *q, const w4a8_ssm *m, int64_t T) {
       m->P < 16 || m->P % 16 != 0)
     return W4A8_ESHAPE;
   // (a grid's threads are counted in 32 bits)
-  if (m->NH >= (1 << 16) || m->P > 4096 || q->B * m->NH * m->P >= ((int64_t)1 << 27) ||
+  if (m->NH >= (1 << 16) || m->P > 4096 || q->B * m->NH * m->P >= ((int64_t)1 << 26) ||
       (T / SC + q->B + 3) * (m->NG + m->NH) >= ((int64_t)1 << 21))
     return W4A8_ERANGE;
   return W4A8_OK;

@@ -206,6 +206,15 @@ def test_strong_and_weak_decays_in_turn(n):
     c.check()
 
 
+@pytest.mark.parametrize("n", [8, 150])
+def test_steps_as_large_as_fp32_holds(n):
+    """Decays whose exponents pass fp32's range are 0, and their sums no NaN."""
+    c = Case([28, n], [n], softplus=False, bias=False, gate=False, D=False)
+    c.dt[...] = np.where(c.g.random(c.dt.shape) < 0.3, np.float32(2e38), np.float32(1e-2))
+    c.x *= np.float32(1e-3)
+    c.check()
+
+
 def test_no_decay_and_zero_steps():
     c = Case([16], [150, 5], softplus=False, bias=False)
     c.A[0] = 0.0

@@ -51,7 +51,8 @@ def test_product_errors():
         assert call(**kw) == w4.ENULL, kw
     for kw in (dict(M=-1), dict(N=0), dict(K=0), dict(ys=99)):
         assert call(**kw) == w4.ESHAPE, kw
-    for kw in (dict(K=1 << 17), dict(M=TOP), dict(N=TOP, ys=TOP), dict(ys=TOP)):
+    for kw in (dict(K=1 << 17), dict(M=TOP), dict(N=TOP, ys=TOP), dict(ys=TOP), dict(M=1 << 26, N=1, ys=1),
+               dict(N=1 << 26, ys=1 << 26), dict(M=1 << 20, N=1 << 16, ys=1 << 16)):
         assert call(**kw) == w4.ERANGE, kw
     for kw in (dict(xq=A + 8), dict(wq=A + 4), dict(xd=A + 2), dict(wd=A + 1), dict(bias=A + 3), dict(y=A + 2)):
         assert call(**kw) == w4.EALIGN, kw
