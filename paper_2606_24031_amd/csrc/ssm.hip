@@ -284,12 +284,16 @@ __global__ __launch_bounds__(256) void prep_kernel(ScanArgs a, unsigned ngram) {
 template <int LEN>
 __device__ __forceinline__ int piece_at(int col, int piece) { return col * LEN + 4 * (piece ^ (col & 15)); }
 
+// Two workgroups of the slices of 32 columns of 128 rows share a compute unit: with
+// one buffer each for the state's columns and the sums of y, for a second barrier a
+// step (64 sequences of 128 rows, 64 heads of 64: 313 us; alone 368), and 128 registers.
 template <int N, int PS>
 struct ScanLds {
+  static constexpr int SB = N == 128 && PS == 32 ? 1 : 2;
   float xd[2][PS * SC];             // x by column, times the steps
   float xw[2][PS * SC];             // ... and the decays to the chunk's end
-  float st[2][PS * N];              // the state before the chunk by column
-  float yl[2][N == 64 ? 1 : 2][SC][PS + 4]; // sums of y (N > 64: of either half of the state's rows)
+  float st[SB][PS * N];             // the state before the chunk by column
+  float yl[SB][N == 64 ? 1 : 2][SC][PS + 4]; // sums of y (N > 64: of either half of the state's rows)
   float dec[2][DEC_LDS][SC];
 };
 
@@ -299,12 +303,12 @@ struct ScanLds {
 //   y = diag(e^L) C S + (C B^T o e^{L_i - L_j} o d_j) x   (j <= i)
 //   S <- e^{L_C} S + B^T diag(d e^{L_C - L}) x.
 template <int N, int PS>
-__global__ __launch_bounds__(SNT) void scan_kernel(ScanArgs a) {
+__global__ __launch_bounds__(SNT, (ScanLds<N, PS>::SB == 1 ? 4 : 2)) void scan_kernel(ScanArgs a) {
   // tiles of S a wave: TN of its rows by TC of its columns; of y: CT of its columns, over
   // one of KH parts of S's rows
   constexpr int NT = N / 16, PT = PS / 16, KH = NT < 8 ? 1 : 2, CT = PT * KH / 2;
   constexpr int TN = NT < 8 ? 1 : NT / 8, TC = NT < 8 ? PT * NT / 8 : PT;
-  constexpr int CF = N / KH / 16, GF = KH == 2 ? 2 : 4;
+  constexpr int CF = N / KH / 16, GF = KH == 2 ? 2 : 4, SB = ScanLds<N, PS>::SB;
   static_assert(8 * CT == 4 * KH * PT && 8 * TN * TC == NT * PT, "tiles over the waves");
   __shared__ __align__(16) ScanLds<N, PS> L;
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
@@ -398,10 +402,8 @@ __global__ __launch_bounds__(SNT) void scan_kernel(ScanArgs a) {
     dl = load1(q, row4, 4 * DEC_DL * SC);
     wj = load1(q, row4, 4 * DEC_WJ * SC);
   };
-  const auto load_out = [&]() {
-    xe = load4(next(erows), xat, 0);
-    z = load4(next(zrows), zat, 0);
-  };
+  const auto load_xe = [&]() { xe = load4(next(erows), xat, 0); };
+  const auto load_z = [&]() { z = load4(next(zrows), zat, 0); };
   // x by column, and the decays of a chunk
   const auto stage = [&](int p) {
     if (wave < XW)
@@ -439,13 +441,14 @@ __global__ __launch_bounds__(SNT) void scan_kernel(ScanArgs a) {
   load_c();
   load_b();
   load_g();
-  load_out();
+  if (SB == 2) load_xe();
+  load_z();
   put_state(0);
   stage(0);
   load_x();
   __syncthreads();
   for (int c = 0; c < nch; c++) {
-    const int p = c & 1;
+    const int p = c & 1, ps = p & (SB - 1);
     const auto &dec = L.dec[p];
     // C S
     v4f y0[CT], y1[CT];
@@ -455,11 +458,12 @@ __global__ __launch_bounds__(SNT) void scan_kernel(ScanArgs a) {
     for (int s = 0; s < CF; s++)
 #pragma unroll
       for (int k = 0; k < CT; k++)
-        mm4(cf[s], quad(&L.st[p][piece_at<N>(16 * (yct + k) + l16, 4 * (kh * CF + s) + lq)]), y0[k], y1[k]);
+        mm4(cf[s], quad(&L.st[ps][piece_at<N>(16 * (yct + k) + l16, 4 * (kh * CF + s) + lq)]), y0[k], y1[k]);
 #pragma unroll
     for (int k = 0; k < CT; k++) { pin(y0[k]); pin(y1[k]); }
     __builtin_amdgcn_sched_barrier(0);
     load_c();
+    if (SB == 1) __syncthreads();                // the state before the chunk and the last sums of y are read
     // S
     const float eC = dec[DEC_EL][SC - 1];
 #pragma unroll
@@ -506,24 +510,26 @@ __global__ __launch_bounds__(SNT) void scan_kernel(ScanArgs a) {
     }
     __builtin_amdgcn_sched_barrier(0);
     load_g();
+    if (SB == 1) load_xe();                      // (no registers to spare before)
 #pragma unroll
     for (int k = 0; k < CT; k++)
 #pragma unroll
-      for (int e = 0; e < 4; e++) L.yl[p][kh][16 * r + 4 * lq + e][16 * (yct + k) + l16] = y0[k][e];
-    put_state(p ^ 1);
+      for (int e = 0; e < 4; e++) L.yl[ps][kh][16 * r + 4 * lq + e][16 * (yct + k) + l16] = y0[k][e];
+    put_state((p ^ 1) & (SB - 1));
     stage(p ^ 1);                                // (past the last chunk unused)
     __builtin_amdgcn_sched_barrier(0);
     load_x();
     __syncthreads();
     if (wave < XW) {
-      v4f o = quad(&L.yl[p][0][xr][xc]);
-      if (KH == 2) o += quad(&L.yl[p][1][xr][xc]);
+      v4f o = quad(&L.yl[ps][0][xr][xc]);
+      if (KH == 2) o += quad(&L.yl[ps][1][xr][xc]);
       o += D * xe;
       if (a.z) o *= v4f{silu_f32(z.x), silu_f32(z.y), silu_f32(z.z), silu_f32(z.w)};
       __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(v4u, o), next(yrows), yat, 0, 0);
     }
     __builtin_amdgcn_sched_barrier(0);
-    load_out();
+    if (SB == 2) load_xe();
+    load_z();
     __builtin_amdgcn_sched_barrier(0);
   }
   if (dst >= 0)
@@ -585,8 +591,11 @@ int launch_ssm(ScanArgs a, hipStream_t s) {
   const unsigned ngram = (unsigned)(records(a.q.T, a.q.B) * a.NG * prep_parts(N)), ndec = (unsigned)(records(a.q.T, a.q.B) * ((a.NH + 3) / 4));
   prep_kernel<N><<<dim3(ngram + ndec), dim3(256), 0, s>>>(a, ngram);
   if (int rc = check_launch(); rc != W4A8_OK) return rc;
+  // Slices of 32 columns read the records half as often as those of 16, which fill the
+  // card with half the heads.  64 heads of 64, us: 2 sequences of 2000 rows 136 and
+  // 134, 3 of them 219 and 201, 4 of them 231 and 237.
   if constexpr (N == 128)
-    if ((int64_t)a.q.B * a.NH * (a.P / 32) >= device_cus()) return launch_scan<N, 32>(a, s);
+    if ((int64_t)a.q.B * a.NH * (a.P / 32) >= 2 * device_cus()) return launch_scan<N, 32>(a, s);
   return launch_scan<N, N == 64 ? 32 : 16>(a, s);
 }
 
