@@ -35,7 +35,8 @@ typedef uint32_t v4u __attribute__((ext_vector_type(4)));
 struct ScanArgs {
   Seqs q;
   const float *x, *dt, *b, *c, *z, *A, *D, *bias;
-  float *state, *y, *gram, *dec;    // gram, dec: the workspace
+  float *state, *y, *gram, *dec;    // gram, dec and
+  int4 *order;                      // order: the workspace
   int xs, ds, bs, cs, zs, ys;       // strides
   int NH, G, NG, P, nsl;            // heads, heads of a group, groups, columns, slices of columns
   int softplus;
@@ -196,6 +197,31 @@ __device__ __forceinline__ double scan64(double v) {
 constexpr int DEC = 5, DEC_LH = 0, DEC_LL = 1, DEC_EL = 2, DEC_DL = 3, DEC_WJ = 4;
 constexpr int DEC_LDS = 3;          // the first ones go to LDS, the others into x
 
+// The sequences as the scan takes them, longest first (ties by number), so that no
+// long one starts when the others end: number, first row, end.  6 sequences of 633 to
+// 2000 rows, 64 heads of 64: 236 us, as they come 278.  Places are counted, which
+// for up to ORDER_B sequences ends before the records do; more go as they come.
+constexpr int ORDER_B = 1024, ORDER_NT = 256;
+__device__ __forceinline__ void order_rows(const ScanArgs &a, int block) {
+  __shared__ __align__(16) int rows[ORDER_B];
+  const int B = a.q.B, b = block * ORDER_NT + threadIdx.x;
+  const int begin = seq_begin(a.q, min(b, B - 1)), end = seq_begin(a.q, min(b, B - 1) + 1);
+  int place = b;
+  if (B <= ORDER_B) {
+    for (int j = threadIdx.x; j < (B + 3) / 4 * 4; j += ORDER_NT)
+      rows[j] = j < B ? max(seq_begin(a.q, j + 1) - seq_begin(a.q, j), 0) : -1;
+    __syncthreads();
+    const int n = max(end - begin, 0);
+    place = 0;
+    for (int j = 0; j < B; j += 4) {
+      const int4 m = *reinterpret_cast<const int4 *>(rows + j);
+      place += (m.x > n || (m.x == n && j < b)) + (m.y > n || (m.y == n && j + 1 < b)) +
+               (m.z > n || (m.z == n && j + 2 < b)) + (m.w > n || (m.w == n && j + 3 < b));
+    }
+  }
+  if (b < B) a.order[place] = make_int4(b, begin, end, 0);
+}
+
 // What the chunks need that does not wait for the one before: a record's pieces,
 // a wave each (one trip to memory; a workgroup of four waves for all of a record
 // took 12 us for a 947-token prompt), then the steps and decays, a wave per chunk and
@@ -207,10 +233,12 @@ constexpr int DEC_LDS = 3;          // the first ones go to LDS, the others into
 //   (gathered by the scan 16384 rows of 64 heads of 64 took 718 us, B^T here 631).
 constexpr int prep_parts(int N) { return (10 + N / 16 + 4 + 3) / 4; }
 template <int N>
-__global__ __launch_bounds__(256) void prep_kernel(ScanArgs a, unsigned ngram) {
+__global__ __launch_bounds__(ORDER_NT) void prep_kernel(ScanArgs a, unsigned norder, unsigned ngram) {
+  if (blockIdx.x < norder) return order_rows(a, blockIdx.x);
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
-  const bool gram = blockIdx.x < ngram;
-  const unsigned w = gram ? blockIdx.x : blockIdx.x - ngram, per = gram ? a.NG * prep_parts(N) : (a.NH + 3) / 4;
+  const unsigned block = blockIdx.x - norder;
+  const bool gram = block < ngram;
+  const unsigned w = gram ? block : block - ngram, per = gram ? a.NG * prep_parts(N) : (a.NH + 3) / 4;
   const int rec = w / per, part = w % per;
   int lo = 0, hi = a.q.B;           // the last sequence whose first record is not past rec
   while (hi - lo > 1) {
@@ -316,9 +344,10 @@ __global__ __launch_bounds__(SNT, (ScanLds<N, PS>::SB == 1 ? 4 : 2)) void scan_k
   // all slices of a head on one XCD (workgroup w runs on XCD w mod 8)
   const int k = blockIdx.x >> 3, bh = (k / a.nsl) * 8 + (blockIdx.x & 7);
   if (bh >= a.q.B * a.NH) return;
-  const int b = bh / a.NH, h = bh % a.NH, g = h / a.G, c0 = (k % a.nsl) * PS;
-  const int begin = __builtin_amdgcn_readfirstlane(seq_begin(a.q, b)),
-            end = __builtin_amdgcn_readfirstlane(seq_begin(a.q, b + 1));
+  const int4 place = a.order[bh / a.NH];
+  const int b = __builtin_amdgcn_readfirstlane(place.x), begin = __builtin_amdgcn_readfirstlane(place.y),
+            end = __builtin_amdgcn_readfirstlane(place.z);
+  const int h = bh % a.NH, g = h / a.G, c0 = (k % a.nsl) * PS;
   if (begin >= end || end - begin <= a.done) return;
   const int nch = (end - begin + SC - 1) / SC;
   const float D = a.D ? a.D[h] : 0.0f;
@@ -588,12 +617,14 @@ int launch_ssm(ScanArgs a, hipStream_t s) {
     step_kernel<N, TB><<<dim3(steps), dim3(STEP_NT), 0, s>>>(a, a.done);
     if (int rc = check_launch(); rc != W4A8_OK || a.q.T <= STEP_T) return rc;
   }
-  const unsigned ngram = (unsigned)(records(a.q.T, a.q.B) * a.NG * prep_parts(N)), ndec = (unsigned)(records(a.q.T, a.q.B) * ((a.NH + 3) / 4));
-  prep_kernel<N><<<dim3(ngram + ndec), dim3(256), 0, s>>>(a, ngram);
+  const unsigned norder = (unsigned)((a.q.B + ORDER_NT - 1) / ORDER_NT);
+  const unsigned ngram = (unsigned)(records(a.q.T, a.q.B) * a.NG * prep_parts(N)),
+                 ndec = (unsigned)(records(a.q.T, a.q.B) * ((a.NH + 3) / 4));
+  prep_kernel<N><<<dim3(norder + ngram + ndec), dim3(ORDER_NT), 0, s>>>(a, norder, ngram);
   if (int rc = check_launch(); rc != W4A8_OK) return rc;
   // Slices of 32 columns read the records half as often as those of 16, which fill the
   // card with half the heads.  64 heads of 64, us: 2 sequences of 2000 rows 136 and
-  // 134, 3 of them 219 and 201, 4 of them 231 and 237.
+  // 136, 3 of them 219 and 201, 4 of them 235 and 257.
   if constexpr (N == 128)
     if ((int64_t)a.q.B * a.NH * (a.P / 32) >= 2 * device_cus()) return launch_scan<N, 32>(a, s);
   return launch_scan<N, N == 64 ? 32 : 16>(a, s);
@@ -608,7 +639,8 @@ using namespace w4a8;
 extern "C" size_t ssm_workspace_size(const w4a8_seqs *seqs, const w4a8_ssm *ssm, int64_t T) {
   if (ssm_sizes(seqs, ssm, T) != W4A8_OK) return 0;
   return (size_t)records(T, seqs->B) * (ssm->NG * rec_floats((int)ssm->N) + ssm->NH * DEC * SC) *
-         sizeof(float);
+             sizeof(float) +
+         (size_t)seqs->B * sizeof(int4);
 }
 
 extern "C" int ssm_scan(const w4a8_seqs *seqs, const w4a8_ssm *m, float *state, float *y,
@@ -643,6 +675,7 @@ extern "C" int ssm_scan(const w4a8_seqs *seqs, const w4a8_ssm *m, float *state, 
   a.A = m->A; a.D = m->D; a.bias = m->dt_bias;
   a.state = state; a.y = y; a.gram = reinterpret_cast<float *>(workspace);
   a.dec = a.gram + records(a.q.T, a.q.B) * m->NG * rec_floats((int)m->N);
+  a.order = reinterpret_cast<int4 *>(a.dec + records(a.q.T, a.q.B) * m->NH * DEC * SC);
   a.xs = (int)m->x_stride; a.ds = (int)m->dt_stride; a.bs = (int)m->b_stride; a.cs = (int)m->c_stride;
   a.zs = m->z ? (int)m->z_stride : 0; a.ys = (int)y_stride;
   a.NH = (int)m->NH; a.NG = (int)m->NG; a.G = (int)(m->NH / m->NG); a.P = (int)m->P;

@@ -298,3 +298,18 @@ def test_many_sequences():
 
 def test_long_sequence():
     Case([25], [2500, 5], NH=1, P=32, N=128).check()
+
+
+# (up to 1024 sequences are taken longest first, more as they come)
+@pytest.mark.parametrize("B", [3, 64, 255, 257, 1024, 1025, 1300])
+def test_long_sequences_anywhere_among_short_ones(B):
+    g = np.random.default_rng([30, B])
+    lens = g.choice([0, 1, 3, 9, 64, 70, 193], B, p=[0.2, 0.4, 0.2, 0.08, 0.04, 0.04, 0.04])
+    lens[-1] = 260
+    Case([31, B], lens, NH=1, P=16).check()
+
+
+@pytest.mark.parametrize("order", [1, -1])
+def test_long_sequences_in_either_order_with_wide_slices(order):
+    lens = [330, 200, 200, 129, 64, 9, 1, 0][::order]
+    Case([32], lens, NH=40, P=64, N=128).check()
