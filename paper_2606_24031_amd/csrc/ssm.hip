@@ -255,8 +255,10 @@ __global__ __launch_bounds__(ORDER_NT) void prep_kernel(ScanArgs a, unsigned nor
     const int t = t0 + lane;
     const float d = t < end ? step_of(a.dt[(int64_t)min(t, end - 1) * a.ds + h], a.bias ? a.bias[h] : 0.0f, a.softplus)
                             : 0.0f;
-    // (past 2^20 either way a row's decay is 0 or infinite; kept there, sums stay finite)
-    const double s = scan64(t < end ? fmin(fmax((double)d * A, -1048576.0), 1048576.0) : 0.0);
+    // (past 2^20 either way a row's decay is 0 or infinite; kept there, sums stay finite. A
+    // NaN stays one)
+    const double v = (double)d * A, top = 1048576.0;
+    const double s = scan64(t < end ? (v < -top ? -top : v > top ? top : v) : 0.0);
     const uint64_t u = __builtin_bit_cast(uint64_t, s);
     const double all = __builtin_bit_cast(
         double, (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(u >> 32), 63) << 32 |
