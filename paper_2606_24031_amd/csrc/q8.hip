@@ -18,6 +18,7 @@
 // products are 0.43.  Measured slower: 128 x 128 waves (four a tile; 549 us at 8192^3
 // where eight of 128 x 64 took 523), wave priorities, tiles of 192 (5120 x 12288 x
 // 4096 289 to 312 us).
+#include "choice.h"
 #include "dma_dev.h"
 #include "w4a8_dev.h"
 #include "w4a8_host.h"
@@ -417,36 +418,16 @@ extern "C" int q8q8_gemm(const int8_t *xq, const float *xd, const int8_t *wq, co
   QArgs a{xq, wq, xd, wd, bias, y, y_stride, (int)M, (int)N, (int)q8_row_bytes(K), 0, 0,
           y_stride % 4 == 0 && aligned16(y)};
   hipStream_t s = as_stream(stream);
-  // Up to 16 rows stream the weights; two tiles of channels a wave where there are
-  // several rows and enough channels for all compute units eight times (16 rows over
-  // 151936 x 2048 73 us against 89; one row 64 against 59).  Up to 64 rows do while
-  // one workgroup a compute unit covers the channels (48 over 4096 x 2048 7.5 us, 8.4
-  // on tiles; over 12288 x 2048 15, 9.2 on tiles).
-  const int n16 = (a.N + 15) / 16, cus = device_cus();
-  if (M <= 16) return M > 1 && n16 >= 8 * cus ? launch_few<1, 2>(a, s) : launch_few<1, 1>(a, s);
-  if (M <= 64 && n16 <= cus)
-    return M <= 32 ? launch_few<2, 1>(a, s) : M <= 48 ? launch_few<3, 1>(a, s) : launch_few<4, 1>(a, s);
-  // One tile a compute unit takes `one`, each further round `more` (us at K = 2048;
-  // longer rows in proportion): the kind whose rounds end first.  Measured there:
-  // 947 x 12288 37.5 on the largest tiles and 46, 45, 52, 62 on the others; 947 x
-  // 8192 34, 29.5, 30.5, 38, 43; 947 x 4096 28, 23, 17, 19, 21; 947 x 2048 27, 22, 15,
-  // 12, 12; 200 x 8192 27, 22, 15, 12, 11.5; 100 x 4096 26, 21, 14, 10.5, 8.4.
-  struct Kind { int tn, tm; float one, more; };
-  constexpr Kind kinds[] = {{256, 256, 30.f, 38.f}, {256, 128, 22.f, 25.f}, {128, 128, 14.f, 14.7f},
-                            {128, 64, 10.5f, 8.7f}, {64, 64, 8.f, 5.1f}};
-  int best = 0;
-  float least = 0.0f;
-  for (int i = 0; i < 5; i++) {
-    const Kind &k = kinds[i];
-    const int64_t tiles = ((N + k.tn - 1) / k.tn) * ((M + k.tm - 1) / k.tm);
-    const float t = k.one + k.more * (float)((tiles - 1) / device_cus());
-    if (i == 0 || t < least) { best = i; least = t; }
-  }
-  switch (best) {
-    case 0: return launch_tiles<256, 256, 2, 4, 4>(a, s);
-    case 1: return launch_tiles<256, 128, 2, 2, 3>(a, s);
-    case 2: return launch_tiles<128, 128, 2, 2, 4>(a, s);
-    case 3: return launch_tiles<128, 64, 2, 2, 4>(a, s);
+  switch (q8_way(M, N, device_cus())) {
+    case Q8_FEW_1x1: return launch_few<1, 1>(a, s);
+    case Q8_FEW_1x2: return launch_few<1, 2>(a, s);
+    case Q8_FEW_2x1: return launch_few<2, 1>(a, s);
+    case Q8_FEW_3x1: return launch_few<3, 1>(a, s);
+    case Q8_FEW_4x1: return launch_few<4, 1>(a, s);
+    case Q8_256x256: return launch_tiles<256, 256, 2, 4, 4>(a, s);
+    case Q8_256x128: return launch_tiles<256, 128, 2, 2, 3>(a, s);
+    case Q8_128x128: return launch_tiles<128, 128, 2, 2, 4>(a, s);
+    case Q8_128x64: return launch_tiles<128, 64, 2, 2, 4>(a, s);
     default: return launch_tiles<64, 64, 2, 2, 4>(a, s);
   }
 }
