@@ -562,10 +562,12 @@ int short_conv(const w4a8_seqs *seqs, const float *x, int64_t x_stride, const fl
  *   y[t]  = C[t]^T S + D[h] * x[t],  times z[t] / (1 + exp(-z[t])) if z
  * computed as a chunked scan (chunks of 64 rows: products within a chunk and a
  * group in parallel, then the chunks in order per head and columns of P), or
- * row by row where sequences are short.  Sums and states are fp32; logarithms
- * of decays are summed in fp64.  A sequence's result does not depend on the
- * values of others; which way it is computed, and so its last bits, may depend
- * on the call's sizes.
+ * row by row where sequences are short, and in calls with exactly as many
+ * sequences as rows, which are taken to have one each (a long one there takes
+ * about a microsecond a row).  Sums and states are fp32; logarithms of decays
+ * are summed in fp64.  A sequence's result does not depend on the values of
+ * others; which way it is computed, and so its last bits, may depend on the
+ * call's sizes.
  *   x, z [T][NH][P], b, c [T][NG][N], dt [T][NH] fp32, row t at t times the
  *   row's stride in elements, heads and groups contiguous; A [NH]; D, dt_bias
  *   [NH], z: NULL for none; state [n_slots][NH][N][P] fp32, read and written as

@@ -40,4 +40,42 @@ inline int q8_way(int64_t M, int64_t N, int cus) {
   return Q8_256x256 + best;
 }
 
+// ------------------------------------------------------------------ ssm_scan
+constexpr int SSM_CHUNK = 64;       // rows of a chunk
+constexpr int SSM_STEP_T = 8;       // sequences of up to this many rows may go row by row,
+constexpr int SSM_SPARE_T = 32;     // of up to this many in a plan with places to spare
+constexpr int SSM_ORDER_B = 1024;   // up to this many are taken longest first by chunks
+
+struct SsmWay {
+  int rows;      // sequences of up to so many rows go row by row (0: none)
+  bool single;   // ... one row at a time
+  int chunked;   // so many sequences, the longest, go by chunks (0: none)
+  int slice;     // columns of a workgroup by chunks
+};
+
+inline SsmWay ssm_way(int64_t B, int64_t T, int64_t NH, int64_t P, int N, int cus) {
+  SsmWay w{};
+  // Row by row, one launch, where no sequence can be long (8 rows), or hardly one:
+  // exactly as many sequences as rows are taken to be a token each, and a chunk's
+  // rows in a plan with places to spare are left to it too.  More rows in such a plan
+  // may be one sequence's (947 of them, 64 heads of 64, in a plan of 1024: 1.11 ms row
+  // by row, 0.11 by chunks, 0.04 in a plan of its own): there, up to 32 rows go row by
+  // row, which takes what the chunks' launches do, and the others by chunks (1000
+  // tokens in a plan of 1024: 802 us without those launches, 836 with them).
+  // Batches that may hold many short sequences beside long ones: the short ones in
+  // that launch too (16 of 4 rows: 22 us), the others chunk by chunk; few short ones
+  // do not pay for a launch.
+  w.single = T <= B;
+  const bool all = T <= SSM_STEP_T || T == B || (w.single && T <= SSM_CHUNK);
+  w.rows = all ? (int)T : w.single ? SSM_SPARE_T : T / SSM_CHUNK < B ? SSM_STEP_T : 0;
+  if (all) return w;
+  const int64_t most = T / (w.rows + 1);         // so many can have more rows
+  w.chunked = (int)(B > SSM_ORDER_B || B < most ? B : most);
+  // Slices of 32 columns read the records half as often as those of 16, which fill the
+  // card with half the heads.  64 heads of 64, us: 2 sequences of 2000 rows 136 and
+  // 136, 3 of them 219 and 201, 4 of them 235 and 257.
+  w.slice = N == 64 || (N == 128 && w.chunked * NH * (P / 32) >= 2 * cus) ? 32 : 16;
+  return w;
+}
+
 }  // namespace w4a8

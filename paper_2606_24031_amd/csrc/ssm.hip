@@ -17,6 +17,7 @@
 // KB a step come from the L2 caches (14 TB/s in all).  16384 rows, 64 heads of 64:
 // 525 us and 21 for prep (256 at the products' rate, 164 for the bytes); the
 // 947-token prompt of 32 heads of 128: 35 and 8.
+#include "choice.h"
 #include "seq_dev.h"
 #include "w4a8_dev.h"
 
@@ -24,10 +25,9 @@ namespace w4a8 {
 
 namespace {
 
-constexpr int SC = 64;              // rows of a chunk
+constexpr int SC = SSM_CHUNK;
 constexpr int SNT = 512;            // threads of a scan workgroup: eight waves
 constexpr int STEP_NT = 256;        // ... of a step workgroup
-constexpr int STEP_T = 8;           // sequences of up to this many rows may go row by row
 
 typedef float v4f __attribute__((ext_vector_type(4)));
 typedef uint32_t v4u __attribute__((ext_vector_type(4)));
@@ -40,7 +40,7 @@ struct ScanArgs {
   int xs, ds, bs, cs, zs, ys;       // strides
   int NH, G, NG, P, nsl;            // heads, heads of a group, groups, columns, slices of columns
   int softplus;
-  int done;                         // chunks: sequences of up to so many rows are another launch's
+  int done, n;                      // chunks: sequences of up to so many rows are another launch's; sequences taken
 };
 
 // The step of a row: dt + bias, and log(1 + exp(.)) of it.
@@ -133,14 +133,13 @@ __device__ __forceinline__ void step_rows(const ScanArgs &a, int b, int h, int c
       *reinterpret_cast<v4f *>(a.state + ((dst * a.NH + h) * N + r0 + RG * m) * a.P + c) = S[m];
 }
 
-// Sequences row by row, 64 columns of a head a workgroup; with `most`, those of
-// up to that many rows.
+// Sequences of up to `most` rows row by row, 64 columns of a head a workgroup.
 template <int N, int TB>
 __global__ __launch_bounds__(STEP_NT) void step_kernel(ScanArgs a, int most) {
   __shared__ __align__(16) StepLds<64, STEP_NT, TB> L;
   const int sl = blockIdx.x % a.nsl, bh = blockIdx.x / a.nsl, h = bh % a.NH, b = bh / a.NH;
   const int begin = seq_begin(a.q, b), end = seq_begin(a.q, b + 1);
-  if (begin >= end || (most && end - begin > most)) return;
+  if (begin >= end || end - begin > most) return;
   step_rows<N, 64, STEP_NT, TB>(a, b, h, sl * 64, begin, end, L);
 }
 
@@ -201,7 +200,7 @@ constexpr int DEC_LDS = 3;          // the first ones go to LDS, the others into
 // long one starts when the others end: number, first row, end.  6 sequences of 633 to
 // 2000 rows, 64 heads of 64: 236 us, as they come 278.  Places are counted, which
 // for up to ORDER_B sequences ends before the records do; more go as they come.
-constexpr int ORDER_B = 1024, ORDER_NT = 256;
+constexpr int ORDER_B = SSM_ORDER_B, ORDER_NT = 256;
 __device__ __forceinline__ void order_rows(const ScanArgs &a, int block) {
   __shared__ __align__(16) int rows[ORDER_B];
   const int B = a.q.B, b = block * ORDER_NT + threadIdx.x;
@@ -240,7 +239,8 @@ __global__ __launch_bounds__(ORDER_NT) void prep_kernel(ScanArgs a, unsigned nor
   const bool gram = block < ngram;
   const unsigned w = gram ? block : block - ngram, per = gram ? a.NG * prep_parts(N) : (a.NH + 3) / 4;
   const int rec = w / per, part = w % per;
-  int lo = 0, hi = a.q.B;           // the last sequence whose first record is not past rec
+  // the last sequence whose first record is not past rec: its number plus up to T / 64
+  int lo = min(max(rec - a.q.T / SC, 0), a.q.B - 1), hi = min(rec + 1, a.q.B);
   while (hi - lo > 1) {
     const int m = (lo + hi) >> 1;
     if (record_of(seq_begin(a.q, m), m) <= rec) lo = m; else hi = m;
@@ -345,7 +345,7 @@ __global__ __launch_bounds__(SNT, (ScanLds<N, PS>::SB == 1 ? 4 : 2)) void scan_k
   const int l16 = lane & 15, lq = lane >> 4;
   // all slices of a head on one XCD (workgroup w runs on XCD w mod 8)
   const int k = blockIdx.x >> 3, bh = (k / a.nsl) * 8 + (blockIdx.x & 7);
-  if (bh >= a.q.B * a.NH) return;
+  if (bh >= a.n * a.NH) return;
   const int4 place = a.order[bh / a.NH];
   const int b = __builtin_amdgcn_readfirstlane(place.x), begin = __builtin_amdgcn_readfirstlane(place.y),
             end = __builtin_amdgcn_readfirstlane(place.z);
@@ -596,39 +596,33 @@ int ssm_sizes(const w4a8_seqs *q, const w4a8_ssm *m, int64_t T) {
 template <int N, int PS>
 int launch_scan(ScanArgs a, hipStream_t s) {
   a.nsl = (a.P + PS - 1) / PS;
-  const unsigned pairs = (unsigned)((a.q.B * a.NH + 7) / 8 * 8);
+  const unsigned pairs = (unsigned)((a.n * a.NH + 7) / 8 * 8);
   scan_kernel<N, PS><<<dim3(pairs * a.nsl), dim3(SNT), 0, s>>>(a);
   return check_launch();
 }
 
 template <int N>
 int launch_ssm(ScanArgs a, hipStream_t s) {
-  // Row by row where no sequence can be long, or hardly one (as many sequences as
-  // rows).  Batches that may hold many short sequences beside long ones: the short
-  // ones in that launch too (16 of 4 rows, 64 heads of 64: 26 us), the others chunk
-  // by chunk; few short ones do not pay for a launch.
+  const SsmWay way = ssm_way(a.q.B, a.q.T, a.NH, a.P, N, device_cus());
   constexpr int TB = N == 256 ? 2 : 4;
-  const unsigned steps = (unsigned)(a.q.B * a.NH * ((a.P + 63) / 64));
   a.nsl = (a.P + 63) / 64;
-  if (a.q.T <= a.q.B) {
-    step_kernel<N, 1><<<dim3(steps), dim3(STEP_NT), 0, s>>>(a, 0);
-    return check_launch();
+  if (way.rows) {
+    const dim3 grid((unsigned)(a.q.B * a.NH * a.nsl));
+    if (way.single)
+      step_kernel<N, 1><<<grid, dim3(STEP_NT), 0, s>>>(a, way.rows);
+    else
+      step_kernel<N, TB><<<grid, dim3(STEP_NT), 0, s>>>(a, way.rows);
+    if (int rc = check_launch(); rc != W4A8_OK || !way.chunked) return rc;
   }
-  if (a.q.T <= STEP_T || a.q.T / 64 < a.q.B) {
-    a.done = a.q.T <= STEP_T ? 0 : STEP_T;
-    step_kernel<N, TB><<<dim3(steps), dim3(STEP_NT), 0, s>>>(a, a.done);
-    if (int rc = check_launch(); rc != W4A8_OK || a.q.T <= STEP_T) return rc;
-  }
+  a.done = way.rows;
+  a.n = way.chunked;
   const unsigned norder = (unsigned)((a.q.B + ORDER_NT - 1) / ORDER_NT);
   const unsigned ngram = (unsigned)(records(a.q.T, a.q.B) * a.NG * prep_parts(N)),
                  ndec = (unsigned)(records(a.q.T, a.q.B) * ((a.NH + 3) / 4));
   prep_kernel<N><<<dim3(norder + ngram + ndec), dim3(ORDER_NT), 0, s>>>(a, norder, ngram);
   if (int rc = check_launch(); rc != W4A8_OK) return rc;
-  // Slices of 32 columns read the records half as often as those of 16, which fill the
-  // card with half the heads.  64 heads of 64, us: 2 sequences of 2000 rows 136 and
-  // 136, 3 of them 219 and 201, 4 of them 235 and 257.
   if constexpr (N == 128)
-    if ((int64_t)a.q.B * a.NH * (a.P / 32) >= 2 * device_cus()) return launch_scan<N, 32>(a, s);
+    if (way.slice == 32) return launch_scan<N, 32>(a, s);
   return launch_scan<N, N == 64 ? 32 : 16>(a, s);
 }
 
