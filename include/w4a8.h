@@ -491,9 +491,10 @@ int q8_row_quantize(const float *x, int64_t x_stride, int8_t *q, float *d, int64
  *   quantizer writes them); xd [M], wd [N], bias [N] fp32; y fp32, row m at
  *   m * y_stride elements, written.  One launch, no workspace.
  * Errors: M < 0, N < 1, K < 1, y_stride < N -> W4A8_ESHAPE; K >= 2^17, M or N
- * >= 2^26, y_stride >= 2^31 or 2^23 tiles of 64 rows by 64 channels or more -> W4A8_ERANGE; a NULL pointer (but bias) ->
- * W4A8_ENULL; xq or wq not 16-, xd, wd, bias or y not 4-byte aligned ->
- * W4A8_EALIGN; y equal to an operand -> W4A8_EALIAS.  M == 0 is a no-op.
+ * >= 2^26, y_stride >= 2^31 or 2^23 tiles of 64 rows by 64 channels or more ->
+ * W4A8_ERANGE; a NULL pointer (but bias) -> W4A8_ENULL; xq or wq not 16-, xd,
+ * wd, bias or y not 4-byte aligned -> W4A8_EALIGN; y equal to an operand ->
+ * W4A8_EALIAS.  M == 0 is a no-op.
  */
 int q8q8_gemm(const int8_t *xq, const float *xd, const int8_t *wq, const float *wd,
               const float *bias, float *y, int64_t y_stride, int64_t M, int64_t N, int64_t K,
@@ -541,8 +542,8 @@ typedef struct w4a8_seqs {
  *   reaches the W rows that it is an input of and the state.
  * Errors beside the plan's: T < 0, CH < 4, CH % 4 != 0, W not 2, 3 or 4, act
  * unknown, a stride below CH or not a multiple of 4 -> W4A8_ESHAPE; T >= 2^31,
- * CH >= 2^24 or a stride >= 2^31 -> W4A8_ERANGE; x, w, out, or state with
- * n_slots > 0, NULL -> W4A8_ENULL; a pointer not 16-byte aligned ->
+ * CH >= 2^24, T * CH >= 2^40 or a stride >= 2^31 -> W4A8_ERANGE; x, w, out, or
+ * state with n_slots > 0, NULL -> W4A8_ENULL; a pointer not 16-byte aligned ->
  * W4A8_EALIGN; out or state equal to x or to each other -> W4A8_EALIAS.
  * T == 0 or B == 0 is a no-op.
  */
@@ -575,17 +576,18 @@ int short_conv(const w4a8_seqs *seqs, const float *x, int64_t x_stride, const fl
  *   workspace >= ssm_workspace_size bytes, no initialisation.
  *   Inputs are finite, and so is the growth over 64 rows where delta * A > 0.
  *   (A value that is not reaches rows of its own sequence and head, or group,
- *   only: from its 64-row chunk on.)
+ *   only: from its 64-row chunk on.  One of A, D or dt_bias reaches its head's
+ *   rows of every sequence.)
  * Errors beside the plan's: NULL ssm -> W4A8_ENULL; T < 0, NH or NG < 1,
  * NH % NG != 0, N not 64, 128 or 256, P < 16, P % 16 != 0, a stride below its
  * row's elements, or (but for dt's) not a multiple of 4 -> W4A8_ESHAPE; T >=
- * 2^31, NH >= 2^16, P > 4096, a stride >= 2^24, B * NH * P >= 2^26 or (T / 64 + B + 3)
- * * (NG + NH) >= 2^21 -> W4A8_ERANGE; x, dt, b, c,
- * A, y or workspace, or state with n_slots > 0, NULL -> W4A8_ENULL; dt, A, D or
- * dt_bias not 4-, another pointer not 16-byte aligned -> W4A8_EALIGN; y or
- * state equal to an input or to each other -> W4A8_EALIAS; workspace too small
- * -> W4A8_EWORKSPACE.  T == 0 or B == 0 is a no-op.  ssm_workspace_size returns
- * 0 for invalid sizes; it reads only sizes.
+ * 2^31, NH >= 2^16, P > 4096, a stride >= 2^24, B * NH * P >= 2^26 or
+ * (T / 64 + B + 3) * (NG + NH) >= 2^21 -> W4A8_ERANGE; x, dt, b, c, A, y or
+ * workspace, or state with n_slots > 0, NULL -> W4A8_ENULL; dt, A, D or dt_bias
+ * not 4-, another pointer not 16-byte aligned -> W4A8_EALIGN; y or state equal
+ * to an input or to each other -> W4A8_EALIAS; workspace too small ->
+ * W4A8_EWORKSPACE.  T == 0 or B == 0 is a no-op.  ssm_workspace_size returns 0
+ * for invalid sizes; it reads only sizes.
  */
 typedef struct w4a8_ssm {
   const float *x, *dt, *b, *c, *z;

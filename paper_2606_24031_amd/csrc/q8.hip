@@ -15,7 +15,9 @@
 // fall to 1.6 GHz.  8192^3: 2.23 POP/s (the library's int8 product 2.51), 4096^3
 // 1.87 (2.04).  Tiles that fill the card once (947 x 12288 x 2048: 33 us) are bound
 // by the stages: a 256 x 256 tile's stage of 64 codes takes 0.73 us, of which its
-// products are 0.43.  Measured slower: 128 x 128 waves (four a tile; 549 us at 8192^3
+// products are 0.43, so 23 us for the 32 stages; the rest is the launch, the first
+// loads and the output (46.5 MB, 9 us at a copy's rate), which all tiles store after
+// their last stage, at one time.  64 compute units have no tile.  Measured slower: 128 x 128 waves (four a tile; 549 us at 8192^3
 // where eight of 128 x 64 took 523), wave priorities, tiles of 192 (5120 x 12288 x
 // 4096 289 to 312 us).
 #include "choice.h"
@@ -294,7 +296,9 @@ __global__ __launch_bounds__(64 * WN * WM, 2) void q8_tile_kernel(QArgs a) {
 // codes come from the L2 cache.  The waves' sums (whole numbers: any order
 // gives the same) are added up in LDS.  Small calls are a chain of launch, one
 // or two trips to memory, the join and the store: 1 x 2048 x 4096 5.8 us, 48 x 2048 x
-// 4096 10.8; four or sixteen waves 7.0 and 5.7, 12.0 and 10.6.
+// 4096 10.8; four or sixteen waves 7.0 and 5.7, 12.0 and 10.6.  At 48 rows three of
+// four operand loads are activation codes, all 196 KB of them read by each of the 128
+// workgroups, and the join's atomics meet 16 of the LDS's banks.
 template <int MT, int RN>
 __global__ __launch_bounds__(KNT) void q8_few_kernel(QArgs a) {
   constexpr int OS = 16 * RN + 4, U = RN * MT >= 8 ? 2 : 4;
