@@ -66,3 +66,34 @@ def test_calls_with_fewer_rows_than_a_large_plan():
     lens = [0] * 200
     lens[3], lens[100], lens[150] = 100, 50, 50
     Case([54], lens, NH=2, P=16).check(rows=130)
+
+
+def test_a_graph_whose_plan_changes_between_replays():
+    """Captured once with places to spare, replayed with a prompt, with tokens, with
+    both, with neither: each replay as the same call made eagerly."""
+    B, T = 130, 100
+    plans = [[100], [1] * 100, [3, 40, 1, 33, 2, 21], [0] * 130, [32, 33, 35], [1] * 20 + [60]]
+    c = Case([56], [100] + [0] * (B - 1), NH=2, P=32, N=128, n_slots=B, src=range(B), dst=range(B))
+    dev = lambda a: torch.from_numpy(a).cuda()
+    x, z, dt, A, b, cc = map(dev, (c.x, c.z, c.dt, c.A, c.B, c.C))
+    cu, st, out = i32(np.zeros(B + 1)), dev(c.state), torch.zeros(T, 2, 32, device="cuda")
+    plan = w4.SeqPlan(cu, B)
+    ws = w4.ssm_workspace(plan, T, 2, 1, 128, 32)
+    call = lambda: w4.ssm_scan(plan, x, dt, A, b, cc, st, z=z, out=out, workspace=ws)
+    call()
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        call()
+    for lens in plans * 2:
+        ends = np.concatenate([[0], np.cumsum(lens + [0] * (B - len(lens)))])
+        got = []
+        for f in (call, g.replay):
+            cu.copy_(i32(ends))
+            st.copy_(dev(c.state))
+            out.fill_(7.0)
+            f()
+            torch.cuda.synchronize()
+            got.append((out.clone(), st.clone()))
+        assert torch.equal(got[0][0], got[1][0]) and torch.equal(got[0][1], got[1][1])
+        assert bool((got[0][0][sum(lens):] == 7).all())
